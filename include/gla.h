@@ -5,7 +5,11 @@
  * several scan orders summed (gla_fwd_multi), the backward pass (gla_bwd*), the same
  * with the full gate matrix alpha_t^T beta_t (gla_fwd_gates, gla_fwd_fused_gates,
  * gla_bwd_gates), and the depth-wise convolution of the DiG block's reorientation
- * module (gla_srem_dwconv).
+ * module (gla_srem_dwconv).  Beside them stands a mixer with one decay a head for
+ * sequences of any kind: the recurrence itself (gla_decay_fwd, gla_decay_bwd, and
+ * gla_decay_step for single tokens), the rotation of its queries and keys by the
+ * tokens' positions (gla_rope), and the layer norm of its outputs or of the tokens
+ * with and without the output gate, both directions (gla_norm_fwd, gla_norm_bwd).
  *
  * Operation (DiG paper, Sec. 3.1 "Gated Linear Attention Transformer",
  * Eq. (attn_gla), rows 1-3, with the gate G_t reduced to its key-side factor
@@ -435,6 +439,136 @@ int gla_fwd_fused_gates(const void *q, const void *k, const void *v, const void 
                         int B, int H, int T, int dk, int dv, int grid_h, int grid_w, int scan_dir,
                         int qkv_dtype, int out_dtype, void *out, float *final_state,
                         void *workspace, size_t workspace_bytes, gla_stream_t stream);
+
+/*
+ * gla_decay_fwd - linear attention with one decay a head:
+ *
+ *     S_t = a_t S_{t-1} + k_t^T v_t ,     o_t = q_t S_t ,     S_0 = initial_state or zero
+ *
+ * with a_t = exp(log_decay) a number: Eq. (attn_gla) with the gate row alpha_t replaced by one decay, constant for a
+ * head or given for each token.  No gate rows are read, queries and keys may be rotated (gla_rope; a scalar commutes
+ * with the rotation, a gate row does not), and heads may be wider: 1 <= dk, dv <= 128.
+ *
+ *   q, k, v        DEVICE, qkv_dtype, in `layout` ([B,H,T,d] or [B,T,H,d])                                    (read)
+ *   log_decay      DEVICE, fp32, 16-byte aligned, <= 0 down to -inf (a gate of zero)                          (read)
+ *   decay_kind     a gla_decay_kind: log_decay is [H], or one for each token in the order of `layout`
+ *                  ([B,H,T] or [B,T,H])
+ *   seq_lens       DEVICE, int32 [B], 0 .. T, or NULL: all T.  Sequence b ends after seq_lens[b] tokens: it is walked
+ *                  as if it were that long (ROW_REV begins at its own last token), its final state is the one after
+ *                  them, the rows behind them may hold anything and those of `out` are left as they were.  A length of
+ *                  0 gives the initial state as final state.  Values outside 0 .. T count as the nearer end.
+ *                  Row scans only (GLA_ERR_UNSUPPORTED)                                                       (read)
+ *   grid_h, grid_w, scan_dir   as in gla_fwd; for text and the like grid_h = 1, grid_w = T, GLA_SCAN_ROW_FWD
+ *   initial_state  DEVICE, fp32 [B,H,dk,dv] or NULL                                                           (read)
+ *   out            DEVICE, out_dtype, shaped and laid out like v                                              (written)
+ *   final_state    DEVICE, fp32 [B,H,dk,dv] or NULL; may be initial_state                                     (written)
+ *   workspace      DEVICE, 16-byte aligned, gla_decay_fwd_workspace_bytes(...) bytes (0 for many sequences: then it
+ *                  may be NULL)
+ *
+ * bf16 calls run on bf16 MFMA with every factor that is not an input carried as two bf16 numbers, fp32 calls on fp32
+ * MFMA.  Gates have no lower limit.  Inputs of visited rows have to be finite.  Tuning options have no effect.
+ * Never allocates; nothing is kept between calls.
+ */
+typedef enum { GLA_DECAY_HEAD = 0, GLA_DECAY_TOKEN = 1 } gla_decay_kind;
+int gla_decay_fwd(const void *q, const void *k, const void *v, const float *log_decay, int decay_kind, const int *seq_lens,
+                  int B, int H, int T, int dk, int dv, int grid_h, int grid_w, int scan_dir,
+                  int qkv_dtype, int out_dtype, int layout, const float *initial_state, void *out, float *final_state,
+                  void *workspace, size_t workspace_bytes, gla_stream_t stream);
+size_t gla_decay_fwd_workspace_bytes(int B, int H, int T, int dk, int dv, int qkv_dtype);
+
+/*
+ * gla_decay_bwd - gradients of a loss that depends on `out` and, through d_final_state, on the final state of
+ * gla_decay_fwd.  With G_t = q_t^T dO_t + a_{t+1} G_{t+1} the adjoint state (behind the last token d_final_state):
+ *   dq_t = S_t dO_t^T,  dk_t = G_t v_t^T,  dv_t = k_t G_t,  dlog a_t = <a_t S_{t-1}, G_t>,  d S_0 = a_1 G_1.
+ *
+ *   d_out            DEVICE, qkv_dtype, like v                                                                (read)
+ *   d_final_state    DEVICE, fp32 [B,H,dk,dv] or NULL: zero                                                   (read)
+ *   dq, dk_grad, dv_grad   DEVICE, grad_dtype, like q, k, v; rows behind a sequence's end are cleared         (written)
+ *   dlog_decay       DEVICE, fp32, like log_decay (cleared behind a sequence's end; for GLA_DECAY_HEAD the sum over
+ *                    batches and tokens, always added in one order), or NULL: not wanted                      (written)
+ *   d_initial_state  DEVICE, fp32 [B,H,dk,dv], or NULL: not wanted                                            (written)
+ *   workspace        DEVICE, 16-byte aligned, gla_decay_bwd_workspace_bytes(...) bytes
+ *
+ * Everything else as gla_decay_fwd.  Outputs must not alias inputs.
+ */
+int gla_decay_bwd(const void *q, const void *k, const void *v, const float *log_decay, int decay_kind, const int *seq_lens,
+                  const void *d_out, const float *initial_state, const float *d_final_state,
+                  int B, int H, int T, int dk, int dv, int grid_h, int grid_w, int scan_dir,
+                  int qkv_dtype, int grad_dtype, int layout, void *dq, void *dk_grad, void *dv_grad, float *dlog_decay,
+                  float *d_initial_state, void *workspace, size_t workspace_bytes, gla_stream_t stream);
+size_t gla_decay_bwd_workspace_bytes(int B, int H, int T, int dk, int dv, int qkv_dtype);
+
+/*
+ * gla_decay_step - one token of gla_decay_fwd for each of B sequences:
+ *   state_out = a state + k^T v,   out = q state_out.
+ *
+ *   q, k [B,H,dk], v [B,H,dv]   DEVICE, qkv_dtype                                                             (read)
+ *   log_decay   DEVICE, fp32 [H] or (GLA_DECAY_TOKEN) [B,H]                                                   (read)
+ *   state       DEVICE, fp32 [B,H,dk,dv], 16-byte aligned                                                     (read)
+ *   state_out   the same; may be `state` (in place), GLA_ERR_SHAPE where the two overlap otherwise            (written)
+ *   out         DEVICE, out_dtype [B,H,dv]                                                                    (written)
+ *
+ * q, k, v, log_decay and out may begin at any element.  Arithmetic in fp32.  Needs no workspace and never allocates.
+ */
+int gla_decay_step(const void *q, const void *k, const void *v, const float *log_decay, int decay_kind,
+                   int B, int H, int dk, int dv, int qkv_dtype, int out_dtype, const float *state, float *state_out,
+                   void *out, gla_stream_t stream);
+
+/*
+ * gla_rope - rotary positions with one or several axes.  The first channels of a head fall into sections, one an axis;
+ * pair i of the section of axis x with w channels is turned by the angle position_x * base^(-2 i / w):
+ *   (u, v) -> (u cos - v sin, v cos + u sin).
+ * Channels behind the sections are copied.
+ *
+ *   q, k        DEVICE, dtype, [B,H,T,d] or [B,T,H,d] by `layout`; k (and out_k) may be NULL                  (read)
+ *   positions   DEVICE, int32 [B,T,axes], or NULL: from the grid, for one axis the token's number, for two its row and
+ *               column (T = grid_h * grid_w), for three frame, row and column (T a multiple of it)            (read)
+ *   sections    HOST, axes even numbers whose sum is at most d
+ *   axes        1 .. 4 (1 .. 3 without positions)
+ *   base        > 0, finite; 10000 as a rule
+ *   pairing     a gla_rope_pairing: a pair is two neighbouring channels, or channel i and i + w/2 of a section
+ *   inverse     not 0: turned back, which is also the backward pass
+ *   out_q, out_k   DEVICE, dtype, like q and k; may be q and k                                                (written)
+ *
+ * 1 <= d <= 256.  Angles are formed and reduced in 64 bits: every position of 32 bits is as exact as the first.  grid_h, grid_w are
+ * ignored with positions or one axis.  Needs no workspace and never allocates.
+ */
+typedef enum { GLA_ROPE_ADJACENT = 0, GLA_ROPE_HALVES = 1 } gla_rope_pairing;
+int gla_rope(const void *q, const void *k, const int *positions, const int *sections, int axes, float base, int pairing,
+             int inverse, int B, int H, int T, int d, int grid_h, int grid_w, int dtype, int layout,
+             void *out_q, void *out_k, gla_stream_t stream);
+
+/*
+ * gla_norm_fwd - layer norm of rows of D channels, and with r_pre the output gate behind it (Eq. (attn_gla) rows 4-5, what
+ * gla_fwd_fused has as its epilogue):   y = LN(x) weight + bias,   out = y, or Swish(r) y.
+ *
+ *   x           DEVICE, x_dtype, [B,H,T,D] or [B,T,H,D] by `layout`; H = 1 for tokens                         (read)
+ *   weight, bias   DEVICE, fp32 [H,D], or NULL: ones, zeros                                                   (read)
+ *   eps         >= 0, under the square root
+ *   r_pre       DEVICE, x_dtype, like x, or NULL: no gate                                                     (read)
+ *   out         DEVICE, out_dtype, like x; may be x if the element types agree                                (written)
+ *
+ * 1 <= D <= 8192.  Statistics in fp32.  Needs no workspace and never allocates.
+ */
+int gla_norm_fwd(const void *x, const float *weight, const float *bias, float eps, const void *r_pre,
+                 int B, int H, int T, int D, int x_dtype, int out_dtype, int layout, void *out, gla_stream_t stream);
+
+/*
+ * gla_norm_bwd - gradients of gla_norm_fwd; mean and variance are taken from x again.
+ *
+ *   d_out           DEVICE, x_dtype, like x                                                                   (read)
+ *   dx              DEVICE, grad_dtype, like x                                                                (written)
+ *   dr              DEVICE, grad_dtype, like x; NULL exactly if r_pre is                                      (written)
+ *   dweight, dbias  DEVICE, fp32 [H,D], both or neither (NULL: not wanted); sums over batches and tokens, always added in
+ *                   one order                                                                                 (written)
+ *   workspace       DEVICE, 16-byte aligned, gla_norm_bwd_workspace_bytes(...) bytes
+ *
+ * Everything else as gla_norm_fwd.  Outputs must not alias inputs.
+ */
+int gla_norm_bwd(const void *x, const void *d_out, const float *weight, const float *bias, float eps, const void *r_pre,
+                 int B, int H, int T, int D, int x_dtype, int grad_dtype, int layout, void *dx, void *dr,
+                 float *dweight, float *dbias, void *workspace, size_t workspace_bytes, gla_stream_t stream);
+size_t gla_norm_bwd_workspace_bytes(int B, int H, int T, int D);
 
 /* Bytes of workspace gla_fwd_ex / gla_fwd_layout need for this problem (an upper bound over all
  * launch plans, so it does not depend on tuning options).  0 on invalid sizes. */

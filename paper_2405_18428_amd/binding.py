@@ -17,6 +17,8 @@ DT_F32, DT_BF16 = 0, 1
 OPT_CHUNKS_PER_SPAN, OPT_ENGINE, OPT_CARRY, OPT_BWD_SPLIT, OPT_RANGE_FALLBACK, OPT_LOOK_BACK_POLLS = 0, 1, 2, 3, 4, 5
 CARRY_AUTO, CARRY_KERNEL, CARRY_IN_OUTPUT_PASS = 0, 1, 2
 LAYOUT_BHTD, LAYOUT_BTHD = 0, 1
+DECAY_HEAD, DECAY_TOKEN = 0, 1
+ROPE_ADJACENT, ROPE_HALVES = 0, 1
 ENGINE_AUTO, ENGINE_RECURRENT, ENGINE_MFMA, ENGINE_MFMA_FP16 = 0, 1, 2, 3
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -86,6 +88,24 @@ def load_library():
     lib.gla_bwd_gates_workspace_bytes.argtypes = [i] * 6
     lib.gla_bwd_workspace_bytes.restype = sz
     lib.gla_bwd_workspace_bytes.argtypes = [i] * 6
+    f = ctypes.c_float
+    lib.gla_decay_fwd.restype = i
+    lib.gla_decay_fwd.argtypes = [vp] * 4 + [i, vp] + shape + [i] * 3 + [vp] * 4 + [sz, vp]
+    lib.gla_decay_bwd.restype = i
+    lib.gla_decay_bwd.argtypes = [vp] * 4 + [i] + [vp] * 4 + shape + [i] * 3 + [vp] * 6 + [sz, vp]
+    lib.gla_decay_step.restype = i
+    lib.gla_decay_step.argtypes = [vp] * 4 + [i] * 7 + [vp] * 4
+    for name in ("gla_decay_fwd_workspace_bytes", "gla_decay_bwd_workspace_bytes"):
+        getattr(lib, name).restype = sz
+        getattr(lib, name).argtypes = [i] * 6
+    lib.gla_rope.restype = i
+    lib.gla_rope.argtypes = [vp, vp, vp, ctypes.POINTER(i), i, f] + [i] * 10 + [vp] * 3
+    lib.gla_norm_fwd.restype = i
+    lib.gla_norm_fwd.argtypes = [vp] * 3 + [f, vp] + [i] * 7 + [vp] * 2
+    lib.gla_norm_bwd.restype = i
+    lib.gla_norm_bwd.argtypes = [vp] * 4 + [f, vp] + [i] * 7 + [vp] * 5 + [sz, vp]
+    lib.gla_norm_bwd_workspace_bytes.restype = sz
+    lib.gla_norm_bwd_workspace_bytes.argtypes = [i] * 4
     lib.gla_calibrate_mfma.restype = i
     lib.gla_calibrate_mfma.argtypes = [ctypes.POINTER(ctypes.c_double), vp]
     lib.gla_fwd_timed.restype = i
@@ -598,3 +618,234 @@ def gla_fwd_timed(q, k, v, log_alpha, grid_h, grid_w, scan_dir, out, final_state
                                  workspace.data_ptr(), workspace.numel(), _stream_ptr(stream, q),
                                  int(iters), ms))
     return [float(x) for x in ms]
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _want(name, t, shape, dtype, device):
+    """Raises unless t is a contiguous GPU tensor of this shape and element type on the call's device."""
+    if not t.is_cuda or t.device != device or not t.is_contiguous() or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be a contiguous GPU tensor {list(shape)} on the device of the others")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be of element type {dtype}")
+
+
+def _room(nbytes, workspace, device):
+    if workspace is None:
+        return _torch().empty((max(nbytes, 16),), dtype=_torch().uint8, device=device)
+    if not workspace.is_cuda or workspace.device != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous GPU tensor on the device of the others")
+    return workspace
+
+
+def _prep_decay(q, k, v, log_decay, layout, seq_lens, states):
+    torch = _torch()
+    if layout not in (LAYOUT_BHTD, LAYOUT_BTHD):
+        raise ValueError("unknown layout")
+    if q.dim() != 4 or v.dim() != 4:
+        raise ValueError("q, k, v must be 4-d")
+    _dt(q)
+    dev = q.device
+    _want("q", q, q.shape, q.dtype, dev)
+    _want("k", k, q.shape, q.dtype, dev)
+    _want("v", v, (*q.shape[:3], v.shape[3]), q.dtype, dev)
+    B, H, T, dk = q.shape if layout == LAYOUT_BHTD else (q.shape[0], q.shape[2], q.shape[1], q.shape[3])
+    kind = DECAY_HEAD if log_decay.dim() == 1 else DECAY_TOKEN
+    _want("log_decay", log_decay, (H,) if kind == DECAY_HEAD else q.shape[:3], torch.float32, dev)
+    if seq_lens is not None:
+        _want("seq_lens", seq_lens, (B,), torch.int32, dev)
+    dv = v.shape[3]
+    for name, t in states:
+        if t is not None:
+            _want(name, t, (B, H, dk, dv), torch.float32, dev)
+    return kind, B, H, T, dk, dv
+
+
+def gla_decay_fwd_workspace_bytes(B, H, T, dk, dv, qkv_dtype=DT_BF16) -> int:
+    return int(load_library().gla_decay_fwd_workspace_bytes(B, H, T, dk, dv, qkv_dtype))
+
+
+def gla_decay_bwd_workspace_bytes(B, H, T, dk, dv, qkv_dtype=DT_BF16) -> int:
+    return int(load_library().gla_decay_bwd_workspace_bytes(B, H, T, dk, dv, qkv_dtype))
+
+
+def gla_decay_fwd(q, k, v, log_decay, grid_h, grid_w, scan_dir=SCAN_ROW_FWD, layout=LAYOUT_BHTD, seq_lens=None,
+                  initial_state=None, out_dtype=None, want_final_state=True, out=None, final_state=None,
+                  workspace=None, stream=None):
+    """Linear attention with one decay a head: S_t = exp(log_decay) S_{t-1} + k_t^T v_t, o_t = q_t S_t.  log_decay fp32 [H], or a
+    number for each token ([B,H,T] or [B,T,H] by ``layout``).  ``seq_lens`` int32 [B]: each sequence's own length; rows of ``out``
+    behind it are left as they were.  Returns (out, final_state)."""
+    torch = _torch()
+    lib = load_library()
+    kind, B, H, T, dk, dv = _prep_decay(q, k, v, log_decay, layout, seq_lens,
+                                        (("initial_state", initial_state), ("final_state", final_state)))
+    if out is None:
+        out = _like(v, torch.float32 if out_dtype is None else out_dtype)
+    else:
+        _want("out", out, v.shape, out.dtype, q.device)
+    if final_state is None and want_final_state:
+        final_state = q.new_empty((B, H, dk, dv), dtype=torch.float32)
+    qdt = _dt(q)
+    workspace = _room(gla_decay_fwd_workspace_bytes(B, H, T, dk, dv, qdt), workspace, q.device)
+    with _on_device_of(q):
+        _check(lib.gla_decay_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), kind, _ptr(seq_lens),
+                                 B, H, T, dk, dv, grid_h, grid_w, scan_dir, qdt, _dt(out), layout, _ptr(initial_state),
+                                 out.data_ptr(), _ptr(final_state), workspace.data_ptr(),
+                                 workspace.numel() * workspace.element_size(), _stream_ptr(stream, q)))
+    return out, final_state
+
+
+def gla_decay_bwd(q, k, v, log_decay, d_out, grid_h, grid_w, scan_dir=SCAN_ROW_FWD, layout=LAYOUT_BHTD, seq_lens=None,
+                  initial_state=None, d_final_state=None, grad_dtype=None, want_d_log_decay=True, want_d_initial_state=False,
+                  workspace=None, stream=None):
+    """Gradients of gla_decay_fwd from those of its outputs (``d_out``, like v) and of its final state (``d_final_state`` or None).
+    Returns (dq, dk, dv, dlog_decay or None, d_initial_state or None); the first three of ``grad_dtype`` (fp32)."""
+    torch = _torch()
+    lib = load_library()
+    kind, B, H, T, dk, dv = _prep_decay(q, k, v, log_decay, layout, seq_lens,
+                                        (("initial_state", initial_state), ("d_final_state", d_final_state)))
+    _want("d_out", d_out, v.shape, q.dtype, q.device)
+    gdt = torch.float32 if grad_dtype is None else grad_dtype
+    dq, dk_, dv_ = _like(q, gdt), _like(k, gdt), _like(v, gdt)
+    dg = _like(log_decay, torch.float32) if want_d_log_decay else None
+    ds = q.new_empty((B, H, dk, dv), dtype=torch.float32) if want_d_initial_state else None
+    qdt = _dt(q)
+    workspace = _room(gla_decay_bwd_workspace_bytes(B, H, T, dk, dv, qdt), workspace, q.device)
+    with _on_device_of(q):
+        _check(lib.gla_decay_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), kind, _ptr(seq_lens),
+                                 d_out.data_ptr(), _ptr(initial_state), _ptr(d_final_state), B, H, T, dk, dv, grid_h, grid_w,
+                                 scan_dir, qdt, _dt(dq), layout, dq.data_ptr(), dk_.data_ptr(), dv_.data_ptr(), _ptr(dg), _ptr(ds),
+                                 workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(stream, q)))
+    return dq, dk_, dv_, dg, ds
+
+
+def gla_decay_step(q, k, v, log_decay, state, out_dtype=None, out=None, state_out=None, stream=None):
+    """One token of gla_decay_fwd for each sequence: q, k [B,H,dk], v [B,H,dv], log_decay fp32 [H] or [B,H], state fp32 [B,H,dk,dv].
+    The new state goes to ``state_out``, in place (``state``) if that is None.  Returns (out, state_out)."""
+    torch = _torch()
+    lib = load_library()
+    if q.dim() != 3 or v.dim() != 3:
+        raise ValueError("q, k must be [B,H,dk] and v [B,H,dv]")
+    B, H, dk = q.shape
+    dv = v.shape[2]
+    qdt, dev = _dt(q), q.device
+    _want("q", q, (B, H, dk), q.dtype, dev)
+    _want("k", k, (B, H, dk), q.dtype, dev)
+    _want("v", v, (B, H, dv), q.dtype, dev)
+    kind = DECAY_HEAD if log_decay.dim() == 1 else DECAY_TOKEN
+    _want("log_decay", log_decay, (H,) if kind == DECAY_HEAD else (B, H), torch.float32, dev)
+    _want("state", state, (B, H, dk, dv), torch.float32, dev)
+    if state_out is None:
+        state_out = state
+    else:
+        _want("state_out", state_out, (B, H, dk, dv), torch.float32, dev)
+    if out is None:
+        out = _like(v, torch.float32 if out_dtype is None else out_dtype)
+    else:
+        _want("out", out, v.shape, out.dtype, dev)
+    with _on_device_of(q):
+        _check(lib.gla_decay_step(q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), kind, B, H, dk, dv, qdt, _dt(out),
+                                  state.data_ptr(), state_out.data_ptr(), out.data_ptr(), _stream_ptr(stream, q)))
+    return out, state_out
+
+
+def gla_rope(q, k, sections, grid_h=0, grid_w=0, positions=None, base=10000.0, pairing=ROPE_ADJACENT, inverse=False,
+             layout=LAYOUT_BHTD, out_q=None, out_k=None, stream=None):
+    """Rotary positions: the first channels of each head fall into ``sections`` (even numbers), one an axis, and pair i of a section of w
+    channels is turned by position * base^(-2 i / w).  ``positions`` int32 [B,T,axes], or None: the token's number, its row and
+    column, or its frame, row and column on the grid.  ``inverse`` turns back (the backward pass).  q, k [B,H,T,d] or [B,T,H,d];
+    k may be None; ``out_q`` / ``out_k`` may be q / k.  Returns (q', k')."""
+    torch = _torch()
+    lib = load_library()
+    if layout not in (LAYOUT_BHTD, LAYOUT_BTHD):
+        raise ValueError("unknown layout")
+    if q.dim() != 4:
+        raise ValueError("q must be 4-d")
+    dt, dev = _dt(q), q.device
+    _want("q", q, q.shape, q.dtype, dev)
+    if k is not None:
+        _want("k", k, q.shape, q.dtype, dev)
+    B, H, T, d = q.shape if layout == LAYOUT_BHTD else (q.shape[0], q.shape[2], q.shape[1], q.shape[3])
+    axes = len(sections)
+    if positions is not None:
+        _want("positions", positions, (B, T, axes), torch.int32, dev)
+    if k is None and out_k is not None:
+        raise ValueError("out_k without k")
+    out_q = _like(q, q.dtype) if out_q is None else out_q
+    out_k = _like(k, k.dtype) if out_k is None and k is not None else out_k
+    for name, t in (("out_q", out_q), ("out_k", out_k)):
+        if t is not None:
+            _want(name, t, q.shape, q.dtype, dev)
+    secs = (ctypes.c_int * max(axes, 1))(*[int(w) for w in sections])
+    with _on_device_of(q):
+        _check(lib.gla_rope(q.data_ptr(), _ptr(k), _ptr(positions), secs, axes, float(base), pairing, int(bool(inverse)), B, H, T, d,
+                            grid_h, grid_w, dt, layout, out_q.data_ptr(), _ptr(out_k), _stream_ptr(stream, q)))
+    return out_q, out_k
+
+
+def _prep_norm(x, weight, bias, r_pre, layout):
+    """Sizes (B, H, T, D) of [B,H,T,D], [B,T,H,D] or [B,T,D] rows after checking the tensors."""
+    torch = _torch()
+    if layout not in (LAYOUT_BHTD, LAYOUT_BTHD):
+        raise ValueError("unknown layout")
+    if x.dim() not in (3, 4):
+        raise ValueError("x must be [B,H,T,D], [B,T,H,D] or [B,T,D]")
+    _dt(x)
+    _want("x", x, x.shape, x.dtype, x.device)
+    if x.dim() == 3:
+        B, H, T, D = x.shape[0], 1, x.shape[1], x.shape[2]
+    else:
+        B, H, T, D = x.shape if layout == LAYOUT_BHTD else (x.shape[0], x.shape[2], x.shape[1], x.shape[3])
+    for name, t in (("weight", weight), ("bias", bias)):
+        if t is not None:
+            _want(name, t, (D,) if t.dim() == 1 and H == 1 else (H, D), torch.float32, x.device)
+    if r_pre is not None:
+        _want("r_pre", r_pre, x.shape, x.dtype, x.device)
+    return B, H, T, D
+
+
+def gla_norm_fwd(x, weight=None, bias=None, eps=1e-5, r_pre=None, layout=LAYOUT_BHTD, out_dtype=None, out=None, stream=None):
+    """Layer norm of each row of x ([B,H,T,D], [B,T,H,D] by ``layout``, or tokens [B,T,D]), times Swish(r_pre) if given.  weight,
+    bias fp32 [H,D] ([D] for tokens) or None.  The result has ``out_dtype`` (x's)."""
+    lib = load_library()
+    B, H, T, D = _prep_norm(x, weight, bias, r_pre, layout)
+    if out is None:
+        out = _like(x, x.dtype if out_dtype is None else out_dtype)
+    else:
+        _want("out", out, x.shape, out.dtype, x.device)
+        if out.data_ptr() == x.data_ptr() and out.dtype != x.dtype:
+            raise ValueError("in place only with one element type")
+    with _on_device_of(x):
+        _check(lib.gla_norm_fwd(x.data_ptr(), _ptr(weight), _ptr(bias), float(eps), _ptr(r_pre), B, H, T, D, _dt(x), _dt(out), layout,
+                                out.data_ptr(), _stream_ptr(stream, x)))
+    return out
+
+
+def gla_norm_bwd_workspace_bytes(B, H, T, D) -> int:
+    return int(load_library().gla_norm_bwd_workspace_bytes(B, H, T, D))
+
+
+def gla_norm_bwd(x, d_out, weight=None, bias=None, eps=1e-5, r_pre=None, layout=LAYOUT_BHTD, grad_dtype=None, want_d_weight=None,
+                 workspace=None, stream=None):
+    """Gradients of gla_norm_fwd: (dx, dr or None, dweight, dbias).  dx and dr are of ``grad_dtype`` (fp32), the others fp32 [H,D] (like
+    weight if that is given), or None without ``want_d_weight`` (default: whether there is a weight or a bias)."""
+    torch = _torch()
+    lib = load_library()
+    B, H, T, D = _prep_norm(x, weight, bias, r_pre, layout)
+    _want("d_out", d_out, x.shape, x.dtype, x.device)
+    gdt = torch.float32 if grad_dtype is None else grad_dtype
+    dx = _like(x, gdt)
+    dr = _like(x, gdt) if r_pre is not None else None
+    dw = db = None
+    if want_d_weight or (want_d_weight is None and (weight is not None or bias is not None)):
+        like = weight if weight is not None else bias
+        shape = (H, D) if like is None else like.shape
+        dw, db = x.new_empty(shape, dtype=torch.float32), x.new_empty(shape, dtype=torch.float32)
+    workspace = _room(gla_norm_bwd_workspace_bytes(B, H, T, D), workspace, x.device)
+    with _on_device_of(x):
+        _check(lib.gla_norm_bwd(x.data_ptr(), d_out.data_ptr(), _ptr(weight), _ptr(bias), float(eps), _ptr(r_pre), B, H, T, D, _dt(x), _dt(dx),
+                                layout, dx.data_ptr(), _ptr(dr), _ptr(dw), _ptr(db), workspace.data_ptr(),
+                                workspace.numel() * workspace.element_size(), _stream_ptr(stream, x)))
+    return dx, dr, dw, db

@@ -1,0 +1,295 @@
+// Linear attention with one decay a head: the walks that go forward (outputs; for the backward pass dq), the local states of spans and
+// the chain that joins them, and the form for single tokens.  The mathematics and the chunk are in gla_decay.h and gla_decay_util.h.
+#include "gla_decay_util.h"
+
+namespace gla {
+namespace {
+
+constexpr int kThreads = 256;
+
+template <typename E, int M, int N>
+struct WalkLds {
+    static constexpr int kX = 0, kY = Tile<E, M>::kBytes, kZ = 2 * Tile<E, M>::kBytes, kP = kZ + Tile<E, N>::kBytes,
+                         kG = kP + Pairs<E>::kBytes, kFlow = kG + (int)sizeof(Gates<Elem<E>::kChunk>),
+                         kBytes = kFlow + 4 * Elem<E>::kChunk * 4;
+};
+
+// GRAD: the walk for dq, with the dot products and the states that the gates' gradient takes
+template <typename E, int M, int N, bool GRAD>
+__global__ __launch_bounds__(kThreads, 2) void decay_walk_kernel(const DecayWalk p) {
+    constexpr int C = Elem<E>::kChunk;
+    typedef WalkLds<E, M, N> L;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const Tile<E, M> tx{lds + L::kX}, ty{lds + L::kY};
+    const Tile<E, N> tz{lds + L::kZ};
+    const Pairs<E> P{lds + L::kP};
+    Gates<C> &gt = *reinterpret_cast<Gates<C> *>(lds + L::kG);
+    float *flow_part = reinterpret_cast<float *>(lds + L::kFlow);
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int bh = blockIdx.x / p.c.nspans, sp = blockIdx.x - bh * p.c.nspans;
+    const Order ord = order_of(p.c, bh);
+    const int len = ord.len;
+    const int s0 = sp * p.c.span_len, s1 = min(s0 + p.c.span_len, p.c.T), end = min(s1, len);
+    const int m = p.r.m, n = p.r.n;
+    const size_t cells = (size_t)m * n;
+    const Rows rx = rows_of<E>(p.c, p.r.x, bh, m), ry = rows_of<E>(p.c, p.r.y, bh, m), rz = rows_of<E>(p.c, p.r.z, bh, n);
+    const Rows ro = rows_of<E>(p.c, p.r.out, bh, n, p.out_dtype == GLA_DT_BF16 ? 2 : 4);
+
+    Walker<E, M, N> wk;
+    wk.init(tid);
+    Pieces<E, M, kThreads> px, py;
+    Pieces<E, N, kThreads> pz;
+    float gate = 0.f;
+    auto issue = [&](int s) __attribute__((always_inline)) {
+        const int tid = recompute_per_chunk(threadIdx.x), lane = tid & 63, count = min(C, end - s);
+        auto token = [&](int i) __attribute__((always_inline)) { return (long long)ord.token(s + i); };
+        px.issue(rx, tid, count, token);
+        py.issue(ry, tid, count, token);
+        pz.issue(rz, tid, count, token);
+        if (tid < 64) gate = lane < count ? gate_of(p.c, ord, bh, s + lane) : 0.f;
+    };
+    if (s0 < end) issue(s0);
+    wk.load_state(p.state_in == nullptr ? nullptr : p.state_in + (size_t)blockIdx.x * cells, m, n, p.state_t);
+    for (int s = s0; s < end; s += C) {
+        const int count = min(C, end - s);
+        px.commit(rx, tid, tx);
+        py.commit(ry, tid, ty);
+        pz.commit(rz, tid, tz);
+        if (tid < 64) form_gates(gt, gate, lane);
+        __syncthreads();
+        if (s + C < end) issue(s + C);
+        wk.pairs(tx, ty, P, gt);
+        wk.from_state(tx, gt);
+        __syncthreads();
+        wk.template advance<true>(ty, tz, P, gt);
+        auto token = [&](int i) __attribute__((always_inline)) { return (long long)ord.token(s + i); };
+        wk.store_rows(ro, p.out_dtype, count, token);
+        if (GRAD && p.r.dot != nullptr) {
+            const Rows rd = rows_of<E>(p.c, p.r.dot, bh, n);
+            wk.template dot_rows<false>(rd, tz, flow_part, count, token);
+        }
+        const int e = s + count;
+        if (GRAD && p.anchors != nullptr && (e < len ? e % kFlowBlock == 0 : p.anchor_last != 0))
+            wk.store_state(p.anchors + ((size_t)bh * decay_blocks(p.c.T) + (e - 1) / kFlowBlock) * cells, m, n, p.state_t);
+        __syncthreads();
+        if (GRAD && p.r.dot != nullptr && tid < count)
+            p.r.flow[(size_t)bh * p.c.T + s + tid] =
+                flow_part[tid] + flow_part[C + tid] + flow_part[2 * C + tid] + flow_part[3 * C + tid];
+    }
+    if (p.state_out != nullptr && sp == p.c.nspans - 1) wk.store_state(p.state_out + (size_t)bh * cells, m, n, p.state_t);
+    if (GRAD) clear_behind<kThreads>(ro, p.out_dtype == GLA_DT_BF16 ? 2 : 4, len, s0, s1, tid);
+}
+
+struct StatePair {
+    DecayWalk w[2];
+};
+
+// Local states: y, z of the role only.  blockIdx.y = 1: the reversed recurrence
+template <typename E, int M, int N>
+__global__ __launch_bounds__(kThreads, 2) void decay_state_kernel(const StatePair both) {
+    constexpr int C = Elem<E>::kChunk;
+    typedef WalkLds<E, M, N> L;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const Tile<E, M> ty{lds + L::kY - L::kY};
+    const Tile<E, N> tz{lds + L::kZ - L::kY};
+    Gates<C> &gt = *reinterpret_cast<Gates<C> *>(lds + L::kZ - L::kY + Tile<E, N>::kBytes);
+    const Pairs<E> none{nullptr};
+
+    const bool back = blockIdx.y != 0;
+    const DecayWalk &p = both.w[blockIdx.y];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int walked = p.c.nspans - 1;                   // nobody needs the last one's
+    const int bh = blockIdx.x / walked, sp = blockIdx.x - bh * walked + (back ? 1 : 0);
+    const Order ord = order_of(p.c, bh);
+    const int s0 = sp * p.c.span_len, end = min(min(s0 + p.c.span_len, p.c.T), ord.len);
+    const int m = p.r.m, n = p.r.n;
+    const Rows ry = rows_of<E>(p.c, p.r.y, bh, m), rz = rows_of<E>(p.c, p.r.z, bh, n);
+
+    Walker<E, M, N> wk;
+    wk.init(tid);
+    wk.load_state(nullptr, m, n, false);
+    Pieces<E, M, kThreads> py;
+    Pieces<E, N, kThreads> pz;
+    float gate = 0.f, sum = 0.f;
+    const int chunks = s0 < end ? (end - s0 + C - 1) / C : 0;
+    auto issue = [&](int i) __attribute__((always_inline)) {
+        const int tid = recompute_per_chunk(threadIdx.x), lane = tid & 63;
+        const int s = s0 + (back ? chunks - 1 - i : i) * C, e = min(s + C, end);
+        auto token = [&](int row) __attribute__((always_inline)) { return (long long)ord.token(back ? e - 1 - row : s + row); };
+        py.issue(ry, tid, e - s, token);
+        pz.issue(rz, tid, e - s, token);
+        if (tid < 64) gate = lane < e - s ? gate_of(p.c, ord, bh, back ? e - lane : s + lane) : 0.f;
+    };
+    if (chunks > 0) issue(0);
+    for (int i = 0; i < chunks; ++i) {
+        py.commit(ry, tid, ty);
+        pz.commit(rz, tid, tz);
+        if (tid < 64) form_gates(gt, gate, lane);
+        __syncthreads();
+        if (i + 1 < chunks) issue(i + 1);
+        sum += gt.sum;
+        wk.template advance<false>(ty, tz, none, gt);
+        __syncthreads();
+    }
+    const size_t at = (size_t)bh * p.c.nspans + sp;
+    wk.store_state(p.local + at * m * n, m, n, false);
+    if (tid == 0) p.decay[at] = sum;
+}
+
+// local [B*H, nspans, cells]: entry sp becomes the state that enters span sp
+__global__ __launch_bounds__(kThreads) void decay_carry_kernel(const float *first, float *local, const float *decay, int nspans, int cells,
+                                                               int reversed) {
+    const int bh = blockIdx.y, i = (blockIdx.x * kThreads + threadIdx.x);
+    if (i >= cells) return;
+    float *u = local + (size_t)bh * nspans * cells + i;
+    float s = first != nullptr ? first[(size_t)bh * cells + i] : 0.f;
+    for (int k = 0; k < nspans - 1; ++k) {
+        const int sp = reversed ? nspans - 1 - k : k;
+        const float own = u[(size_t)sp * cells];
+        u[(size_t)sp * cells] = s;
+        s = fmaf(exp2_fast(decay[(size_t)bh * nspans + sp]), s, own);
+    }
+    u[(size_t)(reversed ? 0 : nspans - 1) * cells] = s;
+}
+
+template <typename K>
+hipError_t configured(K kernel, int bytes, std::atomic<bool> (&done)[kMaxDevices]) {
+    return allow_dynamic_lds(reinterpret_cast<const void *>(kernel), bytes, done);
+}
+
+template <typename E, int M, int N, bool GRAD>
+hipError_t walk(const DecayWalk &w, hipStream_t stream) {
+    static std::atomic<bool> done[kMaxDevices];
+    constexpr int bytes = WalkLds<E, M, N>::kBytes;
+    const hipError_t e = configured(decay_walk_kernel<E, M, N, GRAD>, bytes, done);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((decay_walk_kernel<E, M, N, GRAD>), dim3((unsigned)(w.c.B * w.c.H * w.c.nspans)), dim3(kThreads), bytes, stream, w);
+    return hipGetLastError();
+}
+
+template <typename E, int M, int N>
+hipError_t states(const StatePair &w, int directions, hipStream_t stream) {
+    static std::atomic<bool> done[kMaxDevices];
+    constexpr int bytes = Tile<E, M>::kBytes + Tile<E, N>::kBytes + (int)sizeof(Gates<Elem<E>::kChunk>);
+    const hipError_t e = configured(decay_state_kernel<E, M, N>, bytes, done);
+    if (e != hipSuccess) return e;
+    const DecayCall &c = w.w[0].c;
+    hipLaunchKernelGGL((decay_state_kernel<E, M, N>), dim3((unsigned)(c.B * c.H * (c.nspans - 1)), (unsigned)directions), dim3(kThreads),
+                       bytes, stream, w);
+    return hipGetLastError();
+}
+
+// One token: a wave takes 64 / (N / 4) rows of a state at a time, a lane four columns of it; a work-group all rows of one (batch, head).
+// Bound by the state's way in and out.
+template <typename E>
+__device__ inline float element(const void *p, size_t i) {
+    if constexpr (sizeof(E) == 2) return bf16_bits_to_float(static_cast<const uint16_t *>(p)[i]);
+    else return static_cast<const float *>(p)[i];
+}
+
+template <typename E>
+__global__ __launch_bounds__(kThreads) void decay_step_kernel(const void *q, const void *k, const void *v, const float *log_decay, int kind,
+                                                              int H, int dk, int dv, int out_dtype, const float *state, float *state_out,
+                                                              void *out) {
+    __shared__ float s_q[kDecayMaxD], s_k[kDecayMaxD], s_o[8 * kDecayMaxD];
+    const int tid = threadIdx.x, bh = blockIdx.x, h = bh % H;
+    if (tid < dk) {
+        s_q[tid] = element<E>(q, (size_t)bh * dk + tid);
+        s_k[tid] = element<E>(k, (size_t)bh * dk + tid);
+    }
+    const float a = exp2_fast(fmaxf(log_decay[kind == kDecayHead ? h : bh] * kLog2e, -65536.f));
+    __syncthreads();
+    const size_t cells = (size_t)dk * dv;
+    const float *s = state + bh * cells;
+    float *t = state_out + bh * cells;
+    // 32 lanes x 4 columns cover a row of up to 128; 8 rows a step of the work-group
+    const int col = (tid & 31) * 4, row0 = tid >> 5;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    if (col + 4 <= dv) {
+        f32x4 x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = element<E>(v, (size_t)bh * dv + col + j);
+        for (int r = row0; r < dk; r += 8) {
+            f32x4 c;
+            __builtin_memcpy(&c, s + (size_t)r * dv + col, 16);
+            const float kr = s_k[r], qr = s_q[r];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                c[j] = fmaf(a, c[j], kr * x[j]);
+                o[j] = fmaf(qr, c[j], o[j]);
+            }
+            __builtin_memcpy(t + (size_t)r * dv + col, &c, 16);
+        }
+    } else {
+        for (int r = row0; r < dk; r += 8) {
+            const float kr = s_k[r], qr = s_q[r];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (col + j >= dv) continue;
+                const float c = fmaf(a, s[(size_t)r * dv + col + j], kr * element<E>(v, (size_t)bh * dv + col + j));
+                t[(size_t)r * dv + col + j] = c;
+                o[j] = fmaf(qr, c, o[j]);
+            }
+        }
+    }
+    *reinterpret_cast<f32x4 *>(&s_o[row0 * kDecayMaxD + col]) = o;
+    __syncthreads();
+    if (tid < dv) {
+        float y = 0.f;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) y += s_o[r * kDecayMaxD + tid];
+        const size_t at = (size_t)bh * dv + tid;
+        if (out_dtype == GLA_DT_BF16) static_cast<uint16_t *>(out)[at] = float_to_bf16_bits(y);
+        else static_cast<float *>(out)[at] = y;
+    }
+}
+
+}  // namespace
+
+template <typename E, bool GRAD>
+static hipError_t walk_of_size(const DecayWalk &w, hipStream_t stream) {
+    const bool m = w.r.m > 64, n = w.r.n > 64;
+    if (m) return n ? walk<E, 128, 128, GRAD>(w, stream) : walk<E, 128, 64, GRAD>(w, stream);
+    return n ? walk<E, 64, 128, GRAD>(w, stream) : walk<E, 64, 64, GRAD>(w, stream);
+}
+
+hipError_t launch_decay_walk(const DecayWalk &w, int dtype, hipStream_t stream) {
+    if (dtype == GLA_DT_BF16) return w.grad ? walk_of_size<uint16_t, true>(w, stream) : walk_of_size<uint16_t, false>(w, stream);
+    return w.grad ? walk_of_size<float, true>(w, stream) : walk_of_size<float, false>(w, stream);
+}
+
+hipError_t launch_decay_states(const DecayWalk &w, const DecayWalk *back, int dtype, hipStream_t stream) {
+    StatePair both;
+    both.w[0] = w;
+    both.w[1] = back != nullptr ? *back : w;
+    const int d = back != nullptr ? 2 : 1;
+    const bool m = w.r.m > 64, n = w.r.n > 64;
+    if (dtype == GLA_DT_BF16) {
+        if (m) return n ? states<uint16_t, 128, 128>(both, d, stream) : states<uint16_t, 128, 64>(both, d, stream);
+        return n ? states<uint16_t, 64, 128>(both, d, stream) : states<uint16_t, 64, 64>(both, d, stream);
+    }
+    if (m) return n ? states<float, 128, 128>(both, d, stream) : states<float, 128, 64>(both, d, stream);
+    return n ? states<float, 64, 128>(both, d, stream) : states<float, 64, 64>(both, d, stream);
+}
+
+hipError_t launch_decay_carry(const DecayCall &c, const float *first, float *local, const float *decay, bool reversed, hipStream_t stream) {
+    const int cells = c.dk * c.dv;
+    hipLaunchKernelGGL(decay_carry_kernel, dim3((unsigned)((cells + kThreads - 1) / kThreads), (unsigned)(c.B * c.H)), dim3(kThreads), 0,
+                       stream, first, local, decay, c.nspans, cells, reversed ? 1 : 0);
+    return hipGetLastError();
+}
+
+hipError_t launch_decay_step(const void *q, const void *k, const void *v, const float *log_decay, int kind, int B, int H, int dk, int dv,
+                             int dtype, int out_dtype, const float *state, float *state_out, void *out, hipStream_t stream) {
+    const dim3 grid((unsigned)(B * H));
+    if (dtype == GLA_DT_BF16)
+        hipLaunchKernelGGL(decay_step_kernel<uint16_t>, grid, dim3(kThreads), 0, stream, q, k, v, log_decay, kind, H, dk, dv, out_dtype, state,
+                           state_out, out);
+    else
+        hipLaunchKernelGGL(decay_step_kernel<float>, grid, dim3(kThreads), 0, stream, q, k, v, log_decay, kind, H, dk, dv, out_dtype, state,
+                           state_out, out);
+    return hipGetLastError();
+}
+
+}  // namespace gla

@@ -1,0 +1,331 @@
+// Layer norm over the channels of each row, y = (x - mean) / sqrt(var + eps) * weight + bias, with the output gate of the mixer behind it
+// if r is given, y * r sigmoid(r) (Eq. (attn_gla) rows 4-5 of the DiG paper), and both backward:
+//   n = (x - mean) rstd,  dy = dO r sigmoid(r) (or dO),  dn = dy weight,
+//   dx = rstd (dn - mean(dn) - n mean(dn n)),   dr = dO y sigmoid(r) (1 + r (1 - sigmoid(r))),
+//   dweight = sum over rows of dy n,   dbias = sum over rows of dy.
+// A row is held in registers by a group of lanes (16, 64, 256 or 1024 by its width), so it is read once; mean and variance are taken in two
+// steps from these registers, and the backward pass takes them again instead of reading them.  Each group stays with one head, whose weights
+// it holds, and walks the head's rows; the sums for dweight and dbias stay in its registers, one partial sum a slot goes to
+// memory, and a second kernel adds the slots in one order.  Bound by HBM.
+#include "gla_ops.h"
+
+namespace gla {
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+
+constexpr int kEach = 8;             // channels of a piece
+
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), bf16x2));
+}
+
+// Channels c0 .. c0 + 7 of a row of D, those from D on as zeros
+template <typename E>
+__device__ __forceinline__ void load_piece(const char *row, int c0, int D, float (&x)[kEach]) {
+    if (c0 + kEach <= D) {
+        if constexpr (sizeof(E) == 2) {
+            u32x4 b;
+            __builtin_memcpy(&b, row + c0 * 2, 16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x[2 * j] = __builtin_bit_cast(float, b[j] << 16);
+                x[2 * j + 1] = __builtin_bit_cast(float, b[j] & 0xffff0000u);
+            }
+        } else {
+            f32x4 v[2];
+            __builtin_memcpy(v, row + c0 * 4, 32);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = v[j >> 2][j & 3];
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        x[j] = 0.f;
+        if (c0 + j < D) {
+            if constexpr (sizeof(E) == 2) x[j] = bf16_bits_to_float(reinterpret_cast<const uint16_t *>(row)[c0 + j]);
+            else x[j] = reinterpret_cast<const float *>(row)[c0 + j];
+        }
+    }
+}
+__device__ __forceinline__ void store_piece(char *row, int c0, int D, int dtype, const float (&x)[kEach]) {
+    if (c0 + kEach <= D) {
+        if (dtype == GLA_DT_BF16) {
+            const u32x4 b = {pack(x[0], x[1]), pack(x[2], x[3]), pack(x[4], x[5]), pack(x[6], x[7])};
+            __builtin_memcpy(row + c0 * 2, &b, 16);
+        } else {
+            const f32x4 v[2] = {{x[0], x[1], x[2], x[3]}, {x[4], x[5], x[6], x[7]}};
+            __builtin_memcpy(row + c0 * 4, v, 32);
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+        if (c0 + j < D) {
+            if (dtype == GLA_DT_BF16) reinterpret_cast<uint16_t *>(row)[c0 + j] = (uint16_t)pack(x[j], 0.f);
+            else reinterpret_cast<float *>(row)[c0 + j] = x[j];
+        }
+}
+
+// Sum over the LANES lanes of a group, in every lane.  Groups wider than a wave are the whole work-group and go through LDS.
+template <int LANES, int SUMS>
+__device__ __forceinline__ void group_sum(float (&v)[SUMS], float *lds) {
+#pragma unroll
+    for (int s = 0; s < SUMS; ++s)
+#pragma unroll
+        for (int d = 1; d < (LANES < 64 ? LANES : 64); d *= 2) v[s] += __shfl_xor(v[s], d);
+    if constexpr (LANES > 64) {
+        constexpr int kWaves = LANES / 64;
+        const int w = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int s = 0; s < SUMS; ++s) lds[s * kWaves + w] = v[s];
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < SUMS; ++s) {
+            v[s] = 0.f;
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) v[s] += lds[s * kWaves + i];
+        }
+        __syncthreads();
+    }
+}
+
+// Which rows a group takes: head h, rows number first, first + step, ... of the head's B * T
+struct Walk {
+    int h, slot;
+    uint32_t first, step;
+};
+// Neighbouring groups take rows that are neighbours in memory: of one head where a head's rows lie together, of neighbouring heads where a
+// token's heads do
+__device__ __forceinline__ Walk walk_of(const NormParams &p, int groups, int gi) {
+    Walk w;
+    if (p.layout == GLA_LAYOUT_BHTD || p.H == 1) {
+        const int per_head = p.slots / groups;                   // work-groups of a head
+        w.h = blockIdx.x / per_head;
+        w.slot = (blockIdx.x - w.h * per_head) * groups + gi;
+    } else {
+        const uint32_t l = blockIdx.x * (uint32_t)groups + gi;
+        w.slot = (int)(l / (uint32_t)p.H);
+        w.h = (int)(l - (uint32_t)w.slot * p.H);
+    }
+    w.first = (uint32_t)w.slot;
+    w.step = (uint32_t)p.slots;
+    return w;
+}
+__device__ __forceinline__ long long row_of(const NormParams &p, int h, uint32_t i) {
+    if (p.layout != GLA_LAYOUT_BHTD) return (long long)i * p.H + h;
+    const uint32_t b = i / (uint32_t)p.T;
+    return ((long long)b * p.H + h) * p.T + (i - b * (uint32_t)p.T);
+}
+
+template <int LANES>
+struct Shape {
+    static constexpr int kThreads = LANES > 256 ? LANES : 256, kGroups = kThreads / LANES;
+};
+
+template <typename E, int LANES, int NP, bool GATED, bool BACK>
+__global__ __launch_bounds__(Shape<LANES>::kThreads) void norm_kernel(const NormParams p) {
+    constexpr int kGroups = Shape<LANES>::kGroups;
+    __shared__ float lds[2 * (LANES > 64 ? LANES / 64 : 1)];
+    const int gi = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+    const Walk wk = walk_of(p, kGroups, gi);
+    const uint32_t rows = (uint32_t)p.B * (uint32_t)p.T;         // < 2^31 (host check)
+    const int D = p.D;
+    const float inv = 1.f / (float)D;
+    const int out_size = p.out_dtype == GLA_DT_BF16 ? 2 : 4;
+    const bool mine = wk.slot < p.slots && wk.h < p.H;
+
+    float w[NP][kEach], b[NP][kEach], dw[BACK ? NP : 1][kEach], db[BACK ? NP : 1][kEach];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        const int c = (i * LANES + lane) * kEach;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            w[i][j] = 1.f;
+            b[i][j] = 0.f;
+            if constexpr (BACK) dw[i][j] = db[i][j] = 0.f;
+        }
+        if (mine && p.weight != nullptr) load_piece<float>(reinterpret_cast<const char *>(p.weight + (size_t)wk.h * D), c, D, w[i]);
+        if (mine && p.bias != nullptr) load_piece<float>(reinterpret_cast<const char *>(p.bias + (size_t)wk.h * D), c, D, b[i]);
+    }
+    // (groups of one wave or less end on their own; the wider ones are the work-group)
+    for (uint32_t i0 = wk.first; mine && i0 < rows; i0 += wk.step) {
+        const long long row = row_of(p, wk.h, i0);
+        float x[NP][kEach], r[GATED ? NP : 1][kEach], o[BACK ? NP : 1][kEach];
+        const char *px = static_cast<const char *>(p.x) + row * D * (int)sizeof(E);
+        const char *pr = static_cast<const char *>(p.r_pre) + row * D * (int)sizeof(E);
+        const char *po = static_cast<const char *>(p.d_out) + row * D * (int)sizeof(E);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int c = (i * LANES + lane) * kEach;
+            load_piece<E>(px, c, D, x[i]);
+            if constexpr (GATED) load_piece<E>(pr, c, D, r[i]);
+            if constexpr (BACK) load_piece<E>(po, c, D, o[i]);
+        }
+        float s[1] = {0.f};
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) s[0] += x[i][j];
+        group_sum<LANES, 1>(s, lds);
+        const float mean = s[0] * inv;
+        s[0] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                x[i][j] = (i * LANES + lane) * kEach + j < D ? x[i][j] - mean : 0.f;
+                s[0] = fmaf(x[i][j], x[i][j], s[0]);
+            }
+        group_sum<LANES, 1>(s, lds);
+        const float rstd = 1.f / __builtin_sqrtf(fmaf(s[0], inv, p.eps));
+        if constexpr (!BACK) {
+            char *po_ = static_cast<char *>(p.out) + row * D * out_size;
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                float y[kEach];
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) {
+                    y[j] = fmaf(x[i][j] * rstd, w[i][j], b[i][j]);
+                    if constexpr (GATED) y[j] *= r[i][j] / (1.f + __expf(-r[i][j]));
+                }
+                store_piece(po_, (i * LANES + lane) * kEach, D, p.out_dtype, y);
+            }
+        } else {
+            char *pdx = static_cast<char *>(p.dx) + row * D * out_size;
+            char *pdr = static_cast<char *>(p.dr) + row * D * out_size;
+            float m[2] = {0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                float dr[kEach];
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) {
+                    const float n = x[i][j] * rstd;
+                    float dy = o[i][j];
+                    if constexpr (GATED) {
+                        const float sg = 1.f / (1.f + __expf(-r[i][j])), gate = r[i][j] * sg;
+                        dr[j] = o[i][j] * fmaf(n, w[i][j], b[i][j]) * fmaf(gate, 1.f - sg, sg);
+                        dy *= gate;
+                    }
+                    dw[i][j] = fmaf(dy, n, dw[i][j]);
+                    db[i][j] += dy;
+                    const float dn = dy * w[i][j];
+                    m[0] += dn;
+                    m[1] = fmaf(dn, n, m[1]);
+                    x[i][j] = n;
+                    o[i][j] = dn;
+                }
+                if constexpr (GATED) store_piece(pdr, (i * LANES + lane) * kEach, D, p.out_dtype, dr);
+            }
+            group_sum<LANES, 2>(m, lds);
+            const float m0 = m[0] * inv, m1 = m[1] * inv;
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                float dx[kEach];
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) dx[j] = rstd * (o[i][j] - m0 - x[i][j] * m1);
+                store_piece(pdx, (i * LANES + lane) * kEach, D, p.out_dtype, dx);
+            }
+        }
+    }
+    if constexpr (BACK) {
+        if (!mine) return;
+        float *part = p.part + ((size_t)wk.slot * p.H + wk.h) * D;
+        const size_t second = (size_t)p.slots * p.H * D;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int c = (i * LANES + lane) * kEach;
+            store_piece(reinterpret_cast<char *>(part), c, D, GLA_DT_F32, dw[i]);
+            store_piece(reinterpret_cast<char *>(part + second), c, D, GLA_DT_F32, db[i]);
+        }
+    }
+}
+
+// Adds the slots: 16 columns and 16 rows of slots a work-group
+__global__ __launch_bounds__(256) void norm_sum_kernel(const float *part, float *dweight, float *dbias, int slots, int cols) {
+    __shared__ float s[16][17];
+    const int c = threadIdx.x & 15, k = threadIdx.x >> 4;
+    const int col = blockIdx.x * 16 + c;
+    const float *src = part + (blockIdx.y ? (size_t)slots * cols : 0);
+    float x = 0.f;
+    if (col < cols)
+        for (int i = k; i < slots; i += 16) x += src[(size_t)i * cols + col];
+    s[k][c] = x;
+    __syncthreads();
+    if (k == 0 && col < cols) {
+#pragma unroll
+        for (int i = 1; i < 16; ++i) x += s[i][c];
+        (blockIdx.y ? dbias : dweight)[col] = x;
+    }
+}
+
+// lanes of a row's group
+int lanes_of(int D) { return D <= 128 ? 16 : D <= 1536 ? 64 : D <= 4096 ? 256 : 1024; }
+
+// Rows are dealt to as many groups as fill the GPU a few times over, each with a few rows of its own; a multiple of the groups of a
+// work-group where a work-group stays with one head
+int slots_for(const NormParams &p, int rows_each, int work_groups) {
+    const int lanes = lanes_of(p.D), groups = lanes >= 256 ? 1 : 256 / lanes;
+    const long long rows = (long long)p.B * p.T;
+    long long slots = (long long)work_groups * groups / p.H;
+    const long long most = (rows + rows_each - 1) / rows_each;
+    if (slots > most) slots = most;
+    if (slots < 1) slots = 1;
+    if (p.layout == GLA_LAYOUT_BHTD || p.H == 1) slots = (slots + groups - 1) / groups * groups;
+    return (int)slots;
+}
+
+template <typename E, int LANES, int NP, bool BACK>
+hipError_t norm(const NormParams &p, hipStream_t stream) {
+    constexpr int kThreads = Shape<LANES>::kThreads, kGroups = Shape<LANES>::kGroups;
+    const long long groups = (long long)p.slots * p.H;
+    const dim3 grid((unsigned)((groups + kGroups - 1) / kGroups));
+    if (p.r_pre != nullptr) hipLaunchKernelGGL((norm_kernel<E, LANES, NP, true, BACK>), grid, dim3(kThreads), 0, stream, p);
+    else hipLaunchKernelGGL((norm_kernel<E, LANES, NP, false, BACK>), grid, dim3(kThreads), 0, stream, p);
+    return hipGetLastError();
+}
+
+template <typename E, bool BACK>
+hipError_t norm_of_width(const NormParams &p, hipStream_t stream) {
+    if (p.D <= 128) return norm<E, 16, 1, BACK>(p, stream);
+    if (p.D <= 512) return norm<E, 64, 1, BACK>(p, stream);
+    if (p.D <= 1024) return norm<E, 64, 2, BACK>(p, stream);
+    if (p.D <= 1536) return norm<E, 64, 3, BACK>(p, stream);
+    if (p.D <= 2048) return norm<E, 256, 1, BACK>(p, stream);
+    if (p.D <= 4096) return norm<E, 256, 2, BACK>(p, stream);
+    return norm<E, 1024, 1, BACK>(p, stream);
+}
+
+}  // namespace
+
+int norm_slots(int B, int H, int T, int D, int layout) {
+    NormParams p = {};
+    p.B = B;
+    p.H = H;
+    p.T = T;
+    p.D = D;
+    p.layout = layout;
+    return slots_for(p, 4, D > 4096 ? 512 : 1024);
+}
+
+hipError_t launch_norm_fwd(const NormParams &p0, int dtype, hipStream_t stream) {
+    NormParams p = p0;
+    p.slots = slots_for(p, 1, 4096);
+    return dtype == GLA_DT_BF16 ? norm_of_width<uint16_t, false>(p, stream) : norm_of_width<float, false>(p, stream);
+}
+
+hipError_t launch_norm_bwd(const NormParams &p0, int dtype, float *dweight, float *dbias, hipStream_t stream) {
+    NormParams p = p0;
+    const hipError_t e = dtype == GLA_DT_BF16 ? norm_of_width<uint16_t, true>(p, stream) : norm_of_width<float, true>(p, stream);
+    if (e != hipSuccess || dweight == nullptr) return e;
+    const int cols = p.H * p.D;
+    hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)((cols + 15) / 16), 2), dim3(256), 0, stream, p.part, dweight, dbias, p.slots, cols);
+    return hipGetLastError();
+}
+
+}  // namespace gla

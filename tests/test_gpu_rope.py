@@ -1,0 +1,116 @@
+"""Rotary positions with several axes (gla_rope) against 64-bit angles.
+
+Tolerance: an angle is formed and reduced in 64 bits (positions below 2^31 times a frequency: within 2^31 * 2^-52 of a turn), then rounded to
+32 bits of half a turn, 2^-25 * pi, and its sine and cosine are within 2 units of 2^-24: a turned value is off by less than 2^-21 of the pair's length;
+bf16 outputs are rounded once, 2^-8 of the value."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2405_18428_amd as gla
+from oracle import ops_oracle as oo
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF16, F32 = torch.bfloat16, torch.float32
+ROUND = {F32: 2.0 ** -23, BF16: 2.0 ** -8}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    gla.load_library()
+
+
+def grid_positions(T, gh, gw, axes):
+    n = np.arange(T)
+    p = {1: [n], 2: [n // gw, n % gw], 3: [n // (gh * gw), n % (gh * gw) // gw, n % gw]}[axes]
+    return np.stack(p, -1)
+
+
+def check(B, H, T, d, sections, dtype, layout, pairing, inverse, gh=0, gw=0, positions=None, base=10000.0, seed=0, with_k=True, in_place=False):
+    gen = torch.Generator().manual_seed(seed)
+    lead = (B, H, T) if layout == 0 else (B, T, H)
+    q, k = torch.randn(2, *lead, d, generator=gen).to(dtype)
+    pos = grid_positions(T, gh, gw, len(sections))[None].repeat(B, 0) if positions is None else positions.numpy()
+    a, b = q.to(DEV), k.to(DEV) if with_k else None
+    got = gla.gla_rope(a, b, sections, gh, gw, None if positions is None else positions.to(DEV), base, pairing, inverse, layout,
+                       out_q=a if in_place else None, out_k=b if in_place else None)
+    torch.cuda.synchronize()
+    assert (got[1] is None) == (not with_k)
+    lie = (lambda x: x) if layout == 0 else (lambda x: x.transpose(1, 2))
+    for x, y in zip((q, k), got):
+        if y is None:
+            continue
+        X = lie(x).double().numpy()
+        want = oo.rope(X, pos, sections, base, pairing == gla.ROPE_ADJACENT, inverse)
+        length = np.abs(X).max(-1, keepdims=True) * 2
+        turned = np.arange(d) < sum(sections)
+        Y = lie(y).double().cpu().numpy()
+        bad = np.abs(Y - want) - np.where(turned, 2.0 ** -21 * length + ROUND[dtype] * np.abs(want), 0.0)
+        assert bad.max() <= 0, (float(bad.max()), np.unravel_index(bad.argmax(), bad.shape))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("pairing", [gla.ROPE_ADJACENT, gla.ROPE_HALVES])
+@pytest.mark.parametrize("sections,d", [((8,), 8), ((2,), 2), ((2,), 3), ((64,), 64), ((16, 16), 36), ((18, 18), 36), ((32, 48, 48), 128), ((6, 10, 4), 25),
+                                        ((128, 64, 64), 256), ((36, 36), 72)])
+def test_sections(sections, d, pairing, layout, dtype):
+    gh, gw = 5, 7
+    T = {1: 35, 2: 35, 3: 70}[len(sections)]
+    check(2, 3, T, d, sections, dtype, layout, pairing, d % 2 == 1, gh, gw, seed=d)
+
+
+@pytest.mark.parametrize("axes", [1, 2, 3, 4])
+def test_given_positions(axes):
+    """Positions to the ends of 32 bits, negative ones too; one token."""
+    gen = torch.Generator().manual_seed(axes)
+    for T in (1, 33):
+        pos = torch.randint(-2 ** 31, 2 ** 31 - 1, (3, T, axes), generator=gen, dtype=torch.int64).to(torch.int32)
+        pos[0, 0] = 2 ** 31 - 1
+        pos[1, 0] = -2 ** 31
+        check(3, 4, T, 16 * axes, (16,) * axes, F32, 1, gla.ROPE_HALVES, False, positions=pos, seed=axes)
+
+
+def test_many_heads_and_tokens():
+    check(1, 40, 1500, 64, (32, 32), BF16, 1, gla.ROPE_ADJACENT, False, 30, 50)
+    check(2, 7, 6000, 64, (64,), BF16, 0, gla.ROPE_HALVES, False)
+    check(1, 70000, 1, 2, (2,), F32, 1, gla.ROPE_ADJACENT, False, positions=torch.tensor([[[3]]], dtype=torch.int32))
+
+
+def test_in_place_without_keys_and_other_base():
+    check(1, 2, 20, 22, (10, 6), BF16, 0, gla.ROPE_ADJACENT, False, 4, 5, in_place=True)
+    check(1, 2, 20, 24, (8, 8), F32, 1, gla.ROPE_HALVES, True, 4, 5, in_place=True)
+    check(1, 2, 20, 24, (8, 8), F32, 1, gla.ROPE_HALVES, True, 4, 5, with_k=False, base=100.0)
+
+
+def test_turned_there_and_back_in_a_graph():
+    q, k = torch.randn(2, 1, 4, 60, 64, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    gla.gla_rope(q, k, (32, 32), 6, 10)
+    with torch.cuda.graph(graph):
+        a, b = gla.gla_rope(q, k, (32, 32), 6, 10)
+        c, e = gla.gla_rope(a, b, (32, 32), 6, 10, inverse=True)
+    for _ in range(3):
+        for t in (a, b, c, e):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert float((c - q).abs().max()) < 1e-5 and float((e - k).abs().max()) < 1e-5 and float((a - q).abs().max()) > 0.1
+
+
+def test_refusals():
+    q = torch.zeros(2, 3, 12, 16, device=DEV)
+    pos = torch.zeros(2, 12, 2, dtype=torch.int32, device=DEV)
+    for bad in ({"k": q.to(BF16)}, {"k": q[..., :8]}, {"positions": pos[:1]}, {"positions": pos.long()}, {"layout": 3}, {"out_q": q[:1]}, {"k": None, "out_k": q}):
+        args = {"k": q, "sections": (8, 8), "grid_h": 3, "grid_w": 4, **bad}
+        with pytest.raises((ValueError, TypeError)):
+            gla.gla_rope(q, **args)
+    for bad in ({"sections": (8, 10)}, {"sections": (7, 8)}, {"sections": ()}, {"sections": (0, 8)}, {"grid_h": 5}, {"base": 0.0}, {"base": float("inf")},
+                {"pairing": 2}, {"sections": (4, 4, 4, 4)}, {"sections": (2,) * 5, "positions": torch.zeros(2, 12, 5, dtype=torch.int32, device=DEV)}):
+        args = {"sections": (8, 8), "grid_h": 3, "grid_w": 4, **bad}
+        with pytest.raises(gla.GlaError):
+            gla.gla_rope(q, q, **args)
