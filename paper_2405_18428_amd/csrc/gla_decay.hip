@@ -9,21 +9,22 @@ constexpr int kThreads = 256;
 
 template <typename E, int M, int N>
 struct WalkLds {
-    static constexpr int kX = 0, kY = Tile<E, M>::kBytes, kZ = 2 * Tile<E, M>::kBytes, kP = kZ + Tile<E, N>::kBytes,
-                         kG = kP + Pairs<E>::kBytes, kFlow = kG + (int)sizeof(Gates<Elem<E>::kChunk>),
+    static constexpr int kRowsM = Tile<E, M, kBoth>::kBytes, kRowsN = Tile<E, N, kAcross>::kBytes, kX = 0, kY = Tile<E, M, kAlong>::kBytes, kZ = kY + kRowsM,
+                         kP = kZ + kRowsN, kG = kP + Pairs<E>::kBytes, kFlow = kG + 2 * (int)sizeof(Gates<Elem<E>::kChunk>),
                          kBytes = kFlow + 4 * Elem<E>::kChunk * 4;
 };
 
 // GRAD: the walk for dq, with the dot products and the states that the gates' gradient takes
-template <typename E, int M, int N, bool GRAD>
+template <typename E, int M, int N, bool FAST, bool GRAD>
 __global__ __launch_bounds__(kThreads, 2) void decay_walk_kernel(const DecayWalk p) {
     constexpr int C = Elem<E>::kChunk;
     typedef WalkLds<E, M, N> L;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const Tile<E, M> tx{lds + L::kX}, ty{lds + L::kY};
-    const Tile<E, N> tz{lds + L::kZ};
+    const Tile<E, M, kAlong> tx{lds + L::kX};
+    const Tile<E, M, kBoth> ty{lds + L::kY};
+    const Tile<E, N, kAcross> tz{lds + L::kZ};
     const Pairs<E> P{lds + L::kP};
-    Gates<C> &gt = *reinterpret_cast<Gates<C> *>(lds + L::kG);
+    Gates<C> *gates = reinterpret_cast<Gates<C> *>(lds + L::kG);
     float *flow_part = reinterpret_cast<float *>(lds + L::kFlow);
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -36,38 +37,40 @@ __global__ __launch_bounds__(kThreads, 2) void decay_walk_kernel(const DecayWalk
     const Rows rx = rows_of<E>(p.c, p.r.x, bh, m), ry = rows_of<E>(p.c, p.r.y, bh, m), rz = rows_of<E>(p.c, p.r.z, bh, n);
     const Rows ro = rows_of<E>(p.c, p.r.out, bh, n, p.out_dtype == GLA_DT_BF16 ? 2 : 4);
 
-    Walker<E, M, N> wk;
+    Walker<E, M, N, FAST, false> wk;
     wk.init(tid);
-    Pieces<E, M, kThreads> px, py;
-    Pieces<E, N, kThreads> pz;
+    Pieces<E, M, kThreads, FAST> px, py;
+    Pieces<E, N, kThreads, FAST> pz;
     float gate = 0.f;
     auto issue = [&](int s) __attribute__((always_inline)) {
-        const int tid = recompute_per_chunk(threadIdx.x), lane = tid & 63, count = min(C, end - s);
-        auto token = [&](int i) __attribute__((always_inline)) { return (long long)ord.token(s + i); };
-        px.issue(rx, tid, count, token);
-        py.issue(ry, tid, count, token);
-        pz.issue(rz, tid, count, token);
-        if (tid < 64) gate = lane < count ? gate_of(p.c, ord, bh, s + lane) : 0.f;
+        const int tid = recompute_per_chunk(threadIdx.x), lane = tid & 63;
+        const Steps st = ord.steps(s, min(C, end - s), false);
+        if (wk.w == 3) gate = lane < st.count ? gate_of(p.c, ord, bh, s + lane) : 0.f;
+        px.issue(rx, tid, st);
+        py.issue(ry, tid, st);
+        pz.issue(rz, tid, st);
     };
     if (s0 < end) issue(s0);
     wk.load_state(p.state_in == nullptr ? nullptr : p.state_in + (size_t)blockIdx.x * cells, m, n, p.state_t);
-    for (int s = s0; s < end; s += C) {
+    if (wk.w == 3 && s0 < end) form_gates(gates[0], gate, lane);
+    int turn = 0;
+    for (int s = s0; s < end; s += C, turn ^= 1) {
         const int count = min(C, end - s);
+        const Gates<C> &gt = gates[turn];
         px.commit(rx, tid, tx);
         py.commit(ry, tid, ty);
         pz.commit(rz, tid, tz);
-        if (tid < 64) form_gates(gt, gate, lane);
         __syncthreads();
         if (s + C < end) issue(s + C);
-        wk.pairs(tx, ty, P, gt);
-        wk.from_state(tx, gt);
+        wk.begin(tx, ty, P, gt);
         __syncthreads();
+        if (wk.w == 3 && s + C < end) form_gates(gates[turn ^ 1], gate, lane);
         wk.template advance<true>(ty, tz, P, gt);
-        auto token = [&](int i) __attribute__((always_inline)) { return (long long)ord.token(s + i); };
-        wk.store_rows(ro, p.out_dtype, count, token);
+        const Steps st = ord.steps(s, count, false);
+        wk.store_rows(ro, p.out_dtype, st);
         if (GRAD && p.r.dot != nullptr) {
             const Rows rd = rows_of<E>(p.c, p.r.dot, bh, n);
-            wk.template dot_rows<false>(rd, tz, flow_part, count, token);
+            wk.template dot_rows<false>(rd, Tile<E, N, kAlong>{nullptr}, flow_part, st);
         }
         const int e = s + count;
         if (GRAD && p.anchors != nullptr && (e < len ? e % kFlowBlock == 0 : p.anchor_last != 0))
@@ -86,14 +89,14 @@ struct StatePair {
 };
 
 // Local states: y, z of the role only.  blockIdx.y = 1: the reversed recurrence
-template <typename E, int M, int N>
+template <typename E, int M, int N, bool FAST>
 __global__ __launch_bounds__(kThreads, 2) void decay_state_kernel(const StatePair both) {
     constexpr int C = Elem<E>::kChunk;
     typedef WalkLds<E, M, N> L;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const Tile<E, M> ty{lds + L::kY - L::kY};
-    const Tile<E, N> tz{lds + L::kZ - L::kY};
-    Gates<C> &gt = *reinterpret_cast<Gates<C> *>(lds + L::kZ - L::kY + Tile<E, N>::kBytes);
+    const Tile<E, M, kBoth> ty{lds};
+    const Tile<E, N, kAcross> tz{lds + L::kRowsM};
+    Gates<C> *gates = reinterpret_cast<Gates<C> *>(lds + L::kRowsM + L::kRowsN);
     const Pairs<E> none{nullptr};
 
     const bool back = blockIdx.y != 0;
@@ -106,30 +109,34 @@ __global__ __launch_bounds__(kThreads, 2) void decay_state_kernel(const StatePai
     const int m = p.r.m, n = p.r.n;
     const Rows ry = rows_of<E>(p.c, p.r.y, bh, m), rz = rows_of<E>(p.c, p.r.z, bh, n);
 
-    Walker<E, M, N> wk;
+    Walker<E, M, N, FAST, false> wk;
     wk.init(tid);
     wk.load_state(nullptr, m, n, false);
-    Pieces<E, M, kThreads> py;
-    Pieces<E, N, kThreads> pz;
+    Pieces<E, M, kThreads, FAST> py;
+    Pieces<E, N, kThreads, FAST> pz;
     float gate = 0.f, sum = 0.f;
     const int chunks = s0 < end ? (end - s0 + C - 1) / C : 0;
     auto issue = [&](int i) __attribute__((always_inline)) {
         const int tid = recompute_per_chunk(threadIdx.x), lane = tid & 63;
         const int s = s0 + (back ? chunks - 1 - i : i) * C, e = min(s + C, end);
-        auto token = [&](int row) __attribute__((always_inline)) { return (long long)ord.token(back ? e - 1 - row : s + row); };
-        py.issue(ry, tid, e - s, token);
-        pz.issue(rz, tid, e - s, token);
-        if (tid < 64) gate = lane < e - s ? gate_of(p.c, ord, bh, back ? e - lane : s + lane) : 0.f;
+        const Steps st = ord.steps(s, e - s, back);
+        if (wk.w == 3) gate = lane < e - s ? gate_of(p.c, ord, bh, back ? e - lane : s + lane) : 0.f;
+        py.issue(ry, tid, st);
+        pz.issue(rz, tid, st);
     };
-    if (chunks > 0) issue(0);
+    if (chunks > 0) {
+        issue(0);
+        if (wk.w == 3) form_gates(gates[0], gate, lane);
+    }
     for (int i = 0; i < chunks; ++i) {
+        const Gates<C> &gt = gates[i & 1];
         py.commit(ry, tid, ty);
         pz.commit(rz, tid, tz);
-        if (tid < 64) form_gates(gt, gate, lane);
         __syncthreads();
         if (i + 1 < chunks) issue(i + 1);
         sum += gt.sum;
         wk.template advance<false>(ty, tz, none, gt);
+        if (wk.w == 3 && i + 1 < chunks) form_gates(gates[(i + 1) & 1], gate, lane);
         __syncthreads();
     }
     const size_t at = (size_t)bh * p.c.nspans + sp;
@@ -158,24 +165,24 @@ hipError_t configured(K kernel, int bytes, std::atomic<bool> (&done)[kMaxDevices
     return allow_dynamic_lds(reinterpret_cast<const void *>(kernel), bytes, done);
 }
 
-template <typename E, int M, int N, bool GRAD>
+template <typename E, int M, int N, bool FAST, bool GRAD>
 hipError_t walk(const DecayWalk &w, hipStream_t stream) {
     static std::atomic<bool> done[kMaxDevices];
     constexpr int bytes = WalkLds<E, M, N>::kBytes;
-    const hipError_t e = configured(decay_walk_kernel<E, M, N, GRAD>, bytes, done);
+    const hipError_t e = configured(decay_walk_kernel<E, M, N, FAST, GRAD>, bytes, done);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((decay_walk_kernel<E, M, N, GRAD>), dim3((unsigned)(w.c.B * w.c.H * w.c.nspans)), dim3(kThreads), bytes, stream, w);
+    hipLaunchKernelGGL((decay_walk_kernel<E, M, N, FAST, GRAD>), dim3((unsigned)(w.c.B * w.c.H * w.c.nspans)), dim3(kThreads), bytes, stream, w);
     return hipGetLastError();
 }
 
-template <typename E, int M, int N>
+template <typename E, int M, int N, bool FAST>
 hipError_t states(const StatePair &w, int directions, hipStream_t stream) {
     static std::atomic<bool> done[kMaxDevices];
-    constexpr int bytes = Tile<E, M>::kBytes + Tile<E, N>::kBytes + (int)sizeof(Gates<Elem<E>::kChunk>);
-    const hipError_t e = configured(decay_state_kernel<E, M, N>, bytes, done);
+    constexpr int bytes = WalkLds<E, M, N>::kRowsM + WalkLds<E, M, N>::kRowsN + 2 * (int)sizeof(Gates<Elem<E>::kChunk>);
+    const hipError_t e = configured(decay_state_kernel<E, M, N, FAST>, bytes, done);
     if (e != hipSuccess) return e;
     const DecayCall &c = w.w[0].c;
-    hipLaunchKernelGGL((decay_state_kernel<E, M, N>), dim3((unsigned)(c.B * c.H * (c.nspans - 1)), (unsigned)directions), dim3(kThreads),
+    hipLaunchKernelGGL((decay_state_kernel<E, M, N, FAST>), dim3((unsigned)(c.B * c.H * (c.nspans - 1)), (unsigned)directions), dim3(kThreads),
                        bytes, stream, w);
     return hipGetLastError();
 }
@@ -249,9 +256,9 @@ __global__ __launch_bounds__(kThreads) void decay_step_kernel(const void *q, con
 
 template <typename E, bool GRAD>
 static hipError_t walk_of_size(const DecayWalk &w, hipStream_t stream) {
-    const bool m = w.r.m > 64, n = w.r.n > 64;
-    if (m) return n ? walk<E, 128, 128, GRAD>(w, stream) : walk<E, 128, 64, GRAD>(w, stream);
-    return n ? walk<E, 64, 128, GRAD>(w, stream) : walk<E, 64, 64, GRAD>(w, stream);
+    return decay_sizes(w.r.m, w.r.n, w.c.fast, [&](auto m, auto n, auto fast) {
+        return walk<E, decltype(m)::value, decltype(n)::value, decltype(fast)::value, GRAD>(w, stream);
+    });
 }
 
 hipError_t launch_decay_walk(const DecayWalk &w, int dtype, hipStream_t stream) {
@@ -264,13 +271,11 @@ hipError_t launch_decay_states(const DecayWalk &w, const DecayWalk *back, int dt
     both.w[0] = w;
     both.w[1] = back != nullptr ? *back : w;
     const int d = back != nullptr ? 2 : 1;
-    const bool m = w.r.m > 64, n = w.r.n > 64;
-    if (dtype == GLA_DT_BF16) {
-        if (m) return n ? states<uint16_t, 128, 128>(both, d, stream) : states<uint16_t, 128, 64>(both, d, stream);
-        return n ? states<uint16_t, 64, 128>(both, d, stream) : states<uint16_t, 64, 64>(both, d, stream);
-    }
-    if (m) return n ? states<float, 128, 128>(both, d, stream) : states<float, 128, 64>(both, d, stream);
-    return n ? states<float, 64, 128>(both, d, stream) : states<float, 64, 64>(both, d, stream);
+    return decay_sizes(w.r.m, w.r.n, w.c.fast, [&](auto m, auto n, auto fast) {
+        constexpr int M = decltype(m)::value, N = decltype(n)::value;
+        constexpr bool F = decltype(fast)::value;
+        return dtype == GLA_DT_BF16 ? states<uint16_t, M, N, F>(both, d, stream) : states<float, M, N, F>(both, d, stream);
+    });
 }
 
 hipError_t launch_decay_carry(const DecayCall &c, const float *first, float *local, const float *decay, bool reversed, hipStream_t stream) {

@@ -12,20 +12,22 @@ constexpr int kThreads = 512;
 
 template <typename E, int K, int V>
 struct BackLds {
-    static constexpr int kQ = 0, kK = Tile<E, K>::kBytes, kV = 2 * Tile<E, K>::kBytes, kD = kV + Tile<E, V>::kBytes,
-                         kPa = kD + Tile<E, V>::kBytes, kPb = kPa + Pairs<E>::kBytes, kG = kPb + Pairs<E>::kBytes,
-                         kFlow = kG + (int)sizeof(Gates<Elem<E>::kChunk>), kMeet = kFlow + 4 * Elem<E>::kChunk * 4, kBytes = kMeet + 16;
+    static constexpr int kRowsV = Tile<E, V, kBoth>::kBytes, kQ = 0, kK = Tile<E, K, kBoth>::kBytes, kV = kK + Tile<E, K, kAlong>::kBytes,
+                         kD = kV + Tile<E, V, kAlong>::kBytes, kPa = kD + kRowsV, kPb = kPa + Pairs<E>::kBytes, kG = kPb + Pairs<E>::kBytes,
+                         kFlow = kG + 2 * (int)sizeof(Gates<Elem<E>::kChunk>), kMeet = kFlow + 4 * Elem<E>::kChunk * 4, kBytes = kMeet + 16;
 };
 
 // ROLE 0: dv, ROLE 1: dk
-template <typename E, int K, int V, int ROLE>
+template <typename E, int K, int V, bool FAST, int ROLE>
 __device__ __forceinline__ void walk_back(const DecayBack &p, char *lds) {
     constexpr int C = Elem<E>::kChunk, M = ROLE == 0 ? K : V, N = ROLE == 0 ? V : K;
     typedef BackLds<E, K, V> L;
-    const Tile<E, K> tq{lds + L::kQ}, tk{lds + L::kK};
-    const Tile<E, V> tv{lds + L::kV}, td{lds + L::kD};
+    const Tile<E, K, kBoth> tq{lds + L::kQ};
+    const Tile<E, K, kAlong> tk{lds + L::kK};
+    const Tile<E, V, kAlong> tv{lds + L::kV};
+    const Tile<E, V, kBoth> td{lds + L::kD};
     const Pairs<E> P{lds + (ROLE == 0 ? L::kPa : L::kPb)};
-    Gates<C> &gt = *reinterpret_cast<Gates<C> *>(lds + L::kG);
+    Gates<C> *gates = reinterpret_cast<Gates<C> *>(lds + L::kG);
     float *flow_part = reinterpret_cast<float *>(lds + L::kFlow), *meet_part = reinterpret_cast<float *>(lds + L::kMeet);
 
     const int tid = threadIdx.x;
@@ -39,25 +41,29 @@ __device__ __forceinline__ void walk_back(const DecayBack &p, char *lds) {
                rd = rows_of<E>(p.c, p.d_out, bh, dv);
     const Rows ro = rows_of<E>(p.c, ROLE == 0 ? p.dv_grad : p.dk_grad, bh, n, p.grad_dtype == GLA_DT_BF16 ? 2 : 4);
 
-    Walker<E, M, N> wk;
+    Walker<E, M, N, FAST, true> wk;
     wk.init(tid);
-    Pieces<E, K, kThreads> pq, pk;
-    Pieces<E, V, kThreads> pv, pd;
+    Pieces<E, K, kThreads, FAST> pq, pk;
+    Pieces<E, V, kThreads, FAST> pv, pd;
     float gate = 0.f;
     auto issue = [&](int s, int e) __attribute__((always_inline)) {      // steps [s, e), row 0 = step e - 1
-        const int tid = recompute_per_chunk(threadIdx.x), lane = tid & 63, count = e - s;
-        auto token = [&](int i) __attribute__((always_inline)) { return (long long)ord.token(e - 1 - i); };
-        pq.issue(rq, tid, count, token);
-        pk.issue(rk, tid, count, token);
-        pv.issue(rv, tid, count, token);
-        pd.issue(rd, tid, count, token);
-        if (tid < 64) gate = lane < count ? gate_of(p.c, ord, bh, e - lane) : 0.f;   // the gate that led out of the step
+        const int tid = recompute_per_chunk(threadIdx.x), lane = tid & 63;
+        const Steps st = ord.steps(s, e - s, true);
+        if (ROLE == 0 && wk.w == 3) gate = lane < st.count ? gate_of(p.c, ord, bh, e - lane) : 0.f;   // the gate that led out of the step
+        pq.issue(rq, tid, st);
+        pk.issue(rk, tid, st);
+        pv.issue(rv, tid, st);
+        pd.issue(rd, tid, st);
     };
     const int chunks = s0 < end ? (end - s0 + C - 1) / C : 0;
-    if (chunks > 0) issue(s0 + (chunks - 1) * C, end);
+    if (chunks > 0) {
+        issue(s0 + (chunks - 1) * C, end);
+        if (ROLE == 0 && wk.w == 3) form_gates(gates[(chunks - 1) & 1], gate, wk.lane);
+    }
     wk.load_state(p.state_in == nullptr ? nullptr : p.state_in + (size_t)blockIdx.x * cells, m, n, ROLE == 1);
     for (int ci = chunks - 1; ci >= 0; --ci) {
         const int s = s0 + ci * C, e = min(s + C, end), count = e - s;
+        const Gates<C> &gt = gates[ci & 1];
         // the state there met by its adjoint
         const size_t block = (size_t)bh * decay_blocks(p.c.T) + (e - 1) / kFlowBlock;
         const bool meets = ROLE == 1 && p.anchors != nullptr && (e < len ? e % kFlowBlock == 0 : p.anchor_last != 0);
@@ -71,24 +77,22 @@ __device__ __forceinline__ void walk_back(const DecayBack &p, char *lds) {
         pk.commit(rk, tid, tk);
         pv.commit(rv, tid, tv);
         pd.commit(rd, tid, td);
-        if (tid < 64) form_gates(gt, gate, tid);
         __syncthreads();
         if (ci > 0) issue(s - C, s);
         if (meets && tid == 256) p.meet[block] = (meet_part[0] + meet_part[1]) + (meet_part[2] + meet_part[3]);
         if constexpr (ROLE == 0) {
-            wk.pairs(tk, tq, P, gt);
-            wk.from_state(tk, gt);
+            wk.begin(tk, tq, P, gt);
         } else {
-            wk.pairs(tv, td, P, gt);
-            wk.from_state(tv, gt);
+            wk.begin(tv, td, P, gt);
         }
         __syncthreads();
+        if (ROLE == 0 && wk.w == 3 && ci > 0) form_gates(gates[(ci - 1) & 1], gate, wk.lane);
         if constexpr (ROLE == 0) wk.template advance<true>(tq, td, P, gt);
         else wk.template advance<true>(td, tq, P, gt);
-        auto token = [&](int i) __attribute__((always_inline)) { return (long long)ord.token(e - 1 - i); };
-        wk.store_rows(ro, p.grad_dtype, count, token);
+        const Steps st = ord.steps(s, count, true);
+        wk.store_rows(ro, p.grad_dtype, st);
         if constexpr (ROLE == 1) {
-            if (p.anchors != nullptr) wk.template dot_rows<true>(rk, tk, flow_part, count, token);
+            if (p.anchors != nullptr) wk.template dot_rows<true>(rk, tk, flow_part, st);
         }
         __syncthreads();
         if (ROLE == 1 && p.anchors != nullptr && tid - 256 < count) {
@@ -102,12 +106,12 @@ __device__ __forceinline__ void walk_back(const DecayBack &p, char *lds) {
     clear_behind<256>(ro, p.grad_dtype == GLA_DT_BF16 ? 2 : 4, len, s0, s1, tid & 255);
 }
 
-template <typename E, int K, int V>
+template <typename E, int K, int V, bool FAST>
 __global__ __launch_bounds__(kThreads, 2) void decay_back_kernel(const DecayBack p) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     // both branches meet at the same barriers: the same chunks, three each
-    if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 8) == 0) walk_back<E, K, V, 0>(p, lds);
-    else walk_back<E, K, V, 1>(p, lds);
+    if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 8) == 0) walk_back<E, K, V, FAST, 0>(p, lds);
+    else walk_back<E, K, V, FAST, 1>(p, lds);
 }
 
 // A block of kFlowBlock steps a work-group: what flows into each, in 64 bits
@@ -169,27 +173,24 @@ __global__ __launch_bounds__(256) void decay_gate_sum_kernel(const double *part,
     if (t == 0) dlog[h] = (float)sum[0];
 }
 
-template <typename E, int K, int V>
+template <typename E, int K, int V, bool FAST>
 hipError_t back(const DecayBack &w, hipStream_t stream) {
     static std::atomic<bool> done[kMaxDevices];
     constexpr int bytes = BackLds<E, K, V>::kBytes;
-    const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(&decay_back_kernel<E, K, V>), bytes, done);
+    const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(&decay_back_kernel<E, K, V, FAST>), bytes, done);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((decay_back_kernel<E, K, V>), dim3((unsigned)(w.c.B * w.c.H * w.c.nspans)), dim3(kThreads), bytes, stream, w);
+    hipLaunchKernelGGL((decay_back_kernel<E, K, V, FAST>), dim3((unsigned)(w.c.B * w.c.H * w.c.nspans)), dim3(kThreads), bytes, stream, w);
     return hipGetLastError();
-}
-
-template <typename E>
-hipError_t back_of_size(const DecayBack &w, hipStream_t stream) {
-    const bool k = w.c.dk > 64, v = w.c.dv > 64;
-    if (k) return v ? back<E, 128, 128>(w, stream) : back<E, 128, 64>(w, stream);
-    return v ? back<E, 64, 128>(w, stream) : back<E, 64, 64>(w, stream);
 }
 
 }  // namespace
 
 hipError_t launch_decay_back(const DecayBack &w, int dtype, hipStream_t stream) {
-    return dtype == GLA_DT_BF16 ? back_of_size<uint16_t>(w, stream) : back_of_size<float>(w, stream);
+    return decay_sizes(w.c.dk, w.c.dv, w.c.fast, [&](auto k, auto v, auto fast) {
+        constexpr int K = decltype(k)::value, V = decltype(v)::value;
+        constexpr bool F = decltype(fast)::value;
+        return dtype == GLA_DT_BF16 ? back<uint16_t, K, V, F>(w, stream) : back<float, K, V, F>(w, stream);
+    });
 }
 
 hipError_t launch_decay_gate(const DecayGate &w, hipStream_t stream) {

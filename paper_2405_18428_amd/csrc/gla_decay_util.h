@@ -18,8 +18,6 @@
 namespace gla {
 namespace {
 
-constexpr int kPadBytes = 16;        // behind each row of a tile: rows 4 banks apart, 16 of them cover all 64
-
 template <typename E> struct Elem;
 template <> struct Elem<uint16_t> {
     static constexpr int kChunk = 64;            // steps
@@ -53,45 +51,157 @@ __device__ inline int state_row(int t, int g, int r) {
     else return t * 16 + g * 4 + r;
 }
 
-// A tile of C rows of W elements in LDS
-template <typename E, int W>
+// How a tile's rows are read: along them (the row is an operand's other index), across them (the contracted one), or both
+enum Reads { kAlong, kAcross, kBoth };
+
+// A tile of C rows of W elements in LDS.  Rows lie so far apart that the 64 banks are met evenly: 16 rows' same piece when read along, 8
+// rows' 32 bytes (bf16) or 4 rows' 64 (fp32) when read across; only reads along a bf16 tile for both meet a bank twice.  (With rows 16
+// bytes apart throughout, near half of the time that LDS was busy went to conflicts.  An exchange of pieces by the row's number is free
+// of them everywhere, but no read's address is then a constant from another's, which cost more instructions than it saved.)
+// A bf16 tile for both holds each 32 columns in the order in which state_row() counts a state's rows: elements 16 h + 4 c and on are columns
+// 8 c + 4 h and on.
+template <typename E, int W, Reads R>
 struct Tile {
     static constexpr int C = Elem<E>::kChunk;
-    static constexpr int kRow = W * (int)sizeof(E) + kPadBytes;      // bytes
+    static constexpr int kRow = W * (int)sizeof(E) + (sizeof(E) == 2 && R != kAlong ? 32 : 16);      // bytes
     static constexpr int kBytes = C * kRow;
+    static constexpr bool kMoved = R == kBoth && sizeof(E) == 2;
     char *p;
-    // 16 bytes of row `row`: the operand of contraction step ks whose other index is the row
-    __device__ __forceinline__ u32x4 along(int row, int ks, int g) const {
-        return *reinterpret_cast<const u32x4 *>(p + row * kRow + (ks * 4 + g) * 16);
+    // 16 bytes of row 16 tile + lm: the operand of contraction step ks whose other index is the row
+    __device__ __forceinline__ u32x4 along(int tile, int lm, int ks, int g) const {
+        const char *a = p + tile * 16 * kRow + lm * kRow;
+        if constexpr (kMoved) {
+            const u32x2 lo = *reinterpret_cast<const u32x2 *>(a + g * 8 + ks * 64);
+            const u32x2 hi = *reinterpret_cast<const u32x2 *>(a + g * 8 + ks * 64 + 32);
+            return u32x4{lo[0], lo[1], hi[0], hi[1]};
+        } else {
+            return *reinterpret_cast<const u32x4 *>(a + g * 16 + ks * 64);
+        }
     }
-    // the operand that contracts over rows: step jk of kDeep rows, other index = the lane's column `lm` of 16.  With PERM the
-    // columns of state tile t (state_row), else columns 16 t and on.
-    template <bool PERM>
+    // the operand that contracts over rows: step jk of kDeep rows, other index = the lane's of the 16 columns of tile t (in the order
+    // in which they lie)
     __device__ __forceinline__ u32x4 across(int jk, int t, int lm, int g) const {
         if constexpr (sizeof(E) == 2) {
-            const int col = PERM ? state_row<E>(t, lm & 3, 0) : t * 16 + 4 * (lm & 3);
-            const char *a = p + (jk * 32 + g * 4 + (lm >> 2)) * kRow + col * 2;
+            const char *a = p + (g * 4 + (lm >> 2)) * kRow + (lm & 3) * 8 + jk * 32 * kRow + t * 32;
             const u32x2 lo = lds_read_tr(reinterpret_cast<const uint16_t *>(a));
             const u32x2 hi = lds_read_tr(reinterpret_cast<const uint16_t *>(a + 16 * kRow));
             return u32x4{lo[0], lo[1], hi[0], hi[1]};
         } else {
-            const char *a = p + (jk * 16 + g * 4) * kRow + (t * 16 + lm) * 4;
+            const char *a = p + g * 4 * kRow + lm * 4 + jk * 16 * kRow + t * 64;
             u32x4 v;
 #pragma unroll
             for (int r = 0; r < 4; ++r) v[r] = *reinterpret_cast<const uint32_t *>(a + r * kRow);
             return v;
         }
     }
+    // 16 bytes of a row as they come from memory
+    __device__ __forceinline__ void put_piece(int row, int piece, u32x4 x) const {
+        char *a = p + row * kRow;
+        if constexpr (kMoved) {
+            a += (piece >> 2) * 64 + (piece & 3) * 8;
+            *reinterpret_cast<u32x2 *>(a) = u32x2{x[0], x[1]};
+            *reinterpret_cast<u32x2 *>(a + 32) = u32x2{x[2], x[3]};
+        } else {
+            *reinterpret_cast<u32x4 *>(a + piece * 16) = x;
+        }
+    }
+    // neighbouring elements of a row from column `col` on (of a tile in the order of memory)
+    __device__ __forceinline__ const char *at(int row, int col) const {
+        static_assert(!kMoved, "columns as they come");
+        return p + row * kRow + col * (int)sizeof(E);
+    }
 };
+
+// x0, x1 -> packed bf16 pair of the rounded values and packed pair of the remainders.  A remainder x - head is one dot product of
+// the packed heads with (-1, 0) or (0, -1) added to x (exact), where taking a head out of the pair and subtracting it are two.
+struct Heads {
+    bf16x2 first, second;
+    __device__ __forceinline__ Heads() {
+        // (as constants in the instruction these two pairs would be read as other values)
+        uint32_t a = 0x0000bf80u, b = 0xbf800000u;
+        asm("" : "+s"(a));
+        asm("" : "+s"(b));
+        first = __builtin_bit_cast(bf16x2, a);
+        second = __builtin_bit_cast(bf16x2, b);
+    }
+    __device__ __forceinline__ HiLo split(float x0, float x1) const {
+        HiLo r;
+        r.hi = pack_bf16(x0, x1);
+        const bf16x2 h = __builtin_bit_cast(bf16x2, r.hi);
+        r.lo = pack_bf16(__builtin_amdgcn_fdot2_f32_bf16(h, first, x0, false), __builtin_amdgcn_fdot2_f32_bf16(h, second, x1, false));
+        return r;
+    }
+};
+
+// The steps of one chunk and where their rows lie.  Row scans: tokens first .. first + count - 1, rising or falling with the row number;
+// column scans: each row its own token (first = 0).
+struct Steps {
+    int scan_dir, len, grid_h, grid_w;
+    int s, count;                       // first step, steps
+    bool back;                          // row 0 is the last step
+    int first;
+    bool falling;
+    __device__ __forceinline__ int step_of(int i) const { return back ? s + count - 1 - i : s + i; }
+    // token of row i, less `first`
+    __device__ __forceinline__ int at(int i) const {
+        if (scan_dir < GLA_SCAN_COL_FWD) return falling ? count - 1 - i : i;
+        return scan_token(scan_dir, step_of(i), len, grid_h, grid_w);
+    }
+    // byte offsets of rows i0, i0 + di, ... of `step` bytes each behind `first`'s; kNowhere from `most` on
+    template <int K>
+    __device__ __forceinline__ void offsets(uint32_t (&o)[K], int i0, int di, uint32_t step, int most, uint32_t plus) const {
+        if (scan_dir < GLA_SCAN_COL_FWD) {
+            const uint32_t by = falling ? 0u - step : step;
+            const uint32_t at = (falling ? (uint32_t)(count - 1) * step : 0u) + __umul24((uint32_t)i0, step) * (falling ? 0xffffffffu : 1u) + plus;
+#pragma unroll
+            for (int k = 0; k < K; ++k) o[k] = i0 + k * di < most ? at + (uint32_t)(k * di) * by : kNowhere;
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; ++k) o[k] = i0 + k * di < most ? __umul24((uint32_t)at(i0 + k * di), step) + plus : kNowhere;
+        }
+    }
+};
+// Rows of one sequence: what a walk visits in which order.  Chunk number ci covers steps [ci * C, min((ci + 1) * C, len)) whichever
+// way it is walked; backwards row 0 is the last of them.
+struct Order {
+    int scan_dir, len, grid_h, grid_w;
+    __device__ __forceinline__ int token(int s) const { return scan_token(scan_dir, s, len, grid_h, grid_w); }
+    __device__ __forceinline__ Steps steps(int s, int count, bool back) const {
+        Steps x;
+        x.scan_dir = scan_dir;
+        x.len = len;
+        x.grid_h = grid_h;
+        x.grid_w = grid_w;
+        x.s = s;
+        x.count = count;
+        x.back = back;
+        x.first = scan_dir >= GLA_SCAN_COL_FWD ? 0 : scan_dir == GLA_SCAN_ROW_FWD ? s : len - s - count;
+        x.falling = back != (scan_dir == GLA_SCAN_ROW_REV);
+        return x;
+    }
+};
+__device__ __forceinline__ Order order_of(const DecayCall &c, int bh) {
+    Order o;
+    o.scan_dir = c.scan_dir;
+    o.grid_h = c.grid_h;
+    o.grid_w = c.grid_w;
+    o.len = c.T;
+    if (c.seq_lens != nullptr) {
+        const int n = c.seq_lens[bh / c.H];
+        o.len = n < 0 ? 0 : n < c.T ? n : c.T;       // (a length outside 0 .. T counts as the nearer end)
+    }
+    return o;
+}
 
 // Rows of a [.., d] tensor of one (batch, head): 64-bit offsets, so any length does
 struct Rows {
     const char *base;
     long long step;                     // bytes between tokens
     int d;
+    __device__ __forceinline__ const char *token(long long n) const { return base + n * step; }
 };
 template <typename E>
-__device__ inline Rows rows_of(const DecayCall &c, const void *t, int bh, int d, int size = (int)sizeof(E)) {
+__device__ __forceinline__ Rows rows_of(const DecayCall &c, const void *t, int bh, int d, int size = (int)sizeof(E)) {
     const int b = bh / c.H, h = bh - b * c.H;
     Rows r;
     r.d = d;
@@ -104,8 +214,12 @@ __device__ inline Rows rows_of(const DecayCall &c, const void *t, int bh, int d,
     }
     return r;
 }
+// FAST: rows are read and written through views with 32-bit offsets from the chunk's first token, where an offset that is kNowhere reads
+// zeros and writes nothing; the host chooses it where every offset stays below that and rows are whole dwords (DecayCall::fast).  The
+// other form takes any place and width with 64-bit addresses and branches.
+__device__ __forceinline__ Rsrc chunk_view(const Rows &r, const Steps &t) { return view(r.token(t.first), kNowhere); }
 
-__device__ inline u32x4 load16(const char *p) {          // any alignment
+__device__ __forceinline__ u32x4 load16(const char *p) {          // any alignment
     u32x4 v;
     __builtin_memcpy(&v, p, 16);
     return v;
@@ -113,23 +227,30 @@ __device__ inline u32x4 load16(const char *p) {          // any alignment
 
 // The pieces (16 bytes) of a tile that one of THREADS threads brings: issue() asks for them, commit() puts them into the tile once
 // the one before has been used.  Rows from `count` on and columns from d on are zeros and are not read.
-template <typename E, int W, int THREADS>
+template <typename E, int W, int THREADS, bool FAST>
 struct Pieces {
     static constexpr int kPerRow = W * (int)sizeof(E) / 16, kEach = 16 / (int)sizeof(E);
-    static constexpr int kCount = Tile<E, W>::C * kPerRow / THREADS;
-    static_assert(Tile<E, W>::C * kPerRow % THREADS == 0, "whole pieces a thread");
+    static constexpr int kChunk = Elem<E>::kChunk, kCount = (kChunk * kPerRow + THREADS - 1) / THREADS;
+    static_assert(THREADS % kPerRow == 0 && (kChunk * kPerRow % THREADS == 0 || kCount == 1), "whole rows");
     u32x4 v[kCount];
-    template <typename TokenOf>
-    __device__ __forceinline__ void issue(const Rows &r, int tid, int count, TokenOf token) {
-        const int col = tid % kPerRow * kEach;           // (THREADS is a multiple of kPerRow)
-        // the last piece of a row of odd length is read as the row's last 16 bytes and shifted in commit()
+    __device__ __forceinline__ void issue(const Rows &r, int tid, const Steps &t) {
+        const int col = tid % kPerRow * kEach;
+        // the last piece of a row that is no whole number of pieces is read as the row's last 16 bytes and shifted in commit()
         const int at = col + kEach <= r.d ? col : r.d - kEach;
+        if constexpr (FAST) {
+            const Rsrc b = chunk_view(r, t);
+            uint32_t o[kCount];
+            t.offsets(o, tid / kPerRow, THREADS / kPerRow, (uint32_t)r.step, col < r.d ? t.count : 0, (uint32_t)at * sizeof(E));
+#pragma unroll
+            for (int i = 0; i < kCount; ++i) v[i] = fetch<u32x4>(b, o[i]);
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
-            const int row = (i * THREADS + tid) / kPerRow;
+            const int row = i * (THREADS / kPerRow) + tid / kPerRow;
             u32x4 x = {0u, 0u, 0u, 0u};
-            if (row < count && col < r.d) {
-                const char *p = r.base + token(row) * r.step;
+            if (row < t.count && col < r.d) {
+                const char *p = r.token((long long)t.first + t.at(row));
                 if (at >= 0) {
                     x = load16(p + at * (int)sizeof(E));
                 } else {                                 // rows shorter than a piece
@@ -146,16 +267,27 @@ struct Pieces {
             v[i] = x;
         }
     }
-    __device__ __forceinline__ void commit(const Rows &r, int tid, const Tile<E, W> &t) const {
-        const int piece = tid % kPerRow, over = (piece + 1) * kEach - r.d;
+    template <Reads R>
+    __device__ __forceinline__ void commit(const Rows &r, int tid, const Tile<E, W, R> &t) const {
+        const int piece = tid % kPerRow, row = tid / kPerRow, over = (piece + 1) * kEach - r.d;
+        constexpr int by = THREADS / kPerRow;
+        if (kChunk * kPerRow < THREADS && row >= kChunk) return;         // (more threads than pieces)
         const bool shifted = over > 0 && over < kEach && r.d >= kEach;
+        if (r.d % kEach == 0) {
+#pragma unroll
+            for (int i = 0; i < kCount; ++i) t.put_piece(row + i * by, piece, v[i]);
+            return;
+        }
         const int bits = over * (int)sizeof(E) * 8;
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
             u32x4 x = v[i];
-            if (shifted) x = __builtin_bit_cast(u32x4, __builtin_bit_cast(unsigned __int128, x) >> bits);
-            const int row = (i * THREADS + tid) / kPerRow;
-            *reinterpret_cast<u32x4 *>(t.p + row * Tile<E, W>::kRow + piece * 16) = x;
+            if constexpr (FAST) {                        // half a piece
+                if (shifted) x = u32x4{x[2], x[3], 0u, 0u};
+            } else {
+                if (shifted) x = __builtin_bit_cast(u32x4, __builtin_bit_cast(unsigned __int128, x) >> bits);
+            }
+            t.put_piece(row + i * by, piece, x);
         }
     }
 };
@@ -167,6 +299,7 @@ struct Gates {
     float whole[C], rest[C];
     float in[C];                        // exp(b_i)
     float out[C];                       // exp(b_last - b_i)
+    float tile[C];                      // exp(b_t - b_i), t the last step of the 16 that i is one of
     float last;                         // exp(b_last)
     float sum;                          // b_last, base 2
 };
@@ -181,7 +314,9 @@ __device__ inline void form_gates(Gates<C> &s, float gate, int lane) {
     rest = wave_inclusive_scan(rest);
     const float wl = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, whole), 63));
     const float rl = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, rest), 63));
+    const float wt = __shfl(whole, lane | 15), rt = __shfl(rest, lane | 15);
     if (lane < C) {
+        s.tile[lane] = exp2_fast((wt - whole) + (rt - rest));
         s.whole[lane] = whole;
         s.rest[lane] = rest;
         s.in[lane] = exp2_fast(whole + rest);
@@ -202,8 +337,8 @@ struct Pairs {
     __device__ __forceinline__ char *at(int it, int jk, int part, int lane) const { return p + (((it * kJ + jk) * kParts + part) * 64 + lane) * 16; }
 };
 
-// One wave's part of a walk
-template <typename E, int M, int N>
+// One wave's part of a walk.  ZA: z's tile is one for both, so that the state's columns are counted like its rows
+template <typename E, int M, int N, bool FAST, bool ZA>
 struct Walker {
     static constexpr int C = Elem<E>::kChunk, kDeep = Elem<E>::kDeep, kI = C / 16, kJ = C / kDeep;
     static constexpr int kRows = M / 16, kCols = N / 64, kSteps = M / kDeep, kParts = Elem<E>::kParts;
@@ -217,7 +352,12 @@ struct Walker {
         g = lane >> 4;
         w = __builtin_amdgcn_readfirstlane((tid >> 6) & 3);
     }
-    __device__ __forceinline__ int col_tile(int n) const { return w * kCols + n; }
+    __device__ __forceinline__ int col_tile(int c) const { return w * kCols + c; }
+    // column of lane `lm` of tile c, and the first of the four of lane group g in what is formed transposed
+    __device__ __forceinline__ int col_of(int c, int lm) const {
+        return ZA ? state_row<E>(col_tile(c), lm >> 2, lm & 3) : col_tile(c) * 16 + lm;
+    }
+    __device__ __forceinline__ int cols_of(int c, int g) const { return ZA ? state_row<E>(col_tile(c), g, 0) : col_tile(c) * 16 + g * 4; }
     // the same lane, unknown to the optimiser: the addresses and edges of rows and states are formed where they are needed instead of
     // being held over the chunk loop (they would take more registers than the state)
     struct Lane {
@@ -228,36 +368,58 @@ struct Walker {
         return Lane{l & 15, l >> 4};
     }
 
-    // element (row, col) of the state at p[row * n + col], or with t at p[col * m + row]
+    // element (row, col) of the state at p[row * n + col], or with t at p[col * m + row]; what this lane holds of tile (a, c)
+    __device__ __forceinline__ f32x4 state_at(const float *p, const Rsrc &b, int row, int col, int m, int n, bool t) const {
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (FAST) {                            // (m is a multiple of 4)
+            const bool there = col < n && row < m;
+            if (t) return fetch<f32x4>(b, there ? (uint32_t)(col * m + row) * 4u : kNowhere);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = fetch<float>(b, there ? (uint32_t)((row + r) * n + col) * 4u : kNowhere);
+        } else if (col < n && row < m) {
+            if (t && row + 4 <= m) {
+                __builtin_memcpy(&x, p + (size_t)col * m + row, 16);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (row + r < m) x[r] = t ? p[(size_t)col * m + row + r] : p[(size_t)(row + r) * n + col];
+            }
+        }
+        return x;
+    }
     __device__ __forceinline__ void load_state(const float *p, int m, int n, bool t) {
         const auto [lm, g] = fresh();
+        const Rsrc b = view(p, kNowhere);
 #pragma unroll
         for (int a = 0; a < kRows; ++a)
 #pragma unroll
             for (int c = 0; c < kCols; ++c) {
-                const int row = state_row<E>(a, g, 0), col = col_tile(c) * 16 + lm;
-                f32x4 x = {0.f, 0.f, 0.f, 0.f};
-                if (p != nullptr && col < n && row < m) {
-                    if (t && row + 4 <= m) {
-                        __builtin_memcpy(&x, p + (size_t)col * m + row, 16);
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (row + r < m) x[r] = t ? p[(size_t)col * m + row + r] : p[(size_t)(row + r) * n + col];
-                    }
-                }
-                S[a][c] = x;
+                S[a][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (p != nullptr) S[a][c] = state_at(p, b, state_row<E>(a, g, 0), col_of(c, lm), m, n, t);
             }
     }
     __device__ __forceinline__ void store_state(float *p, int m, int n, bool t, float factor = 1.f) const {
         const auto [lm, g] = fresh();
+        const Rsrc b = view(p, kNowhere);
 #pragma unroll
         for (int a = 0; a < kRows; ++a)
 #pragma unroll
             for (int c = 0; c < kCols; ++c) {
-                const int row = state_row<E>(a, g, 0), col = col_tile(c) * 16 + lm;
+                const int row = state_row<E>(a, g, 0), col = col_of(c, lm);
                 const f32x4 x = S[a][c] * factor;
-                if (col < n && row < m) {
+                if constexpr (FAST) {
+                    const bool there = col < n && row < m;
+                    if (t) {
+                        put(b, there ? (uint32_t)(col * m + row) * 4u : kNowhere, x);
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float xr = x[r];
+                            __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, xr), b,
+                                                                  (int)(there ? (uint32_t)((row + r) * n + col) * 4u : kNowhere), 0, 0);
+                        }
+                    }
+                } else if (col < n && row < m) {
                     if (t && row + 4 <= m) {
                         __builtin_memcpy(p + (size_t)col * m + row, &x, 16);
                     } else {
@@ -271,68 +433,73 @@ struct Walker {
     // this lane's part of <state at p, S>
     __device__ __forceinline__ float meet_state(const float *p, int m, int n, bool t) const {
         const auto [lm, g] = fresh();
+        const Rsrc b = view(p, kNowhere);
         float sum = 0.f;
 #pragma unroll
         for (int a = 0; a < kRows; ++a)
 #pragma unroll
             for (int c = 0; c < kCols; ++c) {
-                const int row = state_row<E>(a, g, 0), col = col_tile(c) * 16 + lm;
-                if (col < n && row < m) {
-                    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-                    if (t && row + 4 <= m) {
-                        __builtin_memcpy(&x, p + (size_t)col * m + row, 16);
-                    } else {
+                const f32x4 x = state_at(p, b, state_row<E>(a, g, 0), col_of(c, lm), m, n, t);
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (row + r < m) x[r] = t ? p[(size_t)col * m + row + r] : p[(size_t)(row + r) * n + col];
-                    }
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) sum = fmaf(x[r], S[a][c][r], sum);
-                }
+                for (int r = 0; r < 4; ++r) sum = fmaf(x[r], S[a][c][r], sum);
             }
         return sum;
     }
 
-    // (1) P^T of the lower triangle.  The triangle's tiles are dealt to the waves in turn.
-    __device__ __forceinline__ void pairs(const Tile<E, M> &x, const Tile<E, M> &y, const Pairs<E> &P, const Gates<C> &gt) const {
+    // (1) P^T of the lower triangle, whose tiles are dealt to the waves in turn, and out^T = exp(b_i) S^T x^T of this wave's columns.
+    // Products that add to one accumulator are kept apart: each would wait for the one before.
+    __device__ __forceinline__ void begin(const Tile<E, M, kAlong> &x, const Tile<E, M, kBoth> &y, const Pairs<E> &P, const Gates<C> &gt) {
+        constexpr int kTiles = kI * (kI + 1) / 2, kMine = (kTiles + 3) / 4;
+        const Heads heads;
 #pragma unroll
-        for (int it = 0; it < kI; ++it)
+        for (int t = 0; t < kMine; ++t) {
+            // tile number t * 4 + w of the triangle, row by row (the last one more than once: the same values)
+            const int id = min(t * 4 + w, kTiles - 1);
+            int it = 0;
 #pragma unroll
-            for (int jt = 0; jt < kI; ++jt) {
-                if (jt > it || ((it * (it + 1) / 2 + jt) & 3) != w) continue;
-                f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+            for (int k = 1; k < kI; ++k) it += id >= k * (k + 1) / 2;
+            const int jt = id - it * (it + 1) / 2;
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f}, odd = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int ks = 0; ks < kSteps; ++ks) acc = product<E>(y.along(jt * 16 + lm, ks, g), x.along(it * 16 + lm, ks, g), acc);
-                const int i = it * 16 + lm, j0 = jt * 16 + g * 4;
-                const float wi = gt.whole[i], ri = gt.rest[i];
-                const f32x4 wj = *reinterpret_cast<const f32x4 *>(&gt.whole[j0]), rj = *reinterpret_cast<const f32x4 *>(&gt.rest[j0]);
-                f32x4 p;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) p[r] = j0 + r <= i ? acc[r] * exp2_fast((wi - wj[r]) + (ri - rj[r])) : 0.f;
-                if constexpr (sizeof(E) == 2) {
-                    u32x2 hi, lo;
-                    SPLIT_PAIR(p[0], p[1], hi[0], lo[0]);
-                    SPLIT_PAIR(p[2], p[3], hi[1], lo[1]);
-                    *reinterpret_cast<u32x2 *>(P.at(it, jt >> 1, 0, lane) + 8 * (jt & 1)) = hi;
-                    *reinterpret_cast<u32x2 *>(P.at(it, jt >> 1, 1, lane) + 8 * (jt & 1)) = lo;
-                    // the upper half of a diagonal operand
-                    if (jt == it && (jt & 1) == 0) {
-                        *reinterpret_cast<u32x2 *>(P.at(it, jt >> 1, 0, lane) + 8) = u32x2{0u, 0u};
-                        *reinterpret_cast<u32x2 *>(P.at(it, jt >> 1, 1, lane) + 8) = u32x2{0u, 0u};
-                    }
-                } else {
-                    *reinterpret_cast<f32x4 *>(P.at(it, jt, 0, lane)) = p;
-                }
+            for (int ks = 0; ks < kSteps; ++ks) {
+                f32x4 &to = ks & 1 ? odd : acc;
+                to = product<E>(y.along(jt, lm, ks, g), x.along(it, lm, ks, g), to);
             }
-    }
-    // (1) out^T = exp(b_i) S^T x^T
-    __device__ __forceinline__ void from_state(const Tile<E, M> &x, const Gates<C> &gt) {
+            acc += odd;
+            const int i = it * 16 + lm, j0 = jt * 16 + g * 4;
+            const float wi = gt.whole[i], ri = gt.rest[i];
+            f32x4 p;
+            if (jt == it) {
+                const f32x4 wj = *reinterpret_cast<const f32x4 *>(&gt.whole[j0]), rj = *reinterpret_cast<const f32x4 *>(&gt.rest[j0]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) p[r] = g * 4 + r <= lm ? acc[r] * exp2_fast((wi - wj[r]) + (ri - rj[r])) : 0.f;
+            } else {                                     // by way of the last step of j's tile
+                const float e = exp2_fast((wi - gt.whole[jt * 16 + 15]) + (ri - gt.rest[jt * 16 + 15]));
+                p = acc * (*reinterpret_cast<const f32x4 *>(&gt.tile[j0]) * e);
+            }
+            if constexpr (sizeof(E) == 2) {
+                const HiLo s0 = heads.split(p[0], p[1]), s1 = heads.split(p[2], p[3]);
+                const u32x2 hi = {s0.hi, s1.hi}, lo = {s0.lo, s1.lo};
+                *reinterpret_cast<u32x2 *>(P.at(it, jt >> 1, 0, lane) + 8 * (jt & 1)) = hi;
+                *reinterpret_cast<u32x2 *>(P.at(it, jt >> 1, 1, lane) + 8 * (jt & 1)) = lo;
+                // the upper half of a diagonal operand
+                if (jt == it && (jt & 1) == 0) {
+                    *reinterpret_cast<u32x2 *>(P.at(it, jt >> 1, 0, lane) + 8) = u32x2{0u, 0u};
+                    *reinterpret_cast<u32x2 *>(P.at(it, jt >> 1, 1, lane) + 8) = u32x2{0u, 0u};
+                }
+            } else {
+                *reinterpret_cast<f32x4 *>(P.at(it, jt, 0, lane)) = p;
+            }
+        }
 #pragma unroll
         for (int c = 0; c < kCols; ++c)
 #pragma unroll
             for (int it = 0; it < kI; ++it) O[c][it] = f32x4{0.f, 0.f, 0.f, 0.f};
+        u32x4 b[2][kI];
 #pragma unroll
-        for (int ks = 0; ks < kSteps; ++ks) {
+        for (int it = 0; it < kI; ++it) b[0][it] = x.along(it, lm, 0, g);
+#pragma unroll
+        for (int t = 0; t < kSteps; ++t) {
             u32x4 a[kCols][kParts];
 #pragma unroll
             for (int c = 0; c < kCols; ++c) {
@@ -341,19 +508,25 @@ struct Walker {
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
                         for (int r = 0; r < 2; ++r)
-                            SPLIT_PAIR(S[2 * ks + h][c][2 * r], S[2 * ks + h][c][2 * r + 1], a[c][0][2 * h + r], a[c][1][2 * h + r]);
+                        {
+                            const HiLo s = heads.split(S[2 * t + h][c][2 * r], S[2 * t + h][c][2 * r + 1]);
+                            a[c][0][2 * h + r] = s.hi;
+                            a[c][1][2 * h + r] = s.lo;
+                        }
                 } else {
-                    a[c][0] = __builtin_bit_cast(u32x4, S[ks][c]);
+                    a[c][0] = __builtin_bit_cast(u32x4, S[t][c]);
                 }
             }
+            if (t + 1 < kSteps) {
 #pragma unroll
-            for (int it = 0; it < kI; ++it) {
-                const u32x4 b = x.along(it * 16 + lm, ks, g);
-#pragma unroll
-                for (int c = 0; c < kCols; ++c)
-#pragma unroll
-                    for (int q = 0; q < kParts; ++q) O[c][it] = product<E>(a[c][q], b, O[c][it]);
+                for (int k = 0; k < kI; ++k) b[(t + 1) & 1][k] = x.along(k, lm, t + 1, g);
             }
+#pragma unroll
+            for (int q = 0; q < kParts; ++q)
+#pragma unroll
+                for (int k = 0; k < kI; ++k)
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c) O[c][k] = product<E>(a[c][q], b[t & 1][k], O[c][k]);
         }
 #pragma unroll
         for (int it = 0; it < kI; ++it) {
@@ -364,30 +537,26 @@ struct Walker {
     }
     // (2) OUT: out^T += z^T P^T.  The state: S = exp(b_last) S + y^T (exp(b_last - b_j) z)
     template <bool OUT>
-    __device__ __forceinline__ void advance(const Tile<E, M> &y, const Tile<E, N> &z, const Pairs<E> &P, const Gates<C> &gt) {
+    __device__ __forceinline__ void advance(const Tile<E, M, kBoth> &y, const Tile<E, N, ZA ? kBoth : kAcross> &z, const Pairs<E> &P, const Gates<C> &gt) {
         const float last = gt.last;
-#pragma unroll
-        for (int a = 0; a < kRows; ++a)
-#pragma unroll
-            for (int c = 0; c < kCols; ++c) S[a][c] *= last;
+        const Heads heads;
+        u32x4 zd[kJ][kCols][kParts];
 #pragma unroll
         for (int jk = 0; jk < kJ; ++jk) {
             u32x4 zf[kCols];
 #pragma unroll
-            for (int c = 0; c < kCols; ++c) zf[c] = z.template across<false>(jk, col_tile(c), lm, g);
+            for (int c = 0; c < kCols; ++c) zf[c] = z.across(jk, col_tile(c), lm, g);
             if constexpr (OUT) {
 #pragma unroll
-                for (int it = 0; it < kI; ++it) {
-                    if (jk * kDeep > it * 16 + 15) continue;
+                for (int q = 0; q < kParts; ++q)
 #pragma unroll
-                    for (int q = 0; q < kParts; ++q) {
+                    for (int it = 0; it < kI; ++it) {
+                        if (jk * kDeep > it * 16 + 15) continue;
                         const u32x4 b = *reinterpret_cast<const u32x4 *>(P.at(it, jk, q, lane));
 #pragma unroll
                         for (int c = 0; c < kCols; ++c) O[c][it] = product<E>(zf[c], b, O[c][it]);
                     }
-                }
             }
-            u32x4 zd[kCols][kParts];
             if constexpr (sizeof(E) == 2) {
                 const f32x4 d0 = *reinterpret_cast<const f32x4 *>(&gt.out[jk * 32 + g * 4]);
                 const f32x4 d1 = *reinterpret_cast<const f32x4 *>(&gt.out[jk * 32 + 16 + g * 4]);
@@ -396,56 +565,89 @@ struct Walker {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const f32x4 &d = r < 2 ? d0 : d1;
-                        SPLIT_PAIR(bf16_lo_as_float(zf[c][r]) * d[2 * (r & 1)], bf16_hi_as_float(zf[c][r]) * d[2 * (r & 1) + 1], zd[c][0][r],
-                                   zd[c][1][r]);
+                        const HiLo s = heads.split(bf16_lo_as_float(zf[c][r]) * d[2 * (r & 1)], bf16_hi_as_float(zf[c][r]) * d[2 * (r & 1) + 1]);
+                        zd[jk][c][0][r] = s.hi;
+                        zd[jk][c][1][r] = s.lo;
                     }
             } else {
                 const f32x4 d = *reinterpret_cast<const f32x4 *>(&gt.out[jk * 16 + g * 4]);
 #pragma unroll
-                for (int c = 0; c < kCols; ++c) zd[c][0] = __builtin_bit_cast(u32x4, __builtin_bit_cast(f32x4, zf[c]) * d);
+                for (int c = 0; c < kCols; ++c) zd[jk][c][0] = __builtin_bit_cast(u32x4, __builtin_bit_cast(f32x4, zf[c]) * d);
             }
+        }
+        // two tiles of state rows at a time, so that products of one accumulator are four apart, and the next operands on their way
+        u32x4 yf[2][2][kJ];
+        auto fetch_rows = [&](int a, u32x4(&to)[2][kJ]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int a = 0; a < kRows; ++a) {
-                const u32x4 yf = y.template across<true>(jk, a, lm, g);
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int c = 0; c < kCols; ++c)
+                for (int jk = 0; jk < kJ; ++jk) to[h][jk] = y.across(jk, a + h, lm, g);
+        };
+        fetch_rows(0, yf[0]);
 #pragma unroll
-                    for (int q = 0; q < kParts; ++q) S[a][c] = product<E>(yf, zd[c][q], S[a][c]);
-            }
+        for (int a = 0; a < kRows; a += 2) {
+            if (a + 2 < kRows) fetch_rows(a + 2, yf[(a >> 1) + 1 & 1]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) S[a + h][c] *= last;
+#pragma unroll
+            for (int jk = 0; jk < kJ; ++jk)
+#pragma unroll
+                for (int q = 0; q < kParts; ++q)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int c = 0; c < kCols; ++c) S[a + h][c] = product<E>(yf[a >> 1 & 1][h][jk], zd[jk][c][q], S[a + h][c]);
         }
     }
     // out row . dot row, this wave's columns, to part[w * C + row]; the dot rows from memory, or with LDS_ROWS from the tile
-    template <bool LDS_ROWS, typename TokenOf>
-    __device__ __forceinline__ void dot_rows(const Rows &r, const Tile<E, N> &t, float *part, int count, TokenOf token) const {
+    template <bool LDS_ROWS>
+    __device__ __forceinline__ void dot_rows(const Rows &r, const Tile<E, N, kAlong> &t, float *part, const Steps &st) const {
         const auto [lm, g] = fresh();
+        constexpr int size = (int)sizeof(E);
+        const Rsrc b = chunk_view(r, st);
+        uint32_t o[kI];
+        if constexpr (FAST && !LDS_ROWS) st.offsets(o, lm, 16, (uint32_t)r.step, st.count, 0u);
 #pragma unroll
         for (int it = 0; it < kI; ++it) {
             const int i = it * 16 + lm;
             float sum = 0.f;
-            if (LDS_ROWS || i < count) {
-                const char *row = LDS_ROWS ? t.p + i * Tile<E, N>::kRow : r.base + token(i) * r.step;
 #pragma unroll
-                for (int c = 0; c < kCols; ++c) {
-                    const int col = col_tile(c) * 16 + g * 4;
-                    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-                    if (LDS_ROWS || col + 4 <= r.d) {
-                        if constexpr (sizeof(E) == 2) {
-                            u32x2 b;
-                            __builtin_memcpy(&b, row + col * 2, 8);
-                            x = f32x4{bf16_lo_as_float(b[0]), bf16_hi_as_float(b[0]), bf16_lo_as_float(b[1]), bf16_hi_as_float(b[1])};
-                        } else {
-                            __builtin_memcpy(&x, row + col * 4, 16);
-                        }
+            for (int c = 0; c < kCols; ++c) {
+                const int col = cols_of(c, g);
+                uint32_t bits[4] = {0u, 0u, 0u, 0u};
+                if constexpr (LDS_ROWS) {
+                    __builtin_memcpy(bits, t.at(i, col), 4 * size);
+                } else if constexpr (FAST) {
+                    // (nowhere stays nowhere with a column's offset added)
+                    const uint32_t at = col < r.d ? o[it] + col * size : kNowhere;
+                    if constexpr (size == 2) {
+                        const u32x2 v = fetch<u32x2>(b, at);
+                        __builtin_memcpy(bits, &v, 8);
+                    } else {
+                        const u32x4 v = fetch<u32x4>(b, at);
+                        __builtin_memcpy(bits, &v, 16);
+                    }
+                } else if (i < st.count) {
+                    const char *row = r.token((long long)st.first + st.at(i));
+                    if (col + 4 <= r.d) {
+                        __builtin_memcpy(bits, row + col * size, 4 * size);
                     } else {
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
                             if (col + j < r.d) {
-                                if constexpr (sizeof(E) == 2) x[j] = bf16_bits_to_float(reinterpret_cast<const uint16_t *>(row)[col + j]);
-                                else x[j] = reinterpret_cast<const float *>(row)[col + j];
+                                if constexpr (size == 2) bits[j >> 1] |= (uint32_t)reinterpret_cast<const uint16_t *>(row)[col + j] << (16 * (j & 1));
+                                else bits[j] = reinterpret_cast<const uint32_t *>(row)[col + j];
                             }
                     }
+                }
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) sum = fmaf(x[j], O[c][it][j], sum);
+                for (int j = 0; j < 4; ++j) {
+                    float x;
+                    if constexpr (size == 2) x = j & 1 ? bf16_hi_as_float(bits[j >> 1]) : bf16_lo_as_float(bits[j >> 1]);
+                    else x = __builtin_bit_cast(float, bits[j]);
+                    sum = fmaf(x, O[c][it][j], sum);
                 }
             }
             sum += __shfl_xor(sum, 16);
@@ -453,18 +655,33 @@ struct Walker {
             if (g == 0) part[w * C + i] = sum;
         }
     }
-    // rows of the chunk out of the accumulators; token(i) of row i
-    template <typename TokenOf>
-    __device__ __forceinline__ void store_rows(const Rows &r, int out_dtype, int count, TokenOf token) const {
+    // rows of the chunk out of the accumulators
+    __device__ __forceinline__ void store_rows(const Rows &r, int out_dtype, const Steps &st) const {
         const auto [lm, g] = fresh();
+        const Rsrc b = chunk_view(r, st);
+        uint32_t o[kI];
+        if constexpr (FAST) st.offsets(o, lm, 16, (uint32_t)r.step, st.count, 0u);
 #pragma unroll
         for (int it = 0; it < kI; ++it) {
             const int i = it * 16 + lm;
-            if (i >= count) continue;
-            char *row = const_cast<char *>(r.base) + token(i) * r.step;
+            if constexpr (FAST) {
+                const uint32_t at = o[it];
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) {
+                    const int col = cols_of(c, g);
+                    const f32x4 x = O[c][it];
+                    if (out_dtype == GLA_DT_BF16)
+                        put(b, col < r.d ? at + col * 2 : kNowhere, u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])});
+                    else
+                        put(b, col < r.d ? at + col * 4 : kNowhere, x);
+                }
+                continue;
+            }
+            if (i >= st.count) continue;
+            char *row = const_cast<char *>(r.token((long long)st.first + st.at(i)));
 #pragma unroll
             for (int c = 0; c < kCols; ++c) {
-                const int col = col_tile(c) * 16 + g * 4;
+                const int col = cols_of(c, g);
                 const f32x4 x = O[c][it];
                 if (out_dtype == GLA_DT_BF16) {
                     const u32x2 v = {pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
@@ -486,27 +703,6 @@ struct Walker {
         }
     }
 };
-
-// Rows of one sequence: what a walk visits in which order.  Chunk number ci covers steps [ci * C, min((ci + 1) * C, len)) whichever
-// way it is walked; backwards row 0 is the last of them.
-struct Order {
-    int scan_dir, len, grid_h, grid_w;
-    int T;
-    __device__ __forceinline__ int token(int s) const { return scan_token(scan_dir, s, len, grid_h, grid_w); }
-};
-__device__ inline Order order_of(const DecayCall &c, int bh) {
-    Order o;
-    o.scan_dir = c.scan_dir;
-    o.grid_h = c.grid_h;
-    o.grid_w = c.grid_w;
-    o.T = c.T;
-    o.len = c.T;
-    if (c.seq_lens != nullptr) {
-        const int n = c.seq_lens[bh / c.H];
-        o.len = n < 0 ? 0 : n < c.T ? n : c.T;       // (a length outside 0 .. T counts as the nearer end)
-    }
-    return o;
-}
 
 // log_decay of step s (0 outside the sequence)
 __device__ inline float gate_of(const DecayCall &c, const Order &o, int bh, int s) {
@@ -530,6 +726,18 @@ __device__ inline void clear_behind(const Rows &r, int size, int len, int s0, in
             else reinterpret_cast<float *>(row)[j] = 0.f;
         }
     }
+}
+
+// f(M, N, FAST) of the kernels for states of m x n
+template <typename F>
+hipError_t decay_sizes(int m, int n, bool fast, F f) {
+    typedef std::integral_constant<int, 64> Small;
+    typedef std::integral_constant<int, 128> Large;
+    auto with = [&](auto quick) {
+        if (m > 64) return n > 64 ? f(Large(), Large(), quick) : f(Large(), Small(), quick);
+        return n > 64 ? f(Small(), Large(), quick) : f(Small(), Small(), quick);
+    };
+    return fast ? with(std::true_type()) : with(std::false_type());
 }
 
 }  // namespace

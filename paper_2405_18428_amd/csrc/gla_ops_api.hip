@@ -102,6 +102,12 @@ int check_call(DecayCall &c, const float *log_decay, int kind, const int *seq_le
     c.grid_w = grid_w;
     c.scan_dir = scan_dir;
     c.layout = layout;
+    // rows of whole dwords, at least one piece of 16 bytes long; 24-bit factors; offsets inside a chunk below 2^31 (a column's rows lie
+    // all over the sequence)
+    const long long wide = dk > dv ? dk : dv, least = dk < dv ? dk : dv, step = wide * 4 * (layout == GLA_LAYOUT_BTHD ? H : 1);
+    const long long reach = (scan_dir >= GLA_SCAN_COL_FWD ? T : 64) * step;
+    c.fast = dk % 4 == 0 && dv % 4 == 0 && least * (dtype == GLA_DT_BF16 ? 2 : 4) >= 16 && step < (1LL << 24) && T < (1 << 24) &&
+             reach < (1LL << 31) - (1 << 16);
     c.nspans = spans_of(B, H, T);
     c.span_len = (decay_blocks(T) + c.nspans - 1) / c.nspans * kFlowBlock;
     return GLA_OK;
