@@ -624,18 +624,19 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _want(name, t, shape, dtype, device):
-    """Raises unless t is a contiguous GPU tensor of this shape and element type on the call's device."""
-    if not t.is_cuda or t.device != device or not t.is_contiguous() or tuple(t.shape) != tuple(shape):
+def _want(name, t, shape, dtype, gpu):
+    """Raises unless t is a contiguous tensor of this shape and element type on GPU number `gpu` (-1: not on a GPU)."""
+    if gpu < 0 or t.get_device() != gpu or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous GPU tensor {list(shape)} on the device of the others")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be of element type {dtype}")
 
 
-def _room(nbytes, workspace, device):
+def _room(nbytes, workspace, q):
+    """The caller's workspace, or one of its size for this call; `nbytes` is asked for in that case only."""
     if workspace is None:
-        return _torch().empty((max(nbytes, 16),), dtype=_torch().uint8, device=device)
-    if not workspace.is_cuda or workspace.device != device or not workspace.is_contiguous():
+        return _torch().empty((max(nbytes(), 16),), dtype=_torch().uint8, device=q.device)
+    if workspace.get_device() != q.get_device() or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous GPU tensor on the device of the others")
     return workspace
 
@@ -647,7 +648,7 @@ def _prep_decay(q, k, v, log_decay, layout, seq_lens, states):
     if q.dim() != 4 or v.dim() != 4:
         raise ValueError("q, k, v must be 4-d")
     _dt(q)
-    dev = q.device
+    dev = q.get_device()
     _want("q", q, q.shape, q.dtype, dev)
     _want("k", k, q.shape, q.dtype, dev)
     _want("v", v, (*q.shape[:3], v.shape[3]), q.dtype, dev)
@@ -684,11 +685,11 @@ def gla_decay_fwd(q, k, v, log_decay, grid_h, grid_w, scan_dir=SCAN_ROW_FWD, lay
     if out is None:
         out = _like(v, torch.float32 if out_dtype is None else out_dtype)
     else:
-        _want("out", out, v.shape, out.dtype, q.device)
+        _want("out", out, v.shape, out.dtype, q.get_device())
     if final_state is None and want_final_state:
         final_state = q.new_empty((B, H, dk, dv), dtype=torch.float32)
     qdt = _dt(q)
-    workspace = _room(gla_decay_fwd_workspace_bytes(B, H, T, dk, dv, qdt), workspace, q.device)
+    workspace = _room(lambda: gla_decay_fwd_workspace_bytes(B, H, T, dk, dv, qdt), workspace, q)
     with _on_device_of(q):
         _check(lib.gla_decay_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), kind, _ptr(seq_lens),
                                  B, H, T, dk, dv, grid_h, grid_w, scan_dir, qdt, _dt(out), layout, _ptr(initial_state),
@@ -706,13 +707,13 @@ def gla_decay_bwd(q, k, v, log_decay, d_out, grid_h, grid_w, scan_dir=SCAN_ROW_F
     lib = load_library()
     kind, B, H, T, dk, dv = _prep_decay(q, k, v, log_decay, layout, seq_lens,
                                         (("initial_state", initial_state), ("d_final_state", d_final_state)))
-    _want("d_out", d_out, v.shape, q.dtype, q.device)
+    _want("d_out", d_out, v.shape, q.dtype, q.get_device())
     gdt = torch.float32 if grad_dtype is None else grad_dtype
     dq, dk_, dv_ = _like(q, gdt), _like(k, gdt), _like(v, gdt)
     dg = _like(log_decay, torch.float32) if want_d_log_decay else None
     ds = q.new_empty((B, H, dk, dv), dtype=torch.float32) if want_d_initial_state else None
     qdt = _dt(q)
-    workspace = _room(gla_decay_bwd_workspace_bytes(B, H, T, dk, dv, qdt), workspace, q.device)
+    workspace = _room(lambda: gla_decay_bwd_workspace_bytes(B, H, T, dk, dv, qdt), workspace, q)
     with _on_device_of(q):
         _check(lib.gla_decay_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), kind, _ptr(seq_lens),
                                  d_out.data_ptr(), _ptr(initial_state), _ptr(d_final_state), B, H, T, dk, dv, grid_h, grid_w,
@@ -730,7 +731,7 @@ def gla_decay_step(q, k, v, log_decay, state, out_dtype=None, out=None, state_ou
         raise ValueError("q, k must be [B,H,dk] and v [B,H,dv]")
     B, H, dk = q.shape
     dv = v.shape[2]
-    qdt, dev = _dt(q), q.device
+    qdt, dev = _dt(q), q.get_device()
     _want("q", q, (B, H, dk), q.dtype, dev)
     _want("k", k, (B, H, dk), q.dtype, dev)
     _want("v", v, (B, H, dv), q.dtype, dev)
@@ -763,7 +764,7 @@ def gla_rope(q, k, sections, grid_h=0, grid_w=0, positions=None, base=10000.0, p
         raise ValueError("unknown layout")
     if q.dim() != 4:
         raise ValueError("q must be 4-d")
-    dt, dev = _dt(q), q.device
+    dt, dev = _dt(q), q.get_device()
     _want("q", q, q.shape, q.dtype, dev)
     if k is not None:
         _want("k", k, q.shape, q.dtype, dev)
@@ -793,16 +794,16 @@ def _prep_norm(x, weight, bias, r_pre, layout):
     if x.dim() not in (3, 4):
         raise ValueError("x must be [B,H,T,D], [B,T,H,D] or [B,T,D]")
     _dt(x)
-    _want("x", x, x.shape, x.dtype, x.device)
+    _want("x", x, x.shape, x.dtype, x.get_device())
     if x.dim() == 3:
         B, H, T, D = x.shape[0], 1, x.shape[1], x.shape[2]
     else:
         B, H, T, D = x.shape if layout == LAYOUT_BHTD else (x.shape[0], x.shape[2], x.shape[1], x.shape[3])
     for name, t in (("weight", weight), ("bias", bias)):
         if t is not None:
-            _want(name, t, (D,) if t.dim() == 1 and H == 1 else (H, D), torch.float32, x.device)
+            _want(name, t, (D,) if t.dim() == 1 and H == 1 else (H, D), torch.float32, x.get_device())
     if r_pre is not None:
-        _want("r_pre", r_pre, x.shape, x.dtype, x.device)
+        _want("r_pre", r_pre, x.shape, x.dtype, x.get_device())
     return B, H, T, D
 
 
@@ -814,7 +815,7 @@ def gla_norm_fwd(x, weight=None, bias=None, eps=1e-5, r_pre=None, layout=LAYOUT_
     if out is None:
         out = _like(x, x.dtype if out_dtype is None else out_dtype)
     else:
-        _want("out", out, x.shape, out.dtype, x.device)
+        _want("out", out, x.shape, out.dtype, x.get_device())
         if out.data_ptr() == x.data_ptr() and out.dtype != x.dtype:
             raise ValueError("in place only with one element type")
     with _on_device_of(x):
@@ -834,7 +835,7 @@ def gla_norm_bwd(x, d_out, weight=None, bias=None, eps=1e-5, r_pre=None, layout=
     torch = _torch()
     lib = load_library()
     B, H, T, D = _prep_norm(x, weight, bias, r_pre, layout)
-    _want("d_out", d_out, x.shape, x.dtype, x.device)
+    _want("d_out", d_out, x.shape, x.dtype, x.get_device())
     gdt = torch.float32 if grad_dtype is None else grad_dtype
     dx = _like(x, gdt)
     dr = _like(x, gdt) if r_pre is not None else None
@@ -843,7 +844,7 @@ def gla_norm_bwd(x, d_out, weight=None, bias=None, eps=1e-5, r_pre=None, layout=
         like = weight if weight is not None else bias
         shape = (H, D) if like is None else like.shape
         dw, db = x.new_empty(shape, dtype=torch.float32), x.new_empty(shape, dtype=torch.float32)
-    workspace = _room(gla_norm_bwd_workspace_bytes(B, H, T, D), workspace, x.device)
+    workspace = _room(lambda: gla_norm_bwd_workspace_bytes(B, H, T, D), workspace, x)
     with _on_device_of(x):
         _check(lib.gla_norm_bwd(x.data_ptr(), d_out.data_ptr(), _ptr(weight), _ptr(bias), float(eps), _ptr(r_pre), B, H, T, D, _dt(x), _dt(dx),
                                 layout, dx.data_ptr(), _ptr(dr), _ptr(dw), _ptr(db), workspace.data_ptr(),

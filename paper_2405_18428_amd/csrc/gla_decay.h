@@ -33,7 +33,15 @@ struct DecayCall {
     int B, H, T, dk, dv, grid_h, grid_w, scan_dir;
     int layout;                         // gla_layout
     int fast;                           // rows through 32-bit views (gla_decay_util.h)
-    int nspans, span_len;               // spans a sequence is walked in, steps in each (a multiple of kFlowBlock)
+    int nspans, span_len;               // spans a sequence is walked in, steps in each (a multiple of 64)
+};
+
+// The states that enter the spans: `first` [B*H, dk, dv] (or null: zero) the first span walked; behind it, with `local` [B*H, nspans, dk, dv] and
+// the base-2 logs of the spans' decays, what the walk chains for itself from the local states of the spans before its own, or
+// with `chained` entry sp of `local` as it is.
+struct DecayEntry {
+    const float *first, *local, *decay;
+    int chained;
 };
 
 // One walk: the recurrence of (x, y, z) in place of (q, k, v).  x and y are dk or dv wide (m), z is the other or the same (n);
@@ -50,7 +58,7 @@ struct DecayWalk {
     DecayCall c;
     DecayRole r;
     // states lie as [.., dk, dv]; with state_t a walk whose m is dv reads and writes them transposed
-    const float *state_in;              // [B*H, nspans, dk, dv], or with nspans = 1 [B*H, dk, dv], or null: zero
+    DecayEntry in;
     float *state_out;                   // [B*H, dk, dv] after the last step, or null
     float *anchors;                     // [B*H, blocks, dk, dv] or null: the state at the end of each block of kFlowBlock steps
     int anchor_last;                    // the last block's too
@@ -66,7 +74,7 @@ struct DecayBack {
     DecayCall c;
     const void *q, *k, *v, *d_out;
     void *dk_grad, *dv_grad;
-    const float *state_in;              // adjoint states that enter the spans from behind, like DecayWalk::state_in
+    DecayEntry in;                      // adjoint states, from behind
     float *d_initial;                   // [B*H, dk, dv] or null
     const float *anchors;               // what the walk for dq left, or null: no gate gradient
     int anchor_last;

@@ -51,7 +51,7 @@ __global__ __launch_bounds__(kThreads, 2) void decay_walk_kernel(const DecayWalk
         pz.issue(rz, tid, st);
     };
     if (s0 < end) issue(s0);
-    wk.load_state(p.state_in == nullptr ? nullptr : p.state_in + (size_t)blockIdx.x * cells, m, n, p.state_t);
+    wk.enter(p.in, bh, sp, p.c.nspans, false, m, n, p.state_t);
     if (wk.w == 3 && s0 < end) form_gates(gates[0], gate, lane);
     int turn = 0;
     for (int s = s0; s < end; s += C, turn ^= 1) {
@@ -62,7 +62,9 @@ __global__ __launch_bounds__(kThreads, 2) void decay_walk_kernel(const DecayWalk
         pz.commit(rz, tid, tz);
         __syncthreads();
         if (s + C < end) issue(s + C);
+        __builtin_amdgcn_s_setprio(1);                   // before the other work-group's loads and stores (3 % less time)
         wk.begin(tx, ty, P, gt);
+        __builtin_amdgcn_s_setprio(0);
         __syncthreads();
         if (wk.w == 3 && s + C < end) form_gates(gates[turn ^ 1], gate, lane);
         wk.template advance<true>(ty, tz, P, gt);
@@ -103,6 +105,7 @@ __global__ __launch_bounds__(kThreads, 2) void decay_state_kernel(const StatePai
     const DecayWalk &p = both.w[blockIdx.y];
     const int tid = threadIdx.x, lane = tid & 63;
     const int walked = p.c.nspans - 1;                   // nobody needs the last one's
+    if ((int)blockIdx.x >= p.c.B * p.c.H * walked) return;
     const int bh = blockIdx.x / walked, sp = blockIdx.x - bh * walked + (back ? 1 : 0);
     const Order ord = order_of(p.c, bh);
     const int s0 = sp * p.c.span_len, end = min(min(s0 + p.c.span_len, p.c.T), ord.len);
@@ -140,7 +143,7 @@ __global__ __launch_bounds__(kThreads, 2) void decay_state_kernel(const StatePai
         __syncthreads();
     }
     const size_t at = (size_t)bh * p.c.nspans + sp;
-    wk.store_state(p.local + at * m * n, m, n, false);
+    wk.store_state(p.local + at * m * n, m, n, p.state_t);
     if (tid == 0) p.decay[at] = sum;
 }
 
@@ -182,13 +185,16 @@ hipError_t states(const StatePair &w, int directions, hipStream_t stream) {
     const hipError_t e = configured(decay_state_kernel<E, M, N, FAST>, bytes, done);
     if (e != hipSuccess) return e;
     const DecayCall &c = w.w[0].c;
-    hipLaunchKernelGGL((decay_state_kernel<E, M, N, FAST>), dim3((unsigned)(c.B * c.H * (c.nspans - 1)), (unsigned)directions), dim3(kThreads),
+    const int spans = directions == 2 && w.w[1].c.nspans > c.nspans ? w.w[1].c.nspans : c.nspans;
+    hipLaunchKernelGGL((decay_state_kernel<E, M, N, FAST>), dim3((unsigned)(c.B * c.H * (spans - 1)), (unsigned)directions), dim3(kThreads),
                        bytes, stream, w);
     return hipGetLastError();
 }
 
-// One token: a wave takes 64 / (N / 4) rows of a state at a time, a lane four columns of it; a work-group all rows of one (batch, head).
-// Bound by the state's way in and out.
+// One token.  A work-group takes kStepCols columns of one (batch, head)'s state, eight lanes of four columns by 32 rows, all of whose rows it
+// asks for before it uses the first: columns need nothing of each other, and so 16 heads of one sequence are 64 work-groups.  Bound by the
+// states' way in and out (192 sequences of 16 heads 128 x 128: 77 us, 5.2 TB/s, what a copy reaches), for few sequences by the launch.
+constexpr int kStepCols = 32, kStepRows = kThreads / (kStepCols / 4);
 template <typename E>
 __device__ inline float element(const void *p, size_t i) {
     if constexpr (sizeof(E) == 2) return bf16_bits_to_float(static_cast<const uint16_t *>(p)[i]);
@@ -199,54 +205,62 @@ template <typename E>
 __global__ __launch_bounds__(kThreads) void decay_step_kernel(const void *q, const void *k, const void *v, const float *log_decay, int kind,
                                                               int H, int dk, int dv, int out_dtype, const float *state, float *state_out,
                                                               void *out) {
-    __shared__ float s_q[kDecayMaxD], s_k[kDecayMaxD], s_o[8 * kDecayMaxD];
-    const int tid = threadIdx.x, bh = blockIdx.x, h = bh % H;
-    if (tid < dk) {
-        s_q[tid] = element<E>(q, (size_t)bh * dk + tid);
-        s_k[tid] = element<E>(k, (size_t)bh * dk + tid);
-    }
-    const float a = exp2_fast(fmaxf(log_decay[kind == kDecayHead ? h : bh] * kLog2e, -65536.f));
-    __syncthreads();
+    constexpr int kTimes = kDecayMaxD / kStepRows;
+    __shared__ float s_o[kThreads / 64][kStepCols];
+    const int tid = threadIdx.x, parts = (dv + kStepCols - 1) / kStepCols;
+    const int bh = blockIdx.x / parts, h = bh % H, c0 = (blockIdx.x - bh * parts) * kStepCols;
+    const int col = c0 + (tid & 7) * 4, row0 = tid >> 3;
     const size_t cells = (size_t)dk * dv;
     const float *s = state + bh * cells;
     float *t = state_out + bh * cells;
-    // 32 lanes x 4 columns cover a row of up to 128; 8 rows a step of the work-group
-    const int col = (tid & 31) * 4, row0 = tid >> 5;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    if (col + 4 <= dv) {
-        f32x4 x;
+    f32x4 c[kTimes];
+    float qr[kTimes], kr[kTimes];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = element<E>(v, (size_t)bh * dv + col + j);
-        for (int r = row0; r < dk; r += 8) {
-            f32x4 c;
-            __builtin_memcpy(&c, s + (size_t)r * dv + col, 16);
-            const float kr = s_k[r], qr = s_q[r];
+    for (int i = 0; i < kTimes; ++i) {
+        const int r = row0 + i * kStepRows;
+        c[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        qr[i] = kr[i] = 0.f;
+        if (r >= dk) continue;
+        if (col + 4 <= dv) {
+            __builtin_memcpy(&c[i], s + (size_t)r * dv + col, 16);
+        } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                c[j] = fmaf(a, c[j], kr * x[j]);
-                o[j] = fmaf(qr, c[j], o[j]);
-            }
-            __builtin_memcpy(t + (size_t)r * dv + col, &c, 16);
+            for (int j = 0; j < 4; ++j)
+                if (col + j < dv) c[i][j] = s[(size_t)r * dv + col + j];
         }
-    } else {
-        for (int r = row0; r < dk; r += 8) {
-            const float kr = s_k[r], qr = s_q[r];
+        qr[i] = element<E>(q, (size_t)bh * dk + r);
+        kr[i] = element<E>(k, (size_t)bh * dk + r);
+    }
+    f32x4 x = {0.f, 0.f, 0.f, 0.f}, o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (col + j >= dv) continue;
-                const float c = fmaf(a, s[(size_t)r * dv + col + j], kr * element<E>(v, (size_t)bh * dv + col + j));
-                t[(size_t)r * dv + col + j] = c;
-                o[j] = fmaf(qr, c, o[j]);
-            }
+    for (int j = 0; j < 4; ++j)
+        if (col + j < dv) x[j] = element<E>(v, (size_t)bh * dv + col + j);
+    const float a = exp2_fast(fmaxf(log_decay[kind == kDecayHead ? h : bh] * kLog2e, -65536.f));
+#pragma unroll
+    for (int i = 0; i < kTimes; ++i) {
+        const int r = row0 + i * kStepRows;
+        c[i] = c[i] * a + x * kr[i];
+        o += c[i] * qr[i];
+        if (r >= dk) continue;
+        if (col + 4 <= dv) {
+            __builtin_memcpy(t + (size_t)r * dv + col, &c[i], 16);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (col + j < dv) t[(size_t)r * dv + col + j] = c[i][j];
         }
     }
-    *reinterpret_cast<f32x4 *>(&s_o[row0 * kDecayMaxD + col]) = o;
-    __syncthreads();
-    if (tid < dv) {
-        float y = 0.f;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) y += s_o[r * kDecayMaxD + tid];
-        const size_t at = (size_t)bh * dv + tid;
+    for (int j = 0; j < 4; ++j) {
+        float y = o[j];
+#pragma unroll
+        for (int d = 8; d < 64; d *= 2) y += __shfl_xor(y, d);
+        if ((tid & 56) == 0) s_o[tid >> 6][(tid & 7) * 4 + j] = y;
+    }
+    __syncthreads();
+    if (tid < kStepCols && c0 + tid < dv) {
+        const float y = (s_o[0][tid] + s_o[1][tid]) + (s_o[2][tid] + s_o[3][tid]);
+        const size_t at = (size_t)bh * dv + c0 + tid;
         if (out_dtype == GLA_DT_BF16) static_cast<uint16_t *>(out)[at] = float_to_bf16_bits(y);
         else static_cast<float *>(out)[at] = y;
     }
@@ -287,7 +301,7 @@ hipError_t launch_decay_carry(const DecayCall &c, const float *first, float *loc
 
 hipError_t launch_decay_step(const void *q, const void *k, const void *v, const float *log_decay, int kind, int B, int H, int dk, int dv,
                              int dtype, int out_dtype, const float *state, float *state_out, void *out, hipStream_t stream) {
-    const dim3 grid((unsigned)(B * H));
+    const dim3 grid((unsigned)(B * H * ((dv + kStepCols - 1) / kStepCols)));
     if (dtype == GLA_DT_BF16)
         hipLaunchKernelGGL(decay_step_kernel<uint16_t>, grid, dim3(kThreads), 0, stream, q, k, v, log_decay, kind, H, dk, dv, out_dtype, state,
                            state_out, out);

@@ -60,7 +60,7 @@ __device__ __forceinline__ void walk_back(const DecayBack &p, char *lds) {
         issue(s0 + (chunks - 1) * C, end);
         if (ROLE == 0 && wk.w == 3) form_gates(gates[(chunks - 1) & 1], gate, wk.lane);
     }
-    wk.load_state(p.state_in == nullptr ? nullptr : p.state_in + (size_t)blockIdx.x * cells, m, n, ROLE == 1);
+    wk.enter(p.in, bh, sp, p.c.nspans, true, m, n, ROLE == 1);
     for (int ci = chunks - 1; ci >= 0; --ci) {
         const int s = s0 + ci * C, e = min(s + C, end), count = e - s;
         const Gates<C> &gt = gates[ci & 1];

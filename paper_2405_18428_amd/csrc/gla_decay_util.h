@@ -398,6 +398,29 @@ struct Walker {
                 if (p != nullptr) S[a][c] = state_at(p, b, state_row<E>(a, g, 0), col_of(c, lm), m, n, t);
             }
     }
+    // S = factor S + the state at p
+    __device__ __forceinline__ void add_state(const float *p, int m, int n, bool t, float factor) {
+        const auto [lm, g] = fresh();
+        const Rsrc b = view(p, kNowhere);
+#pragma unroll
+        for (int a = 0; a < kRows; ++a)
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) S[a][c] = S[a][c] * factor + state_at(p, b, state_row<E>(a, g, 0), col_of(c, lm), m, n, t);
+    }
+    // the state that enters span sp, walked forward or (back) from the last span to the first
+    __device__ __forceinline__ void enter(const DecayEntry &e, int bh, int sp, int nspans, bool back, int m, int n, bool t) {
+        const size_t cells = (size_t)m * n;
+        const int before = back ? nspans - 1 - sp : sp;
+        if (e.chained) {
+            load_state(e.local + ((size_t)bh * nspans + sp) * cells, m, n, t);
+            return;
+        }
+        load_state(e.first == nullptr ? nullptr : e.first + (size_t)bh * cells, m, n, t);
+        for (int k = 0; k < before; ++k) {
+            const size_t at = (size_t)bh * nspans + (back ? nspans - 1 - k : k);
+            add_state(e.local + at * cells, m, n, t, exp2_fast(e.decay[at]));
+        }
+    }
     __device__ __forceinline__ void store_state(float *p, int m, int n, bool t, float factor = 1.f) const {
         const auto [lm, g] = fresh();
         const Rsrc b = view(p, kNowhere);

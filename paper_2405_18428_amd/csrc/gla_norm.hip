@@ -3,10 +3,11 @@
 //   n = (x - mean) rstd,  dy = dO r sigmoid(r) (or dO),  dn = dy weight,
 //   dx = rstd (dn - mean(dn) - n mean(dn n)),   dr = dO y sigmoid(r) (1 + r (1 - sigmoid(r))),
 //   dweight = sum over rows of dy n,   dbias = sum over rows of dy.
-// A row is held in registers by a group of lanes (16, 64, 256 or 1024 by its width), so it is read once; mean and variance are taken in two
+// A row is held in registers by a group of lanes (16 to 1024 by its width), so it is read once; mean and variance are taken in two
 // steps from these registers, and the backward pass takes them again instead of reading them.  Each group stays with one head, whose weights
-// it holds, and walks the head's rows; the sums for dweight and dbias stay in its registers, one partial sum a slot goes to
-// memory, and a second kernel adds the slots in one order.  Bound by HBM.
+// it holds, and walks the head's rows, the next of which is on its way while it works on one; the sums for dweight and dbias stay in its
+// registers, are added over the groups of a work-group where these share a head, and go to memory as one partial sum a slot, which a
+// second kernel adds in one order.  Bound by HBM.
 #include "gla_ops.h"
 
 namespace gla {
@@ -23,34 +24,38 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), bf16x2));
 }
 
+// Eight channels as they lie in memory
+template <typename E> struct Raw;
+template <> struct Raw<uint16_t> { u32x4 v; };
+template <> struct Raw<float> { f32x4 v[2]; };
+
 // Channels c0 .. c0 + 7 of a row of D, those from D on as zeros
 template <typename E>
-__device__ __forceinline__ void load_piece(const char *row, int c0, int D, float (&x)[kEach]) {
+__device__ __forceinline__ Raw<E> load_raw(const char *row, int c0, int D) {
+    Raw<E> x = {};
     if (c0 + kEach <= D) {
-        if constexpr (sizeof(E) == 2) {
-            u32x4 b;
-            __builtin_memcpy(&b, row + c0 * 2, 16);
+        __builtin_memcpy(&x, row + c0 * (int)sizeof(E), sizeof(x));
+    } else if (c0 < D) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                x[2 * j] = __builtin_bit_cast(float, b[j] << 16);
-                x[2 * j + 1] = __builtin_bit_cast(float, b[j] & 0xffff0000u);
+        for (int j = 0; j < kEach; ++j)
+            if (c0 + j < D) {
+                if constexpr (sizeof(E) == 2) x.v[j >> 1] |= (uint32_t)reinterpret_cast<const uint16_t *>(row)[c0 + j] << (16 * (j & 1));
+                else x.v[j >> 2][j & 3] = reinterpret_cast<const float *>(row)[c0 + j];
             }
-        } else {
-            f32x4 v[2];
-            __builtin_memcpy(v, row + c0 * 4, 32);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = v[j >> 2][j & 3];
-        }
-        return;
     }
+    return x;
+}
+template <typename E>
+__device__ __forceinline__ void to_floats(const Raw<E> &r, float (&x)[kEach]) {
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
-        x[j] = 0.f;
-        if (c0 + j < D) {
-            if constexpr (sizeof(E) == 2) x[j] = bf16_bits_to_float(reinterpret_cast<const uint16_t *>(row)[c0 + j]);
-            else x[j] = reinterpret_cast<const float *>(row)[c0 + j];
-        }
+        if constexpr (sizeof(E) == 2) x[j] = j & 1 ? __builtin_bit_cast(float, r.v[j >> 1] & 0xffff0000u) : __builtin_bit_cast(float, r.v[j >> 1] << 16);
+        else x[j] = r.v[j >> 2][j & 3];
     }
+}
+template <typename E>
+__device__ __forceinline__ void load_piece(const char *row, int c0, int D, float (&x)[kEach]) {
+    to_floats<E>(load_raw<E>(row, c0, D), x);
 }
 __device__ __forceinline__ void store_piece(char *row, int c0, int D, int dtype, const float (&x)[kEach]) {
     if (c0 + kEach <= D) {
@@ -71,7 +76,8 @@ __device__ __forceinline__ void store_piece(char *row, int c0, int D, int dtype,
         }
 }
 
-// Sum over the LANES lanes of a group, in every lane.  Groups wider than a wave are the whole work-group and go through LDS.
+// Sum over the LANES lanes of a group, in every lane.  Groups wider than a wave are the whole work-group and go through LDS: each of a row's
+// sums has its own place there, so that one barrier a sum does (a place is written again behind the barriers of the others).
 template <int LANES, int SUMS>
 __device__ __forceinline__ void group_sum(float (&v)[SUMS], float *lds) {
 #pragma unroll
@@ -91,7 +97,6 @@ __device__ __forceinline__ void group_sum(float (&v)[SUMS], float *lds) {
 #pragma unroll
             for (int i = 0; i < kWaves; ++i) v[s] += lds[s * kWaves + i];
         }
-        __syncthreads();
     }
 }
 
@@ -100,11 +105,14 @@ struct Walk {
     int h, slot;
     uint32_t first, step;
 };
+// All groups of a work-group walk rows of one head
+__host__ __device__ inline bool one_head(const NormParams &p) { return p.layout == GLA_LAYOUT_BHTD || p.H == 1; }
+__host__ __device__ inline int partial_rows(const NormParams &p, int groups) { return one_head(p) ? p.slots / groups : p.slots; }
 // Neighbouring groups take rows that are neighbours in memory: of one head where a head's rows lie together, of neighbouring heads where a
 // token's heads do
 __device__ __forceinline__ Walk walk_of(const NormParams &p, int groups, int gi) {
     Walk w;
-    if (p.layout == GLA_LAYOUT_BHTD || p.H == 1) {
+    if (one_head(p)) {
         const int per_head = p.slots / groups;                   // work-groups of a head
         w.h = blockIdx.x / per_head;
         w.slot = (blockIdx.x - w.h * per_head) * groups + gi;
@@ -128,10 +136,13 @@ struct Shape {
     static constexpr int kThreads = LANES > 256 ? LANES : 256, kGroups = kThreads / LANES;
 };
 
+// 1 / (1 + exp(-r)); the reciprocal is off by one unit in the last place
+__device__ __forceinline__ float sigmoid(float r) { return __builtin_amdgcn_rcpf(1.f + __expf(-r)); }
+
 template <typename E, int LANES, int NP, bool GATED, bool BACK>
 __global__ __launch_bounds__(Shape<LANES>::kThreads) void norm_kernel(const NormParams p) {
-    constexpr int kGroups = Shape<LANES>::kGroups;
-    __shared__ float lds[2 * (LANES > 64 ? LANES / 64 : 1)];
+    constexpr int kGroups = Shape<LANES>::kGroups, kWaves = LANES > 64 ? LANES / 64 : 1, kWidth = LANES * NP * kEach;
+    __shared__ float lds[BACK && kGroups > 1 ? kGroups * kWidth : 4 * kWaves];
     const int gi = threadIdx.x / LANES, lane = threadIdx.x % LANES;
     const Walk wk = walk_of(p, kGroups, gi);
     const uint32_t rows = (uint32_t)p.B * (uint32_t)p.T;         // < 2^31 (host check)
@@ -153,20 +164,29 @@ __global__ __launch_bounds__(Shape<LANES>::kThreads) void norm_kernel(const Norm
         if (mine && p.weight != nullptr) load_piece<float>(reinterpret_cast<const char *>(p.weight + (size_t)wk.h * D), c, D, w[i]);
         if (mine && p.bias != nullptr) load_piece<float>(reinterpret_cast<const char *>(p.bias + (size_t)wk.h * D), c, D, b[i]);
     }
+    Raw<E> nx[NP], nr[GATED ? NP : 1], no[BACK ? NP : 1];
+    auto ask = [&](uint32_t i0) __attribute__((always_inline)) {
+        const long long at = row_of(p, wk.h, i0) * D * (int)sizeof(E);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int c = (i * LANES + lane) * kEach;
+            nx[i] = load_raw<E>(static_cast<const char *>(p.x) + at, c, D);
+            if constexpr (GATED) nr[i] = load_raw<E>(static_cast<const char *>(p.r_pre) + at, c, D);
+            if constexpr (BACK) no[i] = load_raw<E>(static_cast<const char *>(p.d_out) + at, c, D);
+        }
+    };
+    if (mine && wk.first < rows) ask(wk.first);
     // (groups of one wave or less end on their own; the wider ones are the work-group)
     for (uint32_t i0 = wk.first; mine && i0 < rows; i0 += wk.step) {
         const long long row = row_of(p, wk.h, i0);
         float x[NP][kEach], r[GATED ? NP : 1][kEach], o[BACK ? NP : 1][kEach];
-        const char *px = static_cast<const char *>(p.x) + row * D * (int)sizeof(E);
-        const char *pr = static_cast<const char *>(p.r_pre) + row * D * (int)sizeof(E);
-        const char *po = static_cast<const char *>(p.d_out) + row * D * (int)sizeof(E);
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            const int c = (i * LANES + lane) * kEach;
-            load_piece<E>(px, c, D, x[i]);
-            if constexpr (GATED) load_piece<E>(pr, c, D, r[i]);
-            if constexpr (BACK) load_piece<E>(po, c, D, o[i]);
+            to_floats<E>(nx[i], x[i]);
+            if constexpr (GATED) to_floats<E>(nr[i], r[i]);
+            if constexpr (BACK) to_floats<E>(no[i], o[i]);
         }
+        if (i0 + wk.step < rows) ask(i0 + wk.step);
         float s[1] = {0.f};
 #pragma unroll
         for (int i = 0; i < NP; ++i)
@@ -182,19 +202,19 @@ __global__ __launch_bounds__(Shape<LANES>::kThreads) void norm_kernel(const Norm
                 x[i][j] = (i * LANES + lane) * kEach + j < D ? x[i][j] - mean : 0.f;
                 s[0] = fmaf(x[i][j], x[i][j], s[0]);
             }
-        group_sum<LANES, 1>(s, lds);
+        group_sum<LANES, 1>(s, lds + kWaves);
         const float rstd = 1.f / __builtin_sqrtf(fmaf(s[0], inv, p.eps));
         if constexpr (!BACK) {
-            char *po_ = static_cast<char *>(p.out) + row * D * out_size;
+            char *po = static_cast<char *>(p.out) + row * D * out_size;
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
                 float y[kEach];
 #pragma unroll
                 for (int j = 0; j < kEach; ++j) {
                     y[j] = fmaf(x[i][j] * rstd, w[i][j], b[i][j]);
-                    if constexpr (GATED) y[j] *= r[i][j] / (1.f + __expf(-r[i][j]));
+                    if constexpr (GATED) y[j] *= r[i][j] * sigmoid(r[i][j]);
                 }
-                store_piece(po_, (i * LANES + lane) * kEach, D, p.out_dtype, y);
+                store_piece(po, (i * LANES + lane) * kEach, D, p.out_dtype, y);
             }
         } else {
             char *pdx = static_cast<char *>(p.dx) + row * D * out_size;
@@ -208,7 +228,7 @@ __global__ __launch_bounds__(Shape<LANES>::kThreads) void norm_kernel(const Norm
                     const float n = x[i][j] * rstd;
                     float dy = o[i][j];
                     if constexpr (GATED) {
-                        const float sg = 1.f / (1.f + __expf(-r[i][j])), gate = r[i][j] * sg;
+                        const float sg = sigmoid(r[i][j]), gate = r[i][j] * sg;
                         dr[j] = o[i][j] * fmaf(n, w[i][j], b[i][j]) * fmaf(gate, 1.f - sg, sg);
                         dy *= gate;
                     }
@@ -222,7 +242,7 @@ __global__ __launch_bounds__(Shape<LANES>::kThreads) void norm_kernel(const Norm
                 }
                 if constexpr (GATED) store_piece(pdr, (i * LANES + lane) * kEach, D, p.out_dtype, dr);
             }
-            group_sum<LANES, 2>(m, lds);
+            group_sum<LANES, 2>(m, lds + 2 * kWaves);
             const float m0 = m[0] * inv, m1 = m[1] * inv;
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
@@ -234,49 +254,71 @@ __global__ __launch_bounds__(Shape<LANES>::kThreads) void norm_kernel(const Norm
         }
     }
     if constexpr (BACK) {
-        if (!mine) return;
-        float *part = p.part + ((size_t)wk.slot * p.H + wk.h) * D;
-        const size_t second = (size_t)p.slots * p.H * D;
+        const bool shared = kGroups > 1 && one_head(p);          // the work-group's slots become one
+        const size_t second = (size_t)partial_rows(p, kGroups) * p.H * D;
+        if (shared) {
+            float *part = p.part + ((size_t)(wk.slot / kGroups) * p.H + wk.h) * D;
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const int c = (i * LANES + lane) * kEach;
-            store_piece(reinterpret_cast<char *>(part), c, D, GLA_DT_F32, dw[i]);
-            store_piece(reinterpret_cast<char *>(part + second), c, D, GLA_DT_F32, db[i]);
+            for (int which = 0; which < 2; ++which) {
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < NP; ++i)
+#pragma unroll
+                    for (int j = 0; j < kEach; ++j) lds[gi * kWidth + (i * LANES + lane) * kEach + j] = which ? db[i][j] : dw[i][j];
+                __syncthreads();
+                for (int c = threadIdx.x; c < D; c += Shape<LANES>::kThreads) {
+                    float sum = 0.f;
+#pragma unroll
+                    for (int k = 0; k < kGroups; ++k) sum += lds[k * kWidth + c];
+                    part[which * second + c] = sum;
+                }
+            }
+        } else if (mine) {
+            float *part = p.part + ((size_t)wk.slot * p.H + wk.h) * D;
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const int c = (i * LANES + lane) * kEach;
+                store_piece(reinterpret_cast<char *>(part), c, D, GLA_DT_F32, dw[i]);
+                store_piece(reinterpret_cast<char *>(part + second), c, D, GLA_DT_F32, db[i]);
+            }
         }
     }
 }
 
-// Adds the slots: 16 columns and 16 rows of slots a work-group
-__global__ __launch_bounds__(256) void norm_sum_kernel(const float *part, float *dweight, float *dbias, int slots, int cols) {
-    __shared__ float s[16][17];
+// Adds the partial sums: 16 columns and 64 rows at a time a work-group
+__global__ __launch_bounds__(1024) void norm_sum_kernel(const float *part, float *dweight, float *dbias, int rows, int cols) {
+    __shared__ float s[64][17];
     const int c = threadIdx.x & 15, k = threadIdx.x >> 4;
     const int col = blockIdx.x * 16 + c;
-    const float *src = part + (blockIdx.y ? (size_t)slots * cols : 0);
+    const float *src = part + (blockIdx.y ? (size_t)rows * cols : 0);
     float x = 0.f;
-    if (col < cols)
-        for (int i = k; i < slots; i += 16) x += src[(size_t)i * cols + col];
+    if (col < cols) {
+#pragma unroll 8
+        for (int i = k; i < rows; i += 64) x += src[(size_t)i * cols + col];
+    }
     s[k][c] = x;
     __syncthreads();
-    if (k == 0 && col < cols) {
-#pragma unroll
-        for (int i = 1; i < 16; ++i) x += s[i][c];
-        (blockIdx.y ? dbias : dweight)[col] = x;
+    for (int d = 32; d > 0; d /= 2) {
+        if (k < d) s[k][c] += s[k + d][c];
+        __syncthreads();
     }
+    if (k == 0 && col < cols) (blockIdx.y ? dbias : dweight)[col] = s[0][c];
 }
 
 // lanes of a row's group
-int lanes_of(int D) { return D <= 128 ? 16 : D <= 1536 ? 64 : D <= 4096 ? 256 : 1024; }
+int lanes_of(int D) { return D <= 128 ? 16 : D <= 1536 ? 64 : D <= 2048 ? 256 : D <= 4096 ? 512 : 1024; }
+int groups_of(int D) { return lanes_of(D) >= 256 ? 1 : 256 / lanes_of(D); }
 
 // Rows are dealt to as many groups as fill the GPU a few times over, each with a few rows of its own; a multiple of the groups of a
 // work-group where a work-group stays with one head
 int slots_for(const NormParams &p, int rows_each, int work_groups) {
-    const int lanes = lanes_of(p.D), groups = lanes >= 256 ? 1 : 256 / lanes;
+    const int groups = groups_of(p.D);
     const long long rows = (long long)p.B * p.T;
     long long slots = (long long)work_groups * groups / p.H;
     const long long most = (rows + rows_each - 1) / rows_each;
     if (slots > most) slots = most;
     if (slots < 1) slots = 1;
-    if (p.layout == GLA_LAYOUT_BHTD || p.H == 1) slots = (slots + groups - 1) / groups * groups;
+    if (one_head(p)) slots = (slots + groups - 1) / groups * groups;
     return (int)slots;
 }
 
@@ -297,7 +339,7 @@ hipError_t norm_of_width(const NormParams &p, hipStream_t stream) {
     if (p.D <= 1024) return norm<E, 64, 2, BACK>(p, stream);
     if (p.D <= 1536) return norm<E, 64, 3, BACK>(p, stream);
     if (p.D <= 2048) return norm<E, 256, 1, BACK>(p, stream);
-    if (p.D <= 4096) return norm<E, 256, 2, BACK>(p, stream);
+    if (p.D <= 4096) return norm<E, 512, 1, BACK>(p, stream);
     return norm<E, 1024, 1, BACK>(p, stream);
 }
 
@@ -310,7 +352,7 @@ int norm_slots(int B, int H, int T, int D, int layout) {
     p.T = T;
     p.D = D;
     p.layout = layout;
-    return slots_for(p, 4, D > 4096 ? 512 : 1024);
+    return slots_for(p, 4, D > 2048 ? 512 : 1024);
 }
 
 hipError_t launch_norm_fwd(const NormParams &p0, int dtype, hipStream_t stream) {
@@ -324,7 +366,8 @@ hipError_t launch_norm_bwd(const NormParams &p0, int dtype, float *dweight, floa
     const hipError_t e = dtype == GLA_DT_BF16 ? norm_of_width<uint16_t, true>(p, stream) : norm_of_width<float, true>(p, stream);
     if (e != hipSuccess || dweight == nullptr) return e;
     const int cols = p.H * p.D;
-    hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)((cols + 15) / 16), 2), dim3(256), 0, stream, p.part, dweight, dbias, p.slots, cols);
+    hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)((cols + 15) / 16), 2), dim3(1024), 0, stream, p.part, dweight, dbias,
+                       partial_rows(p, groups_of(p.D)), cols);
     return hipGetLastError();
 }
 

@@ -16,15 +16,25 @@ bool bad_dtype(int d) { return d != GLA_DT_F32 && d != GLA_DT_BF16; }
 size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 
 // Spans a sequence is walked in.  One work-group walks one span, so that few sequences leave most of the GPU idle; spans read y and z once
-// more for their local states.
-int spans_of(int B, int H, int T) {
-    const long long bh = (long long)B * H;
-    const int blocks = decay_blocks(T);
-    long long n = bh >= 256 ? 1 : 512 / bh;
-    if (n > blocks) n = blocks;
-    if (n < 1) n = 1;
-    const int each = (int)((blocks + n - 1) / n);         // blocks a span
-    return (blocks + each - 1) / each;
+// more for their local states, and move their states.  Spans as short as 64 steps pay while there are up to 16 (16 sequences of 512 steps,
+// 128 x 128, forward and back: 90 us in spans of 64, 111 of 128, 133 of 256; of 2048 steps 157 in 32 spans, 141 in 16), beyond that only
+// such of 512 and more, and two chunks do not pay for the second pass (128 steps forward: 34 us in two spans, 20 in one).
+constexpr int kShortSpans = 16, kLongSpan = 512, kWhole = 128;
+// Up to so many spans the walks chain the local states themselves (padded prompts of 128 sequences in 4 spans: 95 us, 104 with the
+// kernel for it; at 8 spans it is even).
+constexpr int kChainSpans = 4;
+void plan_spans(DecayCall &c, long long groups) {
+    const long long bh = (long long)c.B * c.H;
+    const int units = (c.T + 63) / 64;
+    long long most = c.T / kLongSpan;
+    if (most < kShortSpans) most = kShortSpans;
+    if (most > units) most = units;
+    long long n = groups / bh;
+    if (n > most) n = most;
+    if (n < 1 || c.T <= kWhole) n = 1;
+    const int each = (int)((units + n - 1) / n);
+    c.span_len = each * 64;
+    c.nspans = (units + each - 1) / each;
 }
 
 // What a call keeps in the workspace, in floats from its start
@@ -60,6 +70,11 @@ struct BwdRoom {
     double *part;
     size_t bytes;
 };
+// the walk back has work-groups twice as large
+DecayCall back_call(DecayCall c) {
+    plan_spans(c, 256);
+    return c;
+}
 BwdRoom bwd_room(void *p, const DecayCall &c) {
     Room r(p);
     BwdRoom f = {};
@@ -67,8 +82,11 @@ BwdRoom bwd_room(void *p, const DecayCall &c) {
     if (c.nspans > 1) {
         f.local = r.take<float>(bh * c.nspans * cells);
         f.decay = r.take<float>(bh * c.nspans);
-        f.glocal = r.take<float>(bh * c.nspans * cells);
-        f.gdecay = r.take<float>(bh * c.nspans);
+    }
+    const int back = back_call(c).nspans;
+    if (back > 1) {
+        f.glocal = r.take<float>(bh * back * cells);
+        f.gdecay = r.take<float>(bh * back);
     }
     f.flow_q = r.take<float>(bh * c.T);
     f.flow_k = r.take<float>(bh * c.T);
@@ -108,9 +126,17 @@ int check_call(DecayCall &c, const float *log_decay, int kind, const int *seq_le
     const long long reach = (scan_dir >= GLA_SCAN_COL_FWD ? T : 64) * step;
     c.fast = dk % 4 == 0 && dv % 4 == 0 && least * (dtype == GLA_DT_BF16 ? 2 : 4) >= 16 && step < (1LL << 24) && T < (1 << 24) &&
              reach < (1LL << 31) - (1 << 16);
-    c.nspans = spans_of(B, H, T);
-    c.span_len = (decay_blocks(T) + c.nspans - 1) / c.nspans * kFlowBlock;
+    plan_spans(c, 512);                  // two work-groups a compute unit
     return GLA_OK;
+}
+
+// How the walks get at the states that enter their spans: up to kChainSpans they chain the local ones themselves, beyond that a kernel of its
+// own does so in place
+bool entries(DecayEntry &in, const DecayCall &c, float *local, const float *decay, bool reversed, hipStream_t stream) {
+    in.local = local;
+    in.decay = decay;
+    in.chained = c.nspans > kChainSpans;
+    return !in.chained || launch_decay_carry(c, in.first, local, decay, reversed, stream) == hipSuccess;
 }
 
 bool sized(DecayCall &c, int B, int H, int T, int dk, int dv, int dtype) {
@@ -152,15 +178,14 @@ int gla_decay_fwd(const void *q, const void *k, const void *v, const float *log_
     w.r.out = out;
     w.r.m = dk;
     w.r.n = dv;
-    w.state_in = initial_state;
+    w.in.first = initial_state;
     w.state_out = final_state;
     w.out_dtype = out_dtype;
     if (c.nspans > 1) {
         w.local = room.local;
         w.decay = room.decay;
         if (launch_decay_states(w, nullptr, qkv_dtype, stream) != hipSuccess) return GLA_ERR_HIP;
-        if (launch_decay_carry(c, initial_state, room.local, room.decay, false, stream) != hipSuccess) return GLA_ERR_HIP;
-        w.state_in = room.local;
+        if (!entries(w.in, c, room.local, room.decay, false, stream)) return GLA_ERR_HIP;
     }
     return launch_decay_walk(w, qkv_dtype, stream) == hipSuccess ? GLA_OK : GLA_ERR_HIP;
 }
@@ -191,30 +216,31 @@ int gla_decay_bwd(const void *q, const void *k, const void *v, const float *log_
     w.r.flow = room.flow_q;
     w.r.m = dv;
     w.r.n = dk;
-    w.state_in = initial_state;
+    w.in.first = initial_state;
     w.state_t = 1;
     w.anchors = gates ? room.anchors : nullptr;
     w.anchor_last = d_final_state != nullptr;
     w.out_dtype = grad_dtype;
     w.grad = 1;
     DecayBack b = {};
-    b.c = c;
+    b.c = back_call(c);
     b.q = q;
     b.k = k;
     b.v = v;
     b.d_out = d_out;
     b.dk_grad = dk_grad;
     b.dv_grad = dv_grad;
-    b.state_in = d_final_state;
+    b.in.first = d_final_state;
     b.d_initial = d_initial_state;
     b.anchors = w.anchors;
     b.anchor_last = w.anchor_last;
     b.meet = room.meet;
     b.flow_k = room.flow_k;
     b.grad_dtype = grad_dtype;
-    if (c.nspans > 1) {
+    if (c.nspans > 1) {                  // (then perhaps b.c.nspans too)
         DecayWalk s = {}, g = {};
-        s.c = g.c = c;
+        s.c = c;
+        g.c = b.c;
         s.r.y = k;
         s.r.z = v;
         g.r.y = q;
@@ -225,11 +251,9 @@ int gla_decay_bwd(const void *q, const void *k, const void *v, const float *log_
         s.decay = room.decay;
         g.local = room.glocal;
         g.decay = room.gdecay;
-        if (launch_decay_states(s, &g, qkv_dtype, stream) != hipSuccess) return GLA_ERR_HIP;
-        if (launch_decay_carry(c, initial_state, room.local, room.decay, false, stream) != hipSuccess) return GLA_ERR_HIP;
-        if (launch_decay_carry(c, d_final_state, room.glocal, room.gdecay, true, stream) != hipSuccess) return GLA_ERR_HIP;
-        w.state_in = room.local;
-        b.state_in = room.glocal;
+        if (launch_decay_states(s, b.c.nspans > 1 ? &g : nullptr, qkv_dtype, stream) != hipSuccess) return GLA_ERR_HIP;
+        if (!entries(w.in, c, room.local, room.decay, false, stream)) return GLA_ERR_HIP;
+        if (b.c.nspans > 1 && !entries(b.in, b.c, room.glocal, room.gdecay, true, stream)) return GLA_ERR_HIP;
     }
     if (launch_decay_walk(w, qkv_dtype, stream) != hipSuccess) return GLA_ERR_HIP;
     if (launch_decay_back(b, qkv_dtype, stream) != hipSuccess) return GLA_ERR_HIP;
@@ -251,7 +275,7 @@ int gla_decay_step(const void *q, const void *k, const void *v, const float *log
     if (B <= 0 || H <= 0 || dk <= 0 || dv <= 0 || bad_dtype(qkv_dtype) || bad_dtype(out_dtype) ||
         (decay_kind != GLA_DECAY_HEAD && decay_kind != GLA_DECAY_TOKEN))
         return GLA_ERR_SHAPE;
-    if (dk > kDecayMaxD || dv > kDecayMaxD || (long long)B * H >= (1LL << 23)) return GLA_ERR_UNSUPPORTED;
+    if (dk > kDecayMaxD || dv > kDecayMaxD || (long long)B * H >= (1LL << 22)) return GLA_ERR_UNSUPPORTED;
     // (rows of single tokens are often slices of something larger: any place does for them)
     if (any_misaligned((const void *)state, (const void *)state_out) || off_element(q, qkv_dtype) || off_element(k, qkv_dtype) ||
         off_element(v, qkv_dtype) || off_element(out, out_dtype) || off_element(log_decay, GLA_DT_F32))
@@ -288,7 +312,10 @@ int gla_rope(const void *q, const void *k, const int *positions, const int *sect
         if (w < 2 || w % 2 != 0 || w > d - first) return GLA_ERR_SHAPE;
         p.first[a] = first;
         p.half[a] = w / 2;
-        for (int i = 0; i < w / 2; ++i) p.turns[first / 2 + i] = pow((double)base, -2.0 * i / w) / (2.0 * M_PI);
+        // (one power a section: 64 of them took longer than the kernel of a few tokens; each product is off by 2^-53 more)
+        const double ratio = pow((double)base, -2.0 / w);
+        double turns = 1.0 / (2.0 * M_PI);
+        for (int i = 0; i < w / 2; ++i, turns *= ratio) p.turns[first / 2 + i] = turns;
         first += w;
         p.pairs_end[a] = first / 2;
     }
