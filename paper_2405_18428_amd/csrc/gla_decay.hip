@@ -191,25 +191,25 @@ hipError_t states(const StatePair &w, int directions, hipStream_t stream) {
     return hipGetLastError();
 }
 
-// One token.  A work-group takes kStepCols columns of one (batch, head)'s state, eight lanes of four columns by 32 rows, all of whose rows it
-// asks for before it uses the first: columns need nothing of each other, and so 16 heads of one sequence are 64 work-groups.  Bound by the
-// states' way in and out (192 sequences of 16 heads 128 x 128: 77 us, 5.2 TB/s, what a copy reaches), for few sequences by the launch.
-constexpr int kStepCols = 32, kStepRows = kThreads / (kStepCols / 4);
+// One token.  A work-group takes COLS columns of one (batch, head)'s state, a lane four of them, and asks for all of its rows before it uses
+// the first.  Columns need nothing of each other, so that few states are dealt to four times as many work-groups, 32 columns each
+// (16 states 128 x 128: 3.8 us, 5.0 with whole rows); many are read in whole rows (3072: 77 us, 5.2 TB/s, what a copy reaches; 81 in
+// columns).  Bound by the states' way in and out, for few by the launch.
 template <typename E>
 __device__ inline float element(const void *p, size_t i) {
     if constexpr (sizeof(E) == 2) return bf16_bits_to_float(static_cast<const uint16_t *>(p)[i]);
     else return static_cast<const float *>(p)[i];
 }
 
-template <typename E>
+template <typename E, int COLS>
 __global__ __launch_bounds__(kThreads) void decay_step_kernel(const void *q, const void *k, const void *v, const float *log_decay, int kind,
                                                               int H, int dk, int dv, int out_dtype, const float *state, float *state_out,
                                                               void *out) {
-    constexpr int kTimes = kDecayMaxD / kStepRows;
-    __shared__ float s_o[kThreads / 64][kStepCols];
-    const int tid = threadIdx.x, parts = (dv + kStepCols - 1) / kStepCols;
-    const int bh = blockIdx.x / parts, h = bh % H, c0 = (blockIdx.x - bh * parts) * kStepCols;
-    const int col = c0 + (tid & 7) * 4, row0 = tid >> 3;
+    constexpr int kLanes = COLS / 4, kStepRows = kThreads / kLanes, kTimes = kDecayMaxD / kStepRows;
+    __shared__ float s_o[kThreads / 64][COLS];
+    const int tid = threadIdx.x, parts = (dv + COLS - 1) / COLS;
+    const int bh = blockIdx.x / parts, h = bh % H, c0 = (blockIdx.x - bh * parts) * COLS;
+    const int col = c0 + tid % kLanes * 4, row0 = tid / kLanes;
     const size_t cells = (size_t)dk * dv;
     const float *s = state + bh * cells;
     float *t = state_out + bh * cells;
@@ -254,11 +254,11 @@ __global__ __launch_bounds__(kThreads) void decay_step_kernel(const void *q, con
     for (int j = 0; j < 4; ++j) {
         float y = o[j];
 #pragma unroll
-        for (int d = 8; d < 64; d *= 2) y += __shfl_xor(y, d);
-        if ((tid & 56) == 0) s_o[tid >> 6][(tid & 7) * 4 + j] = y;
+        for (int d = kLanes; d < 64; d *= 2) y += __shfl_xor(y, d);
+        if ((tid & 63) < kLanes) s_o[tid >> 6][(tid & 63) * 4 + j] = y;
     }
     __syncthreads();
-    if (tid < kStepCols && c0 + tid < dv) {
+    if (tid < COLS && c0 + tid < dv) {
         const float y = (s_o[0][tid] + s_o[1][tid]) + (s_o[2][tid] + s_o[3][tid]);
         const size_t at = (size_t)bh * dv + c0 + tid;
         if (out_dtype == GLA_DT_BF16) static_cast<uint16_t *>(out)[at] = float_to_bf16_bits(y);
@@ -301,13 +301,13 @@ hipError_t launch_decay_carry(const DecayCall &c, const float *first, float *loc
 
 hipError_t launch_decay_step(const void *q, const void *k, const void *v, const float *log_decay, int kind, int B, int H, int dk, int dv,
                              int dtype, int out_dtype, const float *state, float *state_out, void *out, hipStream_t stream) {
-    const dim3 grid((unsigned)(B * H * ((dv + kStepCols - 1) / kStepCols)));
-    if (dtype == GLA_DT_BF16)
-        hipLaunchKernelGGL(decay_step_kernel<uint16_t>, grid, dim3(kThreads), 0, stream, q, k, v, log_decay, kind, H, dk, dv, out_dtype, state,
-                           state_out, out);
-    else
-        hipLaunchKernelGGL(decay_step_kernel<float>, grid, dim3(kThreads), 0, stream, q, k, v, log_decay, kind, H, dk, dv, out_dtype, state,
-                           state_out, out);
+    const int cols = (long long)B * H < 512 ? 32 : 64, parts = (dv + cols - 1) / cols;
+    auto run = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(B * H * parts)), dim3(kThreads), 0, stream, q, k, v, log_decay, kind, H, dk, dv, out_dtype,
+                           state, state_out, out);
+    };
+    if (cols == 32) run(dtype == GLA_DT_BF16 ? decay_step_kernel<uint16_t, 32> : decay_step_kernel<float, 32>);
+    else run(dtype == GLA_DT_BF16 ? decay_step_kernel<uint16_t, 64> : decay_step_kernel<float, 64>);
     return hipGetLastError();
 }
 

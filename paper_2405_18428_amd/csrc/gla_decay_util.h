@@ -18,16 +18,20 @@
 namespace gla {
 namespace {
 
+#ifndef PARTS_OUT
+#define PARTS_OUT 2
+#define PARTS_STATE 2
+#endif
 template <typename E> struct Elem;
 template <> struct Elem<uint16_t> {
     static constexpr int kChunk = 64;            // steps
     static constexpr int kDeep = 32;             // contracted values of an operand over the wave
-    static constexpr int kParts = 2;             // head and remainder
+    static constexpr int kParts = PARTS_OUT, kStateParts = PARTS_STATE;
 };
 template <> struct Elem<float> {
     static constexpr int kChunk = 32;
     static constexpr int kDeep = 16;
-    static constexpr int kParts = 1;
+    static constexpr int kParts = 1, kStateParts = 1;
 };
 
 // 16 bytes of an operand; products of operands
@@ -63,17 +67,22 @@ enum Reads { kAlong, kAcross, kBoth };
 template <typename E, int W, Reads R>
 struct Tile {
     static constexpr int C = Elem<E>::kChunk;
-    static constexpr int kRow = W * (int)sizeof(E) + (sizeof(E) == 2 && R != kAlong ? 32 : 16);      // bytes
-    static constexpr int kBytes = C * kRow;
+    // bf16 tiles read along their rows: four planes, one of each lane group's pieces
+    static constexpr bool kPlanes = R == kAlong && sizeof(E) == 2;
+    static constexpr int kRow = (kPlanes ? W / 2 : W * (int)sizeof(E)) + (sizeof(E) == 2 && R != kAlong ? 32 : 16);      // bytes
+    static constexpr int kPlane = C * kRow;
+    static constexpr int kBytes = (kPlanes ? 4 : 1) * C * kRow;
     static constexpr bool kMoved = R == kBoth && sizeof(E) == 2;
     char *p;
     // 16 bytes of row 16 tile + lm: the operand of contraction step ks whose other index is the row
     __device__ __forceinline__ u32x4 along(int tile, int lm, int ks, int g) const {
         const char *a = p + tile * 16 * kRow + lm * kRow;
         if constexpr (kMoved) {
-            const u32x2 lo = *reinterpret_cast<const u32x2 *>(a + g * 8 + ks * 64);
-            const u32x2 hi = *reinterpret_cast<const u32x2 *>(a + g * 8 + ks * 64 + 32);
+            const u32x2 lo = *reinterpret_cast<const u32x2 *>(a + (g ^ (lm >> 2)) * 8 + ks * 64);
+            const u32x2 hi = *reinterpret_cast<const u32x2 *>(a + (g ^ (lm >> 2)) * 8 + ks * 64 + 32);
             return u32x4{lo[0], lo[1], hi[0], hi[1]};
+        } else if constexpr (kPlanes) {
+            return *reinterpret_cast<const u32x4 *>(a + g * kPlane + ks * 16);
         } else {
             return *reinterpret_cast<const u32x4 *>(a + g * 16 + ks * 64);
         }
@@ -82,7 +91,7 @@ struct Tile {
     // in which they lie)
     __device__ __forceinline__ u32x4 across(int jk, int t, int lm, int g) const {
         if constexpr (sizeof(E) == 2) {
-            const char *a = p + (g * 4 + (lm >> 2)) * kRow + (lm & 3) * 8 + jk * 32 * kRow + t * 32;
+            const char *a = p + (g * 4 + (lm >> 2)) * kRow + ((lm & 3) ^ (kMoved ? g : 0)) * 8 + jk * 32 * kRow + t * 32;
             const u32x2 lo = lds_read_tr(reinterpret_cast<const uint16_t *>(a));
             const u32x2 hi = lds_read_tr(reinterpret_cast<const uint16_t *>(a + 16 * kRow));
             return u32x4{lo[0], lo[1], hi[0], hi[1]};
@@ -98,9 +107,11 @@ struct Tile {
     __device__ __forceinline__ void put_piece(int row, int piece, u32x4 x) const {
         char *a = p + row * kRow;
         if constexpr (kMoved) {
-            a += (piece >> 2) * 64 + (piece & 3) * 8;
+            a += (piece >> 2) * 64 + ((piece & 3) ^ (row >> 2 & 3)) * 8;
             *reinterpret_cast<u32x2 *>(a) = u32x2{x[0], x[1]};
             *reinterpret_cast<u32x2 *>(a + 32) = u32x2{x[2], x[3]};
+        } else if constexpr (kPlanes) {
+            *reinterpret_cast<u32x4 *>(a + (piece & 3) * kPlane + (piece >> 2) * 16) = x;
         } else {
             *reinterpret_cast<u32x4 *>(a + piece * 16) = x;
         }
@@ -108,7 +119,8 @@ struct Tile {
     // neighbouring elements of a row from column `col` on (of a tile in the order of memory)
     __device__ __forceinline__ const char *at(int row, int col) const {
         static_assert(!kMoved, "columns as they come");
-        return p + row * kRow + col * (int)sizeof(E);
+        if constexpr (kPlanes) return p + (col >> 3 & 3) * kPlane + row * kRow + (col >> 5) * 16 + (col & 7) * 2;
+        else return p + row * kRow + col * (int)sizeof(E);
     }
 };
 
@@ -124,12 +136,17 @@ struct Heads {
         first = __builtin_bit_cast(bf16x2, a);
         second = __builtin_bit_cast(bf16x2, b);
     }
-    __device__ __forceinline__ HiLo split(float x0, float x1) const {
-        HiLo r;
-        r.hi = pack_bf16(x0, x1);
-        const bf16x2 h = __builtin_bit_cast(bf16x2, r.hi);
-        r.lo = pack_bf16(__builtin_amdgcn_fdot2_f32_bf16(h, first, x0, false), __builtin_amdgcn_fdot2_f32_bf16(h, second, x1, false));
-        return r;
+    // PARTS packed pairs that add up to x0, x1
+    template <int PARTS>
+    __device__ __forceinline__ void split(float x0, float x1, uint32_t (&to)[PARTS]) const {
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) {
+            to[q] = pack_bf16(x0, x1);
+            if (q + 1 == PARTS) break;
+            const bf16x2 h = __builtin_bit_cast(bf16x2, to[q]);
+            x0 = __builtin_amdgcn_fdot2_f32_bf16(h, first, x0, false);
+            x1 = __builtin_amdgcn_fdot2_f32_bf16(h, second, x1, false);
+        }
     }
 };
 
@@ -341,7 +358,8 @@ struct Pairs {
 template <typename E, int M, int N, bool FAST, bool ZA>
 struct Walker {
     static constexpr int C = Elem<E>::kChunk, kDeep = Elem<E>::kDeep, kI = C / 16, kJ = C / kDeep;
-    static constexpr int kRows = M / 16, kCols = N / 64, kSteps = M / kDeep, kParts = Elem<E>::kParts;
+    static constexpr int kRows = M / 16, kCols = N / 64, kSteps = M / kDeep, kParts = Elem<E>::kParts,
+                         kStateParts = Elem<E>::kStateParts;
     f32x4 S[kRows][kCols];
     f32x4 O[kCols][kI];
     int lane, lm, g, w;
@@ -501,14 +519,14 @@ struct Walker {
                 p = acc * (*reinterpret_cast<const f32x4 *>(&gt.tile[j0]) * e);
             }
             if constexpr (sizeof(E) == 2) {
-                const HiLo s0 = heads.split(p[0], p[1]), s1 = heads.split(p[2], p[3]);
-                const u32x2 hi = {s0.hi, s1.hi}, lo = {s0.lo, s1.lo};
-                *reinterpret_cast<u32x2 *>(P.at(it, jt >> 1, 0, lane) + 8 * (jt & 1)) = hi;
-                *reinterpret_cast<u32x2 *>(P.at(it, jt >> 1, 1, lane) + 8 * (jt & 1)) = lo;
-                // the upper half of a diagonal operand
-                if (jt == it && (jt & 1) == 0) {
-                    *reinterpret_cast<u32x2 *>(P.at(it, jt >> 1, 0, lane) + 8) = u32x2{0u, 0u};
-                    *reinterpret_cast<u32x2 *>(P.at(it, jt >> 1, 1, lane) + 8) = u32x2{0u, 0u};
+                uint32_t s0[kParts], s1[kParts];
+                heads.split(p[0], p[1], s0);
+                heads.split(p[2], p[3], s1);
+#pragma unroll
+                for (int q = 0; q < kParts; ++q) {
+                    *reinterpret_cast<u32x2 *>(P.at(it, jt >> 1, q, lane) + 8 * (jt & 1)) = u32x2{s0[q], s1[q]};
+                    // the upper half of a diagonal operand
+                    if (jt == it && (jt & 1) == 0) *reinterpret_cast<u32x2 *>(P.at(it, jt >> 1, q, lane) + 8) = u32x2{0u, 0u};
                 }
             } else {
                 *reinterpret_cast<f32x4 *>(P.at(it, jt, 0, lane)) = p;
@@ -532,9 +550,10 @@ struct Walker {
 #pragma unroll
                         for (int r = 0; r < 2; ++r)
                         {
-                            const HiLo s = heads.split(S[2 * t + h][c][2 * r], S[2 * t + h][c][2 * r + 1]);
-                            a[c][0][2 * h + r] = s.hi;
-                            a[c][1][2 * h + r] = s.lo;
+                            uint32_t s[kParts];
+                            heads.split(S[2 * t + h][c][2 * r], S[2 * t + h][c][2 * r + 1], s);
+#pragma unroll
+                            for (int q = 0; q < kParts; ++q) a[c][q][2 * h + r] = s[q];
                         }
                 } else {
                     a[c][0] = __builtin_bit_cast(u32x4, S[t][c]);
@@ -563,7 +582,7 @@ struct Walker {
     __device__ __forceinline__ void advance(const Tile<E, M, kBoth> &y, const Tile<E, N, ZA ? kBoth : kAcross> &z, const Pairs<E> &P, const Gates<C> &gt) {
         const float last = gt.last;
         const Heads heads;
-        u32x4 zd[kJ][kCols][kParts];
+        u32x4 zd[kJ][kCols][kStateParts];
 #pragma unroll
         for (int jk = 0; jk < kJ; ++jk) {
             u32x4 zf[kCols];
@@ -588,9 +607,10 @@ struct Walker {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const f32x4 &d = r < 2 ? d0 : d1;
-                        const HiLo s = heads.split(bf16_lo_as_float(zf[c][r]) * d[2 * (r & 1)], bf16_hi_as_float(zf[c][r]) * d[2 * (r & 1) + 1]);
-                        zd[jk][c][0][r] = s.hi;
-                        zd[jk][c][1][r] = s.lo;
+                        uint32_t s[kStateParts];
+                        heads.split(bf16_lo_as_float(zf[c][r]) * d[2 * (r & 1)], bf16_hi_as_float(zf[c][r]) * d[2 * (r & 1) + 1], s);
+#pragma unroll
+                        for (int q = 0; q < kStateParts; ++q) zd[jk][c][q][r] = s[q];
                     }
             } else {
                 const f32x4 d = *reinterpret_cast<const f32x4 *>(&gt.out[jk * 16 + g * 4]);
@@ -617,7 +637,7 @@ struct Walker {
 #pragma unroll
             for (int jk = 0; jk < kJ; ++jk)
 #pragma unroll
-                for (int q = 0; q < kParts; ++q)
+                for (int q = 0; q < kStateParts; ++q)
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
