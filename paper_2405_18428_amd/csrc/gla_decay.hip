@@ -11,7 +11,7 @@ template <typename E, int M, int N>
 struct WalkLds {
     static constexpr int kRowsM = Tile<E, M, kBoth>::kBytes, kRowsN = Tile<E, N, kAcross>::kBytes, kX = 0, kY = Tile<E, M, kAlong>::kBytes, kZ = kY + kRowsM,
                          kP = kZ + kRowsN, kG = kP + Pairs<E>::kBytes, kFlow = kG + 2 * (int)sizeof(Gates<Elem<E>::kChunk>),
-                         kBytes = kFlow + 4 * Elem<E>::kChunk * 4;
+                         kBytes = kFlow + 2 * 4 * Elem<E>::kChunk * 4;
 };
 
 // GRAD: the walk for dq, with the dot products and the states that the gates' gradient takes
@@ -52,35 +52,46 @@ __global__ __launch_bounds__(kThreads, 2) void decay_walk_kernel(const DecayWalk
     };
     if (s0 < end) issue(s0);
     wk.enter(p.in, bh, sp, p.c.nspans, false, m, n, p.state_t);
-    if (wk.w == 3 && s0 < end) form_gates(gates[0], gate, lane);
-    int turn = 0;
-    for (int s = s0; s < end; s += C, turn ^= 1) {
-        const int count = min(C, end - s);
-        const Gates<C> &gt = gates[turn];
+    auto bring = [&](int turn) __attribute__((always_inline)) {
         px.commit(rx, tid, tx);
         py.commit(ry, tid, ty);
         pz.commit(rz, tid, tz);
+        if (wk.w == 3) form_gates(gates[turn], gate, lane);
+    };
+    const bool dots = GRAD && p.r.dot != nullptr;
+    // the dot products of a chunk are added over the waves once the barrier behind it is passed
+    auto put_flow = [&](int s, int count, int turn) __attribute__((always_inline)) {
+        const float *f = flow_part + 4 * C * turn;
+        if (tid < count) p.r.flow[(size_t)bh * p.c.T + s + tid] = (f[tid] + f[C + tid]) + (f[2 * C + tid] + f[3 * C + tid]);
+    };
+    if (s0 < end) bring(0);
+    int turn = 0;
+    for (int s = s0; s < end; s += C, turn ^= 1) {
+        const int count = min(C, end - s), e = s + count;
+        const Gates<C> &gt = gates[turn];
+        u32x4 zf[C / Elem<E>::kDeep][N / 64];
+        typename Walker<E, M, N, FAST, false>::Dots d;
         __syncthreads();
-        if (s + C < end) issue(s + C);
+        if (dots) wk.fetch_dots(d, rows_of<E>(p.c, p.r.dot, bh, n), ord.steps(s, count, false));
+        if (e < end) issue(e);
+        if (dots && s > s0) put_flow(s - C, C, turn ^ 1);
         __builtin_amdgcn_s_setprio(1);                   // before the other work-group's loads and stores (3 % less time)
         wk.begin(tx, ty, P, gt);
+        wk.update(ty, tz, gt, zf);
         __builtin_amdgcn_s_setprio(0);
         __syncthreads();
-        if (wk.w == 3 && s + C < end) form_gates(gates[turn ^ 1], gate, lane);
-        wk.template advance<true>(ty, tz, P, gt);
+        wk.finish(P, zf);
         const Steps st = ord.steps(s, count, false);
         wk.store_rows(ro, p.out_dtype, st);
-        if (GRAD && p.r.dot != nullptr) {
-            const Rows rd = rows_of<E>(p.c, p.r.dot, bh, n);
-            wk.template dot_rows<false>(rd, Tile<E, N, kAlong>{nullptr}, flow_part, st);
-        }
-        const int e = s + count;
+        if (dots) wk.dot_rows(d, flow_part + 4 * C * turn);
+        if (e < end) bring(turn ^ 1);
         if (GRAD && p.anchors != nullptr && (e < len ? e % kFlowBlock == 0 : p.anchor_last != 0))
             wk.store_state(p.anchors + ((size_t)bh * decay_blocks(p.c.T) + (e - 1) / kFlowBlock) * cells, m, n, p.state_t);
+    }
+    if (dots && s0 < end) {
         __syncthreads();
-        if (GRAD && p.r.dot != nullptr && tid < count)
-            p.r.flow[(size_t)bh * p.c.T + s + tid] =
-                flow_part[tid] + flow_part[C + tid] + flow_part[2 * C + tid] + flow_part[3 * C + tid];
+        const int s = s0 + (end - s0 - 1) / C * C;
+        put_flow(s, end - s, turn ^ 1);
     }
     if (p.state_out != nullptr && sp == p.c.nspans - 1) wk.store_state(p.state_out + (size_t)bh * cells, m, n, p.state_t);
     if (GRAD) clear_behind<kThreads>(ro, p.out_dtype == GLA_DT_BF16 ? 2 : 4, len, s0, s1, tid);
@@ -99,7 +110,6 @@ __global__ __launch_bounds__(kThreads, 2) void decay_state_kernel(const StatePai
     const Tile<E, M, kBoth> ty{lds};
     const Tile<E, N, kAcross> tz{lds + L::kRowsM};
     Gates<C> *gates = reinterpret_cast<Gates<C> *>(lds + L::kRowsM + L::kRowsN);
-    const Pairs<E> none{nullptr};
 
     const bool back = blockIdx.y != 0;
     const DecayWalk &p = both.w[blockIdx.y];
@@ -138,7 +148,8 @@ __global__ __launch_bounds__(kThreads, 2) void decay_state_kernel(const StatePai
         __syncthreads();
         if (i + 1 < chunks) issue(i + 1);
         sum += gt.sum;
-        wk.template advance<false>(ty, tz, none, gt);
+        u32x4 zf[C / Elem<E>::kDeep][N / 64];
+        wk.update(ty, tz, gt, zf);
         if (wk.w == 3 && i + 1 < chunks) form_gates(gates[(i + 1) & 1], gate, lane);
         __syncthreads();
     }

@@ -14,7 +14,7 @@ template <typename E, int K, int V>
 struct BackLds {
     static constexpr int kRowsV = Tile<E, V, kBoth>::kBytes, kQ = 0, kK = Tile<E, K, kBoth>::kBytes, kV = kK + Tile<E, K, kAlong>::kBytes,
                          kD = kV + Tile<E, V, kAlong>::kBytes, kPa = kD + kRowsV, kPb = kPa + Pairs<E>::kBytes, kG = kPb + Pairs<E>::kBytes,
-                         kFlow = kG + 2 * (int)sizeof(Gates<Elem<E>::kChunk>), kMeet = kFlow + 4 * Elem<E>::kChunk * 4, kBytes = kMeet + 16;
+                         kFlow = kG + 2 * (int)sizeof(Gates<Elem<E>::kChunk>), kMeet = kFlow + 2 * 4 * Elem<E>::kChunk * 4, kBytes = kMeet + 16;
 };
 
 // ROLE 0: dv, ROLE 1: dk
@@ -56,49 +56,58 @@ __device__ __forceinline__ void walk_back(const DecayBack &p, char *lds) {
         pd.issue(rd, tid, st);
     };
     const int chunks = s0 < end ? (end - s0 + C - 1) / C : 0;
-    if (chunks > 0) {
-        issue(s0 + (chunks - 1) * C, end);
-        if (ROLE == 0 && wk.w == 3) form_gates(gates[(chunks - 1) & 1], gate, wk.lane);
-    }
-    wk.enter(p.in, bh, sp, p.c.nspans, true, m, n, ROLE == 1);
-    for (int ci = chunks - 1; ci >= 0; --ci) {
-        const int s = s0 + ci * C, e = min(s + C, end), count = e - s;
-        const Gates<C> &gt = gates[ci & 1];
-        // the state there met by its adjoint
-        const size_t block = (size_t)bh * decay_blocks(p.c.T) + (e - 1) / kFlowBlock;
-        const bool meets = ROLE == 1 && p.anchors != nullptr && (e < len ? e % kFlowBlock == 0 : p.anchor_last != 0);
-        if (meets) {
-            float sum = wk.meet_state(p.anchors + block * cells, m, n, true);
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-            if (wk.lane == 0) meet_part[wk.w] = sum;
-        }
+    auto bring = [&](int turn) __attribute__((always_inline)) {
         pq.commit(rq, tid, tq);
         pk.commit(rk, tid, tk);
         pv.commit(rv, tid, tv);
         pd.commit(rd, tid, td);
+        if (ROLE == 0 && wk.w == 3) form_gates(gates[turn], gate, wk.lane);
+    };
+    const bool flows = ROLE == 1 && p.anchors != nullptr;
+    // the dot products of a chunk are added over the waves once the barrier behind it is passed
+    auto put_flow = [&](int s, int e, int turn) __attribute__((always_inline)) {
+        const int i = tid - 256;
+        const float *f = flow_part + 4 * C * turn;
+        if (i < e - s) p.flow_k[(size_t)bh * p.c.T + e - 1 - i] = (f[i] + f[C + i]) + (f[2 * C + i] + f[3 * C + i]);
+    };
+    if (chunks > 0) issue(s0 + (chunks - 1) * C, end);
+    wk.enter(p.in, bh, sp, p.c.nspans, true, m, n, ROLE == 1);
+    if (chunks > 0) bring((chunks - 1) & 1);
+    for (int ci = chunks - 1; ci >= 0; --ci) {
+        const int s = s0 + ci * C, e = min(s + C, end), count = e - s;
+        const Gates<C> &gt = gates[ci & 1];
+        u32x4 zf[C / Elem<E>::kDeep][N / 64];
+        typename Walker<E, M, N, FAST, true>::Dots d;
         __syncthreads();
         if (ci > 0) issue(s - C, s);
-        if (meets && tid == 256) p.meet[block] = (meet_part[0] + meet_part[1]) + (meet_part[2] + meet_part[3]);
+        if (flows && ci < chunks - 1) put_flow(s + C, min(s + 2 * C, end), ci + 1 & 1);
+        // the state at the end of a block, met by its adjoint
+        const size_t block = (size_t)bh * decay_blocks(p.c.T) + (e - 1) / kFlowBlock;
+        const bool meets = flows && (e < len ? e % kFlowBlock == 0 : p.anchor_last != 0);
+        if (meets) {
+            float sum = wk.meet_state(p.anchors + block * cells, m, n, true);
+#pragma unroll
+            for (int k = 1; k < 64; k *= 2) sum += __shfl_xor(sum, k);
+            if (wk.lane == 0) meet_part[wk.w] = sum;
+        }
         if constexpr (ROLE == 0) {
             wk.begin(tk, tq, P, gt);
+            wk.update(tq, td, gt, zf);
         } else {
             wk.begin(tv, td, P, gt);
+            wk.update(td, tq, gt, zf);
+            if (flows) wk.fetch_dots(d, tk);
         }
         __syncthreads();
-        if (ROLE == 0 && wk.w == 3 && ci > 0) form_gates(gates[(ci - 1) & 1], gate, wk.lane);
-        if constexpr (ROLE == 0) wk.template advance<true>(tq, td, P, gt);
-        else wk.template advance<true>(td, tq, P, gt);
-        const Steps st = ord.steps(s, count, true);
-        wk.store_rows(ro, p.grad_dtype, st);
-        if constexpr (ROLE == 1) {
-            if (p.anchors != nullptr) wk.template dot_rows<true>(rk, tk, flow_part, st);
-        }
+        if (meets && tid == 256) p.meet[block] = (meet_part[0] + meet_part[1]) + (meet_part[2] + meet_part[3]);
+        wk.finish(P, zf);
+        wk.store_rows(ro, p.grad_dtype, ord.steps(s, count, true));
+        if (flows) wk.dot_rows(d, flow_part + 4 * C * (ci & 1));
+        if (ci > 0) bring((ci - 1) & 1);
+    }
+    if (chunks > 0) {
         __syncthreads();
-        if (ROLE == 1 && p.anchors != nullptr && tid - 256 < count) {
-            const int i = tid - 256;
-            p.flow_k[(size_t)bh * p.c.T + e - 1 - i] = flow_part[i] + flow_part[C + i] + flow_part[2 * C + i] + flow_part[3 * C + i];
-        }
+        if (flows) put_flow(s0, min(s0 + C, end), 0);
     }
     if (ROLE == 0 && p.d_initial != nullptr && sp == 0)
         wk.store_state(p.d_initial + (size_t)bh * cells, m, n, false,
@@ -109,7 +118,7 @@ __device__ __forceinline__ void walk_back(const DecayBack &p, char *lds) {
 template <typename E, int K, int V, bool FAST>
 __global__ __launch_bounds__(kThreads, 2) void decay_back_kernel(const DecayBack p) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    // both branches meet at the same barriers: the same chunks, three each
+    // both branches meet at the same barriers: the same chunks, two each, and one behind them
     if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 8) == 0) walk_back<E, K, V, FAST, 0>(p, lds);
     else walk_back<E, K, V, FAST, 1>(p, lds);
 }

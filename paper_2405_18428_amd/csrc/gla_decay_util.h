@@ -3,8 +3,9 @@
 //
 // Four waves walk one state [m, n] (padded to M, N): wave w holds all rows of columns w * N/4 .. + N/4 - 1 in registers, as
 // accumulators of 16 x 16 products with lane = column, and works on these columns of the outputs.  A chunk is
-//   (1) P^T = y x^T of the lower triangle, 16 columns a wave, times exp(b_i - b_j), to LDS; and out^T = S^T x^T, all in-wave
-//   (2) out^T = exp(b_i) out^T + z^T P^T, and S = exp(b_last) S + y^T (exp(b_last - b_j) z).
+//   (1) P^T = y x^T of the lower triangle times exp(b_i - b_j), its tiles dealt to the waves, to LDS; out^T = exp(b_i) S^T x^T and then
+//       S = exp(b_last) S + y^T (exp(b_last - b_j) z), all in-wave; a barrier, behind which the rows are not read any more
+//   (2) out^T += z^T P^T with z's operands from registers, out to memory, the next chunk's rows into LDS; a barrier.
 // Everything is formed transposed, so that the accumulators of one product are an operand of the next as they stand: an operand
 // is eight (bf16) or four (fp32) values of the contracted index in a lane, and which index stands where does not matter as long as
 // both operands agree.  The state's rows are ordered (state_row) so that x's operands are 16 contiguous bytes of a row.
@@ -67,11 +68,8 @@ enum Reads { kAlong, kAcross, kBoth };
 template <typename E, int W, Reads R>
 struct Tile {
     static constexpr int C = Elem<E>::kChunk;
-    // bf16 tiles read along their rows: four planes, one of each lane group's pieces
-    static constexpr bool kPlanes = R == kAlong && sizeof(E) == 2;
-    static constexpr int kRow = (kPlanes ? W / 2 : W * (int)sizeof(E)) + (sizeof(E) == 2 && R != kAlong ? 32 : 16);      // bytes
-    static constexpr int kPlane = C * kRow;
-    static constexpr int kBytes = (kPlanes ? 4 : 1) * C * kRow;
+    static constexpr int kRow = W * (int)sizeof(E) + (sizeof(E) == 2 && R != kAlong ? 32 : 16);      // bytes
+    static constexpr int kBytes = C * kRow;
     static constexpr bool kMoved = R == kBoth && sizeof(E) == 2;
     char *p;
     // 16 bytes of row 16 tile + lm: the operand of contraction step ks whose other index is the row
@@ -81,8 +79,6 @@ struct Tile {
             const u32x2 lo = *reinterpret_cast<const u32x2 *>(a + (g ^ (lm >> 2)) * 8 + ks * 64);
             const u32x2 hi = *reinterpret_cast<const u32x2 *>(a + (g ^ (lm >> 2)) * 8 + ks * 64 + 32);
             return u32x4{lo[0], lo[1], hi[0], hi[1]};
-        } else if constexpr (kPlanes) {
-            return *reinterpret_cast<const u32x4 *>(a + g * kPlane + ks * 16);
         } else {
             return *reinterpret_cast<const u32x4 *>(a + g * 16 + ks * 64);
         }
@@ -110,8 +106,6 @@ struct Tile {
             a += (piece >> 2) * 64 + ((piece & 3) ^ (row >> 2 & 3)) * 8;
             *reinterpret_cast<u32x2 *>(a) = u32x2{x[0], x[1]};
             *reinterpret_cast<u32x2 *>(a + 32) = u32x2{x[2], x[3]};
-        } else if constexpr (kPlanes) {
-            *reinterpret_cast<u32x4 *>(a + (piece & 3) * kPlane + (piece >> 2) * 16) = x;
         } else {
             *reinterpret_cast<u32x4 *>(a + piece * 16) = x;
         }
@@ -119,8 +113,7 @@ struct Tile {
     // neighbouring elements of a row from column `col` on (of a tile in the order of memory)
     __device__ __forceinline__ const char *at(int row, int col) const {
         static_assert(!kMoved, "columns as they come");
-        if constexpr (kPlanes) return p + (col >> 3 & 3) * kPlane + row * kRow + (col >> 5) * 16 + (col & 7) * 2;
-        else return p + row * kRow + col * (int)sizeof(E);
+        return p + row * kRow + col * (int)sizeof(E);
     }
 };
 
@@ -577,28 +570,16 @@ struct Walker {
             for (int c = 0; c < kCols; ++c) O[c][it] *= e;
         }
     }
-    // (2) OUT: out^T += z^T P^T.  The state: S = exp(b_last) S + y^T (exp(b_last - b_j) z)
-    template <bool OUT>
-    __device__ __forceinline__ void advance(const Tile<E, M, kBoth> &y, const Tile<E, N, ZA ? kBoth : kAcross> &z, const Pairs<E> &P, const Gates<C> &gt) {
+    // (1) The state: S = exp(b_last) S + y^T (exp(b_last - b_j) z).  zf: z's operands, which finish() takes too
+    __device__ __forceinline__ void update(const Tile<E, M, kBoth> &y, const Tile<E, N, ZA ? kBoth : kAcross> &z, const Gates<C> &gt,
+                                           u32x4 (&zf)[kJ][kCols]) {
         const float last = gt.last;
         const Heads heads;
         u32x4 zd[kJ][kCols][kStateParts];
 #pragma unroll
         for (int jk = 0; jk < kJ; ++jk) {
-            u32x4 zf[kCols];
 #pragma unroll
-            for (int c = 0; c < kCols; ++c) zf[c] = z.across(jk, col_tile(c), lm, g);
-            if constexpr (OUT) {
-#pragma unroll
-                for (int q = 0; q < kParts; ++q)
-#pragma unroll
-                    for (int it = 0; it < kI; ++it) {
-                        if (jk * kDeep > it * 16 + 15) continue;
-                        const u32x4 b = *reinterpret_cast<const u32x4 *>(P.at(it, jk, q, lane));
-#pragma unroll
-                        for (int c = 0; c < kCols; ++c) O[c][it] = product<E>(zf[c], b, O[c][it]);
-                    }
-            }
+            for (int c = 0; c < kCols; ++c) zf[jk][c] = z.across(jk, col_tile(c), lm, g);
             if constexpr (sizeof(E) == 2) {
                 const f32x4 d0 = *reinterpret_cast<const f32x4 *>(&gt.out[jk * 32 + g * 4]);
                 const f32x4 d1 = *reinterpret_cast<const f32x4 *>(&gt.out[jk * 32 + 16 + g * 4]);
@@ -608,14 +589,14 @@ struct Walker {
                     for (int r = 0; r < 4; ++r) {
                         const f32x4 &d = r < 2 ? d0 : d1;
                         uint32_t s[kStateParts];
-                        heads.split(bf16_lo_as_float(zf[c][r]) * d[2 * (r & 1)], bf16_hi_as_float(zf[c][r]) * d[2 * (r & 1) + 1], s);
+                        heads.split(bf16_lo_as_float(zf[jk][c][r]) * d[2 * (r & 1)], bf16_hi_as_float(zf[jk][c][r]) * d[2 * (r & 1) + 1], s);
 #pragma unroll
                         for (int q = 0; q < kStateParts; ++q) zd[jk][c][q][r] = s[q];
                     }
             } else {
                 const f32x4 d = *reinterpret_cast<const f32x4 *>(&gt.out[jk * 16 + g * 4]);
 #pragma unroll
-                for (int c = 0; c < kCols; ++c) zd[jk][c][0] = __builtin_bit_cast(u32x4, __builtin_bit_cast(f32x4, zf[c]) * d);
+                for (int c = 0; c < kCols; ++c) zd[jk][c][0] = __builtin_bit_cast(u32x4, __builtin_bit_cast(f32x4, zf[jk][c]) * d);
             }
         }
         // two tiles of state rows at a time, so that products of one accumulator are four apart, and the next operands on their way
@@ -644,39 +625,53 @@ struct Walker {
                         for (int c = 0; c < kCols; ++c) S[a + h][c] = product<E>(yf[a >> 1 & 1][h][jk], zd[jk][c][q], S[a + h][c]);
         }
     }
-    // out row . dot row, this wave's columns, to part[w * C + row]; the dot rows from memory, or with LDS_ROWS from the tile
-    template <bool LDS_ROWS>
-    __device__ __forceinline__ void dot_rows(const Rows &r, const Tile<E, N, kAlong> &t, float *part, const Steps &st) const {
+    // (2) out^T += z^T P^T
+    __device__ __forceinline__ void finish(const Pairs<E> &P, const u32x4 (&zf)[kJ][kCols]) {
+#pragma unroll
+        for (int jk = 0; jk < kJ; ++jk)
+#pragma unroll
+            for (int q = 0; q < kParts; ++q)
+#pragma unroll
+                for (int it = 0; it < kI; ++it) {
+                    if (jk * kDeep > it * 16 + 15) continue;
+                    const u32x4 b = *reinterpret_cast<const u32x4 *>(P.at(it, jk, q, lane));
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c) O[c][it] = product<E>(zf[jk][c], b, O[c][it]);
+                }
+    }
+    // The rows that the outputs are multiplied with: this lane's four columns of each tile, from memory or from the tile
+    struct Dots {
+        uint32_t bits[kI][kCols][sizeof(E)];             // (four elements)
+    };
+    __device__ __forceinline__ void fetch_dots(Dots &d, const Rows &r, const Steps &st) const {
         const auto [lm, g] = fresh();
         constexpr int size = (int)sizeof(E);
         const Rsrc b = chunk_view(r, st);
         uint32_t o[kI];
-        if constexpr (FAST && !LDS_ROWS) st.offsets(o, lm, 16, (uint32_t)r.step, st.count, 0u);
+        if constexpr (FAST) st.offsets(o, lm, 16, (uint32_t)r.step, st.count, 0u);
 #pragma unroll
-        for (int it = 0; it < kI; ++it) {
-            const int i = it * 16 + lm;
-            float sum = 0.f;
+        for (int it = 0; it < kI; ++it)
 #pragma unroll
             for (int c = 0; c < kCols; ++c) {
-                const int col = cols_of(c, g);
-                uint32_t bits[4] = {0u, 0u, 0u, 0u};
-                if constexpr (LDS_ROWS) {
-                    __builtin_memcpy(bits, t.at(i, col), 4 * size);
-                } else if constexpr (FAST) {
+                const int col = cols_of(c, g), i = it * 16 + lm;
+                uint32_t(&bits)[size] = d.bits[it][c];
+                if constexpr (FAST) {
                     // (nowhere stays nowhere with a column's offset added)
                     const uint32_t at = col < r.d ? o[it] + col * size : kNowhere;
                     if constexpr (size == 2) {
                         const u32x2 v = fetch<u32x2>(b, at);
-                        __builtin_memcpy(bits, &v, 8);
+                        bits[0] = v[0];
+                        bits[1] = v[1];
                     } else {
                         const u32x4 v = fetch<u32x4>(b, at);
-                        __builtin_memcpy(bits, &v, 16);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) bits[j] = v[j];
                     }
-                } else if (i < st.count) {
-                    const char *row = r.token((long long)st.first + st.at(i));
-                    if (col + 4 <= r.d) {
-                        __builtin_memcpy(bits, row + col * size, 4 * size);
-                    } else {
+                } else {
+#pragma unroll
+                    for (int j = 0; j < size; ++j) bits[j] = 0u;
+                    if (i < st.count) {
+                        const char *row = r.token((long long)st.first + st.at(i));
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
                             if (col + j < r.d) {
@@ -685,17 +680,31 @@ struct Walker {
                             }
                     }
                 }
+            }
+    }
+    __device__ __forceinline__ void fetch_dots(Dots &d, const Tile<E, N, kAlong> &t) const {
+#pragma unroll
+        for (int it = 0; it < kI; ++it)
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) __builtin_memcpy(d.bits[it][c], t.at(it * 16 + lm, cols_of(c, g)), 4 * sizeof(E));
+    }
+    // out row . dot row, this wave's columns, to part[w * C + row]
+    __device__ __forceinline__ void dot_rows(const Dots &d, float *part) const {
+#pragma unroll
+        for (int it = 0; it < kI; ++it) {
+            float sum = 0.f;
+#pragma unroll
+            for (int c = 0; c < kCols; ++c)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     float x;
-                    if constexpr (size == 2) x = j & 1 ? bf16_hi_as_float(bits[j >> 1]) : bf16_lo_as_float(bits[j >> 1]);
-                    else x = __builtin_bit_cast(float, bits[j]);
+                    if constexpr (sizeof(E) == 2) x = j & 1 ? bf16_hi_as_float(d.bits[it][c][j >> 1]) : bf16_lo_as_float(d.bits[it][c][j >> 1]);
+                    else x = __builtin_bit_cast(float, d.bits[it][c][j]);
                     sum = fmaf(x, O[c][it][j], sum);
                 }
-            }
             sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
-            if (g == 0) part[w * C + i] = sum;
+            if (g == 0) part[w * C + it * 16 + lm] = sum;
         }
     }
     // rows of the chunk out of the accumulators
