@@ -202,35 +202,32 @@ hipError_t states(const StatePair &w, int directions, hipStream_t stream) {
     return hipGetLastError();
 }
 
-// One token.  A work-group takes COLS columns of one (batch, head)'s state, a lane four of them, and asks for all of its rows before it uses
-// the first.  Columns need nothing of each other, so that few states are dealt to four times as many work-groups, 32 columns each
-// (16 states 128 x 128: 3.8 us, 5.0 with whole rows); many are read in whole rows (3072: 77 us, 5.2 TB/s, what a copy reaches; 81 in
-// columns).  Bound by the states' way in and out, for few by the launch.
+// One token.  A work-group takes 32 columns of one (batch, head)'s state, eight lanes of four columns by 32 rows, all of whose rows it asks for
+// before it uses the first.  Columns need nothing of each other, so that few states are dealt to many work-groups (16 states 128 x 128:
+// 3.8 us, 5.0 with whole rows).  Bound by the states' way in and out (3072 of them: 80 us, 5.1 TB/s, a copy reaches 5.2), for few by the launch.
+constexpr int kStepCols = 32, kStepLanes = kStepCols / 4, kStepRows = kThreads / kStepLanes, kStepTimes = kDecayMaxD / kStepRows;
 template <typename E>
 __device__ inline float element(const void *p, size_t i) {
     if constexpr (sizeof(E) == 2) return bf16_bits_to_float(static_cast<const uint16_t *>(p)[i]);
     else return static_cast<const float *>(p)[i];
 }
 
-template <typename E, int COLS>
+template <typename E>
 __global__ __launch_bounds__(kThreads) void decay_step_kernel(const void *q, const void *k, const void *v, const float *log_decay, int kind,
                                                               int H, int dk, int dv, int out_dtype, const float *state, float *state_out,
                                                               void *out) {
-    constexpr int kLanes = COLS / 4, kStepRows = kThreads / kLanes, kTimes = kDecayMaxD / kStepRows;
-    __shared__ float s_o[kThreads / 64][COLS];
-    const int tid = threadIdx.x, parts = (dv + COLS - 1) / COLS;
-    const int bh = blockIdx.x / parts, h = bh % H, c0 = (blockIdx.x - bh * parts) * COLS;
-    const int col = c0 + tid % kLanes * 4, row0 = tid / kLanes;
+    __shared__ float s_q[kDecayMaxD], s_k[kDecayMaxD], s_o[kThreads / 64][kStepCols];
+    const int tid = threadIdx.x, parts = (dv + kStepCols - 1) / kStepCols;
+    const int bh = blockIdx.x / parts, h = bh % H, c0 = (blockIdx.x - bh * parts) * kStepCols;
+    const int col = c0 + tid % kStepLanes * 4, row0 = tid / kStepLanes;
     const size_t cells = (size_t)dk * dv;
     const float *s = state + bh * cells;
     float *t = state_out + bh * cells;
-    f32x4 c[kTimes];
-    float qr[kTimes], kr[kTimes];
+    f32x4 c[kStepTimes];
 #pragma unroll
-    for (int i = 0; i < kTimes; ++i) {
+    for (int i = 0; i < kStepTimes; ++i) {
         const int r = row0 + i * kStepRows;
         c[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        qr[i] = kr[i] = 0.f;
         if (r >= dk) continue;
         if (col + 4 <= dv) {
             __builtin_memcpy(&c[i], s + (size_t)r * dv + col, 16);
@@ -239,19 +236,20 @@ __global__ __launch_bounds__(kThreads) void decay_step_kernel(const void *q, con
             for (int j = 0; j < 4; ++j)
                 if (col + j < dv) c[i][j] = s[(size_t)r * dv + col + j];
         }
-        qr[i] = element<E>(q, (size_t)bh * dk + r);
-        kr[i] = element<E>(k, (size_t)bh * dk + r);
     }
+    if (tid < kDecayMaxD) s_q[tid] = tid < dk ? element<E>(q, (size_t)bh * dk + tid) : 0.f;
+    else if (tid < 2 * kDecayMaxD) s_k[tid - kDecayMaxD] = tid - kDecayMaxD < dk ? element<E>(k, (size_t)bh * dk + tid - kDecayMaxD) : 0.f;
     f32x4 x = {0.f, 0.f, 0.f, 0.f}, o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         if (col + j < dv) x[j] = element<E>(v, (size_t)bh * dv + col + j);
     const float a = exp2_fast(fmaxf(log_decay[kind == kDecayHead ? h : bh] * kLog2e, -65536.f));
+    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kTimes; ++i) {
+    for (int i = 0; i < kStepTimes; ++i) {
         const int r = row0 + i * kStepRows;
-        c[i] = c[i] * a + x * kr[i];
-        o += c[i] * qr[i];
+        c[i] = c[i] * a + x * s_k[r];
+        o += c[i] * s_q[r];
         if (r >= dk) continue;
         if (col + 4 <= dv) {
             __builtin_memcpy(t + (size_t)r * dv + col, &c[i], 16);
@@ -265,11 +263,11 @@ __global__ __launch_bounds__(kThreads) void decay_step_kernel(const void *q, con
     for (int j = 0; j < 4; ++j) {
         float y = o[j];
 #pragma unroll
-        for (int d = kLanes; d < 64; d *= 2) y += __shfl_xor(y, d);
-        if ((tid & 63) < kLanes) s_o[tid >> 6][(tid & 63) * 4 + j] = y;
+        for (int d = kStepLanes; d < 64; d *= 2) y += __shfl_xor(y, d);
+        if ((tid & 63) < kStepLanes) s_o[tid >> 6][(tid & 63) * 4 + j] = y;
     }
     __syncthreads();
-    if (tid < COLS && c0 + tid < dv) {
+    if (tid < kStepCols && c0 + tid < dv) {
         const float y = (s_o[0][tid] + s_o[1][tid]) + (s_o[2][tid] + s_o[3][tid]);
         const size_t at = (size_t)bh * dv + c0 + tid;
         if (out_dtype == GLA_DT_BF16) static_cast<uint16_t *>(out)[at] = float_to_bf16_bits(y);
@@ -312,13 +310,9 @@ hipError_t launch_decay_carry(const DecayCall &c, const float *first, float *loc
 
 hipError_t launch_decay_step(const void *q, const void *k, const void *v, const float *log_decay, int kind, int B, int H, int dk, int dv,
                              int dtype, int out_dtype, const float *state, float *state_out, void *out, hipStream_t stream) {
-    const int cols = (long long)B * H < 512 ? 32 : 64, parts = (dv + cols - 1) / cols;
-    auto run = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)(B * H * parts)), dim3(kThreads), 0, stream, q, k, v, log_decay, kind, H, dk, dv, out_dtype,
-                           state, state_out, out);
-    };
-    if (cols == 32) run(dtype == GLA_DT_BF16 ? decay_step_kernel<uint16_t, 32> : decay_step_kernel<float, 32>);
-    else run(dtype == GLA_DT_BF16 ? decay_step_kernel<uint16_t, 64> : decay_step_kernel<float, 64>);
+    const dim3 grid((unsigned)(B * H * ((dv + kStepCols - 1) / kStepCols)));
+    hipLaunchKernelGGL((dtype == GLA_DT_BF16 ? decay_step_kernel<uint16_t> : decay_step_kernel<float>), grid, dim3(kThreads), 0, stream, q, k, v,
+                       log_decay, kind, H, dk, dv, out_dtype, state, state_out, out);
     return hipGetLastError();
 }
 

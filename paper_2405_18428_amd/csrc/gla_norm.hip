@@ -309,16 +309,14 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(const float *part, float
 int lanes_of(int D) { return D <= 128 ? 16 : D <= 1536 ? 64 : D <= 2048 ? 256 : D <= 4096 ? 512 : 1024; }
 int groups_of(int D) { return lanes_of(D) >= 256 ? 1 : 256 / lanes_of(D); }
 
-// Rows are dealt to as many groups as fill the GPU a few times over, each with a few rows of its own; a multiple of the groups of a
+// Rows of each head are dealt to `slots` groups: `groups` in all if there are so many rows, `least` rows each; a multiple of the groups of a
 // work-group where a work-group stays with one head
-int slots_for(const NormParams &p, int rows_each, int work_groups) {
-    const int groups = groups_of(p.D);
-    const long long rows = (long long)p.B * p.T;
-    long long slots = (long long)work_groups * groups / p.H;
-    const long long most = (rows + rows_each - 1) / rows_each;
+int slots_for(const NormParams &p, int least, long long groups) {
+    const long long rows = (long long)p.B * p.T, most = (rows + least - 1) / least, of_group = groups_of(p.D);
+    long long slots = groups / p.H;
     if (slots > most) slots = most;
     if (slots < 1) slots = 1;
-    if (one_head(p)) slots = (slots + groups - 1) / groups * groups;
+    if (one_head(p)) slots = (slots + of_group - 1) / of_group * of_group;
     return (int)slots;
 }
 
@@ -352,12 +350,15 @@ int norm_slots(int B, int H, int T, int D, int layout) {
     p.T = T;
     p.D = D;
     p.layout = layout;
-    return slots_for(p, 4, D > 2048 ? 512 : 1024);
+    // 4096 waves (2048 where a lane holds two pieces of a row and more): with twice as many 16384 rows of 1152 took 63 us both ways, 57 with
+    // these, 2000 of 8192 69 and 58; with half as many 16384 rows of 384 took 33, 29 with these
+    return slots_for(p, 1, (long long)(D > 512 && D <= 1536 ? 2048 : 4096) * 64 / lanes_of(D));
 }
 
 hipError_t launch_norm_fwd(const NormParams &p0, int dtype, hipStream_t stream) {
     NormParams p = p0;
-    p.slots = slots_for(p, 1, 4096);
+    // two rows a group at least, if that leaves a thousand groups: it holds the weights (4096 rows of 1152: 9.9 us with one, 8.7 with two)
+    p.slots = slots_for(p, (long long)p.B * p.T * p.H < 2048 ? 1 : 2, 2048LL * groups_of(p.D));
     return dtype == GLA_DT_BF16 ? norm_of_width<uint16_t, false>(p, stream) : norm_of_width<float, false>(p, stream);
 }
 
