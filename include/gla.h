@@ -466,7 +466,7 @@ int gla_fwd_fused_gates(const void *q, const void *k, const void *v, const void 
  *                  may be NULL)
  *
  * bf16 calls run on bf16 MFMA with every factor that is not an input carried as two bf16 numbers, fp32 calls on fp32
- * MFMA.  Gates have no lower limit.  Inputs of visited rows have to be finite.  Tuning options have no effect.
+ * MFMA.  Gates have no lower limit.  Inputs of visited rows have to be finite.  T is at most 2^30.  Tuning options have no effect.
  * Never allocates; nothing is kept between calls.
  */
 typedef enum { GLA_DECAY_HEAD = 0, GLA_DECAY_TOKEN = 1 } gla_decay_kind;
@@ -528,7 +528,7 @@ int gla_decay_step(const void *q, const void *k, const void *v, const float *log
  *   base        > 0, finite; 10000 as a rule
  *   pairing     a gla_rope_pairing: a pair is two neighbouring channels, or channel i and i + w/2 of a section
  *   inverse     not 0: turned back, which is also the backward pass
- *   out_q, out_k   DEVICE, dtype, like q and k; may be q and k                                                (written)
+ *   out_q, out_k   DEVICE, dtype, like q and k; may be q and k (GLA_ERR_SHAPE: out_q = k, out_k = q or out_q = out_k)  (written)
  *
  * 1 <= d <= 256.  Angles are formed and reduced in 64 bits: every position of 32 bits is as exact as the first.  grid_h, grid_w are
  * ignored with positions or one axis.  Needs no workspace and never allocates.

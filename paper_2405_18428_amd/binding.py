@@ -632,10 +632,14 @@ def _want(name, t, shape, dtype, gpu):
         raise TypeError(f"{name} must be of element type {dtype}")
 
 
-def _room(nbytes, workspace, q):
-    """The caller's workspace, or one of its size for this call; `nbytes` is asked for in that case only."""
+def _room(nbytes, workspace, q, stream):
+    """The caller's workspace, or one of its size for this call (`nbytes` is asked for in that case only), which the allocator hands
+    on only when the call's stream is done with it."""
     if workspace is None:
-        return _torch().empty((max(nbytes(), 16),), dtype=_torch().uint8, device=q.device)
+        workspace = _torch().empty((max(nbytes(), 16),), dtype=_torch().uint8, device=q.device)
+        if stream is not None:
+            workspace.record_stream(stream)
+        return workspace
     if workspace.get_device() != q.get_device() or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous GPU tensor on the device of the others")
     return workspace
@@ -689,7 +693,7 @@ def gla_decay_fwd(q, k, v, log_decay, grid_h, grid_w, scan_dir=SCAN_ROW_FWD, lay
     if final_state is None and want_final_state:
         final_state = q.new_empty((B, H, dk, dv), dtype=torch.float32)
     qdt = _dt(q)
-    workspace = _room(lambda: gla_decay_fwd_workspace_bytes(B, H, T, dk, dv, qdt), workspace, q)
+    workspace = _room(lambda: gla_decay_fwd_workspace_bytes(B, H, T, dk, dv, qdt), workspace, q, stream)
     with _on_device_of(q):
         _check(lib.gla_decay_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), kind, _ptr(seq_lens),
                                  B, H, T, dk, dv, grid_h, grid_w, scan_dir, qdt, _dt(out), layout, _ptr(initial_state),
@@ -713,7 +717,7 @@ def gla_decay_bwd(q, k, v, log_decay, d_out, grid_h, grid_w, scan_dir=SCAN_ROW_F
     dg = _like(log_decay, torch.float32) if want_d_log_decay else None
     ds = q.new_empty((B, H, dk, dv), dtype=torch.float32) if want_d_initial_state else None
     qdt = _dt(q)
-    workspace = _room(lambda: gla_decay_bwd_workspace_bytes(B, H, T, dk, dv, qdt), workspace, q)
+    workspace = _room(lambda: gla_decay_bwd_workspace_bytes(B, H, T, dk, dv, qdt), workspace, q, stream)
     with _on_device_of(q):
         _check(lib.gla_decay_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), kind, _ptr(seq_lens),
                                  d_out.data_ptr(), _ptr(initial_state), _ptr(d_final_state), B, H, T, dk, dv, grid_h, grid_w,
@@ -844,7 +848,7 @@ def gla_norm_bwd(x, d_out, weight=None, bias=None, eps=1e-5, r_pre=None, layout=
         like = weight if weight is not None else bias
         shape = (H, D) if like is None else like.shape
         dw, db = x.new_empty(shape, dtype=torch.float32), x.new_empty(shape, dtype=torch.float32)
-    workspace = _room(lambda: gla_norm_bwd_workspace_bytes(B, H, T, D), workspace, x)
+    workspace = _room(lambda: gla_norm_bwd_workspace_bytes(B, H, T, D), workspace, x, stream)
     with _on_device_of(x):
         _check(lib.gla_norm_bwd(x.data_ptr(), d_out.data_ptr(), _ptr(weight), _ptr(bias), float(eps), _ptr(r_pre), B, H, T, D, _dt(x), _dt(dx),
                                 layout, dx.data_ptr(), _ptr(dr), _ptr(dw), _ptr(db), workspace.data_ptr(),

@@ -13,7 +13,7 @@
 namespace gla {
 namespace {
 
-constexpr int kVersion = 330;  // 0.3.3
+constexpr int kVersion = 400;  // 0.4.0
 
 // process-wide options (gla_set_option): atomics, so that a setter on one host thread and calls on another do not
 // race on them; a call reads them as it goes, so options are meant to be set between calls, not during one

@@ -19,20 +19,19 @@
 namespace gla {
 namespace {
 
-#ifndef PARTS_OUT
-#define PARTS_OUT 2
-#define PARTS_STATE 2
-#endif
 template <typename E> struct Elem;
 template <> struct Elem<uint16_t> {
     static constexpr int kChunk = 64;            // steps
     static constexpr int kDeep = 32;             // contracted values of an operand over the wave
-    static constexpr int kParts = PARTS_OUT, kStateParts = PARTS_STATE;
+    // A factor that is no input by itself (the state, P, the decayed z) is two bf16 numbers, head and remainder.  Three would leave what fp32
+    // leaves and took 9 % more time for the decayed z alone (65536 steps of 16 heads 128 x 128: 440 us, 397 with two), 48 % for all; one for
+    // the state and P 7 % less.
+    static constexpr int kParts = 2;
 };
 template <> struct Elem<float> {
     static constexpr int kChunk = 32;
     static constexpr int kDeep = 16;
-    static constexpr int kParts = 1, kStateParts = 1;
+    static constexpr int kParts = 1;
 };
 
 // 16 bytes of an operand; products of operands
@@ -351,8 +350,7 @@ struct Pairs {
 template <typename E, int M, int N, bool FAST, bool ZA>
 struct Walker {
     static constexpr int C = Elem<E>::kChunk, kDeep = Elem<E>::kDeep, kI = C / 16, kJ = C / kDeep;
-    static constexpr int kRows = M / 16, kCols = N / 64, kSteps = M / kDeep, kParts = Elem<E>::kParts,
-                         kStateParts = Elem<E>::kStateParts;
+    static constexpr int kRows = M / 16, kCols = N / 64, kSteps = M / kDeep, kParts = Elem<E>::kParts;
     f32x4 S[kRows][kCols];
     f32x4 O[kCols][kI];
     int lane, lm, g, w;
@@ -575,7 +573,7 @@ struct Walker {
                                            u32x4 (&zf)[kJ][kCols]) {
         const float last = gt.last;
         const Heads heads;
-        u32x4 zd[kJ][kCols][kStateParts];
+        u32x4 zd[kJ][kCols][kParts];
 #pragma unroll
         for (int jk = 0; jk < kJ; ++jk) {
 #pragma unroll
@@ -588,10 +586,10 @@ struct Walker {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const f32x4 &d = r < 2 ? d0 : d1;
-                        uint32_t s[kStateParts];
+                        uint32_t s[kParts];
                         heads.split(bf16_lo_as_float(zf[jk][c][r]) * d[2 * (r & 1)], bf16_hi_as_float(zf[jk][c][r]) * d[2 * (r & 1) + 1], s);
 #pragma unroll
-                        for (int q = 0; q < kStateParts; ++q) zd[jk][c][q][r] = s[q];
+                        for (int q = 0; q < kParts; ++q) zd[jk][c][q][r] = s[q];
                     }
             } else {
                 const f32x4 d = *reinterpret_cast<const f32x4 *>(&gt.out[jk * 16 + g * 4]);
@@ -618,7 +616,7 @@ struct Walker {
 #pragma unroll
             for (int jk = 0; jk < kJ; ++jk)
 #pragma unroll
-                for (int q = 0; q < kStateParts; ++q)
+                for (int q = 0; q < kParts; ++q)
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll

@@ -105,8 +105,8 @@ int check_call(DecayCall &c, const float *log_decay, int kind, const int *seq_le
     if (bad_dtype(dtype) || bad_dtype(out_dtype) || (kind != GLA_DECAY_HEAD && kind != GLA_DECAY_TOKEN)) return GLA_ERR_SHAPE;
     if (dk > kDecayMaxD || dv > kDecayMaxD) return GLA_ERR_UNSUPPORTED;
     if (seq_lens != nullptr && scan_dir > GLA_SCAN_ROW_REV) return GLA_ERR_UNSUPPORTED;
-    // (work-groups of 512 threads, fewer than 2^32 in a launch)
-    if ((long long)B * H * decay_blocks(T) >= (1LL << 23)) return GLA_ERR_UNSUPPORTED;
+    // (work-groups of 512 threads, fewer than 2^32 threads in a launch; steps and spans in 32 bits)
+    if (T > (1 << 30) || (long long)B * H * decay_blocks(T) >= (1LL << 23)) return GLA_ERR_UNSUPPORTED;
     if (misaligned(log_decay) || (reinterpret_cast<uintptr_t>(seq_lens) & 3u) != 0) return GLA_ERR_ALIGN;
     c.log_decay = log_decay;
     c.seq_lens = seq_lens;
@@ -131,11 +131,11 @@ int check_call(DecayCall &c, const float *log_decay, int kind, const int *seq_le
 }
 
 // How the walks get at the states that enter their spans: up to kChainSpans they chain the local ones themselves, beyond that a kernel of its
-// own does so in place
-bool entries(DecayEntry &in, const DecayCall &c, float *local, const float *decay, bool reversed, hipStream_t stream) {
+// own does so in place, and also where the last state is written over the first, which other spans may not have read by then
+bool entries(DecayEntry &in, const DecayCall &c, float *local, const float *decay, bool reversed, const float *last, hipStream_t stream) {
     in.local = local;
     in.decay = decay;
-    in.chained = c.nspans > kChainSpans;
+    in.chained = c.nspans > kChainSpans || (last != nullptr && last == in.first);
     return !in.chained || launch_decay_carry(c, in.first, local, decay, reversed, stream) == hipSuccess;
 }
 
@@ -185,7 +185,7 @@ int gla_decay_fwd(const void *q, const void *k, const void *v, const float *log_
         w.local = room.local;
         w.decay = room.decay;
         if (launch_decay_states(w, nullptr, qkv_dtype, stream) != hipSuccess) return GLA_ERR_HIP;
-        if (!entries(w.in, c, room.local, room.decay, false, stream)) return GLA_ERR_HIP;
+        if (!entries(w.in, c, room.local, room.decay, false, final_state, stream)) return GLA_ERR_HIP;
     }
     return launch_decay_walk(w, qkv_dtype, stream) == hipSuccess ? GLA_OK : GLA_ERR_HIP;
 }
@@ -252,8 +252,8 @@ int gla_decay_bwd(const void *q, const void *k, const void *v, const float *log_
         g.local = room.glocal;
         g.decay = room.gdecay;
         if (launch_decay_states(s, b.c.nspans > 1 ? &g : nullptr, qkv_dtype, stream) != hipSuccess) return GLA_ERR_HIP;
-        if (!entries(w.in, c, room.local, room.decay, false, stream)) return GLA_ERR_HIP;
-        if (b.c.nspans > 1 && !entries(b.in, b.c, room.glocal, room.gdecay, true, stream)) return GLA_ERR_HIP;
+        if (!entries(w.in, c, room.local, room.decay, false, nullptr, stream)) return GLA_ERR_HIP;
+        if (b.c.nspans > 1 && !entries(b.in, b.c, room.glocal, room.gdecay, true, d_initial_state, stream)) return GLA_ERR_HIP;
     }
     if (launch_decay_walk(w, qkv_dtype, stream) != hipSuccess) return GLA_ERR_HIP;
     if (launch_decay_back(b, qkv_dtype, stream) != hipSuccess) return GLA_ERR_HIP;
@@ -320,6 +320,8 @@ int gla_rope(const void *q, const void *k, const int *positions, const int *sect
         p.pairs_end[a] = first / 2;
     }
     if (any_misaligned(q, k, (const void *)out_q, (const void *)out_k) || (reinterpret_cast<uintptr_t>(positions) & 3u) != 0) return GLA_ERR_ALIGN;
+    // in place is each pair's own place: no tensor is turned into another's, nor two into one
+    if (k != nullptr && (out_q == out_k || out_q == k || out_k == q)) return GLA_ERR_SHAPE;
     // 32-bit thread numbers
     if ((long long)B * T >= (1LL << 31) / d) return GLA_ERR_UNSUPPORTED;
     p.x[0] = q;
@@ -359,6 +361,7 @@ int gla_norm_fwd(const void *x, const float *weight, const float *bias, float ep
     if (!x || !out) return GLA_ERR_NULL;
     const int st = check_norm(x, r_pre, weight, bias, eps, B, H, T, D, x_dtype, out_dtype, layout);
     if (st != GLA_OK) return st;
+    if (out == x && x_dtype != out_dtype) return GLA_ERR_SHAPE;
     if (misaligned(out)) return GLA_ERR_ALIGN;
     NormParams p = {};
     p.x = x;

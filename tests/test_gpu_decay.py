@@ -326,3 +326,53 @@ def test_refusals():
     q1 = torch.zeros(1, 3, 8, device=DEV)
     with pytest.raises(gla.GlaError):       # states that overlap without being the same
         gla.gla_decay_step(q1, q1, q1, g, st[:192].view(1, 3, 8, 8), state_out=st[64:].view(1, 3, 8, 8))
+
+
+@pytest.mark.parametrize("T", [128, 200, 256, 500])
+def test_final_state_over_the_initial_one(T):
+    """Written over it, the state of few spans (whose walks all read the first state) is what it is apart from it."""
+    c = make(4, 5, T, 64, 64, BF16, seed=91)
+    d = {n: (t.to(DEV) if torch.is_tensor(t) else t) for n, t in c.items()}
+    want, fin = gla.gla_decay_fwd(d["q"], d["k"], d["v"], d["g"], 1, T, initial_state=d["s0"])
+    s = d["s0"].clone()
+    out, _ = gla.gla_decay_fwd(d["q"], d["k"], d["v"], d["g"], 1, T, initial_state=s, final_state=s)
+    r, a = reference(c, 1, T, 0, back=False)
+    close(out, r["out"], a["out"], TOL[BF16], ROUND[F32], "out")
+    close(s, r["fin"], a["fin"], TOL[BF16], ROUND[F32], "state")
+    close(want, r["out"], a["out"], TOL[BF16], ROUND[F32], "out")
+    close(fin, r["fin"], a["fin"], TOL[BF16], ROUND[F32], "state")
+
+
+def test_call_on_a_given_stream():
+    """On a stream that is not the current one, workspace and outputs of its own: nothing that comes after on the current stream is given its memory
+    too early."""
+    c = make(2, 4, 600, 64, 64, BF16, seed=92)
+    d = {n: (t.to(DEV) if torch.is_tensor(t) else t) for n, t in c.items()}
+    want = gla.gla_decay_bwd(d["q"], d["k"], d["v"], d["g"], d["do"], 1, 600, initial_state=d["s0"])
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    for _ in range(3):
+        got = gla.gla_decay_bwd(d["q"], d["k"], d["v"], d["g"], d["do"], 1, 600, initial_state=d["s0"], stream=st)
+        junk = [torch.full((1 << 20,), 1e30, device=DEV) for _ in range(8)]
+        torch.cuda.synchronize()
+        del junk
+        assert all(torch.equal(x, y) for x, y in zip(got[:4], want[:4]))
+
+
+@pytest.mark.parametrize("scan", [2, 3])
+def test_large_grids_in_columns(scan):
+    """A column's rows lie all over a grid in token order: offsets near and past what the views with 32-bit offsets reach."""
+    for H, gh, gw in ((40, 64, 64), (3000, 40, 50)):
+        T, d = gh * gw, 64
+        q, k, v = (torch.zeros(1, T, H, d, dtype=F32, device=DEV) for _ in range(3))
+        gen = torch.Generator(device=DEV).manual_seed(scan)
+        for t in (q, k, v):
+            t[0, :, H - 1] = torch.randn(T, d, generator=gen, device=DEV) * 0.3
+        g = torch.full((H,), -0.1, device=DEV)
+        out, _ = gla.gla_decay_fwd(q, k, v, g, gh, gw, scan, 1)
+        at = oo.visits(T, gh, gw, scan)
+        rows = [t[0, :, H - 1].double().cpu().numpy()[at][None] for t in (q, k, v)]
+        o, _ = oo.decay_fwd(*rows, np.full((1, T), float(g[0])), np.zeros((1, d, d)))
+        oa, _ = oo.decay_fwd(*(np.abs(x) for x in rows), np.full((1, T), float(g[0])), np.zeros((1, d, d)))
+        close(out[0, torch.from_numpy(at.copy()).to(DEV), H - 1][None], o, oa, TOL[F32], ROUND[F32], "out")
+        del q, k, v, out
