@@ -1,4 +1,4 @@
-"""MI355X-native forward pass of the gated-linear-attention token mixer of DiG.
+"""MI355X-native gated-linear-attention token mixer of DiG, and the operators of a mixer with one decay a head.
 
 The compute lives in hand-written HIP kernels behind the C ABI declared in
 ``include/gla.h`` (built into ``libgla.so`` next to ``csrc/``); this package

@@ -96,9 +96,15 @@ __host__ __device__ inline int decay_blocks(int T) { return (T + kFlowBlock - 1)
 hipError_t launch_decay_walk(const DecayWalk &w, int dtype, hipStream_t stream);
 // local states of every span but the last one walked: of (k, v) to w.local and, with `back`, of the reversed (q, dO) to back->local
 hipError_t launch_decay_states(const DecayWalk &w, const DecayWalk *back, int dtype, hipStream_t stream);
-// chains local states in place: entry sp becomes the state that enters span sp, from `first` [B*H, dk, dv] or zero; with
-// `reversed` the last span comes first
-hipError_t launch_decay_carry(const DecayCall &c, const float *first, float *local, const float *decay, bool reversed, hipStream_t stream);
+// chains local states in place: entry sp of `local` becomes the state that enters span sp, from `first` [B*H, dk, dv] or zero; `reversed`: the
+// last span comes first
+struct DecayChain {
+    const float *first;
+    float *local;
+    const float *decay;
+    int nspans, reversed;
+};
+hipError_t launch_decay_carry(const DecayCall &c, const DecayChain &chain, const DecayChain *other, hipStream_t stream);
 hipError_t launch_decay_back(const DecayBack &w, int dtype, hipStream_t stream);
 hipError_t launch_decay_gate(const DecayGate &w, hipStream_t stream);
 hipError_t launch_decay_step(const void *q, const void *k, const void *v, const float *log_decay, int kind, int B, int H, int dk, int dv,

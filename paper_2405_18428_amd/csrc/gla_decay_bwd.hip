@@ -91,10 +91,12 @@ __device__ __forceinline__ void walk_back(const DecayBack &p, char *lds) {
             if (wk.lane == 0) meet_part[wk.w] = sum;
         }
         if constexpr (ROLE == 0) {
-            wk.begin(tk, tq, P, gt);
+            wk.pairs(tk, tq, P, gt);
+            wk.from_state(tk, gt);
             wk.update(tq, td, gt, zf);
         } else {
-            wk.begin(tv, td, P, gt);
+            wk.pairs(tv, td, P, gt);
+            wk.from_state(tv, gt);
             wk.update(td, tq, gt, zf);
             if (flows) wk.fetch_dots(d, tk);
         }

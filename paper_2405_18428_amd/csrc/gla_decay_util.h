@@ -478,9 +478,9 @@ struct Walker {
         return sum;
     }
 
-    // (1) P^T of the lower triangle, whose tiles are dealt to the waves in turn, and out^T = exp(b_i) S^T x^T of this wave's columns.
-    // Products that add to one accumulator are kept apart: each would wait for the one before.
-    __device__ __forceinline__ void begin(const Tile<E, M, kAlong> &x, const Tile<E, M, kBoth> &y, const Pairs<E> &P, const Gates<C> &gt) {
+    // (1) P^T of the lower triangle, whose tiles are dealt to the waves in turn.  Products that add to one accumulator are kept apart, here and
+    // below: each would wait for the one before.
+    __device__ __forceinline__ void pairs(const Tile<E, M, kAlong> &x, const Tile<E, M, kBoth> &y, const Pairs<E> &P, const Gates<C> &gt) const {
         constexpr int kTiles = kI * (kI + 1) / 2, kMine = (kTiles + 3) / 4;
         const Heads heads;
 #pragma unroll
@@ -523,6 +523,10 @@ struct Walker {
                 *reinterpret_cast<f32x4 *>(P.at(it, jt, 0, lane)) = p;
             }
         }
+    }
+    // (1) out^T = exp(b_i) S^T x^T of this wave's columns
+    __device__ __forceinline__ void from_state(const Tile<E, M, kAlong> &x, const Gates<C> &gt) {
+        const Heads heads;
 #pragma unroll
         for (int c = 0; c < kCols; ++c)
 #pragma unroll

@@ -132,11 +132,10 @@ int check_call(DecayCall &c, const float *log_decay, int kind, const int *seq_le
 
 // How the walks get at the states that enter their spans: up to kChainSpans they chain the local ones themselves, beyond that a kernel of its
 // own does so in place, and also where the last state is written over the first, which other spans may not have read by then
-bool entries(DecayEntry &in, const DecayCall &c, float *local, const float *decay, bool reversed, const float *last, hipStream_t stream) {
+void enter_by(DecayEntry &in, const DecayCall &c, float *local, const float *decay, const float *last) {
     in.local = local;
     in.decay = decay;
-    in.chained = c.nspans > kChainSpans || (last != nullptr && last == in.first);
-    return !in.chained || launch_decay_carry(c, in.first, local, decay, reversed, stream) == hipSuccess;
+    in.chained = c.nspans > 1 && (c.nspans > kChainSpans || (last != nullptr && last == in.first));
 }
 
 bool sized(DecayCall &c, int B, int H, int T, int dk, int dv, int dtype) {
@@ -185,7 +184,9 @@ int gla_decay_fwd(const void *q, const void *k, const void *v, const float *log_
         w.local = room.local;
         w.decay = room.decay;
         if (launch_decay_states(w, nullptr, qkv_dtype, stream) != hipSuccess) return GLA_ERR_HIP;
-        if (!entries(w.in, c, room.local, room.decay, false, final_state, stream)) return GLA_ERR_HIP;
+        enter_by(w.in, c, room.local, room.decay, final_state);
+        const DecayChain chain = {initial_state, room.local, room.decay, c.nspans, 0};
+        if (w.in.chained && launch_decay_carry(c, chain, nullptr, stream) != hipSuccess) return GLA_ERR_HIP;
     }
     return launch_decay_walk(w, qkv_dtype, stream) == hipSuccess ? GLA_OK : GLA_ERR_HIP;
 }
@@ -252,8 +253,14 @@ int gla_decay_bwd(const void *q, const void *k, const void *v, const float *log_
         g.local = room.glocal;
         g.decay = room.gdecay;
         if (launch_decay_states(s, b.c.nspans > 1 ? &g : nullptr, qkv_dtype, stream) != hipSuccess) return GLA_ERR_HIP;
-        if (!entries(w.in, c, room.local, room.decay, false, nullptr, stream)) return GLA_ERR_HIP;
-        if (b.c.nspans > 1 && !entries(b.in, b.c, room.glocal, room.gdecay, true, d_initial_state, stream)) return GLA_ERR_HIP;
+        enter_by(w.in, c, room.local, room.decay, nullptr);
+        enter_by(b.in, b.c, room.glocal, room.gdecay, d_initial_state);
+        const DecayChain chain = {initial_state, room.local, room.decay, c.nspans, 0};
+        const DecayChain back = {d_final_state, room.glocal, room.gdecay, b.c.nspans, 1};
+        if (w.in.chained || b.in.chained) {
+            const DecayChain &one = w.in.chained ? chain : back;
+            if (launch_decay_carry(c, one, w.in.chained && b.in.chained ? &back : nullptr, stream) != hipSuccess) return GLA_ERR_HIP;
+        }
     }
     if (launch_decay_walk(w, qkv_dtype, stream) != hipSuccess) return GLA_ERR_HIP;
     if (launch_decay_back(b, qkv_dtype, stream) != hipSuccess) return GLA_ERR_HIP;
