@@ -489,7 +489,8 @@ size_t gla_decay_fwd_workspace_bytes(int B, int H, int T, int dk, int dv, int qk
  *   d_initial_state  DEVICE, fp32 [B,H,dk,dv], or NULL: not wanted                                            (written)
  *   workspace        DEVICE, 16-byte aligned, gla_decay_bwd_workspace_bytes(...) bytes
  *
- * Everything else as gla_decay_fwd.  Outputs must not alias inputs.
+ * With dlog_decay of GLA_DECAY_HEAD bf16 calls carry three bf16 numbers instead of two (a third more time): that sum over all
+ * steps would add up the errors of two.  Everything else as gla_decay_fwd.  Outputs must not alias inputs.
  */
 int gla_decay_bwd(const void *q, const void *k, const void *v, const float *log_decay, int decay_kind, const int *seq_lens,
                   const void *d_out, const float *initial_state, const float *d_final_state,

@@ -32,6 +32,7 @@ struct DecayCall {
     int kind;                           // DecayKind
     int B, H, T, dk, dv, grid_h, grid_w, scan_dir;
     int layout;                         // gla_layout
+    int exact;                          // bf16: products as exact as fp32's
     int fast;                           // rows through 32-bit views (gla_decay_util.h)
     int nspans, span_len;               // spans a sequence is walked in, steps in each (a multiple of 64)
 };

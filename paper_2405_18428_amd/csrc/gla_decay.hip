@@ -299,7 +299,10 @@ static hipError_t walk_of_size(const DecayWalk &w, hipStream_t stream) {
 }
 
 hipError_t launch_decay_walk(const DecayWalk &w, int dtype, hipStream_t stream) {
-    if (dtype == GLA_DT_BF16) return w.grad ? walk_of_size<uint16_t, true>(w, stream) : walk_of_size<uint16_t, false>(w, stream);
+    if (dtype == GLA_DT_BF16) {
+        if (!w.grad) return walk_of_size<uint16_t, false>(w, stream);
+        return w.c.exact ? walk_of_size<Bf16Exact, true>(w, stream) : walk_of_size<uint16_t, true>(w, stream);
+    }
     return w.grad ? walk_of_size<float, true>(w, stream) : walk_of_size<float, false>(w, stream);
 }
 
@@ -311,7 +314,8 @@ hipError_t launch_decay_states(const DecayWalk &w, const DecayWalk *back, int dt
     return decay_sizes(w.r.m, w.r.n, w.c.fast, [&](auto m, auto n, auto fast) {
         constexpr int M = decltype(m)::value, N = decltype(n)::value;
         constexpr bool F = decltype(fast)::value;
-        return dtype == GLA_DT_BF16 ? states<uint16_t, M, N, F>(both, d, stream) : states<float, M, N, F>(both, d, stream);
+        if (dtype != GLA_DT_BF16) return states<float, M, N, F>(both, d, stream);
+        return w.c.exact ? states<Bf16Exact, M, N, F>(both, d, stream) : states<uint16_t, M, N, F>(both, d, stream);
     });
 }
 

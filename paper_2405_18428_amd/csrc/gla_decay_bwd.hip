@@ -200,7 +200,8 @@ hipError_t launch_decay_back(const DecayBack &w, int dtype, hipStream_t stream) 
     return decay_sizes(w.c.dk, w.c.dv, w.c.fast, [&](auto k, auto v, auto fast) {
         constexpr int K = decltype(k)::value, V = decltype(v)::value;
         constexpr bool F = decltype(fast)::value;
-        return dtype == GLA_DT_BF16 ? back<uint16_t, K, V, F>(w, stream) : back<float, K, V, F>(w, stream);
+        if (dtype != GLA_DT_BF16) return back<float, K, V, F>(w, stream);
+        return w.c.exact ? back<Bf16Exact, K, V, F>(w, stream) : back<uint16_t, K, V, F>(w, stream);
     });
 }
 

@@ -10,7 +10,10 @@
 // is eight (bf16) or four (fp32) values of the contracted index in a lane, and which index stands where does not matter as long as
 // both operands agree.  The state's rows are ordered (state_row) so that x's operands are 16 contiguous bytes of a row.
 // bf16 calls split what is not bf16 by itself (the state, P, the decayed z) into two bf16 numbers, head and remainder: what is
-// lost is 2^-18 of each, so states and gate gradients, which are given in 32 bits, hold about 2e-6 where one bf16 would leave 2e-3.
+// lost is 2^-18 of each, so states, which are given in 32 bits, hold about 2e-6 where one bf16 would leave 2e-3, and a token's gate
+// gradient 7e-6.  The gradient of a head's one decay is a sum over all steps in which each block's flows count by their place, so that
+// errors add up to 256 / (memory in steps) times as much: 2e-5 to 6e-5 for a single head of 30 steps' memory with two numbers, and
+// three are taken (DecayCall::exact; a training step of 64 sequences of 4096 steps, 128 x 128: 640 us, 482 with two).
 // fp32 calls run on the fp32 matrix instructions.
 #pragma once
 #include "gla_decay.h"
@@ -27,6 +30,15 @@ template <> struct Elem<uint16_t> {
     // leaves and took 9 % more time for the decayed z alone (65536 steps of 16 heads 128 x 128: 440 us, 397 with two), 48 % for all; one for
     // the state and P 7 % less.
     static constexpr int kParts = 2;
+};
+// bf16 rows whose products are as exact as fp32's: three numbers
+struct Bf16Exact {
+    uint16_t bits;
+};
+template <> struct Elem<Bf16Exact> {
+    static constexpr int kChunk = 64;
+    static constexpr int kDeep = 32;
+    static constexpr int kParts = 3;
 };
 template <> struct Elem<float> {
     static constexpr int kChunk = 32;

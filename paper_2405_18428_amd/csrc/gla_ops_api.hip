@@ -206,6 +206,7 @@ int gla_decay_bwd(const void *q, const void *k, const void *v, const float *log_
     if (!workspace || misaligned(workspace) || workspace_bytes < room.bytes) return GLA_ERR_WORKSPACE;
     const hipStream_t stream = static_cast<hipStream_t>(stream_);
     const bool gates = dlog_decay != nullptr;
+    c.exact = gates && c.kind == kDecayHead && qkv_dtype == GLA_DT_BF16;
 
     DecayWalk w = {};                    // dq: the recurrence of (dO, v, k) from the transposed states
     w.c = c;

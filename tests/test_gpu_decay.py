@@ -376,3 +376,16 @@ def test_large_grids_in_columns(scan):
         oa, _ = oo.decay_fwd(*(np.abs(x) for x in rows), np.full((1, T), float(g[0])), np.zeros((1, d, d)))
         close(out[0, torch.from_numpy(at.copy()).to(DEV), H - 1][None], o, oa, TOL[F32], ROUND[F32], "out")
         del q, k, v, out
+
+
+@pytest.mark.parametrize("T,dk,dv", [(6000, 16, 16), (3000, 36, 72), (5000, 64, 128)])
+def test_gate_gradient_of_short_memories_bf16(T, dk, dv):
+    """The same from bf16 rows: the one decay of a head is held to what fp32 arithmetic leaves, 2^-24 of every product, as its products are
+    three bf16 numbers each (2^-25)."""
+    c = make(1, 1, T, dk, dv, BF16, gate="head", g_scale=0.0, state=False, seed=43)
+    c["g"].fill_(-0.2)
+    r, a = reference(c, 1, T, 0)
+    d = {n: (t.to(DEV) if torch.is_tensor(t) else t) for n, t in c.items()}
+    dg = gla.gla_decay_bwd(d["q"], d["k"], d["v"], d["g"], d["do"], 1, T)[3]
+    flows = np.sqrt((a["dg"] ** 2).sum()) * 2.0 ** -24 * 8
+    assert abs(float(dg[0]) - r["dg"].sum()) <= flows, (float(dg[0]), r["dg"].sum(), flows)
