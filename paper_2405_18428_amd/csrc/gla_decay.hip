@@ -218,7 +218,7 @@ hipError_t states(const StatePair &w, int directions, hipStream_t stream) {
 
 // One token.  A work-group takes 32 columns of one (batch, head)'s state, eight lanes of four columns by 32 rows, all of whose rows it asks for
 // before it uses the first.  Columns need nothing of each other, so that few states are dealt to many work-groups (16 states 128 x 128:
-// 3.8 us, 5.0 with whole rows).  Bound by the states' way in and out (3072 of them: 80 us, 5.1 TB/s, a copy reaches 5.2), for few by the launch.
+// 3.8 us, 5.0 with whole rows).  Bound by the states' way in and out (192 sequences of 16 heads: 80 us, 5.1 TB/s, a copy reaches 5.2), for few by the launch.
 constexpr int kStepCols = 32, kStepLanes = kStepCols / 4, kStepRows = kThreads / kStepLanes, kStepTimes = kDecayMaxD / kStepRows;
 template <typename E>
 __device__ inline float element(const void *p, size_t i) {

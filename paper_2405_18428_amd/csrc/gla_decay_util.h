@@ -251,8 +251,8 @@ __device__ __forceinline__ u32x4 load16(const char *p) {          // any alignme
 template <typename E, int W, int THREADS, bool FAST>
 struct Pieces {
     static constexpr int kPerRow = W * (int)sizeof(E) / 16, kEach = 16 / (int)sizeof(E);
-    static constexpr int kChunk = Elem<E>::kChunk, kCount = (kChunk * kPerRow + THREADS - 1) / THREADS;
-    static_assert(THREADS % kPerRow == 0 && (kChunk * kPerRow % THREADS == 0 || kCount == 1), "whole rows");
+    static constexpr int kChunk = Elem<E>::kChunk, kCount = kChunk * kPerRow / THREADS;
+    static_assert(THREADS % kPerRow == 0 && kChunk * kPerRow % THREADS == 0, "whole rows, whole pieces a thread");
     u32x4 v[kCount];
     __device__ __forceinline__ void issue(const Rows &r, int tid, const Steps &t) {
         const int col = tid % kPerRow * kEach;
@@ -292,7 +292,6 @@ struct Pieces {
     __device__ __forceinline__ void commit(const Rows &r, int tid, const Tile<E, W, R> &t) const {
         const int piece = tid % kPerRow, row = tid / kPerRow, over = (piece + 1) * kEach - r.d;
         constexpr int by = THREADS / kPerRow;
-        if (kChunk * kPerRow < THREADS && row >= kChunk) return;         // (more threads than pieces)
         const bool shifted = over > 0 && over < kEach && r.d >= kEach;
         if (r.d % kEach == 0) {
 #pragma unroll
