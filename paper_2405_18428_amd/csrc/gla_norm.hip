@@ -3,7 +3,7 @@
 //   n = (x - mean) rstd,  dy = dO r sigmoid(r) (or dO),  dn = dy weight,
 //   dx = rstd (dn - mean(dn) - n mean(dn n)),   dr = dO y sigmoid(r) (1 + r (1 - sigmoid(r))),
 //   dweight = sum over rows of dy n,   dbias = sum over rows of dy.
-// A row is held in registers by a group of lanes (16 to 1024 by its width), so it is read once; mean and variance are taken in two
+// A row is held in registers by a group of lanes (4 to 1024 by its width), so it is read once; mean and variance are taken in two
 // steps from these registers, and the backward pass takes them again instead of reading them.  Each group stays with one head, whose weights
 // it holds, and walks the head's rows, the next of which is on its way while it works on one; the sums for dweight and dbias stay in its
 // registers, are added over the groups of a work-group where these share a head, and go to memory as one partial sum a slot, which a
@@ -15,6 +15,7 @@ namespace {
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
@@ -35,6 +36,23 @@ __device__ __forceinline__ Raw<E> load_raw(const char *row, int c0, int D) {
     Raw<E> x = {};
     if (c0 + kEach <= D) {
         __builtin_memcpy(&x, row + c0 * (int)sizeof(E), sizeof(x));
+    } else if (c0 < D && D >= kEach) {                   // the row's last eight, moved down (element by element D = 36 took twice as long)
+        __builtin_memcpy(&x, row + (D - kEach) * (int)sizeof(E), sizeof(x));
+        const int over = c0 + kEach - D;
+        if constexpr (sizeof(E) == 2) {
+            x.v = __builtin_bit_cast(u32x4, __builtin_bit_cast(unsigned __int128, x.v) >> (16 * over));
+        } else {
+            float e[kEach];
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) e[j] = x.v[j >> 2][j & 3];
+#pragma unroll
+            for (int k = 4; k > 0; k /= 2)
+#pragma unroll
+                for (int j = 0; j < kEach; ++j)
+                    if (over & k) e[j] = j + k < kEach ? e[j + k] : 0.f;
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) x.v[j >> 2][j & 3] = e[j];
+        }
     } else if (c0 < D) {
 #pragma unroll
         for (int j = 0; j < kEach; ++j)
@@ -68,9 +86,21 @@ __device__ __forceinline__ void store_piece(char *row, int c0, int D, int dtype,
         }
         return;
     }
+    int from = 0;
+    if (c0 + 4 <= D) {
+        if (dtype == GLA_DT_BF16) {
+            const u32x2 b = {pack(x[0], x[1]), pack(x[2], x[3])};
+            __builtin_memcpy(row + c0 * 2, &b, 8);
+        } else {
+            const f32x4 v = {x[0], x[1], x[2], x[3]};
+            __builtin_memcpy(row + c0 * 4, &v, 16);
+        }
+        from = 4;
+    }
+    if (c0 + from >= D) return;
 #pragma unroll
     for (int j = 0; j < kEach; ++j)
-        if (c0 + j < D) {
+        if (j >= from && c0 + j < D) {
             if (dtype == GLA_DT_BF16) reinterpret_cast<uint16_t *>(row)[c0 + j] = (uint16_t)pack(x[j], 0.f);
             else reinterpret_cast<float *>(row)[c0 + j] = x[j];
         }
@@ -305,14 +335,19 @@ __global__ __launch_bounds__(1024) void norm_sum_kernel(const float *part, float
     if (k == 0 && col < cols) (blockIdx.y ? dbias : dweight)[col] = s[0][c];
 }
 
-// lanes of a row's group
-int lanes_of(int D) { return D <= 128 ? 16 : D <= 1536 ? 64 : D <= 2048 ? 256 : D <= 4096 ? 512 : 1024; }
-int groups_of(int D) { return lanes_of(D) >= 256 ? 1 : 256 / lanes_of(D); }
+// lanes of a row's group: as few as hold it (16 for rows of 64 took 37 us forward where 8 take 21, 4 x 16 x 4096 of them).  Rows of 65 to 96,
+// nine pieces for 72, leave lanes of 16 idle: forward four lanes of three take them in 19 us instead of 22 (2 x 16 x 4096), backward
+// they take as long in head order and 67 us instead of 55 in token order, both directions together, where each group's sums go to memory.
+int lanes_of(int D, bool back) {
+    if (!back && D > 64 && D <= 96) return 4;
+    return D <= 32 ? 4 : D <= 64 ? 8 : D <= 128 ? 16 : D <= 1536 ? 64 : D <= 2048 ? 256 : D <= 4096 ? 512 : 1024;
+}
+int groups_of(int D, bool back) { return lanes_of(D, back) >= 256 ? 1 : 256 / lanes_of(D, back); }
 
 // Rows of each head are dealt to `slots` groups: `groups` in all if there are so many rows, `least` rows each; a multiple of the groups of a
 // work-group where a work-group stays with one head
-int slots_for(const NormParams &p, int least, long long groups) {
-    const long long rows = (long long)p.B * p.T, most = (rows + least - 1) / least, of_group = groups_of(p.D);
+int slots_for(const NormParams &p, int least, long long groups, bool back) {
+    const long long rows = (long long)p.B * p.T, most = (rows + least - 1) / least, of_group = groups_of(p.D, back);
     long long slots = groups / p.H;
     if (slots > most) slots = most;
     if (slots < 1) slots = 1;
@@ -332,6 +367,11 @@ hipError_t norm(const NormParams &p, hipStream_t stream) {
 
 template <typename E, bool BACK>
 hipError_t norm_of_width(const NormParams &p, hipStream_t stream) {
+    if (p.D <= 32) return norm<E, 4, 1, BACK>(p, stream);
+    if (p.D <= 64) return norm<E, 8, 1, BACK>(p, stream);
+    if constexpr (!BACK) {
+        if (p.D <= 96) return norm<E, 4, 3, BACK>(p, stream);
+    }
     if (p.D <= 128) return norm<E, 16, 1, BACK>(p, stream);
     if (p.D <= 512) return norm<E, 64, 1, BACK>(p, stream);
     if (p.D <= 1024) return norm<E, 64, 2, BACK>(p, stream);
@@ -352,13 +392,13 @@ int norm_slots(int B, int H, int T, int D, int layout) {
     p.layout = layout;
     // 4096 waves (2048 where a lane holds two pieces of a row and more): with twice as many 16384 rows of 1152 took 63 us both ways, 57 with
     // these, 2000 of 8192 69 and 58; with half as many 16384 rows of 384 took 33, 29 with these
-    return slots_for(p, 1, (long long)(D > 512 && D <= 1536 ? 2048 : 4096) * 64 / lanes_of(D));
+    return slots_for(p, 1, (long long)(D > 512 && D <= 1536 ? 2048 : 4096) * 64 / lanes_of(D, true), true);
 }
 
 hipError_t launch_norm_fwd(const NormParams &p0, int dtype, hipStream_t stream) {
     NormParams p = p0;
     // two rows a group at least, if that leaves a thousand groups: it holds the weights (4096 rows of 1152: 9.9 us with one, 8.7 with two)
-    p.slots = slots_for(p, (long long)p.B * p.T * p.H < 2048 ? 1 : 2, 2048LL * groups_of(p.D));
+    p.slots = slots_for(p, (long long)p.B * p.T * p.H < 2048 ? 1 : 2, 2048LL * groups_of(p.D, false), false);
     return dtype == GLA_DT_BF16 ? norm_of_width<uint16_t, false>(p, stream) : norm_of_width<float, false>(p, stream);
 }
 
@@ -368,7 +408,7 @@ hipError_t launch_norm_bwd(const NormParams &p0, int dtype, float *dweight, floa
     if (e != hipSuccess || dweight == nullptr) return e;
     const int cols = p.H * p.D;
     hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)((cols + 15) / 16), 2), dim3(1024), 0, stream, p.part, dweight, dbias,
-                       partial_rows(p, groups_of(p.D)), cols);
+                       partial_rows(p, groups_of(p.D, true)), cols);
     return hipGetLastError();
 }
 
