@@ -70,12 +70,13 @@ __device__ inline int state_row(int t, int g, int r) {
 // How a tile's rows are read: along them (the row is an operand's other index), across them (the contracted one), or both
 enum Reads { kAlong, kAcross, kBoth };
 
-// A tile of C rows of W elements in LDS.  Rows lie so far apart that the 64 banks are met evenly: 16 rows' same piece when read along, 8
-// rows' 32 bytes (bf16) or 4 rows' 64 (fp32) when read across; only reads along a bf16 tile for both meet a bank twice.  (With rows 16
-// bytes apart throughout, near half of the time that LDS was busy went to conflicts.  An exchange of pieces by the row's number is free
-// of them everywhere, but no read's address is then a constant from another's, which cost more instructions than it saved.)
-// A bf16 tile for both holds each 32 columns in the order in which state_row() counts a state's rows: elements 16 h + 4 c and on are columns
-// 8 c + 4 h and on.
+// A tile of C rows of W elements in LDS.  Rows lie so far apart that the banks are met evenly: 16 rows' same piece when read along, 8 rows' 32
+// bytes (bf16) or 4 rows' 64 (fp32) when read across.  (With rows 16 bytes apart throughout, near half of the time that LDS was busy
+// went to conflicts.  An exchange of pieces by the row's number is free of them, but then no read's address is a constant from
+// another's: 6 % more instructions.)
+// A bf16 tile for both holds each 32 columns in the order in which state_row() counts a state's rows: the 8 bytes number 4 h + c are columns
+// 8 c + 4 h and on.  The four c are exchanged by the row's number over four (xor), which reads across see as a constant of the lane,
+// and without which reads along met each bank four times (2.9e7 cycles of conflicts in the walk of 65536 steps of 16 heads, 1.0e7 with it).
 template <typename E, int W, Reads R>
 struct Tile {
     static constexpr int C = Elem<E>::kChunk;
@@ -128,7 +129,7 @@ struct Tile {
     }
 };
 
-// x0, x1 -> packed bf16 pair of the rounded values and packed pair of the remainders.  A remainder x - head is one dot product of
+// x0, x1 -> packed bf16 pair of the rounded values and packed pairs of the remainders.  A remainder x - head is one dot product of
 // the packed heads with (-1, 0) or (0, -1) added to x (exact), where taking a head out of the pair and subtracting it are two.
 struct Heads {
     bf16x2 first, second;

@@ -37,7 +37,7 @@ void plan_spans(DecayCall &c, long long groups) {
     c.nspans = (units + each - 1) / each;
 }
 
-// What a call keeps in the workspace, in floats from its start
+// Cuts a workspace into a call's arrays; without one (null) it only counts
 struct Room {
     size_t used = 0;
     char *base;

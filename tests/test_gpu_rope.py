@@ -26,8 +26,10 @@ def _need_gpu():
 
 def grid_positions(T, gh, gw, axes):
     n = np.arange(T)
-    p = {1: [n], 2: [n // gw, n % gw], 3: [n // (gh * gw), n % (gh * gw) // gw, n % gw]}[axes]
-    return np.stack(p, -1)
+    if axes == 1:
+        return n[:, None]
+    cell = [n % (gh * gw) // gw, n % gw]
+    return np.stack(cell if axes == 2 else [n // (gh * gw)] + cell, -1)
 
 
 def check(B, H, T, d, sections, dtype, layout, pairing, inverse, gh=0, gw=0, positions=None, base=10000.0, seed=0, with_k=True, in_place=False):
