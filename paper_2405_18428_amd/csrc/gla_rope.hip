@@ -110,27 +110,43 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeParams p) {
         if (p.x[t] == nullptr) continue;
         const char *x = static_cast<const char *>(p.x[t]) + row;
         char *y = static_cast<char *>(p.y[t]) + row;
-        for (int h = h0; h < h1; ++h) {
-            const long long a0 = h * head + c0 * (int)sizeof(E), a1 = h * head + c1 * (int)sizeof(E);
-            if constexpr (VP == 4) {
-                const f32x4 u = load4<E>(x + a0), v = load4<E>(x + a1);
-                f32x4 s, w;
-                if (p.adjacent) {
-                    s = f32x4{u[0] * cs[0] - u[1] * sn[0], u[1] * cs[0] + u[0] * sn[0], u[2] * cs[1] - u[3] * sn[1], u[3] * cs[1] + u[2] * sn[1]};
-                    w = f32x4{v[0] * cs[2] - v[1] * sn[2], v[1] * cs[2] + v[0] * sn[2], v[2] * cs[3] - v[3] * sn[3], v[3] * cs[3] + v[2] * sn[3]};
-                } else {
+        const long long a0 = c0 * (int)sizeof(E), a1 = c1 * (int)sizeof(E);
+        if constexpr (VP == 4) {
+            // two heads at once, whose loads come before the first store (a video's 46665 tokens of 16 heads of 128: 165 us, one at a time 176, four 171)
+            constexpr int kAtOnce = 2;
+            for (int h = h0; h < h1; h += kAtOnce) {
+                f32x4 u[kAtOnce], v[kAtOnce];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        s[j] = u[j] * cs[j] - v[j] * sn[j];
-                        w[j] = v[j] * cs[j] + u[j] * sn[j];
-                    }
+                for (int k = 0; k < kAtOnce; ++k) {
+                    if (h + k >= h1) continue;
+                    u[k] = load4<E>(x + (h + k) * head + a0);
+                    v[k] = load4<E>(x + (h + k) * head + a1);
                 }
-                store4<E>(y + a0, s);
-                store4<E>(y + a1, w);
-            } else {
-                const float u = load1<E>(x + a0), v = load1<E>(x + a1);
-                store1<E>(y + a0, u * cs[0] - v * sn[0]);
-                store1<E>(y + a1, v * cs[0] + u * sn[0]);
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) {
+                    if (h + k >= h1) continue;
+                    f32x4 s, w;
+                    if (p.adjacent) {
+                        s = f32x4{u[k][0] * cs[0] - u[k][1] * sn[0], u[k][1] * cs[0] + u[k][0] * sn[0], u[k][2] * cs[1] - u[k][3] * sn[1],
+                                  u[k][3] * cs[1] + u[k][2] * sn[1]};
+                        w = f32x4{v[k][0] * cs[2] - v[k][1] * sn[2], v[k][1] * cs[2] + v[k][0] * sn[2], v[k][2] * cs[3] - v[k][3] * sn[3],
+                                  v[k][3] * cs[3] + v[k][2] * sn[3]};
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            s[j] = u[k][j] * cs[j] - v[k][j] * sn[j];
+                            w[j] = v[k][j] * cs[j] + u[k][j] * sn[j];
+                        }
+                    }
+                    store4<E>(y + (h + k) * head + a0, s);
+                    store4<E>(y + (h + k) * head + a1, w);
+                }
+            }
+        } else {
+            for (int h = h0; h < h1; ++h) {
+                const float u = load1<E>(x + h * head + a0), v = load1<E>(x + h * head + a1);
+                store1<E>(y + h * head + a0, u * cs[0] - v * sn[0]);
+                store1<E>(y + h * head + a1, v * cs[0] + u * sn[0]);
             }
         }
     }
