@@ -362,7 +362,7 @@ def test_call_on_a_given_stream():
 @pytest.mark.parametrize("scan", [2, 3])
 def test_large_grids_in_columns(scan):
     """A column's rows lie all over a grid in token order: offsets near and past what the views with 32-bit offsets reach."""
-    for H, gh, gw in ((40, 64, 64), (3000, 40, 50)):
+    for H, gh, gw in ((40, 64, 64), (3000, 40, 50), (3000, 50, 60)):
         T, d = gh * gw, 64
         q, k, v = (torch.zeros(1, T, H, d, dtype=F32, device=DEV) for _ in range(3))
         gen = torch.Generator(device=DEV).manual_seed(scan)
@@ -389,3 +389,34 @@ def test_gate_gradient_of_short_memories_bf16(T, dk, dv):
     dg = gla.gla_decay_bwd(d["q"], d["k"], d["v"], d["g"], d["do"], 1, T)[3]
     flows = np.sqrt((a["dg"] ** 2).sum()) * 2.0 ** -24 * 8
     assert abs(float(dg[0]) - r["dg"].sum()) <= flows, (float(dg[0]), r["dg"].sum(), flows)
+
+
+def test_many_heads_in_token_order():
+    """Tokens farther apart than the views' factors of 24 bits."""
+    H, T, d = 66000, 70, 64
+    q, k, v = (torch.zeros(1, T, H, d, dtype=F32, device=DEV) for _ in range(3))
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    for t in (q, k, v):
+        t[0, :, H - 1] = torch.randn(T, d, generator=gen, device=DEV) * 0.3
+    g = torch.full((H,), -0.1, device=DEV)
+    out, _ = gla.gla_decay_fwd(q, k, v, g, 1, T, layout=1, want_final_state=False)
+    rows = [t[0, :, H - 1].double().cpu().numpy()[None] for t in (q, k, v)]
+    o, _ = oo.decay_fwd(*rows, np.full((1, T), float(g[0])), np.zeros((1, d, d)))
+    oa, _ = oo.decay_fwd(*(np.abs(x) for x in rows), np.full((1, T), float(g[0])), np.zeros((1, d, d)))
+    close(out[0, :, H - 1][None], o, oa, TOL[F32], ROUND[F32], "out")
+    assert float(out[0, :, :H - 1].abs().max()) == 0.0
+
+
+@pytest.mark.parametrize("scan", [0, 1])
+def test_many_padded_sequences_in_one_span(scan):
+    lens = [(37 * b) % 400 if b else 0 for b in range(40)]
+    lens[7] = 399
+    check(make(40, 8, 399, 12, 20, BF16, 1, "head", lens=lens, seed=13), 1, 399, scan)
+    check(make(40, 8, 399, 12, 20, F32, 0, "token", lens=lens, seed=14), 1, 399, scan)
+
+
+@pytest.mark.parametrize("dk,dv", [(36, 72), (64, 128), (128, 128), (7, 100)])
+def test_one_decay_a_head_from_bf16(dk, dv):
+    """The backward pass with three bf16 numbers a factor: states in several spans, both orders, padded."""
+    check(make(2, 2, 900, dk, dv, BF16, 0, "head", seed=15), 30, 30, 3)
+    check(make(3, 2, 700, dk, dv, BF16, 1, "head", lens=[700, 0, 333], seed=16), 1, 700, 1, out_dtype=BF16)
