@@ -467,7 +467,8 @@ int gla_fwd_fused_gates(const void *q, const void *k, const void *v, const void 
  *
  * bf16 calls run on bf16 MFMA with every factor that is not an input carried as two bf16 numbers, fp32 calls on fp32
  * MFMA.  Gates have no lower limit.  Inputs of visited rows have to be finite.  T is at most 2^30.  Tuning options have no effect.
- * Never allocates; nothing is kept between calls.
+ * Never allocates; nothing is kept between calls.  Calls that may overlap, captured ones among them, need workspaces of
+ * their own.
  */
 typedef enum { GLA_DECAY_HEAD = 0, GLA_DECAY_TOKEN = 1 } gla_decay_kind;
 int gla_decay_fwd(const void *q, const void *k, const void *v, const float *log_decay, int decay_kind, const int *seq_lens,
