@@ -13,7 +13,9 @@
 //   gate of step t + 1,  dv_t = k_t G_t  that of (k, q, dO) and  dk_t = G_t v_t^T  that of (v, dO, q).
 // What a log_decay changes is what flows from the state before step t into all that comes after,
 //   dL/dlog a_t = <a_t S_{t-1}, G_t> = sum over s >= t of (q_s dq_s - k_s dk_s) + <S_T, dS_T> .
-// The sum's terms cancel to a small rest when it runs far, so it runs to the end of a block of kFlowBlock steps only, and
+// Both dot products hold the step's own (q_s k_s)(v_s dO_s), which no gate scales: it is left out of both (dq_s - (v_s dO_s) k_s in place of
+// dq_s, dk_s - (v_s dO_s) q_s in place of dk_s), as what its rounding left would bury the gradients of strong gates, which vanish
+// with a_t.  The sum's terms cancel to a small rest when it runs far, so it runs to the end of a block of kFlowBlock steps only, and
 // what flows across the block's end is the product of the state and the adjoint state there.
 #pragma once
 #include "gla_common.h"

@@ -11,7 +11,7 @@ template <typename E, int M, int N>
 struct WalkLds {
     static constexpr int kRowsM = Tile<E, M, kBoth>::kBytes, kRowsN = Tile<E, N, kAcross>::kBytes, kX = 0, kY = Tile<E, M, kAlong>::kBytes, kZ = kY + kRowsM,
                          kP = kZ + kRowsN, kG = kP + Pairs<E>::kBytes, kFlow = kG + 2 * (int)sizeof(Gates<Elem<E>::kChunk>),
-                         kBytes = kFlow + 2 * 4 * Elem<E>::kChunk * 4;
+                         kDiag = kFlow + 2 * 4 * Elem<E>::kChunk * 4, kBytes = kDiag + Elem<E>::kChunk * 4;
 };
 
 // GRAD: the walk for dq, with the dot products and the states that the gates' gradient takes
@@ -25,7 +25,7 @@ __global__ __launch_bounds__(kThreads, 2) void decay_walk_kernel(const DecayWalk
     const Tile<E, N, kAcross> tz{lds + L::kZ};
     const Pairs<E> P{lds + L::kP};
     Gates<C> *gates = reinterpret_cast<Gates<C> *>(lds + L::kG);
-    float *flow_part = reinterpret_cast<float *>(lds + L::kFlow);
+    float *flow_part = reinterpret_cast<float *>(lds + L::kFlow), *diag = reinterpret_cast<float *>(lds + L::kDiag);
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int bh = blockIdx.x / p.c.nspans, sp = blockIdx.x - bh * p.c.nspans;
@@ -76,15 +76,18 @@ __global__ __launch_bounds__(kThreads, 2) void decay_walk_kernel(const DecayWalk
         if (e < end) issue(e);
         if (dots && s > s0) put_flow(s - C, C, turn ^ 1);
         __builtin_amdgcn_s_setprio(1);                   // before the other work-group's loads and stores (3 % less time)
-        wk.pairs(tx, ty, P, gt);
+        wk.pairs(tx, ty, P, gt, dots, diag);
         wk.from_state(tx, gt);
         wk.update(ty, tz, gt, zf);
         __builtin_amdgcn_s_setprio(0);
         __syncthreads();
         wk.finish(P, zf);
+        if (dots) {                                      // the diagonal has no part in the dot products (gla_decay.h)
+            wk.dot_rows(d, flow_part + 4 * C * turn);
+            wk.add_diagonal(diag, zf);
+        }
         const Steps st = ord.steps(s, count, false);
         wk.store_rows(ro, p.out_dtype, st);
-        if (dots) wk.dot_rows(d, flow_part + 4 * C * turn);
         if (e < end) bring(turn ^ 1);
         if (GRAD && p.anchors != nullptr && (e < len ? e % kFlowBlock == 0 : p.anchor_last != 0))
             wk.store_state(p.anchors + ((size_t)bh * decay_blocks(p.c.T) + (e - 1) / kFlowBlock) * cells, m, n, p.state_t);

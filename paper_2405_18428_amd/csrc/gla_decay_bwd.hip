@@ -14,7 +14,8 @@ template <typename E, int K, int V>
 struct BackLds {
     static constexpr int kRowsV = Tile<E, V, kBoth>::kBytes, kQ = 0, kK = Tile<E, K, kBoth>::kBytes, kV = kK + Tile<E, K, kAlong>::kBytes,
                          kD = kV + Tile<E, V, kAlong>::kBytes, kPa = kD + kRowsV, kPb = kPa + Pairs<E>::kBytes, kG = kPb + Pairs<E>::kBytes,
-                         kFlow = kG + 2 * (int)sizeof(Gates<Elem<E>::kChunk>), kMeet = kFlow + 2 * 4 * Elem<E>::kChunk * 4, kBytes = kMeet + 16;
+                         kFlow = kG + 2 * (int)sizeof(Gates<Elem<E>::kChunk>), kDiag = kFlow + 2 * 4 * Elem<E>::kChunk * 4,
+                         kMeet = kDiag + Elem<E>::kChunk * 4, kBytes = kMeet + 16;
 };
 
 // ROLE 0: dv, ROLE 1: dk
@@ -28,7 +29,8 @@ __device__ __forceinline__ void walk_back(const DecayBack &p, char *lds) {
     const Tile<E, V, kBoth> td{lds + L::kD};
     const Pairs<E> P{lds + (ROLE == 0 ? L::kPa : L::kPb)};
     Gates<C> *gates = reinterpret_cast<Gates<C> *>(lds + L::kG);
-    float *flow_part = reinterpret_cast<float *>(lds + L::kFlow), *meet_part = reinterpret_cast<float *>(lds + L::kMeet);
+    float *flow_part = reinterpret_cast<float *>(lds + L::kFlow), *diag = reinterpret_cast<float *>(lds + L::kDiag),
+          *meet_part = reinterpret_cast<float *>(lds + L::kMeet);
 
     const int tid = threadIdx.x;
     const int bh = blockIdx.x / p.c.nspans, sp = blockIdx.x - bh * p.c.nspans;
@@ -95,7 +97,7 @@ __device__ __forceinline__ void walk_back(const DecayBack &p, char *lds) {
             wk.from_state(tk, gt);
             wk.update(tq, td, gt, zf);
         } else {
-            wk.pairs(tv, td, P, gt);
+            wk.pairs(tv, td, P, gt, flows, diag);
             wk.from_state(tv, gt);
             wk.update(td, tq, gt, zf);
             if (flows) wk.fetch_dots(d, tk);
@@ -103,8 +105,11 @@ __device__ __forceinline__ void walk_back(const DecayBack &p, char *lds) {
         __syncthreads();
         if (meets && tid == 256) p.meet[block] = (meet_part[0] + meet_part[1]) + (meet_part[2] + meet_part[3]);
         wk.finish(P, zf);
+        if (flows) {                                     // the diagonal has no part in the dot products (gla_decay.h)
+            wk.dot_rows(d, flow_part + 4 * C * (ci & 1));
+            wk.add_diagonal(diag, zf);
+        }
         wk.store_rows(ro, p.grad_dtype, ord.steps(s, count, true));
-        if (flows) wk.dot_rows(d, flow_part + 4 * C * (ci & 1));
         if (ci > 0) bring((ci - 1) & 1);
     }
     if (chunks > 0) {
@@ -149,7 +154,9 @@ __global__ __launch_bounds__(kFlowBlock) void decay_gate_kernel(const DecayGate 
         sum[t] += y;
         __syncthreads();
     }
-    const double flow = s < len ? sum[t] + across : 0.0;
+    // (what a gate that lets nothing through adds up to is rounding)
+    const bool open = s < len && exp2_fast(fmaxf(gate_of(p.c, ord, bh, s) * kLog2e, -65536.f)) != 0.f;
+    const double flow = open ? sum[t] + across : 0.0;
     if (p.c.kind == kDecayToken) {
         if (s < p.c.T) {
             const int h = bh % p.c.H;

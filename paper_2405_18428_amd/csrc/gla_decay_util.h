@@ -492,8 +492,9 @@ struct Walker {
     }
 
     // (1) P^T of the lower triangle, whose tiles are dealt to the waves in turn.  Products that add to one accumulator are kept apart, here and
-    // below: each would wait for the one before.
-    __device__ __forceinline__ void pairs(const Tile<E, M, kAlong> &x, const Tile<E, M, kBoth> &y, const Pairs<E> &P, const Gates<C> &gt) const {
+    // below: each would wait for the one before.  With `diag` the diagonal goes there instead of into P, for add_diagonal().
+    __device__ __forceinline__ void pairs(const Tile<E, M, kAlong> &x, const Tile<E, M, kBoth> &y, const Pairs<E> &P, const Gates<C> &gt,
+                                          bool apart = false, float *diag = nullptr) const {
         constexpr int kTiles = kI * (kI + 1) / 2, kMine = (kTiles + 3) / 4;
         const Heads heads;
 #pragma unroll
@@ -518,6 +519,15 @@ struct Walker {
                 const f32x4 wj = *reinterpret_cast<const f32x4 *>(&gt.whole[j0]), rj = *reinterpret_cast<const f32x4 *>(&gt.rest[j0]);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) p[r] = g * 4 + r <= lm ? acc[r] * exp2_fast((wi - wj[r]) + (ri - rj[r])) : 0.f;
+                if (apart) {
+                    const auto [lm, g] = fresh();
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (g * 4 + r == lm) {
+                            diag[i] = acc[r];
+                            p[r] = 0.f;
+                        }
+                }
             } else {                                     // by way of the last step of j's tile
                 const float e = exp2_fast((wi - gt.whole[jt * 16 + 15]) + (ri - gt.rest[jt * 16 + 15]));
                 p = acc * (*reinterpret_cast<const f32x4 *>(&gt.tile[j0]) * e);
@@ -653,6 +663,32 @@ struct Walker {
 #pragma unroll
                     for (int c = 0; c < kCols; ++c) O[c][it] = product<E>(zf[jk][c], b, O[c][it]);
                 }
+    }
+    // out^T += z^T diag, where pairs() left the diagonal apart: a product of each tile with an operand that is the diagonal and zeros
+    __device__ __forceinline__ void add_diagonal(const float *diag, const u32x4 (&zf)[kJ][kCols]) {
+        const Heads heads;
+        const auto [lm, g] = fresh();
+#pragma unroll
+        for (int it = 0; it < kI; ++it) {
+            const float d = g == lm >> 2 ? diag[it * 16 + lm] : 0.f;
+            if constexpr (sizeof(E) == 2) {
+                uint32_t s[kParts];
+                heads.split(lm & 1 ? 0.f : d, lm & 1 ? d : 0.f, s);
+#pragma unroll
+                for (int q = 0; q < kParts; ++q) {
+                    const uint32_t lo = lm & 2 ? 0u : s[q], hi = lm & 2 ? s[q] : 0u;
+                    const u32x4 b = it & 1 ? u32x4{0u, 0u, lo, hi} : u32x4{lo, hi, 0u, 0u};
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c) O[c][it] = product<E>(zf[it >> 1][c], b, O[c][it]);
+                }
+            } else {
+                f32x4 b;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) b[r] = (lm & 3) == r ? d : 0.f;
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) O[c][it] = product<E>(zf[it][c], __builtin_bit_cast(u32x4, b), O[c][it]);
+            }
+        }
     }
     // The rows that the outputs are multiplied with: this lane's four columns of each tile, from memory or from the tile
     struct Dots {
