@@ -466,7 +466,8 @@ int gla_fwd_fused_gates(const void *q, const void *k, const void *v, const void 
  *                  may be NULL)
  *
  * bf16 calls run on bf16 MFMA with every factor that is not an input carried as two bf16 numbers, fp32 calls on fp32
- * MFMA.  Gates have no lower limit.  Inputs of visited rows have to be finite.  T is at most 2^30.  Tuning options have no effect.
+ * MFMA.  Gates have no lower limit; one that is NaN makes NaN of
+ * all that it has a part in.  Inputs of visited rows have to be finite.  T is at most 2^30.  Tuning options have no effect.
  * Never allocates; nothing is kept between calls.  Calls that may overlap, captured ones among them, need workspaces of
  * their own.
  */

@@ -260,7 +260,7 @@ __global__ __launch_bounds__(kThreads) void decay_step_kernel(const void *q, con
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         if (col + j < dv) x[j] = element<E>(v, (size_t)bh * dv + col + j);
-    const float a = exp2_fast(fmaxf(log_decay[kind == kDecayHead ? h : bh] * kLog2e, -65536.f));
+    const float a = exp2_fast(gate_log2(log_decay[kind == kDecayHead ? h : bh]));
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kStepTimes; ++i) {

@@ -117,8 +117,7 @@ __device__ __forceinline__ void walk_back(const DecayBack &p, char *lds) {
         if (flows) put_flow(s0, min(s0 + C, end), 0);
     }
     if (ROLE == 0 && p.d_initial != nullptr && sp == 0)
-        wk.store_state(p.d_initial + (size_t)bh * cells, m, n, false,
-                       exp2_fast(fmaxf(gate_of(p.c, ord, bh, 0) * kLog2e, -65536.f)));
+        wk.store_state(p.d_initial + (size_t)bh * cells, m, n, false, exp2_fast(gate_log2(gate_of(p.c, ord, bh, 0))));
     clear_behind<256>(ro, p.grad_dtype == GLA_DT_BF16 ? 2 : 4, len, s0, s1, tid & 255);
 }
 
@@ -143,7 +142,7 @@ __global__ __launch_bounds__(kFlowBlock) void decay_gate_kernel(const DecayGate 
     // across the block's end: the adjoint state behind it decays once more on its way to the state before it
     double across = 0.0;
     if (k * kFlowBlock < len) {
-        if (e < len) across = (double)p.meet[blockIdx.x] * (double)exp2_fast(fmaxf(gate_of(p.c, ord, bh, e) * kLog2e, -65536.f));
+        if (e < len) across = (double)p.meet[blockIdx.x] * (double)exp2_fast(gate_log2(gate_of(p.c, ord, bh, e)));
         else if (p.anchor_last) across = (double)p.meet[blockIdx.x];
     }
     sum[t] = x;
@@ -155,7 +154,7 @@ __global__ __launch_bounds__(kFlowBlock) void decay_gate_kernel(const DecayGate 
         __syncthreads();
     }
     // (what a gate that lets nothing through adds up to is rounding)
-    const bool open = s < len && exp2_fast(fmaxf(gate_of(p.c, ord, bh, s) * kLog2e, -65536.f)) != 0.f;
+    const bool open = s < len && exp2_fast(gate_log2(gate_of(p.c, ord, bh, s))) != 0.f;
     const double flow = open ? sum[t] + across : 0.0;
     if (p.c.kind == kDecayToken) {
         if (s < p.c.T) {

@@ -313,6 +313,12 @@ struct Pieces {
     }
 };
 
+// A gate, base 2.  One of exactly zero (-inf) has to stay a number: 2^-1024 is zero too, and 64 of them are 2^23 units of 2^-7; a NaN stays one.
+__device__ __forceinline__ float gate_log2(float log_decay) {
+    const float g = log_decay * kLog2e;
+    return g < -1024.f ? -1024.f : g;
+}
+
 // What a chunk needs of the gates.  A sum of gates b (base 2) is held as a number of units of 2^-7 (`whole`) and a rest, so that differences of
 // near steps keep their digits whatever lies before them: sums of units are exact, and sums of 64 rests stay below 1/4.  (With units
 // of 1 the rests of gates of -0.2 added up to 18, and exp(b_i - b_j) was off by 16 * 2^-24; by 2^-25 of its own with these.)
@@ -329,8 +335,7 @@ struct Gates {
 // One wave forms them: lane i brings gate i (natural log; 0 where there is no step)
 template <int C>
 __device__ inline void form_gates(Gates<C> &s, float gate, int lane) {
-    // a gate of exactly zero (-inf) has to stay a number: 2^-1024 is one too, and 64 of them are 2^23 units
-    const float g2 = fmaxf(gate * kLog2e, -1024.f);
+    const float g2 = gate_log2(gate);
     float whole = __builtin_rintf(g2 * 128.f) * 0.0078125f, rest = g2 - whole;
     whole = wave_inclusive_scan(whole);
     rest = wave_inclusive_scan(rest);

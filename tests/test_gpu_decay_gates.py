@@ -155,3 +155,52 @@ def test_weights_of_a_chunk(gate):
     want = np.where(i >= j, np.exp(float(np.float32(gate)) * (i - j)), 0.0)
     worst = np.abs(out.double().cpu().numpy()[0, :, :, 0] - want).max() * 2.0 ** 24
     assert worst <= 4, worst
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("gate", ["head", "token"])
+@pytest.mark.parametrize("scan", [0, 1])
+def test_nan_gate(scan, gate, dtype):
+    """A gate that is NaN reaches all that depends on it, and nothing else: states and outputs from its step on, gradients of keys and values before
+    it, the gates' gradient; other heads and what lies on the other side have the bits of a call without it."""
+    n, t = 600, 300
+    c = make(2, 3, n, 24, 40, dtype, 0, gate, seed=30)
+    at = 299 if scan else t                 # token of step 300
+    d = {m: x.to(DEV) for m, x in c.items()}
+
+    def call(g):
+        x = d["q"], d["k"], d["v"], g
+        return [*gla.gla_decay_fwd(*x, 1, n, scan, initial_state=d["s0"]),
+                *gla.gla_decay_bwd(*x, d["do"], 1, n, scan, initial_state=d["s0"], d_final_state=d["ds"], want_d_initial_state=True)]
+    want = call(d["g"])
+    g = d["g"].clone()
+    (g[1:2] if gate == "head" else g[0, 1, at:at + 1]).fill_(float("nan"))
+    got = call(g)
+    torch.cuda.synchronize()
+    steps = torch.arange(n, device=DEV)
+    steps = n - 1 - steps if scan else steps
+    after = steps >= t if gate == "token" else steps >= 0
+    before = steps < t if gate == "token" else steps < n - 1        # (a head's gate leads from every step to the next)
+    for name, x, y in zip(("out", "state", "dq", "dk", "dv", "dg", "ds0"), got, want):
+        assert torch.isfinite(y).all(), name
+        hit = torch.zeros_like(y, dtype=torch.bool)
+        if name == "dg" and gate == "head":
+            hit[1] = True
+        else:
+            which = hit[:, 1] if gate == "head" else hit[:1, 1]
+            which[:, {"out": after, "dq": after, "dk": before, "dv": before}[name] if name in ("out", "dq", "dk", "dv") else slice(None)] = True
+        assert torch.isnan(x[hit]).all() and torch.equal(x[~hit], y[~hit]), name
+
+
+@pytest.mark.parametrize("gate", ["head", "token"])
+def test_nan_gate_of_a_step(gate):
+    q, k, v = (torch.randn(2, 3, w, device=DEV) for w in (24, 24, 40))
+    g = torch.full((3,) if gate == "head" else (2, 3), -0.5, device=DEV)
+    s = torch.randn(2, 3, 24, 40, device=DEV)
+    want, state = gla.gla_decay_step(q, k, v, g, s, state_out=torch.empty_like(s))
+    (g[1:2] if gate == "head" else g[0, 1:2]).fill_(float("nan"))
+    got, new = gla.gla_decay_step(q, k, v, g, s, state_out=torch.empty_like(s))
+    hit = torch.zeros(2, 3, dtype=torch.bool, device=DEV)
+    hit[slice(None) if gate == "head" else 0, 1] = True
+    for x, y in ((got, want), (new, state)):
+        assert torch.isnan(x[hit]).all() and torch.equal(x[~hit], y[~hit])
