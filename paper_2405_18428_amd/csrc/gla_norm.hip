@@ -315,24 +315,28 @@ __global__ __launch_bounds__(Shape<LANES>::kThreads) void norm_kernel(const Norm
     }
 }
 
-// Adds the partial sums: 16 columns and 64 rows at a time a work-group
+// Adds the partial sums: 16 columns and 64 rows at a time a work-group, which goes on to further columns where there are more than work-groups
+// (of 2^32 threads, a launch's limit, 2^26 columns would need them all)
+constexpr int kMostSums = 1 << 20;
 __global__ __launch_bounds__(1024) void norm_sum_kernel(const float *part, float *dweight, float *dbias, int rows, int cols) {
     __shared__ float s[64][17];
     const int c = threadIdx.x & 15, k = threadIdx.x >> 4;
-    const int col = blockIdx.x * 16 + c;
     const float *src = part + (blockIdx.y ? (size_t)rows * cols : 0);
-    float x = 0.f;
-    if (col < cols) {
+    for (int col0 = blockIdx.x * 16; col0 < cols; col0 += gridDim.x * 16) {
+        const int col = col0 + c;
+        float x = 0.f;
+        if (col < cols) {
 #pragma unroll 8
-        for (int i = k; i < rows; i += 64) x += src[(size_t)i * cols + col];
-    }
-    s[k][c] = x;
-    __syncthreads();
-    for (int d = 32; d > 0; d /= 2) {
-        if (k < d) s[k][c] += s[k + d][c];
+            for (int i = k; i < rows; i += 64) x += src[(size_t)i * cols + col];
+        }
+        s[k][c] = x;
         __syncthreads();
+        for (int d = 32; d > 0; d /= 2) {
+            if (k < d) s[k][c] += s[k + d][c];
+            __syncthreads();
+        }
+        if (k == 0 && col < cols) (blockIdx.y ? dbias : dweight)[col] = s[0][c];
     }
-    if (k == 0 && col < cols) (blockIdx.y ? dbias : dweight)[col] = s[0][c];
 }
 
 // lanes of a row's group: as few as hold it (16 for rows of 64 took 37 us forward where 8 take 21, 4 x 16 x 4096 of them).  Rows of 65 to 96,
@@ -406,8 +410,8 @@ hipError_t launch_norm_bwd(const NormParams &p0, int dtype, float *dweight, floa
     NormParams p = p0;
     const hipError_t e = dtype == GLA_DT_BF16 ? norm_of_width<uint16_t, true>(p, stream) : norm_of_width<float, true>(p, stream);
     if (e != hipSuccess || dweight == nullptr) return e;
-    const int cols = p.H * p.D;
-    hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)((cols + 15) / 16), 2), dim3(1024), 0, stream, p.part, dweight, dbias,
+    const int cols = p.H * p.D, tiles = (cols + 15) / 16;
+    hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)(tiles < kMostSums ? tiles : kMostSums), 2), dim3(1024), 0, stream, p.part, dweight, dbias,
                        partial_rows(p, groups_of(p.D, true)), cols);
     return hipGetLastError();
 }
