@@ -533,7 +533,8 @@ int gla_decay_step(const void *q, const void *k, const void *v, const float *log
  *   inverse     not 0: turned back, which is also the backward pass
  *   out_q, out_k   DEVICE, dtype, like q and k; may be q and k (GLA_ERR_SHAPE: out_q = k, out_k = q or out_q = out_k)  (written)
  *
- * 1 <= d <= 256.  Angles are formed and reduced in 64 bits: every position of 32 bits is as exact as the first.  grid_h, grid_w are
+ * 1 <= d <= 256.  Frequencies restart with every section.  Angles are formed and reduced from frequencies in two 64-bit numbers: with a base of 1 or
+ * more every position of 32 bits is as exact as the first, with less an angle is off by up to 2^-25 / base besides.  grid_h, grid_w are
  * ignored with positions or one axis.  Needs no workspace and never allocates.
  */
 typedef enum { GLA_ROPE_ADJACENT = 0, GLA_ROPE_HALVES = 1 } gla_rope_pairing;

@@ -27,7 +27,8 @@ struct RopeParams {
     const void *x[2];                   // q, k (k may be null)
     void *y[2];
     const int *positions;               // [B, T, axes] or null: from the grid
-    double turns[kRopeMaxD / 2];        // of each pair, full turns a position
+    // of each pair, full turns a position: `turns` has 21 bits, so that its product with a position of 32 is exact, `rest` what is missing
+    double turns[kRopeMaxD / 2], rest[kRopeMaxD / 2];
     int first[kRopeMaxAxes], pairs_end[kRopeMaxAxes], half[kRopeMaxAxes];   // of each section: first channel, pairs up to its end, its pairs
     int axes, pairs, adjacent, inverse;
     int B, H, T, d, grid_h, grid_w, layout;

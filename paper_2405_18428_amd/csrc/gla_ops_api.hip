@@ -1,6 +1,7 @@
 // Host side of the C ABI for linear attention with one decay a head, rotary positions and layer norm: argument checks, span plan,
 // workspaces.
 #include <math.h>
+#include <string.h>
 
 #include "gla_decay.h"
 #include "gla_ops.h"
@@ -320,10 +321,20 @@ int gla_rope(const void *q, const void *k, const int *positions, const int *sect
         if (w < 2 || w % 2 != 0 || w > d - first) return GLA_ERR_SHAPE;
         p.first[a] = first;
         p.half[a] = w / 2;
-        // (one power a section: 64 of them took longer than the kernel of a few tokens; each product is off by 2^-53 more)
-        const double ratio = pow((double)base, -2.0 / w);
-        double turns = 1.0 / (2.0 * M_PI);
-        for (int i = 0; i < w / 2; ++i, turns *= ratio) p.turns[first / 2 + i] = turns;
+        // One power a section: 64 of them took longer than the kernel of a few tokens.  Each product is off by 2^-63 more at most, in 64 bits of
+        // mantissa: 128 pairs by 2^-56, which 2^31 / (2 pi) turns make 2^-25 of an angle (of the first pairs' a position; with a base below 1 the
+        // last pairs turn faster and are off by as much more).
+        const long double ratio = powl((long double)base, -2.0L / w);
+        long double turns = 0.159154943091895335768883763372514362L;     // 1 / (2 pi)
+        for (int i = 0; i < w / 2; ++i, turns *= ratio) {
+            double head = (double)turns;
+            uint64_t bits;
+            memcpy(&bits, &head, sizeof bits);
+            bits &= ~0xffffffffull;
+            memcpy(&head, &bits, sizeof bits);
+            p.turns[first / 2 + i] = head;
+            p.rest[first / 2 + i] = (double)(turns - head);
+        }
         first += w;
         p.pairs_end[a] = first / 2;
     }

@@ -3,8 +3,9 @@
 // position * base^(-2 i / w).
 //
 // A thread turns four neighbouring pairs of a token, for several heads and for queries and keys, by the same sines and cosines: these
-// cost far more than the rotation.  Angles are formed in turns, in 64 bits, and reduced there: in 32 a position of some ten thousand
-// would be off by 1e-3 of a turn, and a sine's own reduction is not needed any more.  Bound by HBM.
+// cost far more than the rotation.  Angles are formed in turns, from a frequency in two 64-bit numbers, and reduced there: in 32 bits a position
+// of some ten thousand would be off by 1e-3 of a turn, with one number of 64 one of 2^31 by 1e-7 and more, and a sine's own reduction is not
+// needed any more.  Bound by HBM.
 #include "gla_ops.h"
 
 namespace gla {
@@ -99,7 +100,8 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeParams p) {
     float cs[VP], sn[VP];
 #pragma unroll
     for (int j = 0; j < VP; ++j) {
-        const double turns = pos * p.turns[pair + j];
+        const double whole = pos * p.turns[pair + j];                    // exact
+        const double turns = __builtin_fma(pos, p.rest[pair + j], whole - __builtin_rint(whole));
         const float f = (float)(turns - __builtin_rint(turns));          // -1/2 .. 1/2
         sincospif(2.f * f, &sn[j], &cs[j]);
         if (p.inverse) sn[j] = -sn[j];
