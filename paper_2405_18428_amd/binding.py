@@ -227,9 +227,38 @@ def _stream_ptr(stream, t=None) -> int:
     return int(_raw_stream(torch.cuda.current_device() if t is None else t.get_device()))
 
 
+def _elsewhere(stream, t) -> bool:
+    """Whether a call on tensors like t goes to a torch stream that is not the current one (an object that only has a ``cuda_stream`` leaves the
+    tensors' lives to the caller)."""
+    if stream is None or not isinstance(stream, _torch().cuda.Stream):
+        return False
+    if stream.device_index != t.get_device():
+        raise ValueError("stream must be one of the tensors' device")
+    return int(stream.cuda_stream) != int(_raw_stream(stream.device_index))
+
+
+def _call_on(stream, call, args):
+    """call(**args) with the given stream as the current one.  What the call allocates comes from that stream's memory, where nothing of the caller's
+    current stream is still at work; the tensors given are recorded on it and those returned on the caller's, so that their memory is handed
+    on only when both are done with it, whenever the caller drops them."""
+    torch = _torch()
+    given = [t for t in args.values() if isinstance(t, torch.Tensor)]
+    before = torch.cuda.current_stream(stream.device_index)
+    with torch.cuda.stream(stream):
+        result = call(**{**args, "stream": None})
+    for t in given:
+        t.record_stream(stream)
+    for t in result if isinstance(result, tuple) else (result,):
+        if isinstance(t, torch.Tensor):
+            t.record_stream(before)
+    return result
+
+
 def gla_fwd(q, k, v, log_alpha, grid_h, grid_w, scan_dir=SCAN_ROW_FWD,
             want_final_state=True, out=None, final_state=None, stream=None):
     """bf16 q/k/v -> fp32 out (and fp32 final state); library-owned scratch."""
+    if _elsewhere(stream, q):
+        return _call_on(stream, gla_fwd, locals())
     torch = _torch()
     lib = load_library()
     B, H, T, dk, dv = _prep(q, k, v, log_alpha, grid_h, grid_w)
@@ -251,6 +280,8 @@ def gla_fwd_static(q, k, v, log_alpha, grid_h, grid_w, scan_dir=SCAN_ROW_FWD, ou
                    stream=None):
     """gla_fwd with the span states in the library's static device array (no allocation inside the call):
     the caller passes ``out`` (fp32 [B,H,T,dv]) and, if wanted, ``final_state`` (fp32 [B,H,dk,dv])."""
+    if _elsewhere(stream, q):
+        return _call_on(stream, gla_fwd_static, locals())
     torch = _torch()
     lib = load_library()
     B, H, T, dk, dv = _prep(q, k, v, log_alpha, grid_h, grid_w)
@@ -270,6 +301,8 @@ def gla_fwd_ex(q, k, v, log_alpha, grid_h, grid_w, scan_dir=SCAN_ROW_FWD,
                out_dtype=None, want_final_state=True, out=None, final_state=None,
                workspace=None, stream=None):
     """Explicit element types and caller-owned workspace (a uint8 GPU tensor)."""
+    if _elsewhere(stream, q):
+        return _call_on(stream, gla_fwd_ex, locals())
     torch = _torch()
     lib = load_library()
     B, H, T, dk, dv = _prep(q, k, v, log_alpha, grid_h, grid_w)
@@ -295,6 +328,8 @@ def gla_fwd_layout(q, k, v, log_alpha, grid_h, grid_w, scan_dir=SCAN_ROW_FWD, la
                    workspace=None, stream=None):
     """gla_fwd_ex for [B,H,T,d] (LAYOUT_BHTD) or [B,T,H,d] (LAYOUT_BTHD) tensors, starting from
     ``initial_state`` ([B,H,dk,dv] fp32, or None for zero)."""
+    if _elsewhere(stream, q):
+        return _call_on(stream, gla_fwd_layout, locals())
     torch = _torch()
     lib = load_library()
     if layout not in (LAYOUT_BHTD, LAYOUT_BTHD):
@@ -337,6 +372,8 @@ def gla_fwd_gates(q, k, v, log_alpha, log_beta, grid_h, grid_w, scan_dir=SCAN_RO
                   initial_state=None, out_dtype=None, want_final_state=True, out=None, final_state=None,
                   workspace=None, stream=None):
     """The recurrence with the two-sided gate alpha_t^T beta_t; ``log_beta`` is fp32, shaped like v."""
+    if _elsewhere(stream, q):
+        return _call_on(stream, gla_fwd_gates, locals())
     torch = _torch()
     lib = load_library()
     if layout not in (LAYOUT_BHTD, LAYOUT_BTHD):
@@ -377,6 +414,8 @@ def gla_fwd_gates(q, k, v, log_alpha, log_beta, grid_h, grid_w, scan_dir=SCAN_RO
 def gla_srem_dwconv(x, weight, bias, grid_h, grid_w, orient=0, out_dtype=None, out=None, stream=None):
     """3x3 depth-wise convolution of the SREM on tokens x [B, T, D] (canonical order); weight fp32 [D,3,3], bias
     fp32 [D] or None; ``orient`` = the scan order the paper's sequence would be in at this block."""
+    if _elsewhere(stream, x):
+        return _call_on(stream, gla_srem_dwconv, locals())
     torch = _torch()
     lib = load_library()
     if not x.is_cuda or not x.is_contiguous() or x.dim() != 3:
@@ -399,6 +438,8 @@ def gla_srem_dwconv(x, weight, bias, grid_h, grid_w, orient=0, out_dtype=None, o
 def gla_fwd_multi(q, k, v, log_alpha, grid_h, grid_w, scan_dirs=(SCAN_ROW_FWD, SCAN_ROW_REV), out=None,
                   workspace=None, stream=None):
     """Sum over the scan orders in ``scan_dirs`` of the forward outputs (fp32, canonical token order)."""
+    if _elsewhere(stream, q):
+        return _call_on(stream, gla_fwd_multi, locals())
     torch = _torch()
     lib = load_library()
     for name, t in (("q", q), ("k", k), ("v", v), ("log_alpha", log_alpha)):
@@ -434,6 +475,8 @@ def gla_fwd_fused(q, k, v, z_alpha, tau, grid_h, grid_w, scan_dir=SCAN_ROW_FWD, 
     """Forward pass with the gates taken from their pre-activations (``log_alpha = logsigmoid(z_alpha) / tau``) and,
     if ``r_pre`` is given, ``Swish(r_pre) * LayerNorm_head(o)`` stored instead of ``o``.  q, k, v, z_alpha, r_pre
     share one element type; ln_weight / ln_bias are fp32 [H, dv] or None."""
+    if _elsewhere(stream, q):
+        return _call_on(stream, gla_fwd_fused, locals())
     torch = _torch()
     lib = load_library()
     tensors = [("q", q), ("k", k), ("v", v), ("z_alpha", z_alpha)] + ([("r_pre", r_pre)] if r_pre is not None else [])
@@ -489,6 +532,8 @@ def gla_bwd_gates(q, k, v, log_alpha, log_beta, d_out, grid_h, grid_w, scan_dir=
                   workspace=None, stream=None):
     """Gradients of the two-sided-gate recurrence: returns (dq, dk, dv, dlog_alpha, dlog_beta), all fp32.
     ``out_fwd``: the fp32 outputs of gla_fwd_gates on the same inputs, if the caller still holds them."""
+    if _elsewhere(stream, q):
+        return _call_on(stream, gla_bwd_gates, locals())
     torch = _torch()
     lib = load_library()
     for name, t in (("q", q), ("k", k), ("v", v), ("log_alpha", log_alpha), ("log_beta", log_beta), ("d_out", d_out)):
@@ -532,6 +577,8 @@ def gla_bwd_workspace_bytes(B, H, T, dk, dv, qkv_dtype=DT_BF16) -> int:
 def gla_bwd_layout(q, k, v, log_alpha, d_out, grid_h, grid_w, scan_dir=SCAN_ROW_FWD, layout=LAYOUT_BHTD,
                    fwd_workspace=None, workspace=None, stream=None):
     """gla_bwd for [B,H,T,d] (LAYOUT_BHTD) or [B,T,H,d] (LAYOUT_BTHD) tensors; the gradients come in the same order."""
+    if _elsewhere(stream, q):
+        return _call_on(stream, gla_bwd_layout, locals())
     torch = _torch()
     lib = load_library()
     if layout not in (LAYOUT_BHTD, LAYOUT_BTHD):
@@ -570,6 +617,8 @@ def gla_bwd(q, k, v, log_alpha, d_out, grid_h, grid_w, scan_dir=SCAN_ROW_FWD, wo
     q, k, v, d_out share one element type (bf16 or fp32); [B,H,T,d] order.  ``fwd_workspace``: the workspace
     tensor of the gla_fwd_ex call on the same tensors and scan order (untouched since, same options): its span
     states are reused instead of recomputed (gla_bwd_reuse)."""
+    if _elsewhere(stream, q):
+        return _call_on(stream, gla_bwd, locals())
     torch = _torch()
     lib = load_library()
     B, H, T, dk, dv = _prep(q, k, v, log_alpha, grid_h, grid_w)
@@ -607,6 +656,8 @@ def gla_calibrate_mfma(stream=None):
 def gla_fwd_timed(q, k, v, log_alpha, grid_h, grid_w, scan_dir, out, final_state,
                   workspace, iters=10, stream=None):
     """Mean milliseconds per call: [span-state kernel, carry kernel, output kernel, whole call]."""
+    if _elsewhere(stream, q):
+        return _call_on(stream, gla_fwd_timed, locals())
     torch = _torch()
     lib = load_library()
     B, H, T, dk, dv = _prep(q, k, v, log_alpha, grid_h, grid_w)
@@ -632,14 +683,10 @@ def _want(name, t, shape, dtype, gpu):
         raise TypeError(f"{name} must be of element type {dtype}")
 
 
-def _room(nbytes, workspace, q, stream):
-    """The caller's workspace, or one of its size for this call (`nbytes` is asked for in that case only), which the allocator hands
-    on only when the call's stream is done with it."""
+def _room(nbytes, workspace, q):
+    """The caller's workspace, or one of its size for this call (`nbytes` is asked for in that case only)."""
     if workspace is None:
-        workspace = _torch().empty((max(nbytes(), 16),), dtype=_torch().uint8, device=q.device)
-        if stream is not None:
-            workspace.record_stream(stream)
-        return workspace
+        return _torch().empty((max(nbytes(), 16),), dtype=_torch().uint8, device=q.device)
     if workspace.get_device() != q.get_device() or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous GPU tensor on the device of the others")
     return workspace
@@ -682,6 +729,8 @@ def gla_decay_fwd(q, k, v, log_decay, grid_h, grid_w, scan_dir=SCAN_ROW_FWD, lay
     """Linear attention with one decay a head: S_t = exp(log_decay) S_{t-1} + k_t^T v_t, o_t = q_t S_t.  log_decay fp32 [H], or a
     number for each token ([B,H,T] or [B,T,H] by ``layout``).  ``seq_lens`` int32 [B]: each sequence's own length; rows of ``out``
     behind it are left as they were.  Returns (out, final_state)."""
+    if _elsewhere(stream, q):
+        return _call_on(stream, gla_decay_fwd, locals())
     torch = _torch()
     lib = load_library()
     kind, B, H, T, dk, dv = _prep_decay(q, k, v, log_decay, layout, seq_lens,
@@ -693,7 +742,7 @@ def gla_decay_fwd(q, k, v, log_decay, grid_h, grid_w, scan_dir=SCAN_ROW_FWD, lay
     if final_state is None and want_final_state:
         final_state = q.new_empty((B, H, dk, dv), dtype=torch.float32)
     qdt = _dt(q)
-    workspace = _room(lambda: gla_decay_fwd_workspace_bytes(B, H, T, dk, dv, qdt), workspace, q, stream)
+    workspace = _room(lambda: gla_decay_fwd_workspace_bytes(B, H, T, dk, dv, qdt), workspace, q)
     with _on_device_of(q):
         _check(lib.gla_decay_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), kind, _ptr(seq_lens),
                                  B, H, T, dk, dv, grid_h, grid_w, scan_dir, qdt, _dt(out), layout, _ptr(initial_state),
@@ -707,6 +756,8 @@ def gla_decay_bwd(q, k, v, log_decay, d_out, grid_h, grid_w, scan_dir=SCAN_ROW_F
                   workspace=None, stream=None):
     """Gradients of gla_decay_fwd from those of its outputs (``d_out``, like v) and of its final state (``d_final_state`` or None).
     Returns (dq, dk, dv, dlog_decay or None, d_initial_state or None); the first three of ``grad_dtype`` (fp32)."""
+    if _elsewhere(stream, q):
+        return _call_on(stream, gla_decay_bwd, locals())
     torch = _torch()
     lib = load_library()
     kind, B, H, T, dk, dv = _prep_decay(q, k, v, log_decay, layout, seq_lens,
@@ -717,7 +768,7 @@ def gla_decay_bwd(q, k, v, log_decay, d_out, grid_h, grid_w, scan_dir=SCAN_ROW_F
     dg = _like(log_decay, torch.float32) if want_d_log_decay else None
     ds = q.new_empty((B, H, dk, dv), dtype=torch.float32) if want_d_initial_state else None
     qdt = _dt(q)
-    workspace = _room(lambda: gla_decay_bwd_workspace_bytes(B, H, T, dk, dv, qdt), workspace, q, stream)
+    workspace = _room(lambda: gla_decay_bwd_workspace_bytes(B, H, T, dk, dv, qdt), workspace, q)
     with _on_device_of(q):
         _check(lib.gla_decay_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), kind, _ptr(seq_lens),
                                  d_out.data_ptr(), _ptr(initial_state), _ptr(d_final_state), B, H, T, dk, dv, grid_h, grid_w,
@@ -729,6 +780,8 @@ def gla_decay_bwd(q, k, v, log_decay, d_out, grid_h, grid_w, scan_dir=SCAN_ROW_F
 def gla_decay_step(q, k, v, log_decay, state, out_dtype=None, out=None, state_out=None, stream=None):
     """One token of gla_decay_fwd for each sequence: q, k [B,H,dk], v [B,H,dv], log_decay fp32 [H] or [B,H], state fp32 [B,H,dk,dv].
     The new state goes to ``state_out``, in place (``state``) if that is None.  Returns (out, state_out)."""
+    if _elsewhere(stream, q):
+        return _call_on(stream, gla_decay_step, locals())
     torch = _torch()
     lib = load_library()
     if q.dim() != 3 or v.dim() != 3:
@@ -762,6 +815,8 @@ def gla_rope(q, k, sections, grid_h=0, grid_w=0, positions=None, base=10000.0, p
     channels is turned by position * base^(-2 i / w).  ``positions`` int32 [B,T,axes], or None: the token's number, its row and
     column, or its frame, row and column on the grid.  ``inverse`` turns back (the backward pass).  q, k [B,H,T,d] or [B,T,H,d];
     k may be None; ``out_q`` / ``out_k`` may be q / k.  Returns (q', k')."""
+    if _elsewhere(stream, q):
+        return _call_on(stream, gla_rope, locals())
     torch = _torch()
     lib = load_library()
     if layout not in (LAYOUT_BHTD, LAYOUT_BTHD):
@@ -814,6 +869,8 @@ def _prep_norm(x, weight, bias, r_pre, layout):
 def gla_norm_fwd(x, weight=None, bias=None, eps=1e-5, r_pre=None, layout=LAYOUT_BHTD, out_dtype=None, out=None, stream=None):
     """Layer norm of each row of x ([B,H,T,D], [B,T,H,D] by ``layout``, or tokens [B,T,D]), times Swish(r_pre) if given.  weight,
     bias fp32 [H,D] ([D] for tokens) or None.  The result has ``out_dtype`` (x's)."""
+    if _elsewhere(stream, x):
+        return _call_on(stream, gla_norm_fwd, locals())
     lib = load_library()
     B, H, T, D = _prep_norm(x, weight, bias, r_pre, layout)
     if out is None:
@@ -836,6 +893,8 @@ def gla_norm_bwd(x, d_out, weight=None, bias=None, eps=1e-5, r_pre=None, layout=
                  workspace=None, stream=None):
     """Gradients of gla_norm_fwd: (dx, dr or None, dweight, dbias).  dx and dr are of ``grad_dtype`` (fp32), the others fp32 [H,D] (like
     weight if that is given), or None without ``want_d_weight`` (default: whether there is a weight or a bias)."""
+    if _elsewhere(stream, x):
+        return _call_on(stream, gla_norm_bwd, locals())
     torch = _torch()
     lib = load_library()
     B, H, T, D = _prep_norm(x, weight, bias, r_pre, layout)
@@ -848,7 +907,7 @@ def gla_norm_bwd(x, d_out, weight=None, bias=None, eps=1e-5, r_pre=None, layout=
         like = weight if weight is not None else bias
         shape = (H, D) if like is None else like.shape
         dw, db = x.new_empty(shape, dtype=torch.float32), x.new_empty(shape, dtype=torch.float32)
-    workspace = _room(lambda: gla_norm_bwd_workspace_bytes(B, H, T, D), workspace, x, stream)
+    workspace = _room(lambda: gla_norm_bwd_workspace_bytes(B, H, T, D), workspace, x)
     with _on_device_of(x):
         _check(lib.gla_norm_bwd(x.data_ptr(), d_out.data_ptr(), _ptr(weight), _ptr(bias), float(eps), _ptr(r_pre), B, H, T, D, _dt(x), _dt(dx),
                                 layout, dx.data_ptr(), _ptr(dr), _ptr(dw), _ptr(db), workspace.data_ptr(),
