@@ -565,7 +565,7 @@ int gla_norm_fwd(const void *x, const float *weight, const float *bias, float ep
  *   dr              DEVICE, grad_dtype, like x; NULL exactly if r_pre is                                      (written)
  *   dweight, dbias  DEVICE, fp32 [H,D], both or neither (NULL: not wanted); sums over batches and tokens, always added in
  *                   one order                                                                                 (written)
- *   workspace       DEVICE, 16-byte aligned, gla_norm_bwd_workspace_bytes(...) bytes
+ *   workspace       DEVICE, 16-byte aligned, gla_norm_bwd_workspace_bytes(...) bytes (written only for dweight, dbias)
  *
  * Everything else as gla_norm_fwd.  Outputs must not alias inputs.
  */

@@ -284,6 +284,7 @@ __global__ __launch_bounds__(Shape<LANES>::kThreads) void norm_kernel(const Norm
         }
     }
     if constexpr (BACK) {
+        if (p.part == nullptr) return;
         const bool shared = kGroups > 1 && one_head(p);          // the work-group's slots become one
         const size_t second = (size_t)partial_rows(p, kGroups) * p.H * D;
         if (shared) {
@@ -397,6 +398,14 @@ int norm_slots(int B, int H, int T, int D, int layout) {
     // 4096 waves (2048 where a lane holds two pieces of a row and more): with twice as many 16384 rows of 1152 took 63 us both ways, 57 with
     // these, 2000 of 8192 69 and 58; with half as many 16384 rows of 384 took 33, 29 with these
     return slots_for(p, 1, (long long)(D > 512 && D <= 1536 ? 2048 : 4096) * 64 / lanes_of(D, true), true);
+}
+
+int norm_partial_rows(int B, int H, int T, int D, int layout) {
+    NormParams p = {};
+    p.H = H;
+    p.layout = layout;
+    p.slots = norm_slots(B, H, T, D, layout);
+    return partial_rows(p, groups_of(D, true));
 }
 
 hipError_t launch_norm_fwd(const NormParams &p0, int dtype, hipStream_t stream) {

@@ -13,13 +13,14 @@ struct NormParams {
     const float *weight, *bias;         // null: ones, zeros
     void *out;                          // forward
     void *dx, *dr;                      // backward
-    float *part;                        // [2, slots, H, D]: sums for dweight and dbias of each slot
+    float *part;                        // [2, norm_partial_rows(), H, D]: sums for dweight and dbias, or null: not wanted
     float eps;
     int B, H, T, D, layout, out_dtype;
     int slots;                          // row groups that a head's rows are dealt to
 };
-// what the backward pass takes for the sums of its slots
+// the backward pass's slots, and the partial sums of each head that these leave
 int norm_slots(int B, int H, int T, int D, int layout);
+int norm_partial_rows(int B, int H, int T, int D, int layout);
 hipError_t launch_norm_fwd(const NormParams &p, int dtype, hipStream_t stream);
 hipError_t launch_norm_bwd(const NormParams &p, int dtype, float *dweight, float *dbias, hipStream_t stream);
 

@@ -399,7 +399,7 @@ int gla_norm_fwd(const void *x, const float *weight, const float *bias, float ep
 }
 
 static size_t norm_bytes(int B, int H, int T, int D) {
-    const int a = norm_slots(B, H, T, D, GLA_LAYOUT_BHTD), b = norm_slots(B, H, T, D, GLA_LAYOUT_BTHD);
+    const int a = norm_partial_rows(B, H, T, D, GLA_LAYOUT_BHTD), b = norm_partial_rows(B, H, T, D, GLA_LAYOUT_BTHD);
     return align_up((size_t)2 * (a > b ? a : b) * H * D * sizeof(float));
 }
 size_t gla_norm_bwd_workspace_bytes(int B, int H, int T, int D) {
@@ -423,7 +423,7 @@ int gla_norm_bwd(const void *x, const void *d_out, const float *weight, const fl
     p.bias = bias;
     p.dx = dx;
     p.dr = dr;
-    p.part = static_cast<float *>(workspace);
+    p.part = dweight != nullptr ? static_cast<float *>(workspace) : nullptr;
     p.eps = eps;
     p.B = B;
     p.H = H;
