@@ -461,15 +461,16 @@ int gla_fwd_fused_gates(const void *q, const void *k, const void *v, const void 
  *   grid_h, grid_w, scan_dir   as in gla_fwd; for text and the like grid_h = 1, grid_w = T, GLA_SCAN_ROW_FWD
  *   initial_state  DEVICE, fp32 [B,H,dk,dv] or NULL                                                           (read)
  *   out            DEVICE, out_dtype, shaped and laid out like v                                              (written)
- *   final_state    DEVICE, fp32 [B,H,dk,dv] or NULL; may be initial_state                                     (written)
+ *   final_state    DEVICE, fp32 [B,H,dk,dv] or NULL; may be initial_state, GLA_ERR_SHAPE where the two overlap
+ *                  otherwise                                                                                  (written)
  *   workspace      DEVICE, 16-byte aligned, gla_decay_fwd_workspace_bytes(...) bytes (0 for many sequences: then it
  *                  may be NULL)
  *
  * bf16 calls run on bf16 MFMA with every factor that is not an input carried as two bf16 numbers, fp32 calls on fp32
  * MFMA.  Gates have no lower limit; one that is NaN makes NaN of
  * all that it has a part in.  Inputs of visited rows have to be finite.  T is at most 2^30.  Tuning options have no effect.
- * Never allocates; nothing is kept between calls.  Calls that may overlap, captured ones among them, need workspaces of
- * their own.
+ * Never allocates; nothing is kept between calls.  `out` must not overlap the inputs.  Calls that may overlap, captured ones
+ * among them, need workspaces of their own.
  */
 typedef enum { GLA_DECAY_HEAD = 0, GLA_DECAY_TOKEN = 1 } gla_decay_kind;
 int gla_decay_fwd(const void *q, const void *k, const void *v, const float *log_decay, int decay_kind, const int *seq_lens,
@@ -531,7 +532,8 @@ int gla_decay_step(const void *q, const void *k, const void *v, const float *log
  *   base        > 0, finite; 10000 as a rule
  *   pairing     a gla_rope_pairing: a pair is two neighbouring channels, or channel i and i + w/2 of a section
  *   inverse     not 0: turned back, which is also the backward pass
- *   out_q, out_k   DEVICE, dtype, like q and k; may be q and k (GLA_ERR_SHAPE: out_q = k, out_k = q or out_q = out_k)  (written)
+ *   out_q, out_k   DEVICE, dtype, like q and k; may be q and k (GLA_ERR_SHAPE: out_q = k, out_k = q or out_q = out_k, and where an
+ *               output overlaps another tensor otherwise)                                                       (written)
  *
  * 1 <= d <= 256.  Frequencies restart with every section.  Angles are formed and reduced from frequencies in two 64-bit numbers: with a base of 1 or
  * more every position of 32 bits is as exact as the first, with less an angle is off by up to 2^-25 / base besides.  grid_h, grid_w are
@@ -550,7 +552,8 @@ int gla_rope(const void *q, const void *k, const int *positions, const int *sect
  *   weight, bias   DEVICE, fp32 [H,D], or NULL: ones, zeros                                                   (read)
  *   eps         >= 0, under the square root
  *   r_pre       DEVICE, x_dtype, like x, or NULL: no gate                                                     (read)
- *   out         DEVICE, out_dtype, like x; may be x if the element types agree                                (written)
+ *   out         DEVICE, out_dtype, like x; may be x or r_pre if the element types agree, GLA_ERR_SHAPE where it overlaps
+ *               them otherwise                                                                                  (written)
  *
  * 1 <= D <= 8192.  Statistics in fp32.  Needs no workspace and never allocates.
  */

@@ -14,6 +14,12 @@ template <typename... P>
 bool any_misaligned(P... p) { return (misaligned(p) || ...); }
 bool off_element(const void *p, int dtype) { return (reinterpret_cast<uintptr_t>(p) & (dtype == GLA_DT_BF16 ? 1u : 3u)) != 0; }
 bool bad_dtype(int d) { return d != GLA_DT_F32 && d != GLA_DT_BF16; }
+// whether two tensors share memory without beginning at one place (null: none)
+bool overlap(const void *p, size_t p_bytes, const void *q, size_t q_bytes) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return a != 0 && b != 0 && a != b && a < b + q_bytes && b < a + p_bytes;
+}
+size_t size_of(int dtype) { return dtype == GLA_DT_BF16 ? 2 : 4; }
 size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 
 // Spans a sequence is walked in.  One work-group walks one span, so that few sequences leave most of the GPU idle; spans read y and z once
@@ -167,6 +173,9 @@ int gla_decay_fwd(const void *q, const void *k, const void *v, const float *log_
     const int st = check_call(c, log_decay, decay_kind, seq_lens, B, H, T, dk, dv, grid_h, grid_w, scan_dir, qkv_dtype, out_dtype, layout);
     if (st != GLA_OK) return st;
     if (any_misaligned(q, k, v, (const void *)initial_state, (const void *)out, (const void *)final_state)) return GLA_ERR_ALIGN;
+    // in place, or apart from each other: elsewhere one state would be written over another that is still to be read
+    const size_t state_bytes = (size_t)B * H * dk * dv * sizeof(float);
+    if (overlap(initial_state, state_bytes, final_state, state_bytes)) return GLA_ERR_SHAPE;
     const FwdRoom room = fwd_room(workspace, c);
     if (room.bytes > 0 && (!workspace || misaligned(workspace) || workspace_bytes < room.bytes)) return GLA_ERR_WORKSPACE;
     const hipStream_t stream = static_cast<hipStream_t>(stream_);
@@ -289,10 +298,9 @@ int gla_decay_step(const void *q, const void *k, const void *v, const float *log
     if (any_misaligned((const void *)state, (const void *)state_out) || off_element(q, qkv_dtype) || off_element(k, qkv_dtype) ||
         off_element(v, qkv_dtype) || off_element(out, out_dtype) || off_element(log_decay, GLA_DT_F32))
         return GLA_ERR_ALIGN;
-    // in place, or apart from each other: elsewhere one state would be written over another that is still to be read
-    const uintptr_t a = reinterpret_cast<uintptr_t>(state), b = reinterpret_cast<uintptr_t>(state_out);
+    // (as gla_decay_fwd's)
     const size_t bytes = (size_t)B * H * dk * dv * sizeof(float);
-    if (a != b && a < b + bytes && b < a + bytes) return GLA_ERR_SHAPE;
+    if (overlap(state, bytes, state_out, bytes)) return GLA_ERR_SHAPE;
     return launch_decay_step(q, k, v, log_decay, decay_kind == GLA_DECAY_HEAD ? kDecayHead : kDecayToken, B, H, dk, dv, qkv_dtype, out_dtype,
                              state, state_out, out, static_cast<hipStream_t>(stream)) == hipSuccess
                ? GLA_OK
@@ -343,6 +351,10 @@ int gla_rope(const void *q, const void *k, const int *positions, const int *sect
     if (k != nullptr && (out_q == out_k || out_q == k || out_k == q)) return GLA_ERR_SHAPE;
     // 32-bit thread numbers
     if ((long long)B * T >= (1LL << 31) / d) return GLA_ERR_UNSUPPORTED;
+    const size_t bytes = (size_t)B * T * H * d * size_of(dtype);
+    if (overlap(out_q, bytes, q, bytes) || overlap(out_q, bytes, k, bytes) || overlap(out_k, bytes, q, bytes) || overlap(out_k, bytes, k, bytes) ||
+        overlap(out_q, bytes, out_k, bytes))
+        return GLA_ERR_SHAPE;
     p.x[0] = q;
     p.x[1] = k;
     p.y[0] = out_q;
@@ -382,6 +394,8 @@ int gla_norm_fwd(const void *x, const float *weight, const float *bias, float ep
     if (st != GLA_OK) return st;
     if (out == x && x_dtype != out_dtype) return GLA_ERR_SHAPE;
     if (misaligned(out)) return GLA_ERR_ALIGN;
+    const size_t elements = (size_t)B * T * H * D, bytes = elements * size_of(out_dtype), read = elements * size_of(x_dtype);
+    if (overlap(out, bytes, x, read) || overlap(out, bytes, r_pre, read) || (out == r_pre && x_dtype != out_dtype)) return GLA_ERR_SHAPE;
     NormParams p = {};
     p.x = x;
     p.r_pre = r_pre;
