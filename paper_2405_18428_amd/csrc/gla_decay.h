@@ -27,6 +27,13 @@ constexpr int kFlowBlock = 256;      // steps between two states that the backwa
 
 enum DecayKind : int { kDecayHead = 0, kDecayToken = 1 };   // log_decay [H], or one for each token
 
+// What calls on bf16 rows carry in three bf16 numbers instead of two (gla_decay_util.h)
+enum DecayDigits : int {
+    kDigitsRows = 0,                    // nothing: rows come out, or the gradients of tokens' gates
+    kDigitsStates = 1,                  // what states take up: a state comes out
+    kDigitsAll = 2                      // everything: the gradient of heads' gates comes out
+};
+
 // What all walks of one call share.
 struct DecayCall {
     const float *log_decay;
@@ -34,7 +41,7 @@ struct DecayCall {
     int kind;                           // DecayKind
     int B, H, T, dk, dv, grid_h, grid_w, scan_dir;
     int layout;                         // gla_layout
-    int exact;                          // bf16: products as exact as fp32's
+    int digits;                         // bf16 calls: DecayDigits
     int fast;                           // rows through 32-bit views (gla_decay_util.h)
     int nspans, span_len;               // spans a sequence is walked in, steps in each (a multiple of 64)
 };

@@ -303,8 +303,9 @@ static hipError_t walk_of_size(const DecayWalk &w, hipStream_t stream) {
 
 hipError_t launch_decay_walk(const DecayWalk &w, int dtype, hipStream_t stream) {
     if (dtype == GLA_DT_BF16) {
-        if (!w.grad) return walk_of_size<uint16_t, false>(w, stream);
-        return w.c.exact ? walk_of_size<Bf16Exact, true>(w, stream) : walk_of_size<uint16_t, true>(w, stream);
+        // (the walk for dq gives no state)
+        if (w.grad) return w.c.digits == kDigitsAll ? walk_of_size<Bf16<3, 3>, true>(w, stream) : walk_of_size<Bf16<2, 2>, true>(w, stream);
+        return w.c.digits == kDigitsStates ? walk_of_size<Bf16<3, 2>, false>(w, stream) : walk_of_size<Bf16<2, 2>, false>(w, stream);
     }
     return w.grad ? walk_of_size<float, true>(w, stream) : walk_of_size<float, false>(w, stream);
 }
@@ -318,7 +319,7 @@ hipError_t launch_decay_states(const DecayWalk &w, const DecayWalk *back, int dt
         constexpr int M = decltype(m)::value, N = decltype(n)::value;
         constexpr bool F = decltype(fast)::value;
         if (dtype != GLA_DT_BF16) return states<float, M, N, F>(both, d, stream);
-        return w.c.exact ? states<Bf16Exact, M, N, F>(both, d, stream) : states<uint16_t, M, N, F>(both, d, stream);
+        return w.c.digits == kDigitsRows ? states<Bf16<2, 2>, M, N, F>(both, d, stream) : states<Bf16<3, 3>, M, N, F>(both, d, stream);
     });
 }
 

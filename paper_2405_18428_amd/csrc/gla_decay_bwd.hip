@@ -10,19 +10,18 @@ namespace {
 // sum over waves that a product along a wave's own columns would need.
 constexpr int kThreads = 512;
 
-template <typename E, int K, int V>
+template <typename E, typename E1, int K, int V>
 struct BackLds {
     static constexpr int kRowsV = Tile<E, V, kBoth>::kBytes, kQ = 0, kK = Tile<E, K, kBoth>::kBytes, kV = kK + Tile<E, K, kAlong>::kBytes,
-                         kD = kV + Tile<E, V, kAlong>::kBytes, kPa = kD + kRowsV, kPb = kPa + Pairs<E>::kBytes, kG = kPb + Pairs<E>::kBytes,
+                         kD = kV + Tile<E, V, kAlong>::kBytes, kPa = kD + kRowsV, kPb = kPa + Pairs<E>::kBytes, kG = kPb + Pairs<E1>::kBytes,
                          kFlow = kG + 2 * (int)sizeof(Gates<Elem<E>::kChunk>), kDiag = kFlow + 2 * 4 * Elem<E>::kChunk * 4,
                          kMeet = kDiag + Elem<E>::kChunk * 4, kBytes = kMeet + 16;
 };
 
-// ROLE 0: dv, ROLE 1: dk
-template <typename E, int K, int V, bool FAST, int ROLE>
+// ROLE 0: dv and the initial state's gradient, ROLE 1: dk and the flows.  L: where what both share lies in LDS
+template <typename E, typename L, int K, int V, bool FAST, int ROLE>
 __device__ __forceinline__ void walk_back(const DecayBack &p, char *lds) {
     constexpr int C = Elem<E>::kChunk, M = ROLE == 0 ? K : V, N = ROLE == 0 ? V : K;
-    typedef BackLds<E, K, V> L;
     const Tile<E, K, kBoth> tq{lds + L::kQ};
     const Tile<E, K, kAlong> tk{lds + L::kK};
     const Tile<E, V, kAlong> tv{lds + L::kV};
@@ -121,12 +120,13 @@ __device__ __forceinline__ void walk_back(const DecayBack &p, char *lds) {
     clear_behind<256>(ro, p.grad_dtype == GLA_DT_BF16 ? 2 : 4, len, s0, s1, tid & 255);
 }
 
-template <typename E, int K, int V, bool FAST>
+template <typename E0, typename E1, int K, int V, bool FAST>
 __global__ __launch_bounds__(kThreads, 2) void decay_back_kernel(const DecayBack p) {
+    typedef BackLds<E0, E1, K, V> L;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     // both branches meet at the same barriers: the same chunks, two each, and one behind them
-    if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 8) == 0) walk_back<E, K, V, FAST, 0>(p, lds);
-    else walk_back<E, K, V, FAST, 1>(p, lds);
+    if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 8) == 0) walk_back<E0, L, K, V, FAST, 0>(p, lds);
+    else walk_back<E1, L, K, V, FAST, 1>(p, lds);
 }
 
 // A block of kFlowBlock steps a work-group: what flows into each, in 64 bits
@@ -190,13 +190,13 @@ __global__ __launch_bounds__(256) void decay_gate_sum_kernel(const double *part,
     if (t == 0) dlog[h] = (float)sum[0];
 }
 
-template <typename E, int K, int V, bool FAST>
+template <typename E0, typename E1, int K, int V, bool FAST>
 hipError_t back(const DecayBack &w, hipStream_t stream) {
     static std::atomic<bool> done[kMaxDevices];
-    constexpr int bytes = BackLds<E, K, V>::kBytes;
-    const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(&decay_back_kernel<E, K, V, FAST>), bytes, done);
+    constexpr int bytes = BackLds<E0, E1, K, V>::kBytes;
+    const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(&decay_back_kernel<E0, E1, K, V, FAST>), bytes, done);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((decay_back_kernel<E, K, V, FAST>), dim3((unsigned)(w.c.B * w.c.H * w.c.nspans)), dim3(kThreads), bytes, stream, w);
+    hipLaunchKernelGGL((decay_back_kernel<E0, E1, K, V, FAST>), dim3((unsigned)(w.c.B * w.c.H * w.c.nspans)), dim3(kThreads), bytes, stream, w);
     return hipGetLastError();
 }
 
@@ -206,8 +206,9 @@ hipError_t launch_decay_back(const DecayBack &w, int dtype, hipStream_t stream) 
     return decay_sizes(w.c.dk, w.c.dv, w.c.fast, [&](auto k, auto v, auto fast) {
         constexpr int K = decltype(k)::value, V = decltype(v)::value;
         constexpr bool F = decltype(fast)::value;
-        if (dtype != GLA_DT_BF16) return back<float, K, V, F>(w, stream);
-        return w.c.exact ? back<Bf16Exact, K, V, F>(w, stream) : back<uint16_t, K, V, F>(w, stream);
+        if (dtype != GLA_DT_BF16) return back<float, float, K, V, F>(w, stream);
+        if (w.c.digits == kDigitsRows) return back<Bf16<2, 2>, Bf16<2, 2>, K, V, F>(w, stream);
+        return w.c.digits == kDigitsStates ? back<Bf16<3, 2>, Bf16<2, 2>, K, V, F>(w, stream) : back<Bf16<3, 3>, Bf16<3, 3>, K, V, F>(w, stream);
     });
 }
 

@@ -9,11 +9,16 @@
 // Everything is formed transposed, so that the accumulators of one product are an operand of the next as they stand: an operand
 // is eight (bf16) or four (fp32) values of the contracted index in a lane, and which index stands where does not matter as long as
 // both operands agree.  The state's rows are ordered (state_row) so that x's operands are 16 contiguous bytes of a row.
-// bf16 calls split what is not bf16 by itself (the state, P, the decayed z) into two bf16 numbers, head and remainder: what is
-// lost is 2^-18 of each, so states, which are given in 32 bits, hold about 2e-6 where one bf16 would leave 2e-3, and a token's gate
-// gradient 7e-6.  The gradient of a head's one decay is a sum over all steps in which each block's flows count by their place, so that
-// errors add up to 256 / (memory in steps) times as much: 2e-5 to 6e-5 for a single head of 30 steps' memory with two numbers, and
-// three are taken (DecayCall::exact; a training step of 64 sequences of 4096 steps, 128 x 128: 640 us, 482 with two).
+// bf16 calls split what is not bf16 by itself (the state, P, the decayed z) into bf16 numbers, head and remainders (Elem).  Two leave 2^-18 of
+// each: outputs in 32 bits and a token's gate gradient hold 2e-6 to 7e-6 where one bf16 would leave 2e-3, which rows of 16 bits (2^-9) do not show.
+// Three leave what fp32 leaves, 1e-7 to 4e-7.  They are taken (DecayDigits)
+//   for the decayed z where a state is given back, which stands in 32 bits for all that comes after it (2.4e-6 with two; forward, 65536 steps
+//   of 16 heads 128 x 128: 420 us, 392 with two; prompts of 128 sequences 100 us, 92);
+//   for all where a head's one decay is learnt: its gradient is a sum over all steps in which each block's flows count by their place, so that errors
+//   add up to 256 / (memory in steps) times as much, 2e-5 to 6e-5 for a single head of 30 steps' memory with two (a training step of 64
+//   sequences of 4096 steps, 128 x 128: 660 us, 490 with two).
+// For all that a bf16 call gives in 32 bits they would cost as much again for tokens' gates and 10 to 60 % forward; calls on the same rows in fp32 have
+// these digits.
 // fp32 calls run on the fp32 matrix instructions.
 #pragma once
 #include "gla_decay.h"
@@ -23,27 +28,22 @@ namespace gla {
 namespace {
 
 template <typename E> struct Elem;
-template <> struct Elem<uint16_t> {
-    static constexpr int kChunk = 64;            // steps
-    static constexpr int kDeep = 32;             // contracted values of an operand over the wave
-    // A factor that is no input by itself (the state, P, the decayed z) is two bf16 numbers, head and remainder.  Three would leave what fp32
-    // leaves and took 9 % more time for the decayed z alone (65536 steps of 16 heads 128 x 128: 440 us, 397 with two), 48 % for all; one for
-    // the state and P 7 % less.
-    static constexpr int kParts = 2;
-};
-// bf16 rows whose products are as exact as fp32's: three numbers
-struct Bf16Exact {
+// bf16 rows.  A factor that is no input by itself is as many bf16 numbers, head and remainders: STATE the decayed z that the state takes up, OUT the
+// state and P that the outputs are formed from (DecayDigits).
+template <int STATE, int OUT>
+struct Bf16 {
     uint16_t bits;
 };
-template <> struct Elem<Bf16Exact> {
-    static constexpr int kChunk = 64;
-    static constexpr int kDeep = 32;
-    static constexpr int kParts = 3;
+template <int STATE, int OUT>
+struct Elem<Bf16<STATE, OUT>> {
+    static constexpr int kChunk = 64;            // steps
+    static constexpr int kDeep = 32;             // contracted values of an operand over the wave
+    static constexpr int kStateParts = STATE, kOutParts = OUT;
 };
 template <> struct Elem<float> {
     static constexpr int kChunk = 32;
     static constexpr int kDeep = 16;
-    static constexpr int kParts = 1;
+    static constexpr int kStateParts = 1, kOutParts = 1;
 };
 
 // 16 bytes of an operand; products of operands
@@ -358,7 +358,7 @@ __device__ inline void form_gates(Gates<C> &s, float gate, int lane) {
 // P^T of a chunk in LDS, as the operands that (2) reads: entry (i tile, jk, part) of 64 lanes x 16 bytes
 template <typename E>
 struct Pairs {
-    static constexpr int C = Elem<E>::kChunk, kI = C / 16, kJ = C / Elem<E>::kDeep, kParts = Elem<E>::kParts;
+    static constexpr int C = Elem<E>::kChunk, kI = C / 16, kJ = C / Elem<E>::kDeep, kParts = Elem<E>::kOutParts;
     static constexpr int kBytes = kI * kJ * kParts * 1024;
     char *p;
     __device__ __forceinline__ char *at(int it, int jk, int part, int lane) const { return p + (((it * kJ + jk) * kParts + part) * 64 + lane) * 16; }
@@ -368,7 +368,7 @@ struct Pairs {
 template <typename E, int M, int N, bool FAST, bool ZA>
 struct Walker {
     static constexpr int C = Elem<E>::kChunk, kDeep = Elem<E>::kDeep, kI = C / 16, kJ = C / kDeep;
-    static constexpr int kRows = M / 16, kCols = N / 64, kSteps = M / kDeep, kParts = Elem<E>::kParts;
+    static constexpr int kRows = M / 16, kCols = N / 64, kSteps = M / kDeep, kParts = Elem<E>::kOutParts, kStateParts = Elem<E>::kStateParts;
     f32x4 S[kRows][kCols];
     f32x4 O[kCols][kI];
     int lane, lm, g, w;
@@ -605,7 +605,7 @@ struct Walker {
                                            u32x4 (&zf)[kJ][kCols]) {
         const float last = gt.last;
         const Heads heads;
-        u32x4 zd[kJ][kCols][kParts];
+        u32x4 zd[kJ][kCols][kStateParts];
 #pragma unroll
         for (int jk = 0; jk < kJ; ++jk) {
 #pragma unroll
@@ -618,10 +618,10 @@ struct Walker {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const f32x4 &d = r < 2 ? d0 : d1;
-                        uint32_t s[kParts];
+                        uint32_t s[kStateParts];
                         heads.split(bf16_lo_as_float(zf[jk][c][r]) * d[2 * (r & 1)], bf16_hi_as_float(zf[jk][c][r]) * d[2 * (r & 1) + 1], s);
 #pragma unroll
-                        for (int q = 0; q < kParts; ++q) zd[jk][c][q][r] = s[q];
+                        for (int q = 0; q < kStateParts; ++q) zd[jk][c][q][r] = s[q];
                     }
             } else {
                 const f32x4 d = *reinterpret_cast<const f32x4 *>(&gt.out[jk * 16 + g * 4]);
@@ -648,7 +648,7 @@ struct Walker {
 #pragma unroll
             for (int jk = 0; jk < kJ; ++jk)
 #pragma unroll
-                for (int q = 0; q < kParts; ++q)
+                for (int q = 0; q < kStateParts; ++q)
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll

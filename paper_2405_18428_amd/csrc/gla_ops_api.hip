@@ -179,6 +179,7 @@ int gla_decay_fwd(const void *q, const void *k, const void *v, const float *log_
     const FwdRoom room = fwd_room(workspace, c);
     if (room.bytes > 0 && (!workspace || misaligned(workspace) || workspace_bytes < room.bytes)) return GLA_ERR_WORKSPACE;
     const hipStream_t stream = static_cast<hipStream_t>(stream_);
+    c.digits = final_state != nullptr ? kDigitsStates : kDigitsRows;
     DecayWalk w = {};
     w.c = c;
     w.r.x = q;
@@ -216,7 +217,7 @@ int gla_decay_bwd(const void *q, const void *k, const void *v, const float *log_
     if (!workspace || misaligned(workspace) || workspace_bytes < room.bytes) return GLA_ERR_WORKSPACE;
     const hipStream_t stream = static_cast<hipStream_t>(stream_);
     const bool gates = dlog_decay != nullptr;
-    c.exact = gates && c.kind == kDecayHead && qkv_dtype == GLA_DT_BF16;
+    c.digits = gates && c.kind == kDecayHead ? kDigitsAll : d_initial_state != nullptr ? kDigitsStates : kDigitsRows;
 
     DecayWalk w = {};                    // dq: the recurrence of (dO, v, k) from the transposed states
     w.c = c;
