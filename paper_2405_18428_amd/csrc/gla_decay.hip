@@ -163,7 +163,7 @@ __global__ __launch_bounds__(kThreads, 2) void decay_state_kernel(const StatePai
 }
 
 // local [B*H, nspans, cells]: entry sp becomes the state that enters span sp.  A thread has one element of all of a sequence's spans; it asks
-// for eight of them before it uses the first, as each one's place is written in turn (65536 steps of 16 heads 128 x 128 in 32 spans: 18 us, 3.7 TB/s).
+// for eight of them before it uses the first, as each one's place is written in turn (65536 steps of 16 heads 128 x 128 in 32 spans: 19 us, 3.5 TB/s).
 // blockIdx.y: the forward and the reversed chain.
 __global__ __launch_bounds__(kThreads) void decay_carry_kernel(const DecayChain c0, const DecayChain c1, int cells) {
     constexpr int kAhead = 8;

@@ -24,10 +24,10 @@ size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 
 // Spans a sequence is walked in.  One work-group walks one span, so that few sequences leave most of the GPU idle; spans read y and z once
 // more for their local states, and move their states.  Spans as short as 64 steps pay while there are up to 16 (16 sequences of 512 steps,
-// 128 x 128, forward and back: 90 us in spans of 64, 111 of 128, 133 of 256; of 2048 steps 157 in 32 spans, 141 in 16), beyond that only
-// such of 512 and more, and two chunks do not pay for the second pass (128 steps forward: 34 us in two spans, 20 in one).
+// 128 x 128, forward and back: 83 us in spans of 64, 108 of 128, 133 of 256; of 2048 steps 148 in 32 spans, 134 in 16), beyond that only
+// such of 512 and more, and two chunks do not pay for the second pass (64 sequences of 128 steps forward: 23 us in two spans, 17 in one).
 constexpr int kShortSpans = 16, kLongSpan = 512, kWhole = 128;
-// Up to so many spans the walks chain the local states themselves (padded prompts of 128 sequences in 4 spans: 95 us, 104 with the
+// Up to so many spans the walks chain the local states themselves (padded prompts of 128 sequences in 4 spans: 101 us, 112 with the
 // kernel for it; at 8 spans it is even).
 constexpr int kChainSpans = 4;
 void plan_spans(DecayCall &c, long long groups) {
