@@ -581,6 +581,69 @@ int gla_norm_bwd(const void *x, const void *d_out, const float *weight, const fl
                  float *dweight, float *dbias, void *workspace, size_t workspace_bytes, gla_stream_t stream);
 size_t gla_norm_bwd_workspace_bytes(int B, int H, int T, int D);
 
+/*
+ * gla_recur_fwd - gated recurrence of channels:
+ *
+ *     h_t = a_t h_{t-1} + u_t ,     u_t = x_t or (1 - a_t) x_t ,     out = h ,     h_0 = initial_state or zero
+ *
+ * with a gate a_t for every channel and token: a mixer whose state is one number a channel.
+ *
+ *   x              DEVICE, x_dtype, [B,T,D]                                                                   (read)
+ *   gate           DEVICE, [B,T,D] (read): by gate_kind (a gla_gate_kind)
+ *                  GLA_GATE_LOG: log a in fp32, <= 0 down to -inf (a gate of zero)
+ *                  GLA_GATE_PRE: z in x_dtype, a = sigmoid(z)^(1/tau)   (Eq. (gate_gla))
+ *   tau            > 0, finite; ignored for GLA_GATE_LOG
+ *   complement     not 0: u_t = (1 - a_t) x_t
+ *   seq_lens       DEVICE, int32 [B], 0 .. T, or NULL: all T; as in gla_decay_fwd (row scans only): rows behind a sequence's end may hold
+ *                  anything and those of `out` are left as they were                                          (read)
+ *   grid_h, grid_w, scan_dir   as in gla_fwd; for text and the like grid_h = 1, grid_w = T, GLA_SCAN_ROW_FWD
+ *   initial_state  DEVICE, fp32 [B,D] or NULL                                                                 (read)
+ *   out            DEVICE, out_dtype, [B,T,D]; may be x or the gate if the element types agree, GLA_ERR_SHAPE where it overlaps them
+ *                  otherwise                                                                                  (written)
+ *   final_state    DEVICE, fp32 [B,D] or NULL; may be initial_state, GLA_ERR_SHAPE where the two overlap otherwise   (written)
+ *   workspace      DEVICE, 16-byte aligned, gla_recur_fwd_workspace_bytes(...) bytes (0: may be NULL)
+ *
+ * Arithmetic in fp32, gates summed as logarithms: memories of any length are as exact as short ones.  Inputs of visited rows have to be
+ * finite, but for gates of zero; a NaN makes NaN of what comes after it in its channel.  T is at most 2^30.  Tensors 16-byte aligned.  Never
+ * allocates; nothing is kept between calls.  Calls that may overlap, captured ones among them, need workspaces of their own.
+ */
+typedef enum { GLA_GATE_LOG = 0, GLA_GATE_PRE = 1 } gla_gate_kind;
+int gla_recur_fwd(const void *x, const void *gate, int gate_kind, float tau, int complement, const int *seq_lens,
+                  int B, int T, int D, int grid_h, int grid_w, int scan_dir, int x_dtype, int out_dtype,
+                  const float *initial_state, void *out, float *final_state, void *workspace, size_t workspace_bytes, gla_stream_t stream);
+size_t gla_recur_fwd_workspace_bytes(int B, int T, int D);
+
+/*
+ * gla_recur_bwd - gradients of a loss that depends on `out` and, through d_final_state, on the final state of gla_recur_fwd.  With
+ * G_t = dO_t + a_{t+1} G_{t+1} (behind the last token d_final_state):
+ *   dx_t = G_t or (1 - a_t) G_t,  dlog a_t = a_t (h_{t-1} - (0 or x_t)) G_t,  dz_t = dlog a_t sigmoid(-z_t) / tau,  d h_0 = a_1 G_1.
+ *
+ *   d_out            DEVICE, x_dtype, like x                                                                  (read)
+ *   d_final_state    DEVICE, fp32 [B,D] or NULL: zero                                                         (read)
+ *   dx, d_gate       DEVICE, grad_dtype, [B,T,D]; the gradient of what `gate` holds; rows behind a sequence's end are cleared   (written)
+ *   d_initial_state  DEVICE, fp32 [B,D], or NULL: not wanted                                                  (written)
+ *   workspace        DEVICE, 16-byte aligned, gla_recur_bwd_workspace_bytes(...) bytes (0: may be NULL)
+ *
+ * The states are formed again from x and the gates.  Everything else as gla_recur_fwd.  Outputs must not overlap inputs (GLA_ERR_SHAPE).
+ */
+int gla_recur_bwd(const void *x, const void *gate, int gate_kind, float tau, int complement, const int *seq_lens, const void *d_out,
+                  const float *initial_state, const float *d_final_state, int B, int T, int D, int grid_h, int grid_w, int scan_dir,
+                  int x_dtype, int grad_dtype, void *dx, void *d_gate, float *d_initial_state,
+                  void *workspace, size_t workspace_bytes, gla_stream_t stream);
+size_t gla_recur_bwd_workspace_bytes(int B, int T, int D);
+
+/*
+ * gla_recur_step - one token of gla_recur_fwd for each of B sequences: state_out = a state + u, out = state_out.
+ *
+ *   x [B,D], gate [B,D], state [B,D]   DEVICE, as in gla_recur_fwd                                            (read)
+ *   state_out   DEVICE, fp32 [B,D]; may be `state` (in place), GLA_ERR_SHAPE where the two overlap otherwise  (written)
+ *   out         DEVICE, out_dtype [B,D]; must not overlap the others (GLA_ERR_SHAPE)                          (written)
+ *
+ * x, gate and out may begin at any element, the states at 16 bytes.  Needs no workspace and never allocates.
+ */
+int gla_recur_step(const void *x, const void *gate, int gate_kind, float tau, int complement, int B, int D, int x_dtype, int out_dtype,
+                   const float *state, float *state_out, void *out, gla_stream_t stream);
+
 /* Bytes of workspace gla_fwd_ex / gla_fwd_layout need for this problem (an upper bound over all
  * launch plans, so it does not depend on tuning options).  0 on invalid sizes. */
 size_t gla_fwd_workspace_bytes(int B, int H, int T, int dk, int dv, int qkv_dtype);

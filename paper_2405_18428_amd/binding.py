@@ -19,6 +19,7 @@ CARRY_AUTO, CARRY_KERNEL, CARRY_IN_OUTPUT_PASS = 0, 1, 2
 LAYOUT_BHTD, LAYOUT_BTHD = 0, 1
 DECAY_HEAD, DECAY_TOKEN = 0, 1
 ROPE_ADJACENT, ROPE_HALVES = 0, 1
+GATE_LOG, GATE_PRE = 0, 1
 ENGINE_AUTO, ENGINE_RECURRENT, ENGINE_MFMA, ENGINE_MFMA_FP16 = 0, 1, 2, 3
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -106,6 +107,15 @@ def load_library():
     lib.gla_norm_bwd.argtypes = [vp] * 4 + [f, vp] + [i] * 7 + [vp] * 5 + [sz, vp]
     lib.gla_norm_bwd_workspace_bytes.restype = sz
     lib.gla_norm_bwd_workspace_bytes.argtypes = [i] * 4
+    lib.gla_recur_fwd.restype = i
+    lib.gla_recur_fwd.argtypes = [vp, vp, i, f, i, vp] + [i] * 8 + [vp] * 4 + [sz, vp]
+    lib.gla_recur_bwd.restype = i
+    lib.gla_recur_bwd.argtypes = [vp, vp, i, f, i] + [vp] * 4 + [i] * 8 + [vp] * 4 + [sz, vp]
+    lib.gla_recur_step.restype = i
+    lib.gla_recur_step.argtypes = [vp, vp, i, f] + [i] * 5 + [vp] * 4
+    for name in ("gla_recur_fwd_workspace_bytes", "gla_recur_bwd_workspace_bytes"):
+        getattr(lib, name).restype = sz
+        getattr(lib, name).argtypes = [i] * 3
     lib.gla_calibrate_mfma.restype = i
     lib.gla_calibrate_mfma.argtypes = [ctypes.POINTER(ctypes.c_double), vp]
     lib.gla_fwd_timed.restype = i
@@ -913,3 +923,100 @@ def gla_norm_bwd(x, d_out, weight=None, bias=None, eps=1e-5, r_pre=None, layout=
                                 layout, dx.data_ptr(), _ptr(dr), _ptr(dw), _ptr(db), workspace.data_ptr(),
                                 workspace.numel() * workspace.element_size(), _stream_ptr(stream, x)))
     return dx, dr, dw, db
+
+
+def _prep_recur(x, gate, gate_kind, shape, seq_lens, states):
+    """Checks the tensors of a gated recurrence; x has `shape`, states its first and last size."""
+    torch = _torch()
+    if gate_kind not in (GATE_LOG, GATE_PRE):
+        raise ValueError("unknown gate kind")
+    _dt(x)
+    dev = x.get_device()
+    _want("x", x, shape, x.dtype, dev)
+    _want("gate", gate, shape, torch.float32 if gate_kind == GATE_LOG else x.dtype, dev)
+    if seq_lens is not None:
+        _want("seq_lens", seq_lens, shape[:1], torch.int32, dev)
+    for name, t in states:
+        if t is not None:
+            _want(name, t, (shape[0], shape[-1]), torch.float32, dev)
+
+
+def gla_recur_fwd_workspace_bytes(B, T, D) -> int:
+    return int(load_library().gla_recur_fwd_workspace_bytes(B, T, D))
+
+
+def gla_recur_bwd_workspace_bytes(B, T, D) -> int:
+    return int(load_library().gla_recur_bwd_workspace_bytes(B, T, D))
+
+
+def gla_recur_fwd(x, gate, grid_h, grid_w, scan_dir=SCAN_ROW_FWD, gate_kind=GATE_PRE, tau=16.0, complement=False, seq_lens=None,
+                  initial_state=None, out_dtype=None, want_final_state=True, out=None, final_state=None, workspace=None, stream=None):
+    """Gated recurrence of channels: h_t = a_t h_{t-1} + u_t, u = x or (``complement``) (1 - a) x.  x [B,T,D]; gate [B,T,D]: log a in fp32
+    (GATE_LOG), or z of x's element type with a = sigmoid(z)^(1/tau) (GATE_PRE).  ``seq_lens`` int32 [B]: each sequence's own length; rows
+    of ``out`` behind it are left as they were.  States fp32 [B,D].  The result has ``out_dtype`` (x's).  Returns (out, final_state)."""
+    if _elsewhere(stream, x):
+        return _call_on(stream, gla_recur_fwd, locals())
+    lib = load_library()
+    if x.dim() != 3:
+        raise ValueError("x must be [B,T,D]")
+    B, T, D = x.shape
+    _prep_recur(x, gate, gate_kind, x.shape, seq_lens, (("initial_state", initial_state), ("final_state", final_state)))
+    if out is None:
+        out = _like(x, x.dtype if out_dtype is None else out_dtype)
+    else:
+        _want("out", out, x.shape, out.dtype, x.get_device())
+    if final_state is None and want_final_state:
+        final_state = x.new_empty((B, D), dtype=_torch().float32)
+    workspace = _room(lambda: gla_recur_fwd_workspace_bytes(B, T, D), workspace, x)
+    with _on_device_of(x):
+        _check(lib.gla_recur_fwd(x.data_ptr(), gate.data_ptr(), gate_kind, float(tau), int(bool(complement)), _ptr(seq_lens), B, T, D, grid_h,
+                                 grid_w, scan_dir, _dt(x), _dt(out), _ptr(initial_state), out.data_ptr(), _ptr(final_state),
+                                 workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(stream, x)))
+    return out, final_state
+
+
+def gla_recur_bwd(x, gate, d_out, grid_h, grid_w, scan_dir=SCAN_ROW_FWD, gate_kind=GATE_PRE, tau=16.0, complement=False, seq_lens=None,
+                  initial_state=None, d_final_state=None, grad_dtype=None, want_d_initial_state=False, workspace=None, stream=None):
+    """Gradients of gla_recur_fwd from those of its outputs (``d_out``, like x) and of its final state (``d_final_state`` or None).
+    Returns (dx, d_gate, d_initial_state or None); the first two of ``grad_dtype`` (fp32)."""
+    if _elsewhere(stream, x):
+        return _call_on(stream, gla_recur_bwd, locals())
+    torch = _torch()
+    lib = load_library()
+    if x.dim() != 3:
+        raise ValueError("x must be [B,T,D]")
+    B, T, D = x.shape
+    _prep_recur(x, gate, gate_kind, x.shape, seq_lens, (("initial_state", initial_state), ("d_final_state", d_final_state)))
+    _want("d_out", d_out, x.shape, x.dtype, x.get_device())
+    gdt = torch.float32 if grad_dtype is None else grad_dtype
+    dx, dg = _like(x, gdt), _like(gate, gdt)
+    ds = x.new_empty((B, D), dtype=torch.float32) if want_d_initial_state else None
+    workspace = _room(lambda: gla_recur_bwd_workspace_bytes(B, T, D), workspace, x)
+    with _on_device_of(x):
+        _check(lib.gla_recur_bwd(x.data_ptr(), gate.data_ptr(), gate_kind, float(tau), int(bool(complement)), _ptr(seq_lens), d_out.data_ptr(),
+                                 _ptr(initial_state), _ptr(d_final_state), B, T, D, grid_h, grid_w, scan_dir, _dt(x), _dt(dx), dx.data_ptr(),
+                                 dg.data_ptr(), _ptr(ds), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                 _stream_ptr(stream, x)))
+    return dx, dg, ds
+
+
+def gla_recur_step(x, gate, state, gate_kind=GATE_PRE, tau=16.0, complement=False, out_dtype=None, out=None, state_out=None, stream=None):
+    """One token of gla_recur_fwd for each sequence: x, gate [B,D], state fp32 [B,D].  The new state goes to ``state_out``, in place
+    (``state``) if that is None.  Returns (out, state_out)."""
+    if _elsewhere(stream, x):
+        return _call_on(stream, gla_recur_step, locals())
+    lib = load_library()
+    if x.dim() != 2:
+        raise ValueError("x must be [B,D]")
+    B, D = x.shape
+    if state_out is None:
+        state_out = state
+    _prep_recur(x, gate, gate_kind, x.shape, None, (("state", state), ("state_out", state_out)))
+    if out is None:
+        out = _like(x, x.dtype if out_dtype is None else out_dtype)
+    else:
+        _want("out", out, x.shape, out.dtype, x.get_device())
+    with _on_device_of(x):
+        _check(lib.gla_recur_step(x.data_ptr(), gate.data_ptr(), gate_kind, float(tau), int(bool(complement)), B, D, _dt(x), _dt(out),
+                                  state.data_ptr(), state_out.data_ptr(), out.data_ptr(), _stream_ptr(stream, x)))
+    return out, state_out

@@ -1,0 +1,199 @@
+// Host side of the C ABI for what stands around the mixer in a block: the gated recurrence of channels, the norm and rotation of queries and
+// keys, the gated feed-forward product.  Argument checks, plans, workspaces.
+#include <math.h>
+
+#include "gla_recur.h"
+
+namespace gla {
+namespace {
+
+bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+template <typename... P>
+bool any_misaligned(P... p) { return (misaligned(p) || ...); }
+bool off_element(const void *p, int dtype) { return (reinterpret_cast<uintptr_t>(p) & (dtype == GLA_DT_BF16 ? 1u : 3u)) != 0; }
+bool bad_dtype(int d) { return d != GLA_DT_F32 && d != GLA_DT_BF16; }
+size_t size_of(int dtype) { return dtype == GLA_DT_BF16 ? 2 : 4; }
+size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
+
+// A tensor's place in memory (null: none)
+struct Span {
+    const void *p;
+    size_t bytes;
+};
+bool touch(Span a, Span b) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(a.p), q = reinterpret_cast<uintptr_t>(b.p);
+    return p != 0 && q != 0 && p < q + b.bytes && q < p + a.bytes;
+}
+// whether one of some tensors shares memory with another one of them or with one of `others`
+template <size_t N, size_t M>
+bool any_touch(const Span (&mine)[N], const Span (&others)[M]) {
+    for (size_t i = 0; i < N; ++i) {
+        for (size_t j = 0; j < i; ++j)
+            if (touch(mine[i], mine[j])) return true;
+        for (size_t j = 0; j < M; ++j)
+            if (touch(mine[i], others[j])) return true;
+    }
+    return false;
+}
+
+// --- gated recurrence of channels ---
+
+// Units of the forward pass.  Work-groups have 256 channels (fewer where rows allow only narrow loads); spans so short that about kWantGroups
+// of them run, none shorter than four rounds where that still fills the GPU.
+constexpr int kWantGroups = 1024, kWholeSteps = 128;
+void plan_forward(RecurCall &c) {
+    const long long groups = ((long long)c.B * c.D + 255) / 256;
+    long long n = kWantGroups / groups;
+    const int rounds = (c.T + kRecurRound - 1) / kRecurRound;
+    if (n > rounds) n = rounds;
+    if (n < 2 || c.T <= kWholeSteps) n = 1;
+    const int each = (int)((rounds + n - 1) / n);
+    c.unit = each * kRecurRound;
+    c.nunits = (rounds + each - 1) / each;
+}
+void plan_backward(RecurCall &c) {
+    c.unit = kRecurRound;
+    c.nunits = (c.T + kRecurRound - 1) / kRecurRound;
+}
+size_t units_bytes(const RecurCall &c, int numbers) {
+    return c.nunits > 1 ? numbers * align_up((size_t)c.B * c.nunits * c.D * sizeof(float)) : 0;
+}
+RecurUnits units_in(const RecurCall &c, void *workspace, bool adjoint) {
+    const size_t each = align_up((size_t)c.B * c.nunits * c.D * sizeof(float));
+    char *p = static_cast<char *>(workspace);
+    if (c.nunits == 1) return {};
+    return {reinterpret_cast<float *>(p), reinterpret_cast<float *>(p + each), adjoint ? reinterpret_cast<float *>(p + 2 * each) : nullptr};
+}
+
+int check_recur(RecurCall &c, const void *x, const void *gate, int kind, float tau, int complement, const int *seq_lens, int B, int T, int D,
+                int grid_h, int grid_w, int scan_dir, int dtype, int other_dtype) {
+    if (B <= 0 || T <= 0 || D <= 0 || grid_h <= 0 || grid_w <= 0) return GLA_ERR_SHAPE;
+    if ((long long)grid_h * grid_w != T || scan_dir < 0 || scan_dir > 3) return GLA_ERR_SHAPE;
+    if (bad_dtype(dtype) || bad_dtype(other_dtype) || (kind != GLA_GATE_LOG && kind != GLA_GATE_PRE)) return GLA_ERR_SHAPE;
+    if (kind == GLA_GATE_PRE && (!(tau > 0.f) || isinf(tau))) return GLA_ERR_SHAPE;
+    if (seq_lens != nullptr && scan_dir > GLA_SCAN_ROW_REV) return GLA_ERR_UNSUPPORTED;
+    // work-groups of 512 threads for as few as 64 channels and 64 steps, fewer than 2^32 threads in a launch; D as 32-bit byte offsets
+    if (T > (1 << 30) || D > (1 << 26)) return GLA_ERR_UNSUPPORTED;
+    if ((long long)B * ((D + 63) / 64) * ((T + kRecurRound - 1) / kRecurRound) >= (1LL << 22)) return GLA_ERR_UNSUPPORTED;
+    if (any_misaligned(x, gate) || (reinterpret_cast<uintptr_t>(seq_lens) & 3u) != 0) return GLA_ERR_ALIGN;
+    c = {};
+    c.x = x;
+    c.gate = gate;
+    c.seq_lens = seq_lens;
+    c.B = B;
+    c.T = T;
+    c.D = D;
+    c.grid_h = grid_h;
+    c.grid_w = grid_w;
+    c.scan_dir = scan_dir;
+    c.dtype = dtype;
+    c.kind = kind;
+    c.rest = complement != 0;
+    c.inv_tau = kind == GLA_GATE_PRE ? 1.f / tau : 1.f;
+    return GLA_OK;
+}
+bool sized_recur(RecurCall &c, int B, int T, int D) {
+    return check_recur(c, nullptr, nullptr, GLA_GATE_LOG, 1.f, 0, nullptr, B, T, D, 1, T, 0, GLA_DT_F32, GLA_DT_F32) == GLA_OK;
+}
+
+}  // namespace
+}  // namespace gla
+
+using namespace gla;
+
+extern "C" {
+
+size_t gla_recur_fwd_workspace_bytes(int B, int T, int D) {
+    RecurCall c;
+    if (!sized_recur(c, B, T, D)) return 0;
+    plan_forward(c);
+    return units_bytes(c, 2);
+}
+size_t gla_recur_bwd_workspace_bytes(int B, int T, int D) {
+    RecurCall c;
+    if (!sized_recur(c, B, T, D)) return 0;
+    plan_backward(c);
+    return units_bytes(c, 3);
+}
+
+int gla_recur_fwd(const void *x, const void *gate, int gate_kind, float tau, int complement, const int *seq_lens, int B, int T, int D,
+                  int grid_h, int grid_w, int scan_dir, int x_dtype, int out_dtype, const float *initial_state, void *out, float *final_state,
+                  void *workspace, size_t workspace_bytes, gla_stream_t stream_) {
+    if (!x || !gate || !out) return GLA_ERR_NULL;
+    RecurCall c;
+    const int st = check_recur(c, x, gate, gate_kind, tau, complement, seq_lens, B, T, D, grid_h, grid_w, scan_dir, x_dtype, out_dtype);
+    if (st != GLA_OK) return st;
+    if (any_misaligned((const void *)initial_state, (const void *)out, (const void *)final_state)) return GLA_ERR_ALIGN;
+    plan_forward(c);
+    const int gate_dtype = gate_kind == GLA_GATE_LOG ? GLA_DT_F32 : x_dtype;
+    const size_t n = (size_t)B * T * D, state_bytes = (size_t)B * D * sizeof(float);
+    const Span xs = {x, n * size_of(x_dtype)}, gs = {gate, n * size_of(gate_dtype)}, os = {out, n * size_of(out_dtype)};
+    const Span first = {initial_state, state_bytes}, last = {final_state, state_bytes};
+    // (in place is each element's own place: a wave has read its rows before it writes them, and the first pass is over by then)
+    if (touch(os, xs) && (out != x || out_dtype != x_dtype)) return GLA_ERR_SHAPE;
+    if (touch(os, gs) && (out != gate || out_dtype != gate_dtype)) return GLA_ERR_SHAPE;
+    if (touch(os, first) || touch(os, last) || touch(last, xs) || touch(last, gs) || (touch(first, last) && initial_state != final_state)) return GLA_ERR_SHAPE;
+    if (units_bytes(c, 2) > 0 && (!workspace || misaligned(workspace) || workspace_bytes < units_bytes(c, 2))) return GLA_ERR_WORKSPACE;
+    const hipStream_t stream = static_cast<hipStream_t>(stream_);
+    const RecurUnits u = units_in(c, workspace, false);
+    if (c.nunits > 1) {
+        if (launch_recur_units(c, nullptr, u, stream) != hipSuccess) return GLA_ERR_HIP;
+        if (launch_recur_carry(c, u, initial_state, nullptr, nullptr, stream) != hipSuccess) return GLA_ERR_HIP;
+    }
+    return launch_recur_walk(c, u, initial_state, out, out_dtype, final_state, stream) == hipSuccess ? GLA_OK : GLA_ERR_HIP;
+}
+
+int gla_recur_bwd(const void *x, const void *gate, int gate_kind, float tau, int complement, const int *seq_lens, const void *d_out,
+                  const float *initial_state, const float *d_final_state, int B, int T, int D, int grid_h, int grid_w, int scan_dir, int x_dtype,
+                  int grad_dtype, void *dx, void *d_gate, float *d_initial_state, void *workspace, size_t workspace_bytes, gla_stream_t stream_) {
+    if (!x || !gate || !d_out || !dx || !d_gate) return GLA_ERR_NULL;
+    RecurCall c;
+    const int st = check_recur(c, x, gate, gate_kind, tau, complement, seq_lens, B, T, D, grid_h, grid_w, scan_dir, x_dtype, grad_dtype);
+    if (st != GLA_OK) return st;
+    if (any_misaligned(d_out, (const void *)initial_state, (const void *)d_final_state, (const void *)dx, (const void *)d_gate, (const void *)d_initial_state))
+        return GLA_ERR_ALIGN;
+    plan_backward(c);
+    const size_t n = (size_t)B * T * D, state_bytes = (size_t)B * D * sizeof(float);
+    const Span outs[] = {{dx, n * size_of(grad_dtype)}, {d_gate, n * size_of(grad_dtype)}, {d_initial_state, state_bytes}};
+    const Span ins[] = {{x, n * size_of(x_dtype)}, {gate, n * size_of(gate_kind == GLA_GATE_LOG ? GLA_DT_F32 : x_dtype)}, {d_out, n * size_of(x_dtype)},
+                        {initial_state, state_bytes}, {d_final_state, state_bytes}};
+    if (any_touch(outs, ins)) return GLA_ERR_SHAPE;
+    if (units_bytes(c, 3) > 0 && (!workspace || misaligned(workspace) || workspace_bytes < units_bytes(c, 3))) return GLA_ERR_WORKSPACE;
+    const hipStream_t stream = static_cast<hipStream_t>(stream_);
+    const RecurUnits u = units_in(c, workspace, true);
+    if (c.nunits > 1) {
+        if (launch_recur_units(c, d_out, u, stream) != hipSuccess) return GLA_ERR_HIP;
+        if (launch_recur_carry(c, u, initial_state, d_final_state, d_initial_state, stream) != hipSuccess) return GLA_ERR_HIP;
+    }
+    return launch_recur_back(c, d_out, u, initial_state, d_final_state, dx, d_gate, grad_dtype, d_initial_state, stream) == hipSuccess ? GLA_OK : GLA_ERR_HIP;
+}
+
+int gla_recur_step(const void *x, const void *gate, int gate_kind, float tau, int complement, int B, int D, int x_dtype, int out_dtype,
+                   const float *state, float *state_out, void *out, gla_stream_t stream) {
+    if (!x || !gate || !state || !state_out || !out) return GLA_ERR_NULL;
+    if (B <= 0 || D <= 0 || bad_dtype(x_dtype) || bad_dtype(out_dtype) || (gate_kind != GLA_GATE_LOG && gate_kind != GLA_GATE_PRE)) return GLA_ERR_SHAPE;
+    if (gate_kind == GLA_GATE_PRE && (!(tau > 0.f) || isinf(tau))) return GLA_ERR_SHAPE;
+    if ((long long)B * D >= (1LL << 31)) return GLA_ERR_UNSUPPORTED;
+    const int gate_dtype = gate_kind == GLA_GATE_LOG ? GLA_DT_F32 : x_dtype;
+    if (any_misaligned((const void *)state, (const void *)state_out) || off_element(x, x_dtype) || off_element(gate, gate_dtype) || off_element(out, out_dtype))
+        return GLA_ERR_ALIGN;
+    const size_t n = (size_t)B * D;
+    const Span outs[] = {{out, n * size_of(out_dtype)}};
+    const Span others[] = {{x, n * size_of(x_dtype)}, {gate, n * size_of(gate_dtype)}, {state, n * 4}, {state_out, n * 4}};
+    if (any_touch(outs, others)) return GLA_ERR_SHAPE;
+    if (touch(others[2], others[3]) && state != state_out) return GLA_ERR_SHAPE;
+    if (touch(others[3], others[0]) || touch(others[3], others[1])) return GLA_ERR_SHAPE;
+    RecurCall c = {};
+    c.x = x;
+    c.gate = gate;
+    c.B = B;
+    c.T = 1;
+    c.D = D;
+    c.dtype = x_dtype;
+    c.kind = gate_kind;
+    c.rest = complement != 0;
+    c.inv_tau = gate_kind == GLA_GATE_PRE ? 1.f / tau : 1.f;
+    return launch_recur_step(c, state, state_out, out, out_dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? GLA_OK : GLA_ERR_HIP;
+}
+
+}  // extern "C"
