@@ -644,6 +644,45 @@ size_t gla_recur_bwd_workspace_bytes(int B, int T, int D);
 int gla_recur_step(const void *x, const void *gate, int gate_kind, float tau, int complement, int B, int D, int x_dtype, int out_dtype,
                    const float *state, float *state_out, void *out, gla_stream_t stream);
 
+/*
+ * gla_qk_norm_fwd - norm of each head's query and key row by its root mean square, and the rotation of gla_rope behind it, in one pass:
+ *   n = x / sqrt(mean(x^2) + eps),   y = R (n weight).
+ *
+ *   q, k        DEVICE, dtype, rows of d channels: B x H x T of queries, B x Hk x T of keys; k (and out_k) may be NULL   (read)
+ *   q_strides, k_strides   HOST, elements from one batch, head and token to the next (0 and more; a packed projection's rows, say), or
+ *               NULL: dense, [B,H,T,d] or [B,T,H,d] by `layout`
+ *   q_weight, k_weight   DEVICE, fp32 [d], shared by the heads, or NULL: ones                                 (read)
+ *   eps         >= 0, finite, under the square root
+ *   positions, sections, axes, base, pairing, grid_h, grid_w   as in gla_rope; axes = 0: no rotation (sections may be NULL)
+ *   out_q, out_k   DEVICE, out_dtype, dense in `layout`; may be q and k if these are dense and the element types agree, GLA_ERR_SHAPE where
+ *               they overlap the inputs or each other otherwise                                                 (written)
+ *
+ * 1 <= d <= 256.  q and k may begin at any element, the other tensors at 16 bytes.  Sums and angles as in gla_norm_fwd and gla_rope; a row's
+ * squares have to add up to a finite fp32 number.  Needs no workspace and never allocates.
+ */
+int gla_qk_norm_fwd(const void *q, const long long *q_strides, int H, const void *k, const long long *k_strides, int Hk, const float *q_weight,
+                    const float *k_weight, float eps, const int *positions, const int *sections, int axes, float base, int pairing,
+                    int B, int T, int d, int grid_h, int grid_w, int dtype, int out_dtype, int layout, void *out_q, void *out_k,
+                    gla_stream_t stream);
+
+/*
+ * gla_qk_norm_bwd - gradients of gla_qk_norm_fwd; norms and angles are formed again.
+ *
+ *   d_out_q, d_out_k   DEVICE, dtype, dense in `layout`; the latter NULL exactly if k is                      (read)
+ *   dq, dk      DEVICE, grad_dtype, dense in `layout`                                                         (written)
+ *   dq_weight, dk_weight   DEVICE, fp32 [d], or NULL: not wanted; sums over batches, heads and tokens, always added in one order   (written)
+ *   workspace   DEVICE, 16-byte aligned, gla_qk_norm_bwd_workspace_bytes(...) bytes (Hk = 0 without keys); may be NULL where neither
+ *               weight's gradient is wanted
+ *
+ * Everything else as gla_qk_norm_fwd.  Outputs must not overlap inputs (GLA_ERR_SHAPE).
+ */
+int gla_qk_norm_bwd(const void *q, const long long *q_strides, int H, const void *k, const long long *k_strides, int Hk,
+                    const void *d_out_q, const void *d_out_k, const float *q_weight, const float *k_weight, float eps,
+                    const int *positions, const int *sections, int axes, float base, int pairing, int B, int T, int d, int grid_h, int grid_w,
+                    int dtype, int grad_dtype, int layout, void *dq, void *dk, float *dq_weight, float *dk_weight,
+                    void *workspace, size_t workspace_bytes, gla_stream_t stream);
+size_t gla_qk_norm_bwd_workspace_bytes(int B, int H, int Hk, int T, int d);
+
 /* Bytes of workspace gla_fwd_ex / gla_fwd_layout need for this problem (an upper bound over all
  * launch plans, so it does not depend on tuning options).  0 on invalid sizes. */
 size_t gla_fwd_workspace_bytes(int B, int H, int T, int dk, int dv, int qkv_dtype);

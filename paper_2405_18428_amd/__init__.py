@@ -11,6 +11,7 @@ from .binding import (  # noqa: F401
     gla_decay_fwd, gla_decay_bwd, gla_decay_step, gla_decay_fwd_workspace_bytes, gla_decay_bwd_workspace_bytes, gla_rope,
     gla_norm_fwd, gla_norm_bwd, gla_norm_bwd_workspace_bytes,
     gla_recur_fwd, gla_recur_bwd, gla_recur_step, gla_recur_fwd_workspace_bytes, gla_recur_bwd_workspace_bytes,
+    gla_qk_norm_fwd, gla_qk_norm_bwd, gla_qk_norm_bwd_workspace_bytes,
     gla_set_option, gla_get_option, gla_status_string, gla_version, gla_block_scan_dir,
     SCHEDULE_BLOCK_PROCESS, SCHEDULE_BLOCK_SCAN,
     library_path, load_library, lib_symbols,

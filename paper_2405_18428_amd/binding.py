@@ -116,6 +116,13 @@ def load_library():
     for name in ("gla_recur_fwd_workspace_bytes", "gla_recur_bwd_workspace_bytes"):
         getattr(lib, name).restype = sz
         getattr(lib, name).argtypes = [i] * 3
+    lp, ip = ctypes.POINTER(ctypes.c_longlong), ctypes.POINTER(i)
+    lib.gla_qk_norm_fwd.restype = i
+    lib.gla_qk_norm_fwd.argtypes = [vp, lp, i, vp, lp, i, vp, vp, f, vp, ip, i, f] + [i] * 9 + [vp] * 3
+    lib.gla_qk_norm_bwd.restype = i
+    lib.gla_qk_norm_bwd.argtypes = [vp, lp, i, vp, lp, i] + [vp] * 4 + [f, vp, ip, i, f] + [i] * 9 + [vp] * 5 + [sz, vp]
+    lib.gla_qk_norm_bwd_workspace_bytes.restype = sz
+    lib.gla_qk_norm_bwd_workspace_bytes.argtypes = [i] * 5
     lib.gla_calibrate_mfma.restype = i
     lib.gla_calibrate_mfma.argtypes = [ctypes.POINTER(ctypes.c_double), vp]
     lib.gla_fwd_timed.restype = i
@@ -1020,3 +1027,90 @@ def gla_recur_step(x, gate, state, gate_kind=GATE_PRE, tau=16.0, complement=Fals
         _check(lib.gla_recur_step(x.data_ptr(), gate.data_ptr(), gate_kind, float(tau), int(bool(complement)), B, D, _dt(x), _dt(out),
                                   state.data_ptr(), state_out.data_ptr(), out.data_ptr(), _stream_ptr(stream, x)))
     return out, state_out
+
+
+def _prep_qk(q, k, q_weight, k_weight, positions, sections, layout):
+    """Sizes (B, H, Hk, T, d), both tensors' strides and the sections of a call on rows of queries and keys, after checking the tensors."""
+    torch = _torch()
+    if layout not in (LAYOUT_BHTD, LAYOUT_BTHD):
+        raise ValueError("unknown layout")
+    dev = q.get_device()
+    strides, sizes = [], []
+    for name, t, w in (("q", q, q_weight), ("k", k, k_weight)):
+        if t is None:
+            if w is not None:
+                raise ValueError("k_weight without k")
+            strides.append(None)
+            sizes.append(0)
+            continue
+        if dev < 0 or t.get_device() != dev or t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] > 1):
+            raise ValueError(f"{name} must be a 4-d GPU tensor on the device of the others whose rows' channels lie side by side")
+        if t.dtype is not q.dtype:
+            raise TypeError(f"{name} must be of element type {q.dtype}")
+        B, H, T, d = t.shape if layout == LAYOUT_BHTD else (t.shape[0], t.shape[2], t.shape[1], t.shape[3])
+        if (B, T, d) != (q.shape[0], q.shape[2 if layout == LAYOUT_BHTD else 1], q.shape[3]):
+            raise ValueError("q and k must agree in batches, tokens and channels")
+        if w is not None:
+            _want(name + "_weight", w, (d,), torch.float32, dev)
+        s = t.stride()
+        strides.append((ctypes.c_longlong * 3)(s[0], *((s[1], s[2]) if layout == LAYOUT_BHTD else (s[2], s[1]))))
+        sizes.append(H)
+    _dt(q)
+    axes = len(sections)
+    if positions is not None:
+        _want("positions", positions, (B, T, axes), torch.int32, dev)
+    return (q.shape[0], sizes[0], sizes[1], T, d), strides, (ctypes.c_int * max(axes, 1))(*[int(w) for w in sections])
+
+
+def gla_qk_norm_fwd(q, k, q_weight=None, k_weight=None, sections=(), eps=1e-6, grid_h=0, grid_w=0, positions=None, base=10000.0,
+                    pairing=ROPE_ADJACENT, layout=LAYOUT_BHTD, out_dtype=None, out_q=None, out_k=None, stream=None):
+    """Queries' and keys' rows over their root mean square, times weights fp32 [d], then turned by their positions as in gla_rope (no
+    ``sections``: not turned).  q [B,H,T,d], k [B,Hk,T,d] or None, or [B,T,H,d] by ``layout``; they may be views, of a packed projection
+    for instance, whose last dimension is dense.  The results are dense, of ``out_dtype`` (q's).  Returns (q', k')."""
+    if _elsewhere(stream, q):
+        return _call_on(stream, gla_qk_norm_fwd, locals())
+    lib = load_library()
+    (B, H, Hk, T, d), strides, secs = _prep_qk(q, k, q_weight, k_weight, positions, sections, layout)
+    if k is None and out_k is not None:
+        raise ValueError("out_k without k")
+    dt = q.dtype if out_dtype is None else out_dtype
+    out_q = _like(q, dt) if out_q is None else out_q
+    out_k = _like(k, out_q.dtype) if out_k is None and k is not None else out_k
+    for name, t, like in (("out_q", out_q, q), ("out_k", out_k, k)):
+        if t is not None:
+            _want(name, t, like.shape, out_q.dtype, q.get_device())
+    with _on_device_of(q):
+        _check(lib.gla_qk_norm_fwd(q.data_ptr(), strides[0], H, _ptr(k), strides[1], Hk, _ptr(q_weight), _ptr(k_weight), float(eps), _ptr(positions), secs,
+                                   len(sections), float(base), pairing, B, T, d, grid_h, grid_w, _dt(q), _dt(out_q), layout, out_q.data_ptr(), _ptr(out_k),
+                                   _stream_ptr(stream, q)))
+    return out_q, out_k
+
+
+def gla_qk_norm_bwd_workspace_bytes(B, H, Hk, T, d) -> int:
+    return int(load_library().gla_qk_norm_bwd_workspace_bytes(B, H, Hk, T, d))
+
+
+def gla_qk_norm_bwd(q, k, d_out_q, d_out_k, q_weight=None, k_weight=None, sections=(), eps=1e-6, grid_h=0, grid_w=0, positions=None, base=10000.0,
+                    pairing=ROPE_ADJACENT, layout=LAYOUT_BHTD, grad_dtype=None, want_d_weight=True, workspace=None, stream=None):
+    """Gradients of gla_qk_norm_fwd from those of its outputs (dense, of q's element type): (dq, dk or None, dq_weight or None, dk_weight or
+    None); the first two dense, of ``grad_dtype`` (fp32), the others fp32 where there is a weight and ``want_d_weight``."""
+    if _elsewhere(stream, q):
+        return _call_on(stream, gla_qk_norm_bwd, locals())
+    torch = _torch()
+    lib = load_library()
+    (B, H, Hk, T, d), strides, secs = _prep_qk(q, k, q_weight, k_weight, positions, sections, layout)
+    if (k is None) != (d_out_k is None):
+        raise ValueError("d_out_k belongs to k")
+    _want("d_out_q", d_out_q, q.shape, q.dtype, q.get_device())
+    if k is not None:
+        _want("d_out_k", d_out_k, k.shape, q.dtype, q.get_device())
+    gdt = torch.float32 if grad_dtype is None else grad_dtype
+    dq, dk = _like(q, gdt), None if k is None else _like(k, gdt)
+    dqw, dkw = (w.new_empty(d) if w is not None and want_d_weight else None for w in (q_weight, k_weight))
+    workspace = _room(lambda: gla_qk_norm_bwd_workspace_bytes(B, H, Hk, T, d), workspace, q)
+    with _on_device_of(q):
+        _check(lib.gla_qk_norm_bwd(q.data_ptr(), strides[0], H, _ptr(k), strides[1], Hk, d_out_q.data_ptr(), _ptr(d_out_k), _ptr(q_weight), _ptr(k_weight),
+                                   float(eps), _ptr(positions), secs, len(sections), float(base), pairing, B, T, d, grid_h, grid_w, _dt(q), _dt(dq), layout,
+                                   dq.data_ptr(), _ptr(dk), _ptr(dqw), _ptr(dkw), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                   _stream_ptr(stream, q)))
+    return dq, dk, dqw, dkw

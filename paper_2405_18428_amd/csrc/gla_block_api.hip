@@ -2,6 +2,7 @@
 // keys, the gated feed-forward product.  Argument checks, plans, workspaces.
 #include <math.h>
 
+#include "gla_qk.h"
 #include "gla_recur.h"
 
 namespace gla {
@@ -94,6 +95,65 @@ int check_recur(RecurCall &c, const void *x, const void *gate, int kind, float t
 }
 bool sized_recur(RecurCall &c, int B, int T, int D) {
     return check_recur(c, nullptr, nullptr, GLA_GATE_LOG, 1.f, 0, nullptr, B, T, D, 1, T, 0, GLA_DT_F32, GLA_DT_F32) == GLA_OK;
+}
+
+// --- norm and rotation of queries and keys ---
+
+// Bytes from the first element of a tensor's first row to behind the last of its last
+size_t reach(const QkSide &s, int B, int T, int d, int dtype) {
+    return (size_t)((B - 1) * s.sb + (s.heads - 1) * s.sh + (T - 1) * s.st + d) * size_of(dtype);
+}
+int side_in(QkSide &s, const void *x, const long long *strides, const float *weight, int heads, int T, int d, int layout) {
+    s.x = x;
+    s.weight = weight;
+    s.heads = x != nullptr ? heads : 0;
+    if (strides != nullptr) {
+        s.sb = strides[0];
+        s.sh = strides[1];
+        s.st = strides[2];
+        if (s.sb < 0 || s.sh < 0 || s.st < 0 || s.sb > (1LL << 40) || s.sh > (1LL << 40) || s.st > (1LL << 40)) return GLA_ERR_SHAPE;
+    } else {
+        s.sb = (long long)heads * T * d;
+        s.sh = layout == GLA_LAYOUT_BHTD ? (long long)T * d : d;
+        s.st = layout == GLA_LAYOUT_BHTD ? d : (long long)heads * d;
+    }
+    return GLA_OK;
+}
+int check_qk(QkParams &p, const void *q, const long long *q_strides, int H, const void *k, const long long *k_strides, int Hk, const float *q_weight,
+             const float *k_weight, float eps, const int *positions, const int *sections, int axes, float base, int pairing, int B, int T, int d, int grid_h,
+             int grid_w, int dtype, int other_dtype, int layout) {
+    if (!q || (axes > 0 && !sections) || (!k && k_weight)) return GLA_ERR_NULL;
+    if (B <= 0 || H <= 0 || T <= 0 || d <= 0 || (k && Hk <= 0) || axes < 0 || bad_dtype(dtype) || bad_dtype(other_dtype) ||
+        (layout != GLA_LAYOUT_BHTD && layout != GLA_LAYOUT_BTHD) || (pairing != GLA_ROPE_ADJACENT && pairing != GLA_ROPE_HALVES) || !(eps >= 0.f) || isinf(eps))
+        return GLA_ERR_SHAPE;
+    if (axes > 0 && (!(base > 0.f) || isinf(base))) return GLA_ERR_SHAPE;
+    if (axes > kRopeMaxAxes || d > kRopeMaxD) return GLA_ERR_UNSUPPORTED;
+    p = {};
+    if (axes > 0) {
+        const int st = rope_turns(p.rope, positions, sections, axes, base, T, d, grid_h, grid_w);
+        if (st != GLA_OK) return st;
+    }
+    // 32-bit numbers of tokens and heads
+    if ((long long)B * T >= (1LL << 31) || H > (1 << 20) || Hk > (1 << 20)) return GLA_ERR_UNSUPPORTED;
+    int st = side_in(p.side[0], q, q_strides, q_weight, H, T, d, layout);
+    if (st == GLA_OK) st = side_in(p.side[1], k, k_strides, k_weight, Hk, T, d, layout);
+    if (st != GLA_OK) return st;
+    if (off_element(q, dtype) || off_element(k, dtype) || any_misaligned((const void *)q_weight, (const void *)k_weight) ||
+        (reinterpret_cast<uintptr_t>(positions) & 3u) != 0)
+        return GLA_ERR_ALIGN;
+    p.rope.B = B;
+    p.rope.T = T;
+    p.rope.d = d;
+    p.rope.layout = layout;
+    p.rope.adjacent = pairing == GLA_ROPE_ADJACENT;
+    p.eps = eps;
+    p.out_dtype = other_dtype;
+    return GLA_OK;
+}
+// whether a tensor of rows lies dense in the layout's order
+bool dense(const QkSide &s, int B, int T, int d, int layout) {
+    return (B == 1 || s.sb == (long long)s.heads * T * d) && (s.heads == 1 || s.sh == (layout == GLA_LAYOUT_BHTD ? (long long)T * d : d)) &&
+           (T == 1 || s.st == (layout == GLA_LAYOUT_BHTD ? d : (long long)s.heads * d));
 }
 
 }  // namespace
@@ -194,6 +254,63 @@ int gla_recur_step(const void *x, const void *gate, int gate_kind, float tau, in
     c.rest = complement != 0;
     c.inv_tau = gate_kind == GLA_GATE_PRE ? 1.f / tau : 1.f;
     return launch_recur_step(c, state, state_out, out, out_dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? GLA_OK : GLA_ERR_HIP;
+}
+
+int gla_qk_norm_fwd(const void *q, const long long *q_strides, int H, const void *k, const long long *k_strides, int Hk, const float *q_weight,
+                    const float *k_weight, float eps, const int *positions, const int *sections, int axes, float base, int pairing, int B, int T, int d,
+                    int grid_h, int grid_w, int dtype, int out_dtype, int layout, void *out_q, void *out_k, gla_stream_t stream) {
+    if (!out_q || (k == nullptr) != (out_k == nullptr)) return GLA_ERR_NULL;
+    QkParams p;
+    const int st = check_qk(p, q, q_strides, H, k, k_strides, Hk, q_weight, k_weight, eps, positions, sections, axes, base, pairing, B, T, d, grid_h, grid_w, dtype,
+                            out_dtype, layout);
+    if (st != GLA_OK) return st;
+    if (any_misaligned((const void *)out_q, (const void *)out_k)) return GLA_ERR_ALIGN;
+    const size_t row = (size_t)B * T * d * size_of(out_dtype);
+    const Span xs[] = {{q, reach(p.side[0], B, T, d, dtype)}, {k, k != nullptr ? reach(p.side[1], B, T, d, dtype) : 0}};
+    const Span ys[] = {{out_q, H * row}, {out_k, Hk * row}};
+    // in place is each row's own place
+    if (touch(ys[0], ys[1]) || touch(ys[0], xs[1]) || touch(ys[1], xs[0])) return GLA_ERR_SHAPE;
+    for (int i = 0; i < 2; ++i)
+        if (touch(xs[i], ys[i]) && (xs[i].p != ys[i].p || dtype != out_dtype || !dense(p.side[i], B, T, d, layout))) return GLA_ERR_SHAPE;
+    p.side[0].out = out_q;
+    p.side[1].out = out_k;
+    return launch_qk_fwd(p, dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? GLA_OK : GLA_ERR_HIP;
+}
+
+size_t gla_qk_norm_bwd_workspace_bytes(int B, int H, int Hk, int T, int d) {
+    if (B <= 0 || H <= 0 || Hk < 0 || T <= 0 || d <= 0 || d > kRopeMaxD || (long long)B * T >= (1LL << 31)) return 0;
+    return 2 * align_up((size_t)qk_slots(B, T) * d * sizeof(float));
+}
+
+int gla_qk_norm_bwd(const void *q, const long long *q_strides, int H, const void *k, const long long *k_strides, int Hk, const void *d_out_q, const void *d_out_k,
+                    const float *q_weight, const float *k_weight, float eps, const int *positions, const int *sections, int axes, float base, int pairing, int B,
+                    int T, int d, int grid_h, int grid_w, int dtype, int grad_dtype, int layout, void *dq, void *dk, float *dq_weight, float *dk_weight,
+                    void *workspace, size_t workspace_bytes, gla_stream_t stream) {
+    if (!d_out_q || !dq || (k == nullptr) != (dk == nullptr) || (k == nullptr) != (d_out_k == nullptr) || (!k && dk_weight)) return GLA_ERR_NULL;
+    QkParams p;
+    const int st = check_qk(p, q, q_strides, H, k, k_strides, Hk, q_weight, k_weight, eps, positions, sections, axes, base, pairing, B, T, d, grid_h, grid_w, dtype,
+                            grad_dtype, layout);
+    if (st != GLA_OK) return st;
+    if (any_misaligned(d_out_q, d_out_k, (const void *)dq, (const void *)dk, (const void *)dq_weight, (const void *)dk_weight)) return GLA_ERR_ALIGN;
+    const size_t n = (size_t)B * T * d;
+    const Span outs[] = {{dq, n * H * size_of(grad_dtype)}, {dk, n * Hk * size_of(grad_dtype)}, {dq_weight, d * sizeof(float)}, {dk_weight, d * sizeof(float)}};
+    const Span ins[] = {{q, reach(p.side[0], B, T, d, dtype)}, {k, k != nullptr ? reach(p.side[1], B, T, d, dtype) : 0}, {d_out_q, n * H * size_of(dtype)},
+                        {d_out_k, n * Hk * size_of(dtype)}, {q_weight, d * sizeof(float)}, {k_weight, d * sizeof(float)}};
+    if (any_touch(outs, ins)) return GLA_ERR_SHAPE;
+    if ((dq_weight || dk_weight) && (!workspace || misaligned(workspace) || workspace_bytes < gla_qk_norm_bwd_workspace_bytes(B, H, k ? Hk : 0, T, d)))
+        return GLA_ERR_WORKSPACE;
+    p.slots = qk_slots(B, T);
+    char *room = static_cast<char *>(workspace);
+    const void *ups[] = {d_out_q, d_out_k};
+    void *const downs[] = {dq, dk};
+    float *const sums[] = {dq_weight, dk_weight};
+    for (int i = 0; i < 2; ++i) {
+        p.side[i].d_out = ups[i];
+        p.side[i].out = downs[i];
+        p.side[i].dweight = sums[i];
+        p.side[i].part = sums[i] != nullptr ? reinterpret_cast<float *>(room + i * align_up((size_t)p.slots * d * sizeof(float))) : nullptr;
+    }
+    return launch_qk_bwd(p, dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? GLA_OK : GLA_ERR_HIP;
 }
 
 }  // extern "C"

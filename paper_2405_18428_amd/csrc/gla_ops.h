@@ -35,6 +35,8 @@ struct RopeParams {
     int B, H, T, d, grid_h, grid_w, layout;
     int heads_each;                     // heads a thread turns by one angle
 };
+// Checks and fills in what sections, base and grid say; a status of the C ABI
+int rope_turns(RopeParams &p, const int *positions, const int *sections, int axes, float base, int T, int d, int grid_h, int grid_w);
 hipError_t launch_rope(const RopeParams &p, int dtype, hipStream_t stream);
 
 }  // namespace gla

@@ -150,6 +150,50 @@ bool sized(DecayCall &c, int B, int H, int T, int dk, int dv, int dtype) {
 }
 
 }  // namespace
+
+// Sections, frequencies and grid of a rotation; its other fields are the caller's
+int rope_turns(RopeParams &p, const int *positions, const int *sections, int axes, float base, int T, int d, int grid_h, int grid_w) {
+    if (positions == nullptr) {          // from the grid: the token, its row and column, or its frame, row and column
+        if (axes > 3) return GLA_ERR_SHAPE;
+        if (axes > 1) {
+            if (grid_h <= 0 || grid_w <= 0) return GLA_ERR_SHAPE;
+            const long long cell = (long long)grid_h * grid_w;
+            if (axes == 2 ? cell != T : T % cell != 0) return GLA_ERR_SHAPE;
+        }
+    }
+    int first = 0;
+    for (int a = 0; a < axes; ++a) {
+        const int w = sections[a];
+        if (w < 2 || w % 2 != 0 || w > d - first) return GLA_ERR_SHAPE;
+        p.first[a] = first;
+        p.half[a] = w / 2;
+        // One power a section: 64 of them took longer than the kernel of a few tokens.  Each product is off by 2^-63 more at most, in 64 bits of
+        // mantissa: 128 pairs by 2^-56, which 2^31 / (2 pi) turns make 2^-25 of an angle (of the first pairs' a position; with a base below 1 the
+        // last pairs turn faster and are off by as much more).
+        const long double ratio = powl((long double)base, -2.0L / w);
+        long double turns = 0.159154943091895335768883763372514362L;     // 1 / (2 pi)
+        for (int i = 0; i < w / 2; ++i, turns *= ratio) {
+            double head = (double)turns;
+            uint64_t bits;
+            memcpy(&bits, &head, sizeof bits);
+            bits &= ~0xffffffffull;
+            memcpy(&head, &bits, sizeof bits);
+            p.turns[first / 2 + i] = head;
+            p.rest[first / 2 + i] = (double)(turns - head);
+        }
+        first += w;
+        p.pairs_end[a] = first / 2;
+    }
+    p.positions = positions;
+    p.axes = axes;
+    p.pairs = first / 2;
+    p.T = T;
+    p.d = d;
+    p.grid_h = grid_h;
+    p.grid_w = grid_w;
+    return GLA_OK;
+}
+
 }  // namespace gla
 
 using namespace gla;
@@ -315,38 +359,9 @@ int gla_rope(const void *q, const void *k, const int *positions, const int *sect
         (pairing != GLA_ROPE_ADJACENT && pairing != GLA_ROPE_HALVES) || !(base > 0.f) || isinf(base))
         return GLA_ERR_SHAPE;
     if (axes > kRopeMaxAxes || d > kRopeMaxD) return GLA_ERR_UNSUPPORTED;
-    if (positions == nullptr) {          // from the grid: the token, its row and column, or its frame, row and column
-        if (axes > 3) return GLA_ERR_SHAPE;
-        if (axes > 1) {
-            if (grid_h <= 0 || grid_w <= 0) return GLA_ERR_SHAPE;
-            const long long cell = (long long)grid_h * grid_w;
-            if (axes == 2 ? cell != T : T % cell != 0) return GLA_ERR_SHAPE;
-        }
-    }
     RopeParams p = {};
-    int first = 0;
-    for (int a = 0; a < axes; ++a) {
-        const int w = sections[a];
-        if (w < 2 || w % 2 != 0 || w > d - first) return GLA_ERR_SHAPE;
-        p.first[a] = first;
-        p.half[a] = w / 2;
-        // One power a section: 64 of them took longer than the kernel of a few tokens.  Each product is off by 2^-63 more at most, in 64 bits of
-        // mantissa: 128 pairs by 2^-56, which 2^31 / (2 pi) turns make 2^-25 of an angle (of the first pairs' a position; with a base below 1 the
-        // last pairs turn faster and are off by as much more).
-        const long double ratio = powl((long double)base, -2.0L / w);
-        long double turns = 0.159154943091895335768883763372514362L;     // 1 / (2 pi)
-        for (int i = 0; i < w / 2; ++i, turns *= ratio) {
-            double head = (double)turns;
-            uint64_t bits;
-            memcpy(&bits, &head, sizeof bits);
-            bits &= ~0xffffffffull;
-            memcpy(&head, &bits, sizeof bits);
-            p.turns[first / 2 + i] = head;
-            p.rest[first / 2 + i] = (double)(turns - head);
-        }
-        first += w;
-        p.pairs_end[a] = first / 2;
-    }
+    const int st = rope_turns(p, positions, sections, axes, base, T, d, grid_h, grid_w);
+    if (st != GLA_OK) return st;
     if (any_misaligned(q, k, (const void *)out_q, (const void *)out_k) || (reinterpret_cast<uintptr_t>(positions) & 3u) != 0) return GLA_ERR_ALIGN;
     // in place is each pair's own place: no tensor is turned into another's, nor two into one
     if (k != nullptr && (out_q == out_k || out_q == k || out_k == q)) return GLA_ERR_SHAPE;
@@ -360,17 +375,10 @@ int gla_rope(const void *q, const void *k, const int *positions, const int *sect
     p.x[1] = k;
     p.y[0] = out_q;
     p.y[1] = out_k;
-    p.positions = positions;
-    p.axes = axes;
-    p.pairs = first / 2;
     p.adjacent = pairing == GLA_ROPE_ADJACENT;
     p.inverse = inverse != 0;
     p.B = B;
     p.H = H;
-    p.T = T;
-    p.d = d;
-    p.grid_h = grid_h;
-    p.grid_w = grid_w;
     p.layout = layout;
     p.heads_each = 0;
     return launch_rope(p, dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? GLA_OK : GLA_ERR_HIP;

@@ -7,6 +7,7 @@
 // of some ten thousand would be off by 1e-3 of a turn, with one number of 64 one of 2^31 by 1e-7 and more, and a sine's own reduction is not
 // needed any more.  Bound by HBM.
 #include "gla_ops.h"
+#include "gla_rope_util.h"
 
 namespace gla {
 namespace {
@@ -54,14 +55,6 @@ __device__ inline void store1(char *p, float v) {
     else *reinterpret_cast<float *>(p) = v;
 }
 
-__device__ inline int position(const RopeParams &p, long long token, int n, int axis) {
-    if (p.positions != nullptr) return p.positions[token * p.axes + axis];
-    if (p.axes == 1) return n;
-    const int cell = p.grid_h * p.grid_w, f = n / cell, r = n - f * cell;
-    const int which = p.axes == 2 ? axis + 1 : axis;
-    return which == 0 ? f : which == 1 ? r / p.grid_w : r % p.grid_w;
-}
-
 // VP pairs a thread: 4 where every section has a multiple of 4 pairs, else 1.  Items behind the pairs are the channels behind the last
 // section, copied VP at a time.
 template <typename E, int VP>
@@ -100,10 +93,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeParams p) {
     float cs[VP], sn[VP];
 #pragma unroll
     for (int j = 0; j < VP; ++j) {
-        const double whole = pos * p.turns[pair + j];                    // exact
-        const double turns = __builtin_fma(pos, p.rest[pair + j], whole - __builtin_rint(whole));
-        const float f = (float)(turns - __builtin_rint(turns));          // -1/2 .. 1/2
-        sincospif(2.f * f, &sn[j], &cs[j]);
+        turn(p, pair + j, pos, &cs[j], &sn[j]);
         if (p.inverse) sn[j] = -sn[j];
     }
     const int c0 = p.first[axis] + (p.adjacent ? 2 * i : i), c1 = p.adjacent ? c0 + VP : c0 + p.half[axis];
