@@ -683,6 +683,44 @@ int gla_qk_norm_bwd(const void *q, const long long *q_strides, int H, const void
                     void *workspace, size_t workspace_bytes, gla_stream_t stream);
 size_t gla_qk_norm_bwd_workspace_bytes(int B, int H, int Hk, int T, int d);
 
+/*
+ * gla_glu_fwd - gated feed-forward product: both projections of M tokens, the activation and the product, in one kernel:
+ *   out = act(x w_gate^T) * (x w_up^T).
+ *
+ *   x              DEVICE, dtype, [M,K]                                                                       (read)
+ *   w_gate, w_up   DEVICE, dtype, [F,K]                                                                       (read)
+ *   act            a gla_activation: Swish(g) = g sigmoid(g), GELU g Phi(g), or GELU with
+ *                  Phi(g) ~ (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2
+ *   out            DEVICE, out_dtype, [M,F]                                                                   (written)
+ *   pre            DEVICE, fp32 [2,M,F], or NULL: the two products before the activation, for gla_glu_bwd     (written)
+ *   workspace      DEVICE, 16-byte aligned, gla_glu_fwd_workspace_bytes(...) bytes (0 where rows of K are whole pieces of 16 bytes: may be
+ *                  NULL; else for copies whose rows are)
+ *
+ * Sums in fp32 (bf16 or fp32 MFMA).  Tensors 16-byte aligned.  Outputs must not overlap inputs or each other (GLA_ERR_SHAPE).  K, F up to 2^20.
+ * Never allocates; nothing is kept between calls.  Calls that may overlap, captured ones among them, need workspaces of their own.
+ */
+typedef enum { GLA_ACT_SILU = 0, GLA_ACT_GELU = 1, GLA_ACT_GELU_TANH = 2 } gla_activation;
+int gla_glu_fwd(const void *x, const void *w_gate, const void *w_up, int M, int K, int F, int act, int dtype, int out_dtype,
+                void *out, float *pre, void *workspace, size_t workspace_bytes, gla_stream_t stream);
+size_t gla_glu_fwd_workspace_bytes(int M, int K, int F, int dtype);
+
+/*
+ * gla_glu_bwd - gradients of gla_glu_fwd.  With g, u the two products, dg = d_out u act'(g) and du = d_out act(g):
+ *   dx = dg w_gate + du w_up,   dw_gate = dg^T x,   dw_up = du^T x.
+ *
+ *   d_out       DEVICE, dtype, [M,F]                                                                          (read)
+ *   pre         DEVICE, what gla_glu_fwd left there for the same inputs, or NULL: the products are formed again   (read)
+ *   dx          DEVICE, dtype, [M,K], or NULL: not wanted                                                     (written)
+ *   dw_gate, dw_up   DEVICE, dtype, [F,K], both or neither (NULL: not wanted)                                 (written)
+ *   workspace   DEVICE, 16-byte aligned, gla_glu_bwd_workspace_bytes(...) bytes
+ *
+ * Gradients have the inputs' element type.  From bf16, dg and du are rounded to bf16 once as operands: gradients are off by 1.4 times what
+ * their own rounding takes (2.4e-3 in the 2-norm).  Sums are always added in one order.  Everything else as gla_glu_fwd.
+ */
+int gla_glu_bwd(const void *x, const void *w_gate, const void *w_up, const void *d_out, const float *pre, int M, int K, int F, int act,
+                int dtype, void *dx, void *dw_gate, void *dw_up, void *workspace, size_t workspace_bytes, gla_stream_t stream);
+size_t gla_glu_bwd_workspace_bytes(int M, int K, int F, int dtype);
+
 /* Bytes of workspace gla_fwd_ex / gla_fwd_layout need for this problem (an upper bound over all
  * launch plans, so it does not depend on tuning options).  0 on invalid sizes. */
 size_t gla_fwd_workspace_bytes(int B, int H, int T, int dk, int dv, int qkv_dtype);

@@ -12,11 +12,12 @@ from .binding import (  # noqa: F401
     gla_norm_fwd, gla_norm_bwd, gla_norm_bwd_workspace_bytes,
     gla_recur_fwd, gla_recur_bwd, gla_recur_step, gla_recur_fwd_workspace_bytes, gla_recur_bwd_workspace_bytes,
     gla_qk_norm_fwd, gla_qk_norm_bwd, gla_qk_norm_bwd_workspace_bytes,
+    gla_glu_fwd, gla_glu_bwd, gla_glu_fwd_workspace_bytes, gla_glu_bwd_workspace_bytes,
     gla_set_option, gla_get_option, gla_status_string, gla_version, gla_block_scan_dir,
     SCHEDULE_BLOCK_PROCESS, SCHEDULE_BLOCK_SCAN,
     library_path, load_library, lib_symbols,
     SCAN_ROW_FWD, SCAN_ROW_REV, SCAN_COL_FWD, SCAN_COL_REV, DT_F32, DT_BF16,
     OPT_CHUNKS_PER_SPAN, OPT_ENGINE, OPT_CARRY, OPT_BWD_SPLIT, OPT_RANGE_FALLBACK, OPT_LOOK_BACK_POLLS, ENGINE_AUTO, ENGINE_RECURRENT, ENGINE_MFMA, ENGINE_MFMA_FP16,
     CARRY_AUTO, CARRY_KERNEL, CARRY_IN_OUTPUT_PASS, LAYOUT_BHTD, LAYOUT_BTHD,
-    DECAY_HEAD, DECAY_TOKEN, ROPE_ADJACENT, ROPE_HALVES, GATE_LOG, GATE_PRE,
+    DECAY_HEAD, DECAY_TOKEN, ROPE_ADJACENT, ROPE_HALVES, GATE_LOG, GATE_PRE, ACT_SILU, ACT_GELU, ACT_GELU_TANH,
 )

@@ -20,6 +20,7 @@ LAYOUT_BHTD, LAYOUT_BTHD = 0, 1
 DECAY_HEAD, DECAY_TOKEN = 0, 1
 ROPE_ADJACENT, ROPE_HALVES = 0, 1
 GATE_LOG, GATE_PRE = 0, 1
+ACT_SILU, ACT_GELU, ACT_GELU_TANH = 0, 1, 2
 ENGINE_AUTO, ENGINE_RECURRENT, ENGINE_MFMA, ENGINE_MFMA_FP16 = 0, 1, 2, 3
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -123,6 +124,13 @@ def load_library():
     lib.gla_qk_norm_bwd.argtypes = [vp, lp, i, vp, lp, i] + [vp] * 4 + [f, vp, ip, i, f] + [i] * 9 + [vp] * 5 + [sz, vp]
     lib.gla_qk_norm_bwd_workspace_bytes.restype = sz
     lib.gla_qk_norm_bwd_workspace_bytes.argtypes = [i] * 5
+    lib.gla_glu_fwd.restype = i
+    lib.gla_glu_fwd.argtypes = [vp] * 3 + [i] * 6 + [vp] * 3 + [sz, vp]
+    lib.gla_glu_bwd.restype = i
+    lib.gla_glu_bwd.argtypes = [vp] * 5 + [i] * 5 + [vp] * 4 + [sz, vp]
+    for name in ("gla_glu_fwd_workspace_bytes", "gla_glu_bwd_workspace_bytes"):
+        getattr(lib, name).restype = sz
+        getattr(lib, name).argtypes = [i] * 4
     lib.gla_calibrate_mfma.restype = i
     lib.gla_calibrate_mfma.argtypes = [ctypes.POINTER(ctypes.c_double), vp]
     lib.gla_fwd_timed.restype = i
@@ -1114,3 +1122,62 @@ def gla_qk_norm_bwd(q, k, d_out_q, d_out_k, q_weight=None, k_weight=None, sectio
                                    dq.data_ptr(), _ptr(dk), _ptr(dqw), _ptr(dkw), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                    _stream_ptr(stream, q)))
     return dq, dk, dqw, dkw
+
+
+def _prep_glu(x, w_gate, w_up, pre):
+    """Sizes (M, K, F) of a gated feed-forward product after checking the tensors."""
+    torch = _torch()
+    _dt(x)
+    dev = x.get_device()
+    if x.dim() < 2 or w_gate.dim() != 2:
+        raise ValueError("x must be [..., K], w_gate and w_up [F, K]")
+    K, F = x.shape[-1], w_gate.shape[0]
+    _want("x", x, x.shape, x.dtype, dev)
+    _want("w_gate", w_gate, (F, K), x.dtype, dev)
+    _want("w_up", w_up, (F, K), x.dtype, dev)
+    if pre is not None:
+        _want("pre", pre, (2, *x.shape[:-1], F), torch.float32, dev)
+    return x.numel() // max(K, 1), K, F
+
+
+def gla_glu_fwd_workspace_bytes(M, K, F, dtype=DT_BF16) -> int:
+    return int(load_library().gla_glu_fwd_workspace_bytes(M, K, F, dtype))
+
+
+def gla_glu_bwd_workspace_bytes(M, K, F, dtype=DT_BF16) -> int:
+    return int(load_library().gla_glu_bwd_workspace_bytes(M, K, F, dtype))
+
+
+def gla_glu_fwd(x, w_gate, w_up, act=ACT_SILU, out_dtype=None, out=None, pre=None, workspace=None, stream=None):
+    """Gated feed-forward product act(x w_gate^T) * (x w_up^T): x [..., K], weights [F, K], result [..., F] of ``out_dtype`` (x's).  ``pre``
+    fp32 [2, ..., F] takes the two products before the activation, for gla_glu_bwd."""
+    if _elsewhere(stream, x):
+        return _call_on(stream, gla_glu_fwd, locals())
+    lib = load_library()
+    M, K, F = _prep_glu(x, w_gate, w_up, pre)
+    if out is None:
+        out = x.new_empty((*x.shape[:-1], F), dtype=x.dtype if out_dtype is None else out_dtype)
+    else:
+        _want("out", out, (*x.shape[:-1], F), out.dtype, x.get_device())
+    workspace = _room(lambda: gla_glu_fwd_workspace_bytes(M, K, F, _dt(x)), workspace, x)
+    with _on_device_of(x):
+        _check(lib.gla_glu_fwd(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), M, K, F, act, _dt(x), _dt(out), out.data_ptr(), _ptr(pre),
+                               workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(stream, x)))
+    return out
+
+
+def gla_glu_bwd(x, w_gate, w_up, d_out, act=ACT_SILU, pre=None, want_dx=True, want_dw=True, workspace=None, stream=None):
+    """Gradients of gla_glu_fwd: (dx or None, dw_gate or None, dw_up or None), of x's element type.  ``pre``: what gla_glu_fwd left there for
+    the same inputs; without it the two products are formed again."""
+    if _elsewhere(stream, x):
+        return _call_on(stream, gla_glu_bwd, locals())
+    lib = load_library()
+    M, K, F = _prep_glu(x, w_gate, w_up, pre)
+    _want("d_out", d_out, (*x.shape[:-1], F), x.dtype, x.get_device())
+    dx = _like(x, x.dtype) if want_dx else None
+    dwg, dwu = (_like(w_gate, x.dtype), _like(w_up, x.dtype)) if want_dw else (None, None)
+    workspace = _room(lambda: gla_glu_bwd_workspace_bytes(M, K, F, _dt(x)), workspace, x)
+    with _on_device_of(x):
+        _check(lib.gla_glu_bwd(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), d_out.data_ptr(), _ptr(pre), M, K, F, act, _dt(x), _ptr(dx), _ptr(dwg),
+                               _ptr(dwu), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(stream, x)))
+    return dx, dwg, dwu

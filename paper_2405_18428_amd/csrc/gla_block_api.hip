@@ -2,6 +2,7 @@
 // keys, the gated feed-forward product.  Argument checks, plans, workspaces.
 #include <math.h>
 
+#include "gla_glu.h"
 #include "gla_qk.h"
 #include "gla_recur.h"
 
@@ -154,6 +155,71 @@ int check_qk(QkParams &p, const void *q, const long long *q_strides, int H, cons
 bool dense(const QkSide &s, int B, int T, int d, int layout) {
     return (B == 1 || s.sb == (long long)s.heads * T * d) && (s.heads == 1 || s.sh == (layout == GLA_LAYOUT_BHTD ? (long long)T * d : d)) &&
            (T == 1 || s.st == (layout == GLA_LAYOUT_BHTD ? d : (long long)s.heads * d));
+}
+
+// --- gated feed-forward product ---
+
+constexpr int kGluMost = 1 << 20;       // columns: rows of a tile in 32-bit offsets
+int whole_pieces(int n, int dtype) {    // elements of rows in pieces of 16 bytes
+    const int each = 16 / (int)size_of(dtype);
+    return (n + each - 1) / each * each;
+}
+// Copies of operands whose rows are no whole pieces, and the backward pass's arrays, in a workspace (null: it only counts)
+struct GluRoom {
+    char *x, *w_gate, *w_up, *dg, *du;
+    float *part;
+    size_t bytes;
+};
+GluRoom glu_room(void *workspace, int M, int K, int F, int dtype, bool back) {
+    GluRoom r = {};
+    char *base = static_cast<char *>(workspace);
+    auto take = [&](size_t rows, size_t cols, size_t each) {
+        char *p = base == nullptr ? nullptr : base + r.bytes;
+        r.bytes += align_up(rows * cols * each);
+        return p;
+    };
+    const int ld = whole_pieces(K, dtype);
+    if (ld != K) {
+        r.x = take(M, ld, size_of(dtype));
+        r.w_gate = take(F, ld, size_of(dtype));
+        r.w_up = take(F, ld, size_of(dtype));
+    }
+    if (back) {
+        r.dg = take(M, whole_pieces(F, dtype), size_of(dtype));
+        r.du = take(M, whole_pieces(F, dtype), size_of(dtype));
+        const int splits = glu_splits(M, K, F, dtype);
+        if (splits > 1) r.part = reinterpret_cast<float *>(take((size_t)splits * M, K, sizeof(float)));
+    }
+    return r;
+}
+int check_glu(const void *x, const void *w_gate, const void *w_up, int M, int K, int F, int act, int dtype, int other_dtype) {
+    if (M <= 0 || K <= 0 || F <= 0 || bad_dtype(dtype) || bad_dtype(other_dtype) || act < GLA_ACT_SILU || act > GLA_ACT_GELU_TANH) return GLA_ERR_SHAPE;
+    // (tiles of 128 rows and columns, and four columns a thread, in launches of fewer than 2^32 threads)
+    const long long most = K > F ? K : F;
+    if (K > kGluMost || F > kGluMost || M > (1 << 28) || M * (most + 8) >= (1LL << 34) || F * (long long)(K + 8) >= (1LL << 32)) return GLA_ERR_UNSUPPORTED;
+    return any_misaligned(x, w_gate, w_up) ? GLA_ERR_ALIGN : GLA_OK;
+}
+// The call's operands, copied where their rows are no whole pieces
+int glu_operands(GluCall &c, const GluRoom &room, const void *x, const void *w_gate, const void *w_up, int M, int K, int F, int act, int dtype, hipStream_t stream) {
+    c = {};
+    c.M = M;
+    c.K = K;
+    c.F = F;
+    c.dtype = dtype;
+    c.act = act;
+    c.ld_x = c.ld_w = whole_pieces(K, dtype);
+    c.ld_f = whole_pieces(F, dtype);
+    c.x = x;
+    c.w_gate = w_gate;
+    c.w_up = w_up;
+    if (room.x == nullptr) return GLA_OK;
+    if (launch_glu_pad(x, room.x, M, K, c.ld_x, dtype, stream) != hipSuccess || launch_glu_pad(w_gate, room.w_gate, F, K, c.ld_w, dtype, stream) != hipSuccess ||
+        launch_glu_pad(w_up, room.w_up, F, K, c.ld_w, dtype, stream) != hipSuccess)
+        return GLA_ERR_HIP;
+    c.x = room.x;
+    c.w_gate = room.w_gate;
+    c.w_up = room.w_up;
+    return GLA_OK;
 }
 
 }  // namespace
@@ -311,6 +377,59 @@ int gla_qk_norm_bwd(const void *q, const long long *q_strides, int H, const void
         p.side[i].part = sums[i] != nullptr ? reinterpret_cast<float *>(room + i * align_up((size_t)p.slots * d * sizeof(float))) : nullptr;
     }
     return launch_qk_bwd(p, dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? GLA_OK : GLA_ERR_HIP;
+}
+
+size_t gla_glu_fwd_workspace_bytes(int M, int K, int F, int dtype) {
+    return check_glu(nullptr, nullptr, nullptr, M, K, F, 0, dtype, dtype) == GLA_OK ? glu_room(nullptr, M, K, F, dtype, false).bytes : 0;
+}
+size_t gla_glu_bwd_workspace_bytes(int M, int K, int F, int dtype) {
+    return check_glu(nullptr, nullptr, nullptr, M, K, F, 0, dtype, dtype) == GLA_OK ? glu_room(nullptr, M, K, F, dtype, true).bytes : 0;
+}
+
+int gla_glu_fwd(const void *x, const void *w_gate, const void *w_up, int M, int K, int F, int act, int dtype, int out_dtype, void *out, float *pre, void *workspace,
+                size_t workspace_bytes, gla_stream_t stream_) {
+    if (!x || !w_gate || !w_up || !out) return GLA_ERR_NULL;
+    const int st = check_glu(x, w_gate, w_up, M, K, F, act, dtype, out_dtype);
+    if (st != GLA_OK) return st;
+    if (any_misaligned((const void *)out, (const void *)pre)) return GLA_ERR_ALIGN;
+    const size_t xs = (size_t)M * K * size_of(dtype), ws = (size_t)F * K * size_of(dtype), n = (size_t)M * F;
+    const Span outs[] = {{out, n * size_of(out_dtype)}, {pre, 2 * n * sizeof(float)}};
+    const Span ins[] = {{x, xs}, {w_gate, ws}, {w_up, ws}};
+    if (any_touch(outs, ins)) return GLA_ERR_SHAPE;
+    const GluRoom room = glu_room(workspace, M, K, F, dtype, false);
+    if (room.bytes > 0 && (!workspace || misaligned(workspace) || workspace_bytes < room.bytes)) return GLA_ERR_WORKSPACE;
+    const hipStream_t stream = static_cast<hipStream_t>(stream_);
+    GluCall c;
+    const int laid = glu_operands(c, room, x, w_gate, w_up, M, K, F, act, dtype, stream);
+    if (laid != GLA_OK) return laid;
+    return launch_glu_fwd(c, out, out_dtype, pre, stream) == hipSuccess ? GLA_OK : GLA_ERR_HIP;
+}
+
+int gla_glu_bwd(const void *x, const void *w_gate, const void *w_up, const void *d_out, const float *pre, int M, int K, int F, int act, int dtype, void *dx,
+                void *dw_gate, void *dw_up, void *workspace, size_t workspace_bytes, gla_stream_t stream_) {
+    if (!x || !w_gate || !w_up || !d_out || (dw_gate == nullptr) != (dw_up == nullptr) || (!dx && !dw_gate)) return GLA_ERR_NULL;
+    const int st = check_glu(x, w_gate, w_up, M, K, F, act, dtype, dtype);
+    if (st != GLA_OK) return st;
+    if (any_misaligned(d_out, (const void *)pre, (const void *)dx, (const void *)dw_gate, (const void *)dw_up)) return GLA_ERR_ALIGN;
+    const size_t xs = (size_t)M * K * size_of(dtype), ws = (size_t)F * K * size_of(dtype), n = (size_t)M * F;
+    const Span outs[] = {{dx, xs}, {dw_gate, ws}, {dw_up, ws}};
+    const Span ins[] = {{x, xs}, {w_gate, ws}, {w_up, ws}, {d_out, n * size_of(dtype)}, {pre, 2 * n * sizeof(float)}};
+    if (any_touch(outs, ins)) return GLA_ERR_SHAPE;
+    const GluRoom room = glu_room(workspace, M, K, F, dtype, true);
+    if (!workspace || misaligned(workspace) || workspace_bytes < room.bytes) return GLA_ERR_WORKSPACE;
+    const hipStream_t stream = static_cast<hipStream_t>(stream_);
+    GluCall c;
+    const int laid = glu_operands(c, room, x, w_gate, w_up, M, K, F, act, dtype, stream);
+    if (laid != GLA_OK) return laid;
+    c.d_out = d_out;
+    c.dg = room.dg;
+    c.du = room.du;
+    c.part = room.part;
+    c.splits = glu_splits(M, K, F, dtype);
+    if (launch_glu_slopes(c, pre, stream) != hipSuccess) return GLA_ERR_HIP;
+    if (dx != nullptr && launch_glu_dx(c, dx, stream) != hipSuccess) return GLA_ERR_HIP;
+    if (dw_gate != nullptr && launch_glu_dw(c, dw_gate, dw_up, stream) != hipSuccess) return GLA_ERR_HIP;
+    return GLA_OK;
 }
 
 }  // extern "C"

@@ -1,0 +1,537 @@
+// Gated feed-forward product y = act(x Wg^T) * (x Wu^T) and its backward pass:
+//   g = x Wg^T,  u = x Wu^T,   dg = dy u act'(g),  du = dy act(g),   dx = dg Wg + du Wu,   dWg = dg^T x,  dWu = du^T x.
+//
+// One matrix product kernel serves all four products.  A work-group makes a BM x BN tile of the result from tiles of 128 bytes of the
+// contraction (64 bf16 or 32 fp32 numbers), which go from memory to LDS directly, two of them in turn.  Operands are stored either with the
+// contraction along their rows (x and the weights forward, dg and du for dx) or across them (the weights for dx, both for dW): the latter
+// are transposed on their way from LDS to registers, by the 16-bit transposing read, or number by number in fp32, so that nothing is transposed in memory.
+// Forward the tile's columns are 32 of Wg beside the same 32 of Wu by turns, so that a lane ends with g and u of the same element and the
+// product needs no second pass.  Sums are fp32 MFMA accumulators; fp32 operands go through fp32 MFMA.
+//
+// bf16 calls round dg and du once, to bf16, as operands of the second pair of products: what they lose is as random as the rounding
+// of the results and as large, so that gradients are off by 1.4 times their own rounding.
+#include "gla_glu.h"
+#include "gla_mfma_util.h"
+
+namespace gla {
+namespace {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) void *lds_ptr;
+
+constexpr int kTileBytes = 128;         // of a row of a tile, along the contraction
+enum Product { kForward, kDx, kDw };
+
+struct Activation {
+    float y, slope;
+};
+template <bool SLOPE>
+__device__ __forceinline__ Activation activation(int act, float g) {
+    Activation r;
+    r.slope = 0.f;
+    if (act == GLA_ACT_SILU) {
+        const float s = 1.f / (1.f + __builtin_amdgcn_exp2f(-1.44269504f * g));
+        r.y = g * s;
+        if constexpr (SLOPE) r.slope = s * fmaf(g, 1.f - s, 1.f);
+    } else if (act == GLA_ACT_GELU) {
+        const float phi = 0.5f * erfcf(-0.707106781f * g);
+        r.y = g * phi;
+        if constexpr (SLOPE) r.slope = fmaf(g * 0.398942280f, __builtin_amdgcn_exp2f(-0.721347520f * g * g), phi);
+    } else {                            // g sigmoid(2 k (g + 0.044715 g^3)), k = sqrt(2 / pi)
+        const float q = g * g, s = 1.f / (1.f + __builtin_amdgcn_exp2f(-2.30220819f * g * fmaf(0.044715f, q, 1.f)));
+        r.y = g * s;
+        if constexpr (SLOPE) r.slope = s * fmaf(g * (1.f - s), 1.59576912f * fmaf(0.134145f, q, 1.f), 1.f);
+    }
+    return r;
+}
+
+struct ProductArgs {
+    // operand rows: A has the result's rows, B its columns; second ones for what follows behind the first (see `Product`)
+    const char *a[2], *b[2];
+    long long lda, ldb;                 // bytes
+    int M, N, K;                        // of the result (forward: N = F columns of each product) and of one contraction
+    int tiles_m, tiles_n, splits;
+    int act;
+    void *out[2];                       // forward: [M, N]; dx: [M, N]; dW: two of [M, N]
+    int out_dtype;
+    float *pre, *part;
+    // forward, where dg and du are wanted instead: [M, N], and two of [M, ld_f]
+    const void *d_out;
+    void *slope[2];
+    int ld_f;
+};
+
+template <typename E> struct Frag;
+template <> struct Frag<uint16_t> {
+    u32x4 v;                            // eight numbers along the contraction
+};
+template <> struct Frag<float> {
+    f32x4 v;                            // four
+};
+__device__ __forceinline__ f32x4 mma(const Frag<uint16_t> &n, const Frag<uint16_t> &m, f32x4 acc) {
+    typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, n.v), __builtin_bit_cast(bf16x8, m.v), acc, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma(const Frag<float> &n, const Frag<float> &m, f32x4 acc) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(n.v[j], m.v[j], acc, 0, 0, 0);
+    return acc;
+}
+
+// A tile of one operand, ROWS of the result's rows or columns, in LDS, and what a lane loads and reads of it.
+// Along (ACROSS = false): ROWS rows of 128 bytes, whose eight 16-byte pieces are exchanged by XOR with (row / 2) % 8, so that the 16 rows of a read meet
+// all banks.  ACROSS: 64 (fp32: 32) rows of ROWS numbers, pieces exchanged by a number of the row's that differs between the rows of a read.
+template <typename E, int ROWS, int WAVES, bool ACROSS, bool PAIRED>
+struct Tile {
+    static constexpr int kES = sizeof(E), kDepth = kTileBytes / kES, kBytes = ROWS * kTileBytes, kLoads = kBytes / 1024 / WAVES;
+    static constexpr int kPieces = ROWS * kES / 16;              // of a row, ACROSS
+    uint32_t off[kLoads];               // of the lane's pieces from the operand's first one in the tile, or nowhere
+
+    static __device__ __forceinline__ int turned(int k) { return kES == 2 ? 2 * ((k & 3) | ((k >> 3) & 1) << 2) : 4 * ((k >> 2) & 3); }
+    // row of the tile and piece of the row for the i-th load of a lane
+    static __device__ __forceinline__ void place(int i, int wave, int lane, int &row, int &piece) {
+        const int id = (wave * kLoads + i) * 64 + lane;
+        if constexpr (!ACROSS) {
+            row = id >> 3;
+            piece = (id & 7) ^ ((row >> 1) & 7);
+        } else {
+            row = id / kPieces;
+            piece = (id % kPieces) ^ turned(row);
+        }
+    }
+    // `first`: the tile's first row or column of the result, `limit`: how many there are; `depth`: what is left of the contraction (kDepth and more:
+    // a whole tile); `second`: from the first of a pair of operands to the other, in bytes
+    __device__ __forceinline__ void plan(int wave, int lane, long long ld, int first, int limit, int depth) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            int row, piece;
+            place(i, wave, lane, row, piece);
+            bool in;
+            if constexpr (!ACROSS) {
+                const int r = first + row;
+                in = r < limit && piece * (16 / kES) < depth;
+                off[i] = in ? (uint32_t)(row * ld + piece * 16) : kNowhere;
+            } else {
+                in = row < depth && first + piece * (16 / kES) < limit;
+                off[i] = in ? (uint32_t)(row * ld + piece * 16) : kNowhere;
+            }
+        }
+    }
+    __device__ __forceinline__ void load(const char *base, char *lds, int wave) const {
+        const Rsrc r = view(base, 0x7fffffffu);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)(lds + (wave * kLoads + i) * 1024), 16, (int)off[i], 0, 0, 0);
+    }
+    // 16 rows or columns from `at` on (a multiple of 16), numbers kk of two of the contraction's halves
+    static __device__ __forceinline__ Frag<E> read(const char *lds, int at, int kk, int lane) {
+        const int l = lane & 15, g = lane >> 4;
+        Frag<E> f;
+        if constexpr (!ACROSS) {
+            f.v = *reinterpret_cast<const decltype(f.v) *>(lds + (at + l) * kTileBytes + (((4 * kk + g) ^ ((l >> 1) & 7)) << 4));
+        } else if constexpr (kES == 2) {
+            const int k = 32 * kk + 8 * g + (l >> 2);
+            const char *p = lds + k * (ROWS * 2) + ((((at >> 4) ^ (turned(k) >> 1)) << 5) | ((l & 3) << 3));
+            typedef __attribute__((address_space(3))) s16x4 *lds_s4;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)p), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(p + 4 * ROWS * 2));
+            const u32x2 x = __builtin_bit_cast(u32x2, lo), y = __builtin_bit_cast(u32x2, hi);
+            f.v = u32x4{x[0], x[1], y[0], y[1]};
+        } else {
+            const int k = 16 * kk + 4 * g;
+            const char *p = lds + k * (ROWS * 4) + ((((at >> 4) ^ g) << 6) | (l << 2));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f.v[j] = *reinterpret_cast<const float *>(p + j * ROWS * 4);
+        }
+        return f;
+    }
+};
+
+// Four neighbouring results to a row of a tensor of n columns
+__device__ __forceinline__ void store4(void *base, int dtype, long long row, int col, int n, f32x4 v) {
+    if (dtype == GLA_DT_BF16) {
+        uint16_t *p = static_cast<uint16_t *>(base) + row * n + col;
+        const u32x2 b = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        if (n % 4 == 0) {
+            *reinterpret_cast<u32x2 *>(p) = b;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (col + i < n) p[i] = (uint16_t)(b[i >> 1] >> (16 * (i & 1)));
+        }
+    } else {
+        float *p = static_cast<float *>(base) + row * n + col;
+        if (n % 4 == 0) {
+            *reinterpret_cast<f32x4 *>(p) = v;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (col + i < n) p[i] = v[i];
+        }
+    }
+}
+
+// Eight
+__device__ __forceinline__ void store8(void *base, int dtype, long long row, int col, int n, f32x4 v, f32x4 w) {
+    if (dtype == GLA_DT_BF16 && n % 8 == 0) {
+        if (col < n)
+            *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(base) + row * n + col) =
+                u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3])};
+        return;
+    }
+    if (col < n) store4(base, dtype, row, col, n, v);
+    if (col + 4 < n) store4(base, dtype, row, col + 4, n, w);
+}
+
+// dg = dy u act'(g), du = dy act(g) of four neighbouring columns, those from n on as zeros; dy [., n]
+template <typename E>
+__device__ __forceinline__ void slopes(int act, const E *d_out, long long row, int col, int n, f32x4 g, f32x4 u, f32x4 &dg, f32x4 &du) {
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    const E *p = d_out + row * n + col;
+    if (n % 4 == 0) {
+        if (col < n) {
+            if constexpr (sizeof(E) == 2) {
+                const u32x2 b = *reinterpret_cast<const u32x2 *>(p);
+                o = f32x4{bf16_lo_as_float(b[0]), bf16_hi_as_float(b[0]), bf16_lo_as_float(b[1]), bf16_hi_as_float(b[1])};
+            } else {
+                o = *reinterpret_cast<const f32x4 *>(p);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (col + i < n) {
+                if constexpr (sizeof(E) == 2) o[i] = bf16_bits_to_float(p[i]);
+                else o[i] = p[i];
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const Activation a = activation<true>(act, g[i]);
+        dg[i] = col + i < n ? o[i] * u[i] * a.slope : 0.f;
+        du[i] = col + i < n ? o[i] * a.y : 0.f;
+    }
+}
+
+// Tiles of a work-group: work-groups go to the eight XCDs by turns, so each XCD gets a run of tiles, and a run goes down eight rows of tiles
+// before it goes on to the next column, so that what an XCD reads at a time stays in its L2.
+__device__ __forceinline__ void tile_of(const ProductArgs &p, int &tm, int &tn) {
+    const int count = p.tiles_m * p.tiles_n, id = blockIdx.x;
+    const int xcd = id & 7, each = count >> 3, more = count & 7;
+    const int t = xcd * each + min(xcd, more) + (id >> 3);
+    constexpr int kDown = 8;
+    const int band = t / (kDown * p.tiles_n), in = t - band * kDown * p.tiles_n;
+    const int high = min(kDown, p.tiles_m - band * kDown);
+    tn = in / high;
+    tm = band * kDown + in - tn * high;
+}
+
+template <typename E, Product P, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs p) {
+    constexpr int kWaves = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
+    static_assert(P != kForward || NI == 4, "32 columns of each product a wave");
+    constexpr int kES = sizeof(E);
+    using TA = Tile<E, BM, kWaves, P == kDw, false>;
+    using TB = Tile<E, P == kForward ? BN / 2 : BN, kWaves, P != kForward, false>;     // (forward: one of each matrix)
+    constexpr int kDepth = TA::kDepth, kPair = P == kForward ? 2 : 1;
+    __shared__ __attribute__((aligned(1024))) char lds[2][TA::kBytes + kPair * TB::kBytes];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int wm = wave / WN, wn = wave - wm * WN;
+    int tm, tn;
+    tile_of(p, tm, tn);
+    // dW: tiles of the first matrix' rows, then those of the second
+    const int half_tiles = p.tiles_m / 2, which = P == kDw ? tm >= half_tiles : 0;
+    const int m0 = (P == kDw ? tm - which * half_tiles : tm) * BM, n0 = tn * (P == kForward ? BN / 2 : BN);
+
+    // tiles of the contraction; dx: those of the first product, then those of the second
+    const int tiles = (p.K + kDepth - 1) / kDepth, all = P == kDx ? 2 * tiles : tiles;
+    const int each = (all + p.splits - 1) / p.splits, t0 = min((int)blockIdx.y * each, all), t1 = min(t0 + each, all);
+    TA ta;
+    TB tb;
+    ta.plan(wave, lane, p.lda, m0, p.M, kDepth);
+    tb.plan(wave, lane, p.ldb, n0, p.N, kDepth);
+    auto load = [&](int t, int buf) __attribute__((always_inline)) {
+        const int seg = P == kDx ? t >= tiles : 0, k0 = (P == kDx ? t - seg * tiles : t) * kDepth;
+        const char *a = p.a[P == kDw ? which : seg] + (P == kDw ? k0 * p.lda + (long long)m0 * kES : m0 * p.lda + (long long)k0 * kES);
+        const char *b = p.b[seg] + (P == kForward ? n0 * p.ldb + (long long)k0 * kES : k0 * p.ldb + (long long)n0 * kES);
+        char *at = lds[buf];
+        if (k0 + kDepth <= p.K) {
+            ta.load(a, at, wave);
+            tb.load(b, at + TA::kBytes, wave);
+            if constexpr (P == kForward) tb.load(p.b[1] + n0 * p.ldb + (long long)k0 * kES, at + TA::kBytes + TB::kBytes, wave);
+        } else {
+            TA ea;
+            TB eb;
+            ea.plan(wave, lane, p.lda, m0, p.M, p.K - k0);
+            eb.plan(wave, lane, p.ldb, n0, p.N, p.K - k0);
+            ea.load(a, at, wave);
+            eb.load(b, at + TA::kBytes, wave);
+            if constexpr (P == kForward) eb.load(p.b[1] + n0 * p.ldb + (long long)k0 * kES, at + TA::kBytes + TB::kBytes, wave);
+        }
+    };
+    f32x4 acc[MI][NI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (t0 < t1) load(t0, 0);
+    __syncthreads();                     // (waits for what goes to LDS, too)
+    for (int t = t0; t < t1; ++t) {
+        const int buf = (t - t0) & 1;
+        if (t + 1 < t1) load(t + 1, buf ^ 1);
+        const char *at = lds[buf], *bt = at + TA::kBytes;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            Frag<E> fa[MI], fb[NI];
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                if constexpr (P == kForward) fb[j] = TB::read(bt + (j >> 1) * TB::kBytes, wn * 32 + (j & 1) * 16, kk, lane);
+                else fb[j] = TB::read(bt, (wn * NI + j) * 16, kk, lane);
+            }
+#pragma unroll
+            for (int i = 0; i < MI; ++i) fa[i] = TA::read(at, (wm * MI + i) * 16, kk, lane);
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j) acc[i][j] = mma(fb[j], fa[i], acc[i][j]);
+        }
+        __syncthreads();
+    }
+    // The tile goes through LDS, some rows of each wave at a time, so that a work-group stores whole rows and each result's code stands here once.
+    // A lane has four neighbouring columns of one row of each 16 x 16 piece; pieces of 16 bytes are exchanged by XOR with the row.
+    constexpr int kRows = sizeof(lds) / (BN * 4) < BM ? sizeof(lds) / (BN * 4) : BM, kPasses = BM / kRows, kSub = MI / kPasses;
+    constexpr int kOut = P == kForward ? BN / 2 : BN, kThreadsARow = kOut / 8, kAtOnce = 64 * kWaves / kThreadsARow;
+    static_assert(kRows * kPasses == BM && kSub * kPasses == MI && kRows % kAtOnce == 0, "");
+    char *const tile = lds[0];
+    const int l = lane & 15, g = lane >> 4;
+    const int col = (threadIdx.x % kThreadsARow) * 8, row0 = threadIdx.x / kThreadsARow, n = n0 + col;
+#pragma unroll
+    for (int pass = 0; pass < kPasses; ++pass) {
+        if (pass > 0) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kSub; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                const int r = (wm * kSub + i) * 16 + l, piece = (wn * NI + j) * 4 + g;
+                *reinterpret_cast<f32x4 *>(tile + r * (BN * 4) + ((piece ^ l) << 4)) = acc[pass * kSub + i][j];
+            }
+        __syncthreads();
+        // four at column c of the tile
+        auto at = [&](int r, int c) { return *reinterpret_cast<const f32x4 *>(tile + r * (BN * 4) + (((c >> 2) ^ (r & 15)) << 4)); };
+#pragma unroll 1
+        for (int r = row0; r < kRows; r += kAtOnce) {
+            const int sub = r >> 4, m = m0 + ((sub / kSub) * MI + pass * kSub + sub % kSub) * 16 + (r & 15);
+            if (m >= p.M) continue;
+            if constexpr (P == kForward) {
+                const int c = (col >> 5) * 64 + (col & 31);
+                const f32x4 gt[2] = {at(r, c), at(r, c + 4)}, up[2] = {at(r, c + 32), at(r, c + 36)};
+                if (p.d_out != nullptr) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (n + 4 * h >= p.ld_f) continue;
+                        f32x4 dg, du;
+                        slopes<E>(p.act, static_cast<const E *>(p.d_out), m, n + 4 * h, p.N, gt[h], up[h], dg, du);
+                        store4(p.slope[0], kES == 2 ? GLA_DT_BF16 : GLA_DT_F32, m, n + 4 * h, p.ld_f, dg);
+                        store4(p.slope[1], kES == 2 ? GLA_DT_BF16 : GLA_DT_F32, m, n + 4 * h, p.ld_f, du);
+                    }
+                    continue;
+                }
+                if (p.pre != nullptr) {
+                    store8(p.pre, GLA_DT_F32, m, n, p.N, gt[0], gt[1]);
+                    store8(p.pre + (long long)p.M * p.N, GLA_DT_F32, m, n, p.N, up[0], up[1]);
+                }
+                f32x4 y[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[h][e] = activation<false>(p.act, gt[h][e]).y * up[h][e];
+                store8(p.out[0], p.out_dtype, m, n, p.N, y[0], y[1]);
+            } else if (P == kDx && p.splits > 1) {
+                store8(p.part + (long long)blockIdx.y * p.M * p.N, GLA_DT_F32, m, n, p.N, at(r, col), at(r, col + 4));
+            } else {
+                store8(p.out[which], p.out_dtype, m, n, p.N, at(r, col), at(r, col + 4));
+            }
+        }
+    }
+}
+
+// dx from the parts of its sum, added in one order; four numbers a thread
+__global__ __launch_bounds__(256) void join_kernel(const float *part, void *out, int dtype, long long count, int splits) {
+    const long long at = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (at >= count) return;
+    if (at + 4 <= count && count % 4 == 0) {
+        f32x4 s = *reinterpret_cast<const f32x4 *>(part + at);
+        for (int i = 1; i < splits; ++i) s += *reinterpret_cast<const f32x4 *>(part + i * count + at);
+        if (dtype == GLA_DT_BF16) {
+            const u32x2 b = {pack_bf16(s[0], s[1]), pack_bf16(s[2], s[3])};
+            *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(out) + at) = b;
+        } else {
+            *reinterpret_cast<f32x4 *>(static_cast<float *>(out) + at) = s;
+        }
+        return;
+    }
+    for (long long e = at; e < count && e < at + 4; ++e) {
+        float s = part[e];
+        for (int i = 1; i < splits; ++i) s += part[i * count + e];
+        if (dtype == GLA_DT_BF16) static_cast<uint16_t *>(out)[e] = (uint16_t)pack_bf16(s, 0.f);
+        else static_cast<float *>(out)[e] = s;
+    }
+}
+
+// dg and du of the two products that a forward call has kept: four columns a thread, those from F to the end of a row as zeros
+template <typename E>
+__global__ __launch_bounds__(256) void slopes_kernel(const GluCall c, const float *pre) {
+    const int pieces = c.ld_f / 4;
+    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+    const long long m = id / pieces;
+    const int f = (int)(id - m * pieces) * 4;
+    if (m >= c.M) return;
+    const float *g = pre + m * c.F + f, *u = g + (long long)c.M * c.F;
+    f32x4 gt = {0, 0, 0, 0}, up = gt, dg, du;
+    if (c.F % 4 == 0) {
+        if (f < c.F) {
+            gt = *reinterpret_cast<const f32x4 *>(g);
+            up = *reinterpret_cast<const f32x4 *>(u);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (f + i < c.F) {
+                gt[i] = g[i];
+                up[i] = u[i];
+            }
+    }
+    slopes<E>(c.act, static_cast<const E *>(c.d_out), m, f, c.F, gt, up, dg, du);
+    store4(c.dg, c.dtype, m, f, c.ld_f, dg);
+    store4(c.du, c.dtype, m, f, c.ld_f, du);
+}
+
+template <typename E>
+__global__ __launch_bounds__(256) void pad_kernel(const E *from, E *to, int rows, int cols, int ld) {
+    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+    const long long r = id / ld;
+    const int c = (int)(id - r * ld);
+    if (r < rows) to[id] = c < cols ? from[r * cols + c] : (E)0;
+}
+
+template <typename E, Product P, int BM, int BN, int WM, int WN>
+hipError_t product(ProductArgs p, hipStream_t stream) {
+    p.tiles_m = (p.M + BM - 1) / BM * (P == kDw ? 2 : 1);
+    const int wide = P == kForward ? BN / 2 : BN;
+    p.tiles_n = (p.N + wide - 1) / wide;
+    hipLaunchKernelGGL((product_kernel<E, P, BM, BN, WM, WN>), dim3((unsigned)p.tiles_m * (unsigned)p.tiles_n, (unsigned)p.splits), dim3(64 * WM * WN), 0,
+                       stream, p);
+    return hipGetLastError();
+}
+// whether tiles of 256 x 256 leave few compute units idle
+bool large(long long M, long long N) { return ((M + 255) / 256) * ((N + 255) / 256) >= 192; }
+
+template <Product P>
+hipError_t product_of(const ProductArgs &p, int dtype, hipStream_t stream) {
+    const long long M = (long long)p.M * (P == kDw ? 2 : 1), N = (long long)p.N * (P == kForward ? 2 : 1);
+    if (dtype == GLA_DT_BF16) return large(M, N) ? product<uint16_t, P, 256, 256, 2, 4>(p, stream) : product<uint16_t, P, 128, 128, 2, 2>(p, stream);
+    return large(M, N) ? product<float, P, 256, 256, 2, 4>(p, stream) : product<float, P, 128, 128, 2, 2>(p, stream);
+}
+int element(int dtype) { return dtype == GLA_DT_BF16 ? 2 : 4; }
+
+}  // namespace
+
+static ProductArgs forward_args(const GluCall &c) {
+    ProductArgs p = {};
+    p.a[0] = static_cast<const char *>(c.x);
+    p.b[0] = static_cast<const char *>(c.w_gate);
+    p.b[1] = static_cast<const char *>(c.w_up);
+    p.lda = (long long)c.ld_x * element(c.dtype);
+    p.ldb = (long long)c.ld_w * element(c.dtype);
+    p.M = c.M;
+    p.N = c.F;
+    p.K = c.ld_x;                        // (columns behind K are zeros)
+    p.splits = 1;
+    p.act = c.act;
+    return p;
+}
+
+hipError_t launch_glu_fwd(const GluCall &c, void *out, int out_dtype, float *pre, hipStream_t stream) {
+    ProductArgs p = forward_args(c);
+    p.out[0] = out;
+    p.out_dtype = out_dtype;
+    p.pre = pre;
+    return product_of<kForward>(p, c.dtype, stream);
+}
+
+hipError_t launch_glu_slopes(const GluCall &c, const float *pre, hipStream_t stream) {
+    if (pre == nullptr) {                // the two products again
+        ProductArgs p = forward_args(c);
+        p.d_out = c.d_out;
+        p.slope[0] = c.dg;
+        p.slope[1] = c.du;
+        p.ld_f = c.ld_f;
+        return product_of<kForward>(p, c.dtype, stream);
+    }
+    const long long threads = (long long)c.M * (c.ld_f / 4);
+    const dim3 grid((unsigned)((threads + 255) / 256));
+    if (c.dtype == GLA_DT_BF16) hipLaunchKernelGGL(slopes_kernel<uint16_t>, grid, dim3(256), 0, stream, c, pre);
+    else hipLaunchKernelGGL(slopes_kernel<float>, grid, dim3(256), 0, stream, c, pre);
+    return hipGetLastError();
+}
+
+int glu_splits(int M, int K, int F, int dtype) {
+    // tiles of 128 x 128 that leave compute units idle: the sum over F in parts of eight tiles and more
+    const long long tiles = (long long)((M + 127) / 128) * ((K + 127) / 128);
+    const int depth = kTileBytes / element(dtype), steps = 2 * ((F + depth - 1) / depth);
+    long long n = tiles >= 256 ? 1 : 512 / tiles;
+    if (n > steps / 8) n = steps / 8;
+    if (n > 32) n = 32;
+    return n < 2 ? 1 : (int)n;
+}
+
+hipError_t launch_glu_dx(const GluCall &c, void *dx, hipStream_t stream) {
+    ProductArgs p = {};
+    p.a[0] = static_cast<const char *>(c.dg);
+    p.a[1] = static_cast<const char *>(c.du);
+    p.b[0] = static_cast<const char *>(c.w_gate);
+    p.b[1] = static_cast<const char *>(c.w_up);
+    p.lda = (long long)c.ld_f * element(c.dtype);
+    p.ldb = (long long)c.ld_w * element(c.dtype);
+    p.M = c.M;
+    p.N = c.K;
+    p.K = c.F;
+    p.splits = c.splits;
+    p.out[0] = dx;
+    p.out_dtype = c.dtype;
+    p.part = c.part;
+    if (c.splits == 1) return product_of<kDx>(p, c.dtype, stream);
+    const hipError_t e = c.dtype == GLA_DT_BF16 ? product<uint16_t, kDx, 128, 128, 2, 2>(p, stream) : product<float, kDx, 128, 128, 2, 2>(p, stream);
+    if (e != hipSuccess) return e;
+    const long long count = (long long)c.M * c.K;
+    hipLaunchKernelGGL(join_kernel, dim3((unsigned)((count + 1023) / 1024)), dim3(256), 0, stream, c.part, dx, c.dtype, count, c.splits);
+    return hipGetLastError();
+}
+
+hipError_t launch_glu_dw(const GluCall &c, void *dw_gate, void *dw_up, hipStream_t stream) {
+    ProductArgs p = {};
+    p.a[0] = static_cast<const char *>(c.dg);
+    p.a[1] = static_cast<const char *>(c.du);
+    p.b[0] = static_cast<const char *>(c.x);
+    p.lda = (long long)c.ld_f * element(c.dtype);
+    p.ldb = (long long)c.ld_x * element(c.dtype);
+    p.M = c.F;
+    p.N = c.K;
+    p.K = c.M;
+    p.splits = 1;
+    p.out[0] = dw_gate;
+    p.out[1] = dw_up;
+    p.out_dtype = c.dtype;
+    return product_of<kDw>(p, c.dtype, stream);
+}
+
+hipError_t launch_glu_pad(const void *from, void *to, int rows, int cols, int ld, int dtype, hipStream_t stream) {
+    const dim3 grid((unsigned)(((long long)rows * ld + 255) / 256));
+    if (dtype == GLA_DT_BF16)
+        hipLaunchKernelGGL(pad_kernel<uint16_t>, grid, dim3(256), 0, stream, static_cast<const uint16_t *>(from), static_cast<uint16_t *>(to), rows, cols, ld);
+    else
+        hipLaunchKernelGGL(pad_kernel<float>, grid, dim3(256), 0, stream, static_cast<const float *>(from), static_cast<float *>(to), rows, cols, ld);
+    return hipGetLastError();
+}
+
+}  // namespace gla
