@@ -40,31 +40,33 @@ bool any_touch(const Span (&mine)[N], const Span (&others)[M]) {
 
 // --- gated recurrence of channels ---
 
-// Units of the forward pass.  Work-groups have 256 channels (fewer where rows allow only narrow loads); spans so short that about kWantGroups
-// of them run, none shorter than four rounds where that still fills the GPU.
-constexpr int kWantGroups = 1024, kWholeSteps = 128;
+// Forward: the sequence in units, unless a work-group may as well walk it
+constexpr int kWalkGroups = 512;
 void plan_forward(RecurCall &c) {
-    const long long groups = ((long long)c.B * c.D + 255) / 256;
-    long long n = kWantGroups / groups;
-    const int rounds = (c.T + kRecurRound - 1) / kRecurRound;
-    if (n > rounds) n = rounds;
-    if (n < 2 || c.T <= kWholeSteps) n = 1;
-    const int each = (int)((rounds + n - 1) / n);
-    c.unit = each * kRecurRound;
-    c.nunits = (rounds + each - 1) / each;
+    const bool units = c.T > kRecurChain && ((long long)c.B * c.D + 127) / 128 < kWalkGroups;
+    c.unit = units ? kRecurChain : c.T;
+    c.nunits = units ? (c.T + kRecurChain - 1) / kRecurChain : 1;
 }
 void plan_backward(RecurCall &c) {
     c.unit = kRecurRound;
     c.nunits = (c.T + kRecurRound - 1) / kRecurRound;
 }
-size_t units_bytes(const RecurCall &c, int numbers) {
-    return c.nunits > 1 ? numbers * align_up((size_t)c.B * c.nunits * c.D * sizeof(float)) : 0;
+// The words that units publish, and the ticket
+size_t chain_bytes(const RecurCall &c) { return c.nunits > 1 ? align_up((size_t)(recur_chain_columns(c) * recur_chain_words(c)) * 4) + 256 : 0; }
+RecurChain chain_in(const RecurCall &c, void *workspace, bool in_place) {
+    char *p = static_cast<char *>(workspace);
+    RecurChain r;
+    r.local = reinterpret_cast<unsigned long long *>(p);
+    r.after = reinterpret_cast<uint32_t *>(p + (size_t)recur_chain_columns(c) * c.nunits * 8);
+    r.ticket = reinterpret_cast<uint32_t *>(p + chain_bytes(c) - 256);
+    r.polls = in_place ? 0x7fffffff : gla_get_option(GLA_OPT_LOOK_BACK_POLLS);
+    return r;
 }
-RecurUnits units_in(const RecurCall &c, void *workspace, bool adjoint) {
+size_t units_bytes(const RecurCall &c) { return c.nunits > 1 ? 3 * align_up((size_t)c.B * c.nunits * c.D * sizeof(float)) : 0; }
+RecurUnits units_in(const RecurCall &c, void *workspace) {
     const size_t each = align_up((size_t)c.B * c.nunits * c.D * sizeof(float));
     char *p = static_cast<char *>(workspace);
-    if (c.nunits == 1) return {};
-    return {reinterpret_cast<float *>(p), reinterpret_cast<float *>(p + each), adjoint ? reinterpret_cast<float *>(p + 2 * each) : nullptr};
+    return {reinterpret_cast<float *>(p), reinterpret_cast<float *>(p + each), reinterpret_cast<float *>(p + 2 * each)};
 }
 
 int check_recur(RecurCall &c, const void *x, const void *gate, int kind, float tau, int complement, const int *seq_lens, int B, int T, int D,
@@ -88,6 +90,9 @@ int check_recur(RecurCall &c, const void *x, const void *gate, int kind, float t
     c.grid_h = grid_h;
     c.grid_w = grid_w;
     c.scan_dir = scan_dir;
+    const bool back = scan_dir & 1;
+    c.step = (scan_dir >= GLA_SCAN_COL_FWD ? (long long)grid_w : 1) * (back ? -D : D);
+    c.wrap = (1 - (long long)(grid_h - 1) * grid_w) * (back ? -D : D);
     c.dtype = dtype;
     c.kind = kind;
     c.rest = complement != 0;
@@ -233,13 +238,13 @@ size_t gla_recur_fwd_workspace_bytes(int B, int T, int D) {
     RecurCall c;
     if (!sized_recur(c, B, T, D)) return 0;
     plan_forward(c);
-    return units_bytes(c, 2);
+    return chain_bytes(c);
 }
 size_t gla_recur_bwd_workspace_bytes(int B, int T, int D) {
     RecurCall c;
     if (!sized_recur(c, B, T, D)) return 0;
     plan_backward(c);
-    return units_bytes(c, 3);
+    return units_bytes(c);
 }
 
 int gla_recur_fwd(const void *x, const void *gate, int gate_kind, float tau, int complement, const int *seq_lens, int B, int T, int D,
@@ -255,18 +260,16 @@ int gla_recur_fwd(const void *x, const void *gate, int gate_kind, float tau, int
     const size_t n = (size_t)B * T * D, state_bytes = (size_t)B * D * sizeof(float);
     const Span xs = {x, n * size_of(x_dtype)}, gs = {gate, n * size_of(gate_dtype)}, os = {out, n * size_of(out_dtype)};
     const Span first = {initial_state, state_bytes}, last = {final_state, state_bytes};
-    // (in place is each element's own place: a wave has read its rows before it writes them, and the first pass is over by then)
+    // (in place is each element's own place: a wave has read its rows before it writes them)
+    const bool in_place = touch(os, xs) || touch(os, gs);
     if (touch(os, xs) && (out != x || out_dtype != x_dtype)) return GLA_ERR_SHAPE;
     if (touch(os, gs) && (out != gate || out_dtype != gate_dtype)) return GLA_ERR_SHAPE;
     if (touch(os, first) || touch(os, last) || touch(last, xs) || touch(last, gs) || (touch(first, last) && initial_state != final_state)) return GLA_ERR_SHAPE;
-    if (units_bytes(c, 2) > 0 && (!workspace || misaligned(workspace) || workspace_bytes < units_bytes(c, 2))) return GLA_ERR_WORKSPACE;
+    if (chain_bytes(c) > 0 && (!workspace || misaligned(workspace) || workspace_bytes < chain_bytes(c))) return GLA_ERR_WORKSPACE;
     const hipStream_t stream = static_cast<hipStream_t>(stream_);
-    const RecurUnits u = units_in(c, workspace, false);
-    if (c.nunits > 1) {
-        if (launch_recur_units(c, nullptr, u, stream) != hipSuccess) return GLA_ERR_HIP;
-        if (launch_recur_carry(c, u, initial_state, nullptr, nullptr, stream) != hipSuccess) return GLA_ERR_HIP;
-    }
-    return launch_recur_walk(c, u, initial_state, out, out_dtype, final_state, stream) == hipSuccess ? GLA_OK : GLA_ERR_HIP;
+    const hipError_t e = c.nunits == 1 ? launch_recur_walk(c, initial_state, out, out_dtype, final_state, stream)
+                                       : launch_recur_chain(c, chain_in(c, workspace, in_place), initial_state, out, out_dtype, final_state, stream);
+    return e == hipSuccess ? GLA_OK : GLA_ERR_HIP;
 }
 
 int gla_recur_bwd(const void *x, const void *gate, int gate_kind, float tau, int complement, const int *seq_lens, const void *d_out,
@@ -284,9 +287,9 @@ int gla_recur_bwd(const void *x, const void *gate, int gate_kind, float tau, int
     const Span ins[] = {{x, n * size_of(x_dtype)}, {gate, n * size_of(gate_kind == GLA_GATE_LOG ? GLA_DT_F32 : x_dtype)}, {d_out, n * size_of(x_dtype)},
                         {initial_state, state_bytes}, {d_final_state, state_bytes}};
     if (any_touch(outs, ins)) return GLA_ERR_SHAPE;
-    if (units_bytes(c, 3) > 0 && (!workspace || misaligned(workspace) || workspace_bytes < units_bytes(c, 3))) return GLA_ERR_WORKSPACE;
+    if (units_bytes(c) > 0 && (!workspace || misaligned(workspace) || workspace_bytes < units_bytes(c))) return GLA_ERR_WORKSPACE;
     const hipStream_t stream = static_cast<hipStream_t>(stream_);
-    const RecurUnits u = units_in(c, workspace, true);
+    const RecurUnits u = c.nunits > 1 ? units_in(c, workspace) : RecurUnits{};
     if (c.nunits > 1) {
         if (launch_recur_units(c, d_out, u, stream) != hipSuccess) return GLA_ERR_HIP;
         if (launch_recur_carry(c, u, initial_state, d_final_state, d_initial_state, stream) != hipSuccess) return GLA_ERR_HIP;

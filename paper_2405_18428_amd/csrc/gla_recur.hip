@@ -2,16 +2,25 @@
 // pre-activation z of a = sigmoid(z)^(1/tau), and u_t = x_t or (1 - a_t) x_t.  Backward, from the end:
 //   G_t = dO_t + a_{t+1} G_{t+1},   dx_t = G_t (or (1 - a_t) G_t),   dlog a_t = a_t (h_{t-1} - (0 or x_t)) G_t,   dz = dlog a sigmoid(-z) / tau.
 //
-// A lane has V neighbouring channels of one sequence, a wave 8 steps of them in registers: their decays a and inputs u from what it loads, the
-// state they make of zero, and, once the state that enters them is known, the outputs.  The 8 waves of a work-group take 8 pieces in a row
-// (a round of 64 steps) and hand each other decay and state through LDS.  Where channels alone leave the GPU idle, the sequence is cut into
-// units: a pass over x and the gates leaves each unit's decay and state, a small kernel chains these, and the outputs come from a second pass.
-// The backward pass has both chains at once: its units are rounds, whose states from zero and adjoints from zero come from one reading.
+// A lane has V neighbouring channels of one sequence, a wave 8 or 16 steps of them in registers: their decays a and inputs u from what it loads, the
+// state they make of zero, and, once the state that enters them is known, the outputs.  The 8 waves of a work-group take 8 pieces in a row and
+// hand each other decay and state through LDS.  Where channels alone fill the GPU a work-group walks its channels' whole sequence, else sequences are cut
+// into units of 128 steps (chain_kernel): a work-group publishes its unit's decay and state, looks back over those of the units before it
+// in its block of 16 units and takes the state behind the block before, and goes on to its outputs with its rows still in registers, so that every input is
+// read once.  What a state is made of, and in which order, does not depend on which unit is ready first.
+// The backward pass has chains from both ends, so a first pass leaves the decays, states from zero and adjoints from zero of rounds of 64 steps, a small
+// kernel chains these, and a second pass forms the gradients.
+//
+// Looking back: what is published are words that hold their own validity (all ones: not there yet), written and read at device scope, so nothing
+// has to be ordered.  Work-groups take their units in the order in which they start (a ticket), and a unit waits for earlier ones only, which
+// have all started and publish before they wait: the earliest unit that waits can always go on.  A poll that runs out all the same (`polls`) forms the
+// state that enters its unit from the inputs, step by step: every wait ends.  (Calls in place have no inputs left for that: their waits end because earlier
+// units go on.)
 //
 // Precision: a state's memory can be as long as 1 / (1 - a), and a rounded to 32 bits loses what it lacks of one: with one constant gate of
-// 1 - 1e-4 over many steps the state would be off by 3e-4.  So decays leave a wave's 8 steps as sums of log2 a, which are exact relative to
-// themselves, and a state goes from one round to the next by s + s expm1(sum) where the decay is near one.  log(1 + e) of the pre-activation's
-// gate is 2 atanh(e / (2 + e)), a series that is as exact for small e as for e = 1.  What a gate lacks of one comes from expm1 too.
+// 1 - 1e-4 over many steps the state would be off by 3e-4.  So decays leave a wave's steps as sums of log2 a, which are exact relative to
+// themselves, and a state goes from one round or unit to the next by s + s expm1(sum) where the decay is near one.  log2(1 + e) of the
+// pre-activation's gate gets back what 1 + e rounds off.  What a gate lacks of one comes from expm1 too.
 #include "gla_recur.h"
 
 namespace gla {
@@ -59,12 +68,12 @@ __device__ __forceinline__ void store(void *base, int dtype, long long row, uint
 
 // exp(y) - 1, y <= 0 (natural units); a = exp(y)
 __device__ __forceinline__ float less_one(float y, float a) {
-    float p = 1.f + y * (1.f / 7.f);
-    p = 1.f + y * (1.f / 6.f) * p;
-    p = 1.f + y * (1.f / 5.f) * p;
-    p = 1.f + y * (1.f / 4.f) * p;
-    p = 1.f + y * (1.f / 3.f) * p;
-    p = 1.f + y * (1.f / 2.f) * p;
+    float p = fmaf(y, 1.f / 5040.f, 1.f / 720.f);
+    p = fmaf(y, p, 1.f / 120.f);
+    p = fmaf(y, p, 1.f / 24.f);
+    p = fmaf(y, p, 1.f / 6.f);
+    p = fmaf(y, p, 0.5f);
+    p = fmaf(y, p, 1.f);
     return y > -0.35f ? y * p : a - 1.f;     // (the next term of the series is 2e-8 of the result)
 }
 // 2^lg s
@@ -83,18 +92,12 @@ __device__ __forceinline__ Gate gate_of(float g, float inv_tau) {
         r.lg = g * kLog2E;
         r.slope = 1.f;
     } else {
-        const float e = __builtin_amdgcn_exp2f(-__builtin_fabsf(g) * kLog2E);          // 0 .. 1
-        const float s = e * __builtin_amdgcn_rcpf(2.f + e), q = s * s;                // 0 .. 1/3
-        float p = q * (1.f / 13.f) + 1.f / 11.f;
-        p = p * q + 1.f / 9.f;
-        p = p * q + 1.f / 7.f;
-        p = p * q + 1.f / 5.f;
-        p = p * q + 1.f / 3.f;
-        p = p * q + 1.f;                                                              // the next term is 1.4e-8
-        r.lg = (__builtin_fminf(g, 0.f) - 2.f * s * p) * (kLog2E * inv_tau);
+        const float e = __builtin_amdgcn_exp2f(-__builtin_fabsf(g) * kLog2E), w = 1.f + e;      // e: 0 .. 1
+        const float l = fmaf(e - (w - 1.f), kLog2E, __builtin_amdgcn_logf(w));                  // log2(1 + e)
+        r.lg = fmaf(-l, inv_tau, __builtin_fminf(g, 0.f) * (kLog2E * inv_tau));
         if constexpr (SLOPE) {
-            const float i = __builtin_amdgcn_rcpf(1.f + e) * inv_tau;
-            r.slope = g > 0.f ? e * i : i;                                            // sigmoid(-g) / tau
+            const float i = __builtin_amdgcn_rcpf(w) * inv_tau;
+            r.slope = g > 0.f ? e * i : i;                                                      // sigmoid(-g) / tau
         }
     }
     r.a = __builtin_amdgcn_exp2f(r.lg);
@@ -140,38 +143,41 @@ struct Place {
         if (!any) n = 0;
     }
     __device__ __forceinline__ long long cell(const RecurCall &c) const { return (long long)b * c.D + channel; }
-    // the row of a scan step, uniform, in elements
-    __device__ __forceinline__ long long row(const RecurCall &c, int s) const {
-        long long t;
+};
+
+// The rows of scan steps one after the other, uniform, in elements
+struct Cursor {
+    long long at;
+    int left;                            // steps up to the end of a column (row scans: never)
+    template <int V>
+    __device__ __forceinline__ Cursor(const RecurCall &c, const Place<V> &p, int s) {
         if (c.scan_dir <= GLA_SCAN_ROW_REV) {
-            t = c.scan_dir == GLA_SCAN_ROW_FWD ? s : -s;
+            at = p.row0 * c.D + (long long)s * c.step;
+            left = 1 << 30;
         } else {
             const int k = c.scan_dir == GLA_SCAN_COL_FWD ? s : c.T - 1 - s;
-            const int w = k / c.grid_h;
-            t = (long long)(k - w * c.grid_h) * c.grid_w + w;
+            const int w = k / c.grid_h, r = k - w * c.grid_h;
+            at = (p.row0 + (long long)r * c.grid_w + w) * c.D;
+            left = c.scan_dir == GLA_SCAN_COL_FWD ? c.grid_h - 1 - r : r;
         }
-        return (row0 + t) * c.D;
+    }
+    __device__ __forceinline__ void next(const RecurCall &c) {
+        const bool turn = left == 0;
+        at += turn ? c.wrap : c.step;
+        left = turn ? c.grid_h - 1 : left - 1;
     }
 };
 
-// V channels of the steps s0 .. s0 + 7.  Steps behind the sequence's end (`loads`) get `other`: zeros, and gates that let everything through
-template <typename E, int V>
+// V channels of L steps
+template <typename E, int V, int L>
 struct Rows {
-    RawOf<E, V> r[kSteps];
-    __device__ __forceinline__ void load(const void *base, const RecurCall &c, const Place<V> &p, int s0, bool whole, E other) {
-        const char *x = static_cast<const char *>(base);
-        const uint32_t at = p.at * (uint32_t)sizeof(E);
-        if (whole) {
+    RawOf<E, V> r[L];
+    __device__ __forceinline__ void load(int j, const void *base, long long row, uint32_t at) {
+        r[j] = load_raw<E, V>(static_cast<const char *>(base) + row * (long long)sizeof(E) + at * (uint32_t)sizeof(E));
+    }
+    __device__ __forceinline__ void fill(int j, E other) {
 #pragma unroll
-            for (int j = 0; j < kSteps; ++j) r[j] = load_raw<E, V>(x + p.row(c, s0 + j) * (long long)sizeof(E) + at);
-        } else {
-#pragma unroll
-            for (int j = 0; j < kSteps; ++j) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) r[j].e[i] = other;
-                if (s0 + j < p.loads) r[j] = load_raw<E, V>(x + p.row(c, s0 + j) * (long long)sizeof(E) + at);
-            }
-        }
+        for (int i = 0; i < V; ++i) r[j].e[i] = other;
     }
 };
 // a gate of one: log 1, or the pre-activation +infinity
@@ -182,24 +188,66 @@ __device__ __forceinline__ EG open_gate() {
     else return __builtin_inff();
 }
 
-// Decays and inputs of 8 steps
-template <typename EX, typename EG, int V, int KIND, bool REST>
+// x, gates and (backward) dO of L steps from s on.  Steps behind the sequence's end get zeros, and gates that let everything through
+template <typename EX, typename EG, int V, int L, int KIND, bool BACK>
+struct Given {
+    Rows<EX, V, L> x, o;
+    Rows<EG, V, L> g;
+    bool whole;
+    __device__ __forceinline__ void load(const RecurCall &c, const Place<V> &p, const void *d_out, int s) {
+        whole = __all(s + L <= p.loads);
+        Cursor k(c, p, s);
+        if (whole) {
+#pragma unroll
+            for (int j = 0; j < L; ++j) {
+                x.load(j, c.x, k.at, p.at);
+                g.load(j, c.gate, k.at, p.at);
+                if constexpr (BACK) o.load(j, d_out, k.at, p.at);
+                k.next(c);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < L; ++j) {
+                x.fill(j, (EX)0);
+                g.fill(j, open_gate<EG, KIND>());
+                if constexpr (BACK) o.fill(j, (EX)0);
+                if (s + j < p.loads) {
+                    x.load(j, c.x, k.at, p.at);
+                    g.load(j, c.gate, k.at, p.at);
+                    if constexpr (BACK) o.load(j, d_out, k.at, p.at);
+                }
+                k.next(c);
+            }
+        }
+    }
+};
+
+// Decays and inputs of L steps
+template <typename EX, typename EG, int V, int L, int KIND, bool REST>
 struct Piece {
-    float a[kSteps][V], u[kSteps][V];
-    float lg[V];                         // log2 of all 8 gates
-    __device__ __forceinline__ Piece(const Rows<EX, V> &x, const Rows<EG, V> &g, float inv_tau) {
+    float a[L][V], u[L][V];
+    float lg[V];                         // log2 of all gates
+    template <bool BACK>
+    __device__ __forceinline__ Piece(const Given<EX, EG, V, L, KIND, BACK> &in, float inv_tau) {
 #pragma unroll
         for (int i = 0; i < V; ++i) lg[i] = 0.f;
 #pragma unroll
-        for (int j = 0; j < kSteps; ++j)
+        for (int j = 0; j < L; ++j)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const Gate t = gate_of<KIND, false>(to_float(g.r[j].e[i]), inv_tau);
-                const float v = to_float(x.r[j].e[i]);
+                const Gate t = gate_of<KIND, false>(to_float(in.g.r[j].e[i]), inv_tau);
+                const float v = to_float(in.x.r[j].e[i]);
                 a[j][i] = t.a;
                 u[j][i] = REST ? -less_one(t.lg * kLn2, t.a) * v : v;
                 lg[i] += t.lg;
             }
+    }
+    // the state they make of zero
+    __device__ __forceinline__ float from_zero(int i) const {
+        float h = 0.f;
+#pragma unroll
+        for (int j = 0; j < L; ++j) h = __builtin_fmaf(a[j][i], h, u[j][i]);
+        return h;
     }
 };
 
@@ -212,8 +260,8 @@ __device__ __forceinline__ void store_state(float *p, long long at, const float 
     __builtin_memcpy(__builtin_assume_aligned(p + at, 4 * V), v, sizeof(v));
 }
 
-// First pass: a wave takes one unit of 64 V channels, 8 steps at a time with the next 8 on their way.
-template <typename EX, typename EG, int V, int KIND, bool REST, bool BACK>
+// Backward, first pass: a wave takes one unit of 64 V channels, 8 steps at a time with the next 8 on their way.
+template <typename EX, typename EG, int V, int KIND, bool REST>
 __global__ __launch_bounds__(256) void units_kernel(const RecurCall c, const void *d_out, const RecurUnits u, bool flat, int groups) {
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const long long task = (long long)blockIdx.x * 4 + wave;
@@ -223,37 +271,23 @@ __global__ __launch_bounds__(256) void units_kernel(const RecurCall c, const voi
     const Place<V> p(c, flat, group);
     const int begin = unit * c.unit, end = min(begin + c.unit, c.T);
     float lg[V] = {}, h[V] = {}, adj[V] = {};
-    Rows<EX, V> x, o;
-    Rows<EG, V> g;
-    auto fetch = [&](int s) {
-        const bool whole = __all(s + kSteps <= p.loads);
-        x.load(c.x, c, p, s, whole, (EX)0);
-        g.load(c.gate, c, p, s, whole, open_gate<EG, KIND>());
-        if constexpr (BACK) o.load(d_out, c, p, s, whole, (EX)0);
-    };
-    fetch(begin);                        // (a unit ends at a multiple of 8 steps or at T)
+    Given<EX, EG, V, kSteps, KIND, true> in;
+    in.load(c, p, d_out, begin);         // (a unit ends at a multiple of 8 steps or at T)
     for (int s = begin; s < end; s += kSteps) {
-        const Piece<EX, EG, V, KIND, REST> q(x, g, c.inv_tau);
-        float dd[BACK ? kSteps : 1][V];
-        if constexpr (BACK) {
+        const Piece<EX, EG, V, kSteps, KIND, REST> q(in, c.inv_tau);
+        float dd[kSteps][V];
 #pragma unroll
-            for (int j = 0; j < kSteps; ++j)
+        for (int j = 0; j < kSteps; ++j)
 #pragma unroll
-                for (int i = 0; i < V; ++i) dd[j][i] = to_float(o.r[j].e[i]);
-        }
-        if (s + kSteps < end) fetch(s + kSteps);
+            for (int i = 0; i < V; ++i) dd[j][i] = to_float(in.o.r[j].e[i]);
+        if (s + kSteps < end) in.load(c, p, d_out, s + kSteps);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            float t = 0.f;
+            h[i] = decayed(q.lg[i], h[i]) + q.from_zero(i);
+            float b = 0.f;
 #pragma unroll
-            for (int j = 0; j < kSteps; ++j) t = __builtin_fmaf(q.a[j][i], t, q.u[j][i]);
-            h[i] = decayed(q.lg[i], h[i]) + t;
-            if constexpr (BACK) {
-                float b = 0.f;
-#pragma unroll
-                for (int j = kSteps - 1; j >= 0; --j) b = q.a[j][i] * (dd[j][i] + b);
-                adj[i] += __builtin_amdgcn_exp2f(lg[i]) * b;
-            }
+            for (int j = kSteps - 1; j >= 0; --j) b = q.a[j][i] * (dd[j][i] + b);
+            adj[i] += __builtin_amdgcn_exp2f(lg[i]) * b;
             lg[i] += q.lg[i];
         }
     }
@@ -261,13 +295,12 @@ __global__ __launch_bounds__(256) void units_kernel(const RecurCall c, const voi
     const long long at = ((long long)p.b * c.nunits + unit) * c.D + p.channel;
     store_state<V>(u.decay, at, lg);
     store_state<V>(u.state, at, h);
-    if constexpr (BACK) store_state<V>(u.adjoint, at, adj);
+    store_state<V>(u.adjoint, at, adj);
 }
 
 // Chains the units of 64 channels: 16 waves take as many runs of units, compose each, chain the runs through LDS and walk their runs again, where
 // what enters a unit takes the place of what it makes of zero.
 constexpr int kCarryWaves = 16;
-template <bool BACK>
 __global__ __launch_bounds__(64 * kCarryWaves) void carry_kernel(const RecurCall c, const RecurUnits u, const float *first, const float *last, float *d_first) {
     __shared__ float run_lg[kCarryWaves][64], run_s[kCarryWaves][64];
     constexpr int kAtOnce = 8;           // units whose loads are under way together
@@ -276,7 +309,7 @@ __global__ __launch_bounds__(64 * kCarryWaves) void carry_kernel(const RecurCall
     const int b = blockIdx.x / blocks, ch = (blockIdx.x - b * blocks) * 64 + lane;
     const bool any = ch < c.D;
     const int each = (c.nunits + kCarryWaves - 1) / kCarryWaves;
-    const bool back = BACK && blockIdx.y == 1;
+    const bool back = blockIdx.y == 1;
     float *const own = back ? u.adjoint : u.state;
     const int from = min(wave * each, c.nunits), to = min(from + each, c.nunits);
     const long long base = (long long)b * c.nunits * c.D + (any ? ch : 0);
@@ -314,44 +347,42 @@ __global__ __launch_bounds__(64 * kCarryWaves) void carry_kernel(const RecurCall
     if (back && any && d_first != nullptr && from < to && to == c.nunits) d_first[(long long)b * c.D + ch] = s;
 }
 
-// Second pass: a work-group walks one span (unit) of 64 V channels in rounds, 8 steps a wave.  Bound by HBM.
+// The outputs of a piece from the state that enters it
+template <typename EX, typename EG, int V, int L, int KIND, bool REST>
+__device__ __forceinline__ void put_outputs(const RecurCall &c, const Place<V> &p, const Piece<EX, EG, V, L, KIND, REST> &q, float (&h)[V], void *out, int dtype, int s,
+                                            bool whole) {
+    Cursor k(c, p, s);
+#pragma unroll
+    for (int j = 0; j < L; ++j) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) h[i] = __builtin_fmaf(q.a[j][i], h[i], q.u[j][i]);
+        if (whole || s + j < p.n) store<V>(out, dtype, k.at, p.at, h);
+        k.next(c);
+    }
+}
+
+// Forward pass with a sequence to itself: a work-group walks 64 V channels in rounds, 8 steps a wave, with the next round on its way.  Bound by HBM.
 template <typename EX, typename EG, int V, int KIND, bool REST>
-__global__ __launch_bounds__(64 * kWaves) void walk_kernel(const RecurCall c, const RecurUnits u, const float *first, void *out, int out_dtype,
-                                                           float *final_state, bool flat, int groups) {
+__global__ __launch_bounds__(64 * kWaves) void walk_kernel(const RecurCall c, const float *first, void *out, int out_dtype, float *final_state, bool flat) {
     __shared__ float lds_lg[2][kWaves][64][V], lds_a[2][kWaves][64][V], lds_h[2][kWaves][64][V];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), waves = blockDim.x >> 6;
-    const int unit = blockIdx.x / (unsigned)groups, group = blockIdx.x - (unsigned)unit * (unsigned)groups;
-    const Place<V> p(c, flat, group);
-    const int begin = unit * c.unit, end = min(begin + c.unit, c.T);
+    const Place<V> p(c, flat, blockIdx.x);
     const int round = kSteps * waves;
     float carry[V] = {};
-    if (c.nunits > 1) {
-        if (p.any) load_state<V>(u.state, ((long long)p.b * c.nunits + unit) * c.D + p.channel, carry);
-    } else if (first != nullptr) {
-        if (p.any) load_state<V>(first, p.cell(c), carry);
-    }
-    Rows<EX, V> x;
-    Rows<EG, V> g;
-    auto fetch = [&](int s) {
-        const bool whole = __all(s + kSteps <= p.loads);
-        x.load(c.x, c, p, s, whole, (EX)0);
-        g.load(c.gate, c, p, s, whole, open_gate<EG, KIND>());
-    };
-    fetch(begin + wave * kSteps);
+    if (first != nullptr && p.any) load_state<V>(first, p.cell(c), carry);
+    Given<EX, EG, V, kSteps, KIND, false> in;
+    in.load(c, p, nullptr, wave * kSteps);
     int buf = 0;
-    for (int s0 = begin; s0 < end; s0 += round, buf ^= 1) {
+    for (int s0 = 0; s0 < c.T; s0 += round, buf ^= 1) {
         const int s = s0 + wave * kSteps;
-        const Piece<EX, EG, V, KIND, REST> q(x, g, c.inv_tau);
-        if (s0 + round < end) fetch(s + round);
-        float h[V];
+        const Piece<EX, EG, V, kSteps, KIND, REST> q(in, c.inv_tau);
+        const bool whole = __all(s + kSteps <= p.n);
+        if (s0 + round < c.T) in.load(c, p, nullptr, s + round);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            h[i] = 0.f;
-#pragma unroll
-            for (int j = 0; j < kSteps; ++j) h[i] = __builtin_fmaf(q.a[j][i], h[i], q.u[j][i]);
             lds_lg[buf][wave][lane][i] = q.lg[i];
             lds_a[buf][wave][lane][i] = __builtin_amdgcn_exp2f(q.lg[i]);
-            lds_h[buf][wave][lane][i] = h[i];
+            lds_h[buf][wave][lane][i] = q.from_zero(i);
         }
         __syncthreads();                 // (the other buffer's readers are past the next barrier before it is written again)
         float z[V] = {}, lg[V] = {}, mine[V] = {};
@@ -368,17 +399,154 @@ __global__ __launch_bounds__(64 * kWaves) void walk_kernel(const RecurCall c, co
         }
 #pragma unroll
         for (int i = 0; i < V; ++i) carry[i] = decayed(lg[i], carry[i]) + z[i];
-#pragma unroll
-        for (int j = 0; j < kSteps; ++j) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) mine[i] = __builtin_fmaf(q.a[j][i], mine[i], q.u[j][i]);
-            if (s + j < p.n) store<V>(out, out_dtype, p.row(c, s + j), p.at, mine);
-        }
+        put_outputs(c, p, q, mine, out, out_dtype, s, whole);
     }
-    if (final_state != nullptr && unit == c.nunits - 1 && wave == 0 && p.any) store_state<V>(final_state, p.cell(c), carry);
+    if (final_state != nullptr && wave == 0 && p.any) store_state<V>(final_state, p.cell(c), carry);
 }
 
-// Gradients of one round of 64 V channels: states from the front, adjoints from behind, 8 steps a wave.  Bound by HBM.
+// Words that units publish: all ones are not there yet (a NaN that would look so gets other digits)
+constexpr int kChainSteps = 2 * kSteps, kLook = 4;      // steps a wave; units looked back at together
+typedef unsigned long long word_t;
+__device__ __forceinline__ uint32_t bits_of(float x) { return x != x ? 0x7fc00000u : __builtin_bit_cast(uint32_t, x); }
+__device__ __forceinline__ void publish(word_t *p, float lg, float h) {
+    __hip_atomic_store(p, (word_t)bits_of(lg) << 32 | bits_of(h), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void publish(uint32_t *p, float s) { __hip_atomic_store(p, bits_of(s), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <typename W>
+__device__ __forceinline__ W published(const W *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// All words to "not there", the ticket to zero
+__global__ __launch_bounds__(256) void clear_kernel(uint32_t *words, long long count, uint32_t *ticket) {
+    const long long at = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
+    typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+    if (at < count) *reinterpret_cast<u32x4 *>(words + at) = u32x4{~0u, ~0u, ~0u, ~0u};
+    if (at == 0) *ticket = 0;
+}
+
+// Forward pass in units of 128 steps, 16 a wave.  Bound by HBM.
+template <typename EX, typename EG, int V, int KIND, bool REST>
+__global__ __launch_bounds__(64 * kWaves, 4) void chain_kernel(const RecurCall c, const RecurChain ch, const float *first, void *out, int out_dtype, float *final_state,
+                                                            bool flat, int groups) {
+    __shared__ float lds_lg[kWaves][64][V], lds_a[kWaves][64][V], lds_h[kWaves][64][V], lds_s[64][V];
+    __shared__ uint32_t lds_ticket;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    if (threadIdx.x == 0) lds_ticket = __hip_atomic_fetch_add(ch.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    const uint32_t task = __builtin_amdgcn_readfirstlane((int)lds_ticket);
+    const int unit = (int)(task / (uint32_t)groups), group = (int)(task - (uint32_t)unit * (uint32_t)groups);
+    const Place<V> p(c, flat, group);
+    const int begin = unit * kRecurChain, s = begin + wave * kChainSteps;
+    if (unit > 0 && __all(begin >= p.n)) return;         // behind all its sequences' ends, as are the units after it
+    // of unit n: its decay and state from zero; of block n of units: the state behind it
+    auto local = [&](int n, int i) { return ch.local + (((long long)n * groups + group) * V + i) * 64 + lane; };
+    auto after = [&](int n, int i) { return ch.after + (((long long)n * groups + group) * V + i) * 64 + lane; };
+    Given<EX, EG, V, kChainSteps, KIND, false> in;
+    in.load(c, p, nullptr, s);
+    float enter[V] = {};
+    if (unit < kRecurBlock && first != nullptr && p.any) load_state<V>(first, p.cell(c), enter);
+    const Piece<EX, EG, V, kChainSteps, KIND, REST> q(in, c.inv_tau);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        lds_lg[wave][lane][i] = q.lg[i];
+        lds_a[wave][lane][i] = __builtin_amdgcn_exp2f(q.lg[i]);
+        lds_h[wave][lane][i] = q.from_zero(i);
+    }
+    __syncthreads();
+    float z[V] = {}, lg[V] = {}, my_z[V] = {}, my_lg[V] = {};
+    for (int w = 0; w < kWaves; ++w) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            if (w == wave) {
+                my_z[i] = z[i];
+                my_lg[i] = lg[i];
+            }
+            z[i] = __builtin_fmaf(lds_a[w][lane][i], z[i], lds_h[w][lane][i]);
+            lg[i] += lds_lg[w][lane][i];
+        }
+    }
+    if (wave == 0) {
+        const bool last = unit == c.nunits - 1;
+        const int block = unit / kRecurBlock, begins = block * kRecurBlock;
+        if (!last && unit - begins < kRecurBlock - 1) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) publish(local(unit, i), lg[i], z[i]);
+        }
+        // what the units from n + 1 to the one before this make of the state behind unit n: always added in one order
+        float far_lg[V] = {}, far_z[V] = {};
+        int n = unit - 1, polls = 0;
+        bool ran_out = false;
+        while (n >= begins && !ran_out) {
+            word_t part[kLook][V];
+#pragma unroll
+            for (int k = 0; k < kLook; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) part[k][i] = published(local(max(n - k, begins), i));
+            int passed = 0;
+#pragma unroll
+            for (int k = 0; k < kLook; ++k) {
+                bool there = passed == k && n - k >= begins;
+#pragma unroll
+                for (int i = 0; i < V; ++i) there = there && part[k][i] != ~0ull;
+                if (!__all(there)) continue;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    far_z[i] += decayed(far_lg[i], __builtin_bit_cast(float, (uint32_t)part[k][i]));
+                    far_lg[i] += __builtin_bit_cast(float, (uint32_t)(part[k][i] >> 32));
+                }
+                ++passed;
+            }
+            n -= passed;
+            ran_out = passed == 0 && ++polls > ch.polls;
+        }
+        float state[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) state[i] = enter[i];
+        if (block > 0 || ran_out) {
+            bool there = false;
+            while (!there && !ran_out) {
+                there = true;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const uint32_t w = published(after(block - 1, i));
+                    there = there && w != ~0u;
+                    state[i] = __builtin_bit_cast(float, w);
+                }
+                there = __all(there);
+                ran_out = !there && ++polls > ch.polls;
+            }
+            if (ran_out) {               // from the inputs, up to and with unit n
+#pragma unroll
+                for (int i = 0; i < V; ++i) state[i] = 0.f;
+                if (first != nullptr && p.any) load_state<V>(first, p.cell(c), state);
+                for (int t = 0; t < (n + 1) * kRecurChain; ++t) {
+                    Given<EX, EG, V, 1, KIND, false> again;
+                    again.load(c, p, nullptr, t);
+                    const Piece<EX, EG, V, 1, KIND, REST> r(again, c.inv_tau);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) state[i] = decayed(r.lg[i], state[i]) + r.u[0][i];
+                }
+            }
+        }
+        float leave[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            enter[i] = decayed(far_lg[i], state[i]) + far_z[i];
+            leave[i] = decayed(lg[i], enter[i]) + z[i];
+            if (!last && unit - begins == kRecurBlock - 1) publish(after(block, i), leave[i]);
+            lds_s[lane][i] = enter[i];
+        }
+        // (a sequence's last unit)
+        const bool ends = p.n <= begin + kRecurChain && (p.n > begin || unit == 0);
+        if (ends && final_state != nullptr && p.any) store_state<V>(final_state, p.cell(c), leave);
+    }
+    __syncthreads();
+    float mine[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) mine[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(my_lg[i]), lds_s[lane][i], my_z[i]);
+    put_outputs(c, p, q, mine, out, out_dtype, s, __all(s + kChainSteps <= p.n));
+}
+
+// Gradients of one round of 64 V channels: states from the front, adjoints from behind, 8 steps a wave.
 template <typename EX, typename EG, int V, int KIND, bool REST>
 __global__ __launch_bounds__(64 * kWaves) void back_kernel(const RecurCall c, const void *d_out, const RecurUnits u, const float *first, const float *last,
                                                            void *dx, void *dgate, int grad_dtype, float *d_first, bool flat, int groups) {
@@ -387,12 +555,8 @@ __global__ __launch_bounds__(64 * kWaves) void back_kernel(const RecurCall c, co
     const int unit = blockIdx.x / (unsigned)groups, group = blockIdx.x - (unsigned)unit * (unsigned)groups;
     const Place<V> p(c, flat, group);
     const int s = unit * kRecurRound + wave * kSteps;
-    Rows<EX, V> x, o;
-    Rows<EG, V> g;
-    const bool whole = __all(s + kSteps <= p.loads);
-    x.load(c.x, c, p, s, whole, (EX)0);
-    g.load(c.gate, c, p, s, whole, open_gate<EG, KIND>());
-    o.load(d_out, c, p, s, whole, (EX)0);
+    Given<EX, EG, V, kSteps, KIND, true> in;
+    in.load(c, p, d_out, s);
     float h[V] = {}, adj[V] = {};
     if (p.any) {
         const long long at = ((long long)p.b * c.nunits + unit) * c.D + p.channel;
@@ -404,17 +568,27 @@ __global__ __launch_bounds__(64 * kWaves) void back_kernel(const RecurCall c, co
             if (last != nullptr) load_state<V>(last, p.cell(c), adj);
         }
     }
-    Piece<EX, EG, V, KIND, REST> q(x, g, c.inv_tau);
+    // of each step: the gate, what it lacks of one, its slope; the input, then the state before the step; dO, then the adjoint
+    float a[kSteps][V], rest[REST ? kSteps : 1][V], slope[KIND == GLA_GATE_PRE ? kSteps : 1][V], x[kSteps][V], b[kSteps][V], o[kSteps][V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        float t = 0.f, b = 0.f;
+        float lg = 0.f, t = 0.f, r = 0.f;
 #pragma unroll
-        for (int j = 0; j < kSteps; ++j) t = __builtin_fmaf(q.a[j][i], t, q.u[j][i]);
+        for (int j = 0; j < kSteps; ++j) {
+            const Gate gt = gate_of<KIND, true>(to_float(in.g.r[j].e[i]), c.inv_tau);
+            a[j][i] = gt.a;
+            if constexpr (KIND == GLA_GATE_PRE) slope[j][i] = gt.slope;
+            if constexpr (REST) rest[j][i] = -less_one(gt.lg * kLn2, gt.a);
+            x[j][i] = to_float(in.x.r[j].e[i]);
+            o[j][i] = to_float(in.o.r[j].e[i]);
+            lg += gt.lg;
+            t = REST ? fmaf(a[j][i], t, rest[j][i] * x[j][i]) : fmaf(a[j][i], t, x[j][i]);
+        }
 #pragma unroll
-        for (int j = kSteps - 1; j >= 0; --j) b = q.a[j][i] * (to_float(o.r[j].e[i]) + b);
-        lds_lg[wave][lane][i] = q.lg[i];
+        for (int j = kSteps - 1; j >= 0; --j) r = a[j][i] * (o[j][i] + r);
+        lds_lg[wave][lane][i] = lg;
         lds_h[wave][lane][i] = t;
-        lds_o[wave][lane][i] = b;
+        lds_o[wave][lane][i] = r;
     }
     __syncthreads();
     for (int w = 0; w < wave; ++w)
@@ -423,41 +597,43 @@ __global__ __launch_bounds__(64 * kWaves) void back_kernel(const RecurCall c, co
     for (int w = waves - 1; w > wave; --w)
 #pragma unroll
         for (int i = 0; i < V; ++i) adj[i] = decayed(lds_lg[w][lane][i], adj[i]) + lds_o[w][lane][i];
-    // the state before each step takes the place of its input
 #pragma unroll
     for (int j = 0; j < kSteps; ++j)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float before = h[i];
-            h[i] = __builtin_fmaf(q.a[j][i], h[i], q.u[j][i]);
-            q.u[j][i] = before;
+            // less the input, where 1 - a scales it
+            b[j][i] = REST ? h[i] - x[j][i] : h[i];
+            h[i] = REST ? fmaf(a[j][i], h[i], rest[j][i] * x[j][i]) : fmaf(a[j][i], h[i], x[j][i]);
         }
 #pragma unroll
-    for (int j = kSteps - 1; j >= 0; --j) {
+    for (int j = kSteps - 1; j >= 0; --j)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            o[j][i] += adj[i];
+            adj[i] = a[j][i] * o[j][i];
+        }
+    Cursor k(c, p, s);
+    const bool whole = __all(s + kSteps <= p.n);
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) {
         float gx[V], gg[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const Gate t = gate_of<KIND, true>(to_float(g.r[j].e[i]), c.inv_tau);
-            const float G = to_float(o.r[j].e[i]) + adj[i], v = to_float(x.r[j].e[i]);
-            gx[i] = REST ? -less_one(t.lg * kLn2, t.a) * G : G;
-            // a closed gate lets nothing through, whatever stands before it; nor does the gate of a step behind the end, which is open and has no slope
-            gg[i] = q.a[j][i] * (REST ? q.u[j][i] - v : q.u[j][i]) * G * t.slope;
-            adj[i] = q.a[j][i] * G;
+            gx[i] = REST ? rest[j][i] * o[j][i] : o[j][i];
+            gg[i] = a[j][i] * b[j][i] * o[j][i];
+            if constexpr (KIND == GLA_GATE_PRE) gg[i] *= slope[j][i];
         }
         const int t = s + j;
-        if (t < c.T && p.any) {          // rows behind a sequence's end are cleared
-            if (t >= p.n)
-#pragma unroll
-                for (int i = 0; i < V; ++i) gx[i] = gg[i] = 0.f;
-            if (whole || t < p.n || c.seq_lens == nullptr) {
-                store<V>(dx, grad_dtype, p.row(c, t), p.at, gx);
-                store<V>(dgate, grad_dtype, p.row(c, t), p.at, gg);
-            } else {                     // (step t of a reversed scan would lie before the sequence: its token is t itself)
-                const long long row = ((long long)p.b * c.T + t) * c.D;
-                store<V>(dx, grad_dtype, row, (uint32_t)p.channel, gx);
-                store<V>(dgate, grad_dtype, row, (uint32_t)p.channel, gg);
-            }
+        if (whole || (t < p.n && p.any)) {
+            store<V>(dx, grad_dtype, k.at, p.at, gx);
+            store<V>(dgate, grad_dtype, k.at, p.at, gg);
+        } else if (t < c.T && p.any) {   // rows behind a sequence's end are cleared: step t stands for token t there, in both directions
+            const float zero[V] = {};
+            const long long row = ((long long)p.b * c.T + t) * c.D;
+            store<V>(dx, grad_dtype, row, (uint32_t)p.channel, zero);
+            store<V>(dgate, grad_dtype, row, (uint32_t)p.channel, zero);
         }
+        k.next(c);
     }
     if (unit == 0 && c.nunits == 1 && wave == 0 && d_first != nullptr && p.any) store_state<V>(d_first, p.cell(c), adj);
 }
@@ -511,25 +687,16 @@ Groups groups_of(const RecurCall &c, int V) {
 
 hipError_t launch_recur_units(const RecurCall &c, const void *d_out, const RecurUnits &u, hipStream_t stream) {
     return instance(c, c.D % 2 == 0, [&](auto x, auto g, auto kind, auto rest, auto v) {
-        using EX = decltype(x);
-        using EG = decltype(g);
         constexpr int V = decltype(v)::value;
         const Groups n = groups_of(c, V);
-        const dim3 grid((unsigned)(((long long)n.count * c.nunits + 3) / 4));
-        if (d_out != nullptr)
-            hipLaunchKernelGGL((units_kernel<EX, EG, V, kind.value, rest.value, true>), grid, dim3(256), 0, stream, c, d_out, u, n.flat, n.count);
-        else
-            hipLaunchKernelGGL((units_kernel<EX, EG, V, kind.value, rest.value, false>), grid, dim3(256), 0, stream, c, d_out, u, n.flat, n.count);
+        hipLaunchKernelGGL((units_kernel<decltype(x), decltype(g), V, kind.value, rest.value>), dim3((unsigned)(((long long)n.count * c.nunits + 3) / 4)), dim3(256), 0,
+                           stream, c, d_out, u, n.flat, n.count);
         return hipGetLastError();
     });
 }
 
 hipError_t launch_recur_carry(const RecurCall &c, const RecurUnits &u, const float *first, const float *last, float *d_first, hipStream_t stream) {
-    const unsigned blocks = (unsigned)((c.D + 63) / 64) * (unsigned)c.B;
-    if (u.adjoint != nullptr)
-        hipLaunchKernelGGL(carry_kernel<true>, dim3(blocks, 2), dim3(64 * kCarryWaves), 0, stream, c, u, first, last, d_first);
-    else
-        hipLaunchKernelGGL(carry_kernel<false>, dim3(blocks), dim3(64 * kCarryWaves), 0, stream, c, u, first, last, d_first);
+    hipLaunchKernelGGL(carry_kernel, dim3((unsigned)((c.D + 63) / 64) * (unsigned)c.B, 2), dim3(64 * kCarryWaves), 0, stream, c, u, first, last, d_first);
     return hipGetLastError();
 }
 
@@ -538,13 +705,31 @@ static unsigned waves_for(int steps) {
     return 64u * (unsigned)(w < kWaves ? w : kWaves);
 }
 
-hipError_t launch_recur_walk(const RecurCall &c, const RecurUnits &u, const float *first, void *out, int out_dtype, float *final_state,
-                             hipStream_t stream) {
+hipError_t launch_recur_walk(const RecurCall &c, const float *first, void *out, int out_dtype, float *final_state, hipStream_t stream) {
     return instance(c, c.D % 2 == 0, [&](auto x, auto g, auto kind, auto rest, auto v) {
         constexpr int V = decltype(v)::value;
         const Groups n = groups_of(c, V);
-        hipLaunchKernelGGL((walk_kernel<decltype(x), decltype(g), V, kind.value, rest.value>), dim3((unsigned)((long long)n.count * c.nunits)),
-                           dim3(waves_for(c.unit)), 0, stream, c, u, first, out, out_dtype, final_state, n.flat, n.count);
+        hipLaunchKernelGGL((walk_kernel<decltype(x), decltype(g), V, kind.value, rest.value>), dim3((unsigned)n.count), dim3(waves_for(c.T)), 0, stream, c, first, out,
+                           out_dtype, final_state, n.flat);
+        return hipGetLastError();
+    });
+}
+
+long long recur_chain_columns(const RecurCall &c) {
+    const int V = c.D % 2 == 0 ? 2 : 1;
+    return (long long)groups_of(c, V).count * V * 64;
+}
+
+hipError_t launch_recur_chain(const RecurCall &c, const RecurChain &ch, const float *first, void *out, int out_dtype, float *final_state, hipStream_t stream) {
+    const long long words = recur_chain_columns(c) * recur_chain_words(c);
+    hipLaunchKernelGGL(clear_kernel, dim3((unsigned)((words + 1023) / 1024)), dim3(256), 0, stream, reinterpret_cast<uint32_t *>(ch.local), words, ch.ticket);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    return instance(c, c.D % 2 == 0, [&](auto x, auto g, auto kind, auto rest, auto v) {
+        constexpr int V = decltype(v)::value;
+        const Groups n = groups_of(c, V);
+        hipLaunchKernelGGL((chain_kernel<decltype(x), decltype(g), V, kind.value, rest.value>), dim3((unsigned)((long long)n.count * c.nunits)), dim3(64 * kWaves), 0, stream,
+                           c, ch, first, out, out_dtype, final_state, n.flat, n.count);
         return hipGetLastError();
     });
 }
