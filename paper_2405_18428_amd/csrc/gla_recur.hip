@@ -405,7 +405,7 @@ __global__ __launch_bounds__(64 * kWaves) void walk_kernel(const RecurCall c, co
 }
 
 // Words that units publish: all ones are not there yet (a NaN that would look so gets other digits)
-constexpr int kChainSteps = 2 * kSteps, kLook = 4;      // steps a wave; units looked back at together
+constexpr int kChainSteps = 2 * kSteps;                  // of a wave
 typedef unsigned long long word_t;
 __device__ __forceinline__ uint32_t bits_of(float x) { return x != x ? 0x7fc00000u : __builtin_bit_cast(uint32_t, x); }
 __device__ __forceinline__ void publish(word_t *p, float lg, float h) {
@@ -427,7 +427,8 @@ __global__ __launch_bounds__(256) void clear_kernel(uint32_t *words, long long c
 template <typename EX, typename EG, int V, int KIND, bool REST>
 __global__ __launch_bounds__(64 * kWaves, 4) void chain_kernel(const RecurCall c, const RecurChain ch, const float *first, void *out, int out_dtype, float *final_state,
                                                             bool flat, int groups) {
-    __shared__ float lds_lg[kWaves][64][V], lds_a[kWaves][64][V], lds_h[kWaves][64][V], lds_s[64][V];
+    __shared__ float lds_lg[kWaves][64][V], lds_a[kWaves][64][V], lds_h[kWaves][64][V], far_lgs[kWaves][64][V], far_zs[kWaves][64][V], lds_s[64][V];
+    __shared__ bool outs[kWaves];
     __shared__ uint32_t lds_ticket;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     if (threadIdx.x == 0) lds_ticket = __hip_atomic_fetch_add(ch.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -464,85 +465,97 @@ __global__ __launch_bounds__(64 * kWaves, 4) void chain_kernel(const RecurCall c
             lg[i] += lds_lg[w][lane][i];
         }
     }
-    if (wave == 0) {
-        const bool last = unit == c.nunits - 1;
-        const int block = unit / kRecurBlock, begins = block * kRecurBlock;
-        if (!last && unit - begins < kRecurBlock - 1) {
+    const int block = unit / kRecurBlock, in_block = unit - block * kRecurBlock;
+    const bool last = unit == c.nunits - 1;
+    if (wave == 0 && !last && in_block < kRecurBlock - 1) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) publish(local(unit, i), lg[i], z[i]);
-        }
-        // what the units from n + 1 to the one before this make of the state behind unit n: always added in one order
-        float far_lg[V] = {}, far_z[V] = {};
-        int n = unit - 1, polls = 0;
-        bool ran_out = false;
-        while (n >= begins && !ran_out) {
-            word_t part[kLook][V];
+        for (int i = 0; i < V; ++i) publish(local(unit, i), lg[i], z[i]);
+    }
+    // Looking back: each wave at kRecurBlock / kWaves units of the block, the first also for the state behind the block before
+    constexpr int kEach = kRecurBlock / kWaves;
+    const int begins = block * kRecurBlock + wave * kEach, count = min(max(unit - begins, 0), kEach);
+    float far_lg[V] = {}, far_z[V] = {};
+    bool ran_out = false;
+    if (count > 0) {
+        word_t part[kEach][V];
+        bool there = false;
+        for (int polls = 0; !there && !ran_out; ran_out = !there && ++polls > ch.polls) {
+            there = true;
 #pragma unroll
-            for (int k = 0; k < kLook; ++k)
+            for (int k = 0; k < kEach; ++k)
 #pragma unroll
-                for (int i = 0; i < V; ++i) part[k][i] = published(local(max(n - k, begins), i));
-            int passed = 0;
+                for (int i = 0; i < V; ++i) part[k][i] = published(local(begins + min(k, count - 1), i));
 #pragma unroll
-            for (int k = 0; k < kLook; ++k) {
-                bool there = passed == k && n - k >= begins;
+            for (int k = 0; k < kEach; ++k)
 #pragma unroll
                 for (int i = 0; i < V; ++i) there = there && part[k][i] != ~0ull;
-                if (!__all(there)) continue;
+            there = __all(there);
+        }
+#pragma unroll
+        for (int k = 0; k < kEach; ++k)
+            if (k < count) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    far_z[i] += decayed(far_lg[i], __builtin_bit_cast(float, (uint32_t)part[k][i]));
-                    far_lg[i] += __builtin_bit_cast(float, (uint32_t)(part[k][i] >> 32));
+                    const float d = __builtin_bit_cast(float, (uint32_t)(part[k][i] >> 32));
+                    far_z[i] = decayed(d, far_z[i]) + __builtin_bit_cast(float, (uint32_t)part[k][i]);
+                    far_lg[i] += d;
                 }
-                ++passed;
             }
-            n -= passed;
-            ran_out = passed == 0 && ++polls > ch.polls;
+    }
+    if (wave == 0 && block > 0) {
+        bool there = false;
+        for (int polls = 0; !there && !ran_out; ran_out = !there && ++polls > ch.polls) {
+            there = true;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const uint32_t w = published(after(block - 1, i));
+                there = there && w != ~0u;
+                enter[i] = __builtin_bit_cast(float, w);
+            }
+            there = __all(there);
         }
-        float state[V];
+    }
 #pragma unroll
-        for (int i = 0; i < V; ++i) state[i] = enter[i];
-        if (block > 0 || ran_out) {
-            bool there = false;
-            while (!there && !ran_out) {
-                there = true;
+    for (int i = 0; i < V; ++i) {
+        far_lgs[wave][lane][i] = far_lg[i];
+        far_zs[wave][lane][i] = far_z[i];
+        if (wave == 0) lds_s[lane][i] = enter[i];
+    }
+    if (lane == 0) outs[wave] = ran_out;
+    __syncthreads();
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const uint32_t w = published(after(block - 1, i));
-                    there = there && w != ~0u;
-                    state[i] = __builtin_bit_cast(float, w);
-                }
-                there = __all(there);
-                ran_out = !there && ++polls > ch.polls;
-            }
-            if (ran_out) {               // from the inputs, up to and with unit n
+    for (int i = 0; i < V; ++i) enter[i] = lds_s[lane][i];
+    ran_out = false;
+    for (int w = 0; w < kWaves; ++w) {
+        ran_out = ran_out || outs[w];
 #pragma unroll
-                for (int i = 0; i < V; ++i) state[i] = 0.f;
-                if (first != nullptr && p.any) load_state<V>(first, p.cell(c), state);
-                for (int t = 0; t < (n + 1) * kRecurChain; ++t) {
-                    Given<EX, EG, V, 1, KIND, false> again;
-                    again.load(c, p, nullptr, t);
-                    const Piece<EX, EG, V, 1, KIND, REST> r(again, c.inv_tau);
+        for (int i = 0; i < V; ++i) enter[i] = decayed(far_lgs[w][lane][i], enter[i]) + far_zs[w][lane][i];
+    }
+    if (__builtin_amdgcn_readfirstlane(ran_out)) {       // from the inputs, step by step
 #pragma unroll
-                    for (int i = 0; i < V; ++i) state[i] = decayed(r.lg[i], state[i]) + r.u[0][i];
-                }
-            }
+        for (int i = 0; i < V; ++i) enter[i] = 0.f;
+        if (first != nullptr && p.any) load_state<V>(first, p.cell(c), enter);
+        for (int t = 0; t < begin; ++t) {
+            Given<EX, EG, V, 1, KIND, false> again;
+            again.load(c, p, nullptr, t);
+            const Piece<EX, EG, V, 1, KIND, REST> r(again, c.inv_tau);
+#pragma unroll
+            for (int i = 0; i < V; ++i) enter[i] = decayed(r.lg[i], enter[i]) + r.u[0][i];
         }
+    }
+    if (wave == 0) {
+        const bool ends = p.n <= begin + kRecurChain && (p.n > begin || unit == 0);      // a sequence's last unit
         float leave[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            enter[i] = decayed(far_lg[i], state[i]) + far_z[i];
             leave[i] = decayed(lg[i], enter[i]) + z[i];
-            if (!last && unit - begins == kRecurBlock - 1) publish(after(block, i), leave[i]);
-            lds_s[lane][i] = enter[i];
+            if (!last && in_block == kRecurBlock - 1) publish(after(block, i), leave[i]);
         }
-        // (a sequence's last unit)
-        const bool ends = p.n <= begin + kRecurChain && (p.n > begin || unit == 0);
         if (ends && final_state != nullptr && p.any) store_state<V>(final_state, p.cell(c), leave);
     }
-    __syncthreads();
     float mine[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) mine[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(my_lg[i]), lds_s[lane][i], my_z[i]);
+    for (int i = 0; i < V; ++i) mine[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(my_lg[i]), enter[i], my_z[i]);
     put_outputs(c, p, q, mine, out, out_dtype, s, __all(s + kChainSteps <= p.n));
 }
 
