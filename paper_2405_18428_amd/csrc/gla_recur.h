@@ -5,7 +5,7 @@
 namespace gla {
 
 // Steps of a work-group's round: 8 waves of 8 steps; units of the backward pass are rounds, those of the forward pass two
-constexpr int kRecurSteps = 8, kRecurWaves = 8, kRecurRound = kRecurSteps * kRecurWaves, kRecurChain = 2 * kRecurRound;
+constexpr int kRecurSteps = 8, kRecurWaves = 8, kRecurRound = kRecurSteps * kRecurWaves, kRecurChain = 2 * kRecurRound, kRecurChainWaves = 8;
 constexpr int kRecurBlock = 16;         // units that look back over each other
 
 struct RecurCall {

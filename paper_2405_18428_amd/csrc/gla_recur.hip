@@ -405,7 +405,7 @@ __global__ __launch_bounds__(64 * kWaves) void walk_kernel(const RecurCall c, co
 }
 
 // Words that units publish: all ones are not there yet (a NaN that would look so gets other digits)
-constexpr int kChainSteps = 2 * kSteps;                  // of a wave
+constexpr int kChainWaves = kRecurChainWaves, kChainSteps = kRecurChain / kChainWaves;
 typedef unsigned long long word_t;
 __device__ __forceinline__ uint32_t bits_of(float x) { return x != x ? 0x7fc00000u : __builtin_bit_cast(uint32_t, x); }
 __device__ __forceinline__ void publish(word_t *p, float lg, float h) {
@@ -425,10 +425,10 @@ __global__ __launch_bounds__(256) void clear_kernel(uint32_t *words, long long c
 
 // Forward pass in units of 128 steps, 16 a wave.  Bound by HBM.
 template <typename EX, typename EG, int V, int KIND, bool REST>
-__global__ __launch_bounds__(64 * kWaves, 4) void chain_kernel(const RecurCall c, const RecurChain ch, const float *first, void *out, int out_dtype, float *final_state,
+__global__ __launch_bounds__(64 * kChainWaves, 4) void chain_kernel(const RecurCall c, const RecurChain ch, const float *first, void *out, int out_dtype, float *final_state,
                                                             bool flat, int groups) {
-    __shared__ float lds_lg[kWaves][64][V], lds_a[kWaves][64][V], lds_h[kWaves][64][V], far_lgs[kWaves][64][V], far_zs[kWaves][64][V], lds_s[64][V];
-    __shared__ bool outs[kWaves];
+    __shared__ float lds_lg[kChainWaves][64][V], lds_a[kChainWaves][64][V], lds_h[kChainWaves][64][V], far_lgs[kChainWaves][64][V], far_zs[kChainWaves][64][V], lds_s[64][V];
+    __shared__ bool outs[kChainWaves];
     __shared__ uint32_t lds_ticket;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     if (threadIdx.x == 0) lds_ticket = __hip_atomic_fetch_add(ch.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -453,14 +453,11 @@ __global__ __launch_bounds__(64 * kWaves, 4) void chain_kernel(const RecurCall c
         lds_h[wave][lane][i] = q.from_zero(i);
     }
     __syncthreads();
-    float z[V] = {}, lg[V] = {}, my_z[V] = {}, my_lg[V] = {};
-    for (int w = 0; w < kWaves; ++w) {
+    // of the waves before this one (the first wave: of the whole unit)
+    float z[V] = {}, lg[V] = {};
+    for (int w = 0; w < (wave == 0 ? kChainWaves : wave); ++w) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            if (w == wave) {
-                my_z[i] = z[i];
-                my_lg[i] = lg[i];
-            }
             z[i] = __builtin_fmaf(lds_a[w][lane][i], z[i], lds_h[w][lane][i]);
             lg[i] += lds_lg[w][lane][i];
         }
@@ -471,8 +468,8 @@ __global__ __launch_bounds__(64 * kWaves, 4) void chain_kernel(const RecurCall c
 #pragma unroll
         for (int i = 0; i < V; ++i) publish(local(unit, i), lg[i], z[i]);
     }
-    // Looking back: each wave at kRecurBlock / kWaves units of the block, the first also for the state behind the block before
-    constexpr int kEach = kRecurBlock / kWaves;
+    // Looking back: each wave at kRecurBlock / kChainWaves units of the block, the first also for the state behind the block before
+    constexpr int kEach = kRecurBlock / kChainWaves;
     const int begins = block * kRecurBlock + wave * kEach, count = min(max(unit - begins, 0), kEach);
     float far_lg[V] = {}, far_z[V] = {};
     bool ran_out = false;
@@ -497,7 +494,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void chain_kernel(const RecurCall c
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     const float d = __builtin_bit_cast(float, (uint32_t)(part[k][i] >> 32));
-                    far_z[i] = decayed(d, far_z[i]) + __builtin_bit_cast(float, (uint32_t)part[k][i]);
+                    far_z[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(d), far_z[i], __builtin_bit_cast(float, (uint32_t)part[k][i]));
                     far_lg[i] += d;
                 }
             }
@@ -523,14 +520,20 @@ __global__ __launch_bounds__(64 * kWaves, 4) void chain_kernel(const RecurCall c
     }
     if (lane == 0) outs[wave] = ran_out;
     __syncthreads();
+    // each wave's units through the decay behind them, and the state through all of it
 #pragma unroll
-    for (int i = 0; i < V; ++i) enter[i] = lds_s[lane][i];
+    for (int i = 0; i < V; ++i) far_lg[i] = far_z[i] = 0.f;
     ran_out = false;
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = kChainWaves - 1; w >= 0; --w) {
         ran_out = ran_out || outs[w];
 #pragma unroll
-        for (int i = 0; i < V; ++i) enter[i] = decayed(far_lgs[w][lane][i], enter[i]) + far_zs[w][lane][i];
+        for (int i = 0; i < V; ++i) {
+            far_z[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(far_lg[i]), far_zs[w][lane][i], far_z[i]);
+            far_lg[i] += far_lgs[w][lane][i];
+        }
     }
+#pragma unroll
+    for (int i = 0; i < V; ++i) enter[i] = decayed(far_lg[i], lds_s[lane][i]) + far_z[i];
     if (__builtin_amdgcn_readfirstlane(ran_out)) {       // from the inputs, step by step
 #pragma unroll
         for (int i = 0; i < V; ++i) enter[i] = 0.f;
@@ -553,10 +556,11 @@ __global__ __launch_bounds__(64 * kWaves, 4) void chain_kernel(const RecurCall c
         }
         if (ends && final_state != nullptr && p.any) store_state<V>(final_state, p.cell(c), leave);
     }
-    float mine[V];
+    if (wave > 0) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) mine[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(my_lg[i]), enter[i], my_z[i]);
-    put_outputs(c, p, q, mine, out, out_dtype, s, __all(s + kChainSteps <= p.n));
+        for (int i = 0; i < V; ++i) enter[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(lg[i]), enter[i], z[i]);
+    }
+    put_outputs(c, p, q, enter, out, out_dtype, s, __all(s + kChainSteps <= p.n));
 }
 
 // Gradients of one round of 64 V channels: states from the front, adjoints from behind, 8 steps a wave.
@@ -604,12 +608,27 @@ __global__ __launch_bounds__(64 * kWaves) void back_kernel(const RecurCall c, co
         lds_o[wave][lane][i] = r;
     }
     __syncthreads();
-    for (int w = 0; w < wave; ++w)
+    // the other waves' states and adjoints through the decay between, what enters the round through all of it
+    float z[V] = {}, lg[V] = {};
+    for (int w = wave - 1; w >= 0; --w)
 #pragma unroll
-        for (int i = 0; i < V; ++i) h[i] = decayed(lds_lg[w][lane][i], h[i]) + lds_h[w][lane][i];
-    for (int w = waves - 1; w > wave; --w)
+        for (int i = 0; i < V; ++i) {
+            z[i] = fmaf(__builtin_amdgcn_exp2f(lg[i]), lds_h[w][lane][i], z[i]);
+            lg[i] += lds_lg[w][lane][i];
+        }
 #pragma unroll
-        for (int i = 0; i < V; ++i) adj[i] = decayed(lds_lg[w][lane][i], adj[i]) + lds_o[w][lane][i];
+    for (int i = 0; i < V; ++i) {
+        h[i] = fmaf(__builtin_amdgcn_exp2f(lg[i]), h[i], z[i]);
+        z[i] = lg[i] = 0.f;
+    }
+    for (int w = wave + 1; w < waves; ++w)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            z[i] = fmaf(__builtin_amdgcn_exp2f(lg[i]), lds_o[w][lane][i], z[i]);
+            lg[i] += lds_lg[w][lane][i];
+        }
+#pragma unroll
+    for (int i = 0; i < V; ++i) adj[i] = fmaf(__builtin_amdgcn_exp2f(lg[i]), adj[i], z[i]);
 #pragma unroll
     for (int j = 0; j < kSteps; ++j)
 #pragma unroll
@@ -741,7 +760,7 @@ hipError_t launch_recur_chain(const RecurCall &c, const RecurChain &ch, const fl
     return instance(c, c.D % 2 == 0, [&](auto x, auto g, auto kind, auto rest, auto v) {
         constexpr int V = decltype(v)::value;
         const Groups n = groups_of(c, V);
-        hipLaunchKernelGGL((chain_kernel<decltype(x), decltype(g), V, kind.value, rest.value>), dim3((unsigned)((long long)n.count * c.nunits)), dim3(64 * kWaves), 0, stream,
+        hipLaunchKernelGGL((chain_kernel<decltype(x), decltype(g), V, kind.value, rest.value>), dim3((unsigned)((long long)n.count * c.nunits)), dim3(64 * kChainWaves), 0, stream,
                            c, ch, first, out, out_dtype, final_state, n.flat, n.count);
         return hipGetLastError();
     });
