@@ -47,13 +47,13 @@ __device__ __forceinline__ float to_float(uint16_t e) { return __builtin_bit_cas
 __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), bf16x2));
 }
-// V values to element `at` of a tensor of this type
+// V values to element `at` behind a row that the whole wave shares (bytes of a lane's place in 32 bits)
 template <int V>
 __device__ __forceinline__ void store(void *base, int dtype, long long row, uint32_t at, const float (&v)[V]) {
     if (dtype == GLA_DT_BF16) {
-        uint16_t *p = static_cast<uint16_t *>(base) + row + at;
+        char *p = static_cast<char *>(base) + row * 2 + at * 2u;
         if constexpr (V == 1) {
-            *p = (uint16_t)pack(v[0], 0.f);
+            *reinterpret_cast<uint16_t *>(p) = (uint16_t)pack(v[0], 0.f);
         } else {
             uint32_t b[V / 2];
 #pragma unroll
@@ -61,7 +61,7 @@ __device__ __forceinline__ void store(void *base, int dtype, long long row, uint
             __builtin_memcpy(__builtin_assume_aligned(p, 2 * V), b, sizeof(b));
         }
     } else {
-        float *p = static_cast<float *>(base) + row + at;
+        char *p = static_cast<char *>(base) + row * 4 + at * 4u;
         __builtin_memcpy(__builtin_assume_aligned(p, 4 * V), v, sizeof(v));
     }
 }
@@ -292,6 +292,43 @@ __global__ __launch_bounds__(256) void units_kernel(const RecurCall c, const voi
         }
     }
     if (!p.any) return;
+    const long long at = ((long long)p.b * c.nunits + unit) * c.D + p.channel;
+    store_state<V>(u.decay, at, lg);
+    store_state<V>(u.state, at, h);
+    store_state<V>(u.adjoint, at, adj);
+}
+
+// The same with a work-group for each unit, 8 steps a wave, where there are few units
+template <typename EX, typename EG, int V, int KIND, bool REST>
+__global__ __launch_bounds__(64 * kWaves) void units_apart_kernel(const RecurCall c, const void *d_out, const RecurUnits u, bool flat, int groups) {
+    __shared__ float lds_lg[kWaves][64][V], lds_h[kWaves][64][V], lds_o[kWaves][64][V];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int unit = blockIdx.x / (unsigned)groups, group = blockIdx.x - (unsigned)unit * (unsigned)groups;
+    const Place<V> p(c, flat, group);
+    Given<EX, EG, V, kSteps, KIND, true> in;
+    in.load(c, p, d_out, unit * c.unit + wave * kSteps);
+    const Piece<EX, EG, V, kSteps, KIND, REST> q(in, c.inv_tau);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        float b = 0.f;
+#pragma unroll
+        for (int j = kSteps - 1; j >= 0; --j) b = q.a[j][i] * (to_float(in.o.r[j].e[i]) + b);
+        lds_lg[wave][lane][i] = q.lg[i];
+        lds_h[wave][lane][i] = q.from_zero(i);
+        lds_o[wave][lane][i] = b;
+    }
+    __syncthreads();
+    if (wave > 0 || !p.any) return;
+    float lg[V] = {}, h[V] = {}, adj[V] = {};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float d = lds_lg[w][lane][i];
+            h[i] = decayed(d, h[i]) + lds_h[w][lane][i];
+            adj[i] = fmaf(__builtin_amdgcn_exp2f(lg[i]), lds_o[w][lane][i], adj[i]);
+            lg[i] += d;
+        }
     const long long at = ((long long)p.b * c.nunits + unit) * c.D + p.channel;
     store_state<V>(u.decay, at, lg);
     store_state<V>(u.state, at, h);
@@ -565,7 +602,7 @@ __global__ __launch_bounds__(64 * kChainWaves, 4) void chain_kernel(const RecurC
 
 // Gradients of one round of 64 V channels: states from the front, adjoints from behind, 8 steps a wave.
 template <typename EX, typename EG, int V, int KIND, bool REST>
-__global__ __launch_bounds__(64 * kWaves) void back_kernel(const RecurCall c, const void *d_out, const RecurUnits u, const float *first, const float *last,
+__global__ __launch_bounds__(64 * kWaves, 4) void back_kernel(const RecurCall c, const void *d_out, const RecurUnits u, const float *first, const float *last,
                                                            void *dx, void *dgate, int grad_dtype, float *d_first, bool flat, int groups) {
     __shared__ float lds_lg[kWaves][64][V], lds_h[kWaves][64][V], lds_o[kWaves][64][V];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), waves = blockDim.x >> 6;
@@ -585,31 +622,36 @@ __global__ __launch_bounds__(64 * kWaves) void back_kernel(const RecurCall c, co
             if (last != nullptr) load_state<V>(last, p.cell(c), adj);
         }
     }
-    // of each step: the gate, what it lacks of one, its slope; the input, then the state before the step; dO, then the adjoint
-    float a[kSteps][V], rest[REST ? kSteps : 1][V], slope[KIND == GLA_GATE_PRE ? kSteps : 1][V], x[kSteps][V], b[kSteps][V], o[kSteps][V];
+    // of each step: the gate, what it lacks of one, the gate times its slope, then times what the adjoint meets there
+    float a[kSteps][V], rest[REST ? kSteps : 1][V], b[kSteps][V], lg[V] = {}, z[V] = {};
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const Gate gt = gate_of<KIND, true>(to_float(in.g.r[j].e[i]), c.inv_tau);
+            const float x = to_float(in.x.r[j].e[i]);
+            a[j][i] = gt.a;
+            b[j][i] = KIND == GLA_GATE_PRE ? gt.a * gt.slope : gt.a;
+            asm volatile("" : "+v"(b[j][i]));            // (formed here: left for later its parts take twice the registers)
+            if constexpr (REST) rest[j][i] = -less_one(gt.lg * kLn2, gt.a);
+            lg[i] += gt.lg;
+            z[i] = REST ? fmaf(a[j][i], z[i], rest[j][i] * x) : fmaf(a[j][i], z[i], x);
+        }
+        // (all steps at once take more registers than there are)
+        __builtin_amdgcn_sched_barrier(0);
+    }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        float lg = 0.f, t = 0.f, r = 0.f;
+        lds_lg[wave][lane][i] = lg[i];
+        lds_h[wave][lane][i] = z[i];
+        float r = 0.f;
 #pragma unroll
-        for (int j = 0; j < kSteps; ++j) {
-            const Gate gt = gate_of<KIND, true>(to_float(in.g.r[j].e[i]), c.inv_tau);
-            a[j][i] = gt.a;
-            if constexpr (KIND == GLA_GATE_PRE) slope[j][i] = gt.slope;
-            if constexpr (REST) rest[j][i] = -less_one(gt.lg * kLn2, gt.a);
-            x[j][i] = to_float(in.x.r[j].e[i]);
-            o[j][i] = to_float(in.o.r[j].e[i]);
-            lg += gt.lg;
-            t = REST ? fmaf(a[j][i], t, rest[j][i] * x[j][i]) : fmaf(a[j][i], t, x[j][i]);
-        }
-#pragma unroll
-        for (int j = kSteps - 1; j >= 0; --j) r = a[j][i] * (o[j][i] + r);
-        lds_lg[wave][lane][i] = lg;
-        lds_h[wave][lane][i] = t;
+        for (int j = kSteps - 1; j >= 0; --j) r = a[j][i] * (to_float(in.o.r[j].e[i]) + r);
         lds_o[wave][lane][i] = r;
+        lg[i] = z[i] = 0.f;
     }
     __syncthreads();
     // the other waves' states and adjoints through the decay between, what enters the round through all of it
-    float z[V] = {}, lg[V] = {};
     for (int w = wave - 1; w >= 0; --w)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -629,43 +671,44 @@ __global__ __launch_bounds__(64 * kWaves) void back_kernel(const RecurCall c, co
         }
 #pragma unroll
     for (int i = 0; i < V; ++i) adj[i] = fmaf(__builtin_amdgcn_exp2f(lg[i]), adj[i], z[i]);
-#pragma unroll
-    for (int j = 0; j < kSteps; ++j)
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            // less the input, where 1 - a scales it
-            b[j][i] = REST ? h[i] - x[j][i] : h[i];
-            h[i] = REST ? fmaf(a[j][i], h[i], rest[j][i] * x[j][i]) : fmaf(a[j][i], h[i], x[j][i]);
-        }
-#pragma unroll
-    for (int j = kSteps - 1; j >= 0; --j)
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            o[j][i] += adj[i];
-            adj[i] = a[j][i] * o[j][i];
-        }
     Cursor k(c, p, s);
-    const bool whole = __all(s + kSteps <= p.n);
+    long long rows[kSteps];
 #pragma unroll
     for (int j = 0; j < kSteps; ++j) {
+        rows[j] = k.at;
+        k.next(c);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float x = to_float(in.x.r[j].e[i]);
+            b[j][i] *= REST ? h[i] - x : h[i];           // (the state before the step)
+            h[i] = REST ? fmaf(a[j][i], h[i], rest[j][i] * x) : fmaf(a[j][i], h[i], x);
+        }
+    }
+    const bool whole = __all(s + kSteps <= p.n);
+#pragma unroll
+    for (int j = kSteps - 1; j >= 0; --j) {
         float gx[V], gg[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            gx[i] = REST ? rest[j][i] * o[j][i] : o[j][i];
-            gg[i] = a[j][i] * b[j][i] * o[j][i];
-            if constexpr (KIND == GLA_GATE_PRE) gg[i] *= slope[j][i];
+            const float G = to_float(in.o.r[j].e[i]) + adj[i];
+            gx[i] = REST ? rest[j][i] * G : G;
+            gg[i] = b[j][i] * G;
+            adj[i] = a[j][i] * G;
         }
-        const int t = s + j;
-        if (whole || (t < p.n && p.any)) {
-            store<V>(dx, grad_dtype, k.at, p.at, gx);
-            store<V>(dgate, grad_dtype, k.at, p.at, gg);
-        } else if (t < c.T && p.any) {   // rows behind a sequence's end are cleared: step t stands for token t there, in both directions
-            const float zero[V] = {};
+        if (whole || s + j < p.n) {
+            store<V>(dx, grad_dtype, rows[j], p.at, gx);
+            store<V>(dgate, grad_dtype, rows[j], p.at, gg);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    if (!whole && p.any && c.seq_lens != nullptr) {      // rows behind a sequence's end are cleared: step t stands for token t there, in both directions
+        const float zero[V] = {};
+#pragma unroll 1
+        for (int t = max(s, p.n); t < min(s + kSteps, c.T); ++t) {
             const long long row = ((long long)p.b * c.T + t) * c.D;
             store<V>(dx, grad_dtype, row, (uint32_t)p.channel, zero);
             store<V>(dgate, grad_dtype, row, (uint32_t)p.channel, zero);
         }
-        k.next(c);
     }
     if (unit == 0 && c.nunits == 1 && wave == 0 && d_first != nullptr && p.any) store_state<V>(d_first, p.cell(c), adj);
 }
@@ -717,12 +760,19 @@ Groups groups_of(const RecurCall &c, int V) {
 
 }  // namespace
 
+// Below so many units each gets a work-group, not a wave (backward calls: 192 units 18 us instead of 26, 1152 47 instead of 52, 2048 66 instead of 65)
+constexpr long long kFewUnits = 2048;
 hipError_t launch_recur_units(const RecurCall &c, const void *d_out, const RecurUnits &u, hipStream_t stream) {
     return instance(c, c.D % 2 == 0, [&](auto x, auto g, auto kind, auto rest, auto v) {
         constexpr int V = decltype(v)::value;
         const Groups n = groups_of(c, V);
-        hipLaunchKernelGGL((units_kernel<decltype(x), decltype(g), V, kind.value, rest.value>), dim3((unsigned)(((long long)n.count * c.nunits + 3) / 4)), dim3(256), 0,
-                           stream, c, d_out, u, n.flat, n.count);
+        const long long units = (long long)n.count * c.nunits;
+        if (units < kFewUnits)
+            hipLaunchKernelGGL((units_apart_kernel<decltype(x), decltype(g), V, kind.value, rest.value>), dim3((unsigned)units), dim3(64 * kWaves), 0, stream, c, d_out, u,
+                               n.flat, n.count);
+        else
+            hipLaunchKernelGGL((units_kernel<decltype(x), decltype(g), V, kind.value, rest.value>), dim3((unsigned)((units + 3) / 4)), dim3(256), 0, stream, c, d_out, u,
+                               n.flat, n.count);
         return hipGetLastError();
     });
 }
