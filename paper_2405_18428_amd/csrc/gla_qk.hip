@@ -3,10 +3,12 @@
 // R turning the pairs of channels by the token's angles as in gla_rope.hip; and backward, with dy' = R^-1 dy and dn = dy' w:
 //   dx = r (dn - n mean(dn n)),   dw = sum over rows of dy' n.
 //
-// 4 to 32 lanes hold a row, 8 channels each; they take one token, form the sines and cosines of its angles once and go through some
-// of its heads, queries and keys alike, with the next row on its way.  A pair of neighbouring channels lies in one lane; the other channel of a
-// pair of halves is fetched through LDS, where a row's lanes, which are in one wave, leave their values.  Sums for dw stay in registers, are
-// added over a work-group and go to memory as one partial sum a work-group, which a second kernel adds in one order.  Bound by HBM.
+// A wave takes one token, forms the sines and cosines of its angles, a pair a lane, and goes through its heads, queries and then keys: 4 to 32 lanes hold a
+// row, 8 channels each, so that a wave has 2 to 16 heads at a time, which lie together where a token's heads do, with the next ones on their way.  A pair
+// of neighbouring channels lies in one lane; the other channel of a pair of halves is fetched through LDS, as the sines and cosines are; all of it is
+// one wave's, so there are no barriers.  Forward the norm's factor is applied last, so that the exchange does not wait for the row's sum.  Sums
+// for dw stay in registers, are added over a work-group and go to memory as one partial sum a work-group, which a second kernel adds in one order.
+// Bound by HBM.
 #include "gla_qk.h"
 #include "gla_rope_util.h"
 #include "gla_rows.h"
@@ -16,10 +18,18 @@ namespace {
 
 constexpr int kThreads = 256;
 
+// Over the lanes of a row, in all of them: neighbours, pairs, fours and eights of 16 lanes exchange inside the vector unit
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
 template <int LANES>
 __device__ __forceinline__ float row_sum(float v) {
-#pragma unroll
-    for (int d = 1; d < LANES; d *= 2) v += __shfl_xor(v, d);
+    v += dpp<0xb1>(v);
+    v += dpp<0x4e>(v);
+    if constexpr (LANES >= 8) v += dpp<0x141>(v);        // (lane i and 7 - i)
+    if constexpr (LANES >= 16) v += dpp<0x140>(v);       // (lane i and 15 - i)
+    if constexpr (LANES >= 32) v += __shfl_xor(v, 16);
     return v;
 }
 
@@ -50,26 +60,23 @@ struct Channel {
 
 template <typename E, int LANES, bool BACK>
 __global__ __launch_bounds__(kThreads) void qk_kernel(const QkParams p, int each, int parts) {
-    constexpr int kGroups = kThreads / LANES, kWidth = LANES * kEach;
-    __shared__ __attribute__((aligned(16))) float rows[kGroups][kWidth];
+    constexpr int kRows = 64 / LANES, kWaves = kThreads / 64, kWidth = LANES * kEach, kPairs = kWidth / 2;
+    __shared__ __attribute__((aligned(16))) float rows[kWaves * kRows][kWidth];
+    __shared__ float2 angles[kWaves][kPairs];            // cosine, sine
     const RopeParams &r = p.rope;
-    const int gi = threadIdx.x / LANES, lane = threadIdx.x % LANES;
-    const int c0 = lane * kEach, d = r.d;
-    const int heads = p.side[0].heads + p.side[1].heads;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int gi = threadIdx.x / LANES, sub = lane / LANES, c0 = lane % LANES * kEach, d = r.d;
     const uint32_t items = (uint32_t)r.B * (uint32_t)r.T * (uint32_t)parts;      // < 2^31 (host check)
     const bool halves = r.pairs > 0 && !r.adjacent;
     const float inv = 1.f / (float)d;
     const int out_size = p.out_dtype == GLA_DT_BF16 ? 2 : 4;
 
-    float w[2][kEach], dw[2][kEach];
+    float dw[2][kEach];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) w[t][j] = 1.f, dw[t][j] = 0.f;
-        if (p.side[t].weight != nullptr) load_piece<float>(reinterpret_cast<const char *>(p.side[t].weight), c0, d, w[t]);
-    }
+        for (int j = 0; j < kEach; ++j) dw[t][j] = 0.f;
     Channel ch[kEach];
-    float cs[kEach], sn[kEach];         // y[c] = v[c] cs + v[other] sn
 #pragma unroll
     for (int j = 0; j < kEach; ++j) ch[j] = Channel(r, c0 + j);
     // halves: the others are eight in a row that begin at a multiple of 4
@@ -77,99 +84,138 @@ __global__ __launch_bounds__(kThreads) void qk_kernel(const QkParams p, int each
 #pragma unroll
     for (int j = 1; j < kEach; ++j) together = together && ch[j].other() == ch[0].other() + j;
 
-    auto rotate = [&](float (&v)[kEach], float sign) __attribute__((always_inline)) {
-        if (r.pairs == 0) return;
-        float o[kEach];
+    // the pairs' other channels
+    auto others = [&](const float (&v)[kEach], float (&o)[kEach]) __attribute__((always_inline)) {
         if (!halves) {
 #pragma unroll
             for (int j = 0; j < kEach; ++j) o[j] = v[j ^ 1];
-        } else {
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_memcpy(__builtin_assume_aligned(&rows[gi][c0], 16), v, sizeof(v));
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            if (together) {
-                __builtin_memcpy(o, __builtin_assume_aligned(&rows[gi][ch[0].other()], 16), sizeof(o));
-            } else {
-#pragma unroll
-                for (int j = 0; j < kEach; ++j) o[j] = rows[gi][ch[j].other()];
-            }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            return;
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_memcpy(__builtin_assume_aligned(&rows[gi][c0], 16), v, sizeof(v));
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (together) {
+            __builtin_memcpy(o, __builtin_assume_aligned(&rows[gi][ch[0].other()], 16), sizeof(o));
+        } else {
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) v[j] = fmaf(o[j], sign * sn[j], v[j] * cs[j]);
+            for (int j = 0; j < kEach; ++j) o[j] = rows[gi][ch[j].other()];
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     };
 
-    for (uint32_t item = blockIdx.x * (uint32_t)kGroups + gi; item < items; item += gridDim.x * (uint32_t)kGroups) {
+    for (uint32_t item = blockIdx.x * (uint32_t)kWaves + wave; item < items; item += gridDim.x * (uint32_t)kWaves) {
         const uint32_t token = item / (uint32_t)parts;
         const int part = (int)(item - token * (uint32_t)parts);
         const int b = (int)(token / (uint32_t)r.T), n = (int)(token - (uint32_t)b * (uint32_t)r.T);
-        const int h0 = part * each, h1 = min(h0 + each, heads);
+        float cs[kEach], sn[kEach];      // y[c] = v[c] cs + v[other] sn
         if (r.pairs > 0) {
-            // neighbouring channels of a pair share an angle
+            for (int pair = lane; pair < r.pairs; pair += 64) {
+                int axis = 0;
+                while (pair >= r.pairs_end[axis]) ++axis;
+                float2 a;
+                turn(r, pair, (double)position(r, token, n, axis), &a.x, &a.y);
+                angles[wave][pair] = a;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
             for (int j = 0; j < kEach; ++j) {
-                float c = 1.f, s = 0.f;
-                if (r.adjacent && (j & 1)) {
-                    c = cs[j - 1];
-                    s = -sn[j - 1];
-                } else if (ch[j].turned()) {
-                    turn(r, ch[j].pair(), (double)position(r, token, n, ch[j].axis()), &c, &s);
-                    if (!ch[j].second()) s = -s;
-                }
-                cs[j] = c;
-                sn[j] = s;
+                const float2 a = angles[wave][ch[j].pair()];
+                cs[j] = ch[j].turned() ? a.x : 1.f;
+                sn[j] = ch[j].turned() ? (ch[j].second() ? a.y : -a.y) : 0.f;
             }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        } else {
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) cs[j] = 1.f, sn[j] = 0.f;
         }
-        Raw<E> nx, no;
-        auto ask = [&](int h) __attribute__((always_inline)) {
-            const int t = h >= p.side[0].heads;
+        // the part's turns: those of the queries, then those of the keys
+        const int turns_q = (p.side[0].heads + kRows - 1) / kRows, t0 = part * each, t1 = t0 + each;
+        auto one_side = [&](auto side) __attribute__((always_inline)) {
+            constexpr int t = decltype(side)::value;
             const QkSide &s = p.side[t];
-            const int head = h - (t ? p.side[0].heads : 0);
-            nx = load_raw<E>(static_cast<const char *>(s.x) + (b * s.sb + head * s.sh + n * s.st) * (long long)sizeof(E), c0, d);
-            if constexpr (BACK) {
-                const long long row = r.layout == GLA_LAYOUT_BHTD ? ((long long)b * s.heads + head) * r.T + n : (long long)token * s.heads + head;
-                no = load_raw<E>(static_cast<const char *>(s.d_out) + row * d * (long long)sizeof(E), c0, d);
-            }
-        };
-        ask(h0);
-        for (int h = h0; h < h1; ++h) {
-            const int t = h >= p.side[0].heads;
-            const QkSide &s = p.side[t];
-            const int head = h - (t ? p.side[0].heads : 0);
-            const long long row = r.layout == GLA_LAYOUT_BHTD ? ((long long)b * s.heads + head) * r.T + n : (long long)token * s.heads + head;
-            float x[kEach], o[kEach];
-            to_floats<E>(nx, x);
-            if constexpr (BACK) to_floats<E>(no, o);
-            if (h + 1 < h1) ask(h + 1);
-            float ss = 0.f;
+            const int first = (t ? max(t0 - turns_q, 0) : t0) * kRows, end = min((t ? t1 - turns_q : t1) * kRows, s.heads);
+            if (first >= end) return;
+            // uniform places of the first row, and each lane's row from there
+            const char *x = static_cast<const char *>(s.x) + (b * s.sb + first * s.sh + n * s.st) * (long long)sizeof(E);
+            const long long next_x = s.sh * (long long)sizeof(E), mine_x = sub * next_x;
+            const long long row = (r.layout == GLA_LAYOUT_BHTD ? ((long long)b * s.heads + first) * r.T + n : (long long)token * s.heads + first) * d;
+            const long long next = r.layout == GLA_LAYOUT_BHTD ? (long long)r.T * d : d, mine = sub * next;
+            const char *o = BACK ? static_cast<const char *>(s.d_out) + row * (long long)sizeof(E) : nullptr;
+            char *out = static_cast<char *>(s.out) + row * out_size;
+            float w[kEach], ws[kEach];
 #pragma unroll
-            for (int j = 0; j < kEach; ++j) ss = fmaf(x[j], x[j], ss);
-            const float rstd = 1.f / __builtin_sqrtf(fmaf(row_sum<LANES>(ss), inv, p.eps));
-            char *out = static_cast<char *>(s.out) + row * d * out_size;
-            if constexpr (!BACK) {
-#pragma unroll
-                for (int j = 0; j < kEach; ++j) x[j] *= rstd * (t ? w[1][j] : w[0][j]);
-                rotate(x, 1.f);
-                store_piece(out, c0, d, p.out_dtype, x);
-            } else {
-                rotate(o, -1.f);
-                float m = 0.f;
+            for (int j = 0; j < kEach; ++j) w[j] = 1.f;
+            if (s.weight != nullptr) load_piece<float>(reinterpret_cast<const char *>(s.weight), c0, d, w);
+            if constexpr (!BACK) {       // the weight, through the turning
+                others(w, ws);
 #pragma unroll
                 for (int j = 0; j < kEach; ++j) {
-                    const float nn = x[j] * rstd, g = o[j] * nn;
-                    dw[0][j] += t ? 0.f : g;
-                    dw[1][j] += t ? g : 0.f;
-                    const float dn = o[j] * (t ? w[1][j] : w[0][j]);
-                    m = fmaf(dn, nn, m);
-                    x[j] = nn;
-                    o[j] = dn;
+                    w[j] *= cs[j];
+                    ws[j] *= sn[j];
                 }
-                m = row_sum<LANES>(m) * inv;
-#pragma unroll
-                for (int j = 0; j < kEach; ++j) x[j] = rstd * (o[j] - x[j] * m);
-                store_piece(out, c0, d, p.out_dtype, x);
             }
-        }
+            constexpr int kAhead = 2;
+            Raw<E> nx[kAhead], no[BACK ? kAhead : 1];
+            auto ask = [&](int i, int h) __attribute__((always_inline)) {
+                nx[i] = {};
+                if constexpr (BACK) no[i] = {};
+                if (h + sub < end) {
+                    nx[i] = load_raw<E>(x + mine_x, c0, d);
+                    if constexpr (BACK) no[i] = load_raw<E>(o + mine * (long long)sizeof(E), c0, d);
+                }
+                x += kRows * next_x;
+                if constexpr (BACK) o += kRows * next * (long long)sizeof(E);
+            };
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (first + i * kRows < end) ask(i, first + i * kRows);
+            for (int h0 = first; h0 < end; h0 += kAhead * kRows) {
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    const int h = h0 + i * kRows;
+                    if (h >= end) continue;
+                    float v[kEach], g[kEach], q[kEach];
+                    to_floats<E>(nx[i], v);
+                    if constexpr (BACK) to_floats<E>(no[i], g);
+                    if (h + kAhead * kRows < end) ask(i, h + kAhead * kRows);
+                    float ss = 0.f;
+#pragma unroll
+                    for (int j = 0; j < kEach; ++j) ss = fmaf(v[j], v[j], ss);
+                    if constexpr (!BACK) {
+                        if (r.pairs > 0) others(v, q);
+                        const float rstd = __builtin_amdgcn_rsqf(fmaf(row_sum<LANES>(ss), inv, p.eps));
+#pragma unroll
+                        for (int j = 0; j < kEach; ++j) {
+                            float y = v[j] * w[j];
+                            if (r.pairs > 0) y = fmaf(q[j], ws[j], y);
+                            v[j] = y * rstd;
+                        }
+                    } else {
+                        if (r.pairs > 0) {
+                            others(g, q);
+#pragma unroll
+                            for (int j = 0; j < kEach; ++j) g[j] = fmaf(q[j], -sn[j], g[j] * cs[j]);
+                        }
+                        const float rstd = __builtin_amdgcn_rsqf(fmaf(row_sum<LANES>(ss), inv, p.eps));
+                        float m = 0.f;
+#pragma unroll
+                        for (int j = 0; j < kEach; ++j) {
+                            v[j] *= rstd;
+                            dw[t][j] = fmaf(g[j], v[j], dw[t][j]);
+                            g[j] *= w[j];
+                            m = fmaf(g[j], v[j], m);
+                        }
+                        m = row_sum<LANES>(m) * -inv;
+#pragma unroll
+                        for (int j = 0; j < kEach; ++j) v[j] = rstd * fmaf(v[j], m, g[j]);
+                    }
+                    if (h + sub < end) store_piece(out + mine * out_size, c0, d, p.out_dtype, v);
+                    out += kRows * next * out_size;
+                }
+            }
+        };
+        one_side(std::integral_constant<int, 0>{});
+        one_side(std::integral_constant<int, 1>{});
     }
     if constexpr (BACK) {
 #pragma unroll
@@ -181,7 +227,7 @@ __global__ __launch_bounds__(kThreads) void qk_kernel(const QkParams p, int each
             for (int c = threadIdx.x; c < d; c += kThreads) {
                 float sum = 0.f;
 #pragma unroll 8
-                for (int k = 0; k < kGroups; ++k) sum += rows[k][c];
+                for (int k = 0; k < kWaves * kRows; ++k) sum += rows[k][c];
                 p.side[t].part[(size_t)blockIdx.x * d + c] = sum;
             }
         }
@@ -212,16 +258,14 @@ constexpr int kSlots = 1024;            // work-groups of the backward pass: fou
 
 template <typename E, int LANES, bool BACK>
 hipError_t qk(const QkParams &p, hipStream_t stream) {
-    constexpr int kGroups = kThreads / LANES;
-    const int heads = p.side[0].heads + p.side[1].heads;
+    constexpr int kRows = 64 / LANES, kWaves = kThreads / 64;
+    const int turns = (p.side[0].heads + kRows - 1) / kRows + (p.side[1].heads + kRows - 1) / kRows;
     const long long tokens = (long long)p.rope.B * p.rope.T;
-    // heads that share a token's sines and cosines: all, unless that leaves the GPU idle
-    int each = heads;
-    while (each > 1 && tokens * ((heads + each - 1) / each) < 2048LL * kGroups) each = (each + 1) / 2;
-    // (items in 31 bits)
-    while (each < heads && tokens * ((heads + each - 1) / each) >= (1LL << 31)) each *= 2;
-    const int parts = (heads + each - 1) / each;
-    const long long groups = (tokens * parts + kGroups - 1) / kGroups;
+    // turns that share a token's sines and cosines: all, unless that leaves the GPU idle
+    int each = turns;
+    while (each > 1 && tokens * ((turns + each - 1) / each) < 2048) each = (each + 1) / 2;
+    const int parts = (turns + each - 1) / each;         // (at most 2048 items where there is more than one)
+    const long long groups = (tokens * parts + kWaves - 1) / kWaves;
     const unsigned grid = BACK ? (unsigned)p.slots : (unsigned)(groups < (1 << 23) ? groups : 1 << 23);
     hipLaunchKernelGGL((qk_kernel<E, LANES, BACK>), dim3(grid), dim3(kThreads), 0, stream, p, each, parts);
     return hipGetLastError();
@@ -241,7 +285,6 @@ hipError_t qk_of(const QkParams &p, int dtype, hipStream_t stream) {
 }  // namespace
 
 int qk_slots(int B, int T) {
-    // (a work-group has 8 to 64 rows at a time, and at least one token's heads)
     const long long tokens = (long long)B * T;
     return tokens < kSlots ? (int)tokens : kSlots;
 }
