@@ -58,16 +58,18 @@ struct Channel {
     __device__ __forceinline__ int other() const { return word >> 16; }
 };
 
-template <typename E, int LANES, bool BACK>
+// MODE: any call, or rows that fill their lanes, all turned by neighbours, or by halves that lanes have whole
+enum { kAny, kNeighbours, kHalves };
+template <typename E, int LANES, bool BACK, int MODE>
 __global__ __launch_bounds__(kThreads) void qk_kernel(const QkParams p, int each, int parts) {
     constexpr int kRows = 64 / LANES, kWaves = kThreads / 64, kWidth = LANES * kEach, kPairs = kWidth / 2;
     __shared__ __attribute__((aligned(16))) float rows[kWaves * kRows][kWidth];
     __shared__ float2 angles[kWaves][kPairs];            // cosine, sine
     const RopeParams &r = p.rope;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int gi = threadIdx.x / LANES, sub = lane / LANES, c0 = lane % LANES * kEach, d = r.d;
+    const int gi = threadIdx.x / LANES, sub = lane / LANES, c0 = lane % LANES * kEach, d = MODE == kAny ? r.d : kWidth;
     const uint32_t items = (uint32_t)r.B * (uint32_t)r.T * (uint32_t)parts;      // < 2^31 (host check)
-    const bool halves = r.pairs > 0 && !r.adjacent;
+    const bool turns = MODE != kAny || r.pairs > 0, halves = MODE == kHalves || (MODE == kAny && r.pairs > 0 && !r.adjacent);
     const float inv = 1.f / (float)d;
     const int out_size = p.out_dtype == GLA_DT_BF16 ? 2 : 4;
 
@@ -79,10 +81,6 @@ __global__ __launch_bounds__(kThreads) void qk_kernel(const QkParams p, int each
     Channel ch[kEach];
 #pragma unroll
     for (int j = 0; j < kEach; ++j) ch[j] = Channel(r, c0 + j);
-    // halves: the others are eight in a row that begin at a multiple of 4
-    bool together = ch[0].other() % 4 == 0;
-#pragma unroll
-    for (int j = 1; j < kEach; ++j) together = together && ch[j].other() == ch[0].other() + j;
 
     // the pairs' other channels
     auto others = [&](const float (&v)[kEach], float (&o)[kEach]) __attribute__((always_inline)) {
@@ -94,7 +92,7 @@ __global__ __launch_bounds__(kThreads) void qk_kernel(const QkParams p, int each
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_memcpy(__builtin_assume_aligned(&rows[gi][c0], 16), v, sizeof(v));
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (together) {
+        if constexpr (MODE == kHalves) {
             __builtin_memcpy(o, __builtin_assume_aligned(&rows[gi][ch[0].other()], 16), sizeof(o));
         } else {
 #pragma unroll
@@ -108,7 +106,7 @@ __global__ __launch_bounds__(kThreads) void qk_kernel(const QkParams p, int each
         const int part = (int)(item - token * (uint32_t)parts);
         const int b = (int)(token / (uint32_t)r.T), n = (int)(token - (uint32_t)b * (uint32_t)r.T);
         float cs[kEach], sn[kEach];      // y[c] = v[c] cs + v[other] sn
-        if (r.pairs > 0) {
+        if (turns) {
             for (int pair = lane; pair < r.pairs; pair += 64) {
                 int axis = 0;
                 while (pair >= r.pairs_end[axis]) ++axis;
@@ -120,8 +118,8 @@ __global__ __launch_bounds__(kThreads) void qk_kernel(const QkParams p, int each
 #pragma unroll
             for (int j = 0; j < kEach; ++j) {
                 const float2 a = angles[wave][ch[j].pair()];
-                cs[j] = ch[j].turned() ? a.x : 1.f;
-                sn[j] = ch[j].turned() ? (ch[j].second() ? a.y : -a.y) : 0.f;
+                cs[j] = MODE != kAny || ch[j].turned() ? a.x : 1.f;
+                sn[j] = MODE != kAny || ch[j].turned() ? (ch[j].second() ? a.y : -a.y) : 0.f;
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         } else {
@@ -182,16 +180,16 @@ __global__ __launch_bounds__(kThreads) void qk_kernel(const QkParams p, int each
 #pragma unroll
                     for (int j = 0; j < kEach; ++j) ss = fmaf(v[j], v[j], ss);
                     if constexpr (!BACK) {
-                        if (r.pairs > 0) others(v, q);
+                        if (turns) others(v, q);
                         const float rstd = __builtin_amdgcn_rsqf(fmaf(row_sum<LANES>(ss), inv, p.eps));
 #pragma unroll
                         for (int j = 0; j < kEach; ++j) {
                             float y = v[j] * w[j];
-                            if (r.pairs > 0) y = fmaf(q[j], ws[j], y);
+                            if (turns) y = fmaf(q[j], ws[j], y);
                             v[j] = y * rstd;
                         }
                     } else {
-                        if (r.pairs > 0) {
+                        if (turns) {
                             others(g, q);
 #pragma unroll
                             for (int j = 0; j < kEach; ++j) g[j] = fmaf(q[j], -sn[j], g[j] * cs[j]);
@@ -267,7 +265,12 @@ hipError_t qk(const QkParams &p, hipStream_t stream) {
     const int parts = (turns + each - 1) / each;         // (at most 2048 items where there is more than one)
     const long long groups = (tokens * parts + kWaves - 1) / kWaves;
     const unsigned grid = BACK ? (unsigned)p.slots : (unsigned)(groups < (1 << 23) ? groups : 1 << 23);
-    hipLaunchKernelGGL((qk_kernel<E, LANES, BACK>), dim3(grid), dim3(kThreads), 0, stream, p, each, parts);
+    const RopeParams &r = p.rope;
+    bool whole = 2 * r.pairs == LANES * kEach;           // (sections, or their halves, in whole pieces)
+    for (int x = 0; x < r.axes; ++x) whole = whole && r.first[x] % kEach == 0 && r.half[x] % (r.adjacent ? 1 : kEach) == 0;
+    if (whole && r.adjacent) hipLaunchKernelGGL((qk_kernel<E, LANES, BACK, kNeighbours>), dim3(grid), dim3(kThreads), 0, stream, p, each, parts);
+    else if (whole) hipLaunchKernelGGL((qk_kernel<E, LANES, BACK, kHalves>), dim3(grid), dim3(kThreads), 0, stream, p, each, parts);
+    else hipLaunchKernelGGL((qk_kernel<E, LANES, BACK, kAny>), dim3(grid), dim3(kThreads), 0, stream, p, each, parts);
     return hipGetLastError();
 }
 template <bool BACK>
