@@ -355,6 +355,69 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
     }
 }
 
+// Forward for few rows, where the weights' reading is all: a work-group has 16 NT columns of both products, its waves a part of K each, whose weights go
+// from memory to the matrix units' registers; rows of x, which all work-groups share, come from L2.  The waves' sums meet in LDS.  MT: tiles of 16 rows.
+template <typename E, int WAVES, int MT, int NT>
+__global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(const ProductArgs p) {
+    constexpr int kES = sizeof(E), kAhead = MT + 2 * NT <= 4 ? 8 : MT + 2 * NT <= 8 ? 4 : 2;
+    __shared__ f32x4 sums[WAVES][2 * NT * MT][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), l = lane & 15, g = lane >> 4;
+    const int f0 = blockIdx.x * 16 * NT;
+    const Rsrc rw[2] = {view(p.b[0] + f0 * p.ldb, 0x7fffffffu), view(p.b[1] + f0 * p.ldb, 0x7fffffffu)}, rx = view(p.a[0], 0x7fffffffu);
+    // steps of 64 bytes of a row
+    const int steps = (p.K * kES + 63) / 64, each = (steps + WAVES - 1) / WAVES, s0 = wave * each, s1 = min(s0 + each, steps);
+    f32x4 acc[2 * NT][MT];
+#pragma unroll
+    for (int n = 0; n < 2 * NT; ++n)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s = s0; s < s1; s += kAhead) {
+        Frag<E> w[kAhead][2 * NT], x[kAhead][MT];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int at = (s + k) * 64 + g * 16;
+            const bool in = s + k < s1 && at < p.K * kES;
+#pragma unroll
+            for (int n = 0; n < 2 * NT; ++n) {
+                const int row = (n >> 1) * 16 + l;
+                w[k][n].v = fetch<decltype(w[k][n].v)>(rw[n & 1], in && f0 + row < p.N ? (uint32_t)(row * p.ldb) + at : kNowhere);
+            }
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+                x[k][m].v = fetch<decltype(x[k][m].v)>(rx, in && m * 16 + l < p.M ? (uint32_t)((m * 16 + l) * p.lda) + at : kNowhere);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int n = 0; n < 2 * NT; ++n) acc[n][m] = mma(w[k][n], x[k][m], acc[n][m]);
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < 2 * NT; ++n) sums[wave][m * 2 * NT + n][lane] = acc[n][m];
+    __syncthreads();
+    for (int i = wave; i < MT * NT; i += WAVES) {
+        f32x4 gt = sums[0][2 * i][lane], up = sums[0][2 * i + 1][lane];
+#pragma unroll
+        for (int k = 1; k < WAVES; ++k) {
+            gt += sums[k][2 * i][lane];
+            up += sums[k][2 * i + 1][lane];
+        }
+        const int row = i / NT * 16 + l, n = f0 + i % NT * 16 + 4 * g;
+        if (row >= p.M || n >= p.N) continue;
+        if (p.pre != nullptr) {
+            store4(p.pre, GLA_DT_F32, row, n, p.N, gt);
+            store4(p.pre + (long long)p.M * p.N, GLA_DT_F32, row, n, p.N, up);
+        }
+        f32x4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = activation<false>(p.act, gt[e]).y * up[e];
+        store4(p.out[0], p.out_dtype, row, n, p.N, y);
+    }
+}
+
 // dx from the parts of its sum, added in one order; four numbers a thread
 __global__ __launch_bounds__(256) void join_kernel(const float *part, void *out, int dtype, long long count, int splits) {
     const long long at = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
@@ -451,11 +514,38 @@ static ProductArgs forward_args(const GluCall &c) {
     return p;
 }
 
+// Up to so many rows (2048 x 8192, bf16: 64 rows 21 us, in tiles of 128 x 128 27, 100 rows 37 and 29; fp32: 128 rows 95 and 139)
+constexpr int kFewRows16 = 64, kFewRows32 = 128;
+template <typename E>
+static hipError_t few_rows(const ProductArgs &p, hipStream_t stream) {
+    const int tiles = (p.N + 15) / 16;
+    auto run = [&](auto mt) {
+        constexpr int MT = decltype(mt)::value;
+        // two work-groups a compute unit and more; with fewer columns more waves, each with less of K
+        if constexpr (MT == 3 || MT == 4) {              // (two tiles of columns for each reading of x: 64 rows 24 -> 20.6 us)
+            if (tiles >= 512) {
+                hipLaunchKernelGGL((few_rows_kernel<E, 8, MT, 2>), dim3((unsigned)(tiles + 1) / 2), dim3(512), 0, stream, p);
+                return hipGetLastError();
+            }
+        }
+        if (MT > 4 || tiles >= 512) hipLaunchKernelGGL((few_rows_kernel<E, 4, MT, 1>), dim3((unsigned)tiles), dim3(256), 0, stream, p);
+        else hipLaunchKernelGGL((few_rows_kernel<E, 8, MT <= 4 ? MT : 1, 1>), dim3((unsigned)tiles), dim3(512), 0, stream, p);
+        return hipGetLastError();
+    };
+    if (p.M <= 16) return run(std::integral_constant<int, 1>{});
+    if (p.M <= 32) return run(std::integral_constant<int, 2>{});
+    if (p.M <= 48) return run(std::integral_constant<int, 3>{});
+    if (sizeof(E) == 2 || p.M <= 64) return run(std::integral_constant<int, 4>{});
+    return run(std::integral_constant<int, sizeof(E) == 2 ? 4 : 8>{});
+}
+
 hipError_t launch_glu_fwd(const GluCall &c, void *out, int out_dtype, float *pre, hipStream_t stream) {
     ProductArgs p = forward_args(c);
     p.out[0] = out;
     p.out_dtype = out_dtype;
     p.pre = pre;
+    if (c.dtype == GLA_DT_BF16 && p.M <= kFewRows16) return few_rows<uint16_t>(p, stream);
+    if (c.dtype == GLA_DT_F32 && p.M <= kFewRows32) return few_rows<float>(p, stream);
     return product_of<kForward>(p, c.dtype, stream);
 }
 
