@@ -86,6 +86,7 @@ template <typename E, int ROWS, int WAVES, bool ACROSS, bool PAIRED>
 struct Tile {
     static constexpr int kES = sizeof(E), kDepth = kTileBytes / kES, kBytes = ROWS * kTileBytes, kLoads = kBytes / 1024 / WAVES;
     static constexpr int kPieces = ROWS * kES / 16;              // of a row, ACROSS
+    static constexpr int kReads = !ACROSS ? 1 : kES == 2 ? 2 : 4;
     uint32_t off[kLoads];               // of the lane's pieces from the operand's first one in the tile, or nowhere
 
     static __device__ __forceinline__ int turned(int k) { return kES == 2 ? 2 * ((k & 3) | ((k >> 3) & 1) << 2) : 4 * ((k >> 2) & 3); }
@@ -274,29 +275,56 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
     for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (t0 < t1) load(t0, 0);
-    __syncthreads();                     // (waits for what goes to LDS, too)
-    for (int t = t0; t < t1; ++t) {
-        const int buf = (t - t0) & 1;
-        if (t + 1 < t1) load(t + 1, buf ^ 1);
+    // Fragments of a tile's two halves.  The products of one half run while the other half's fragments are read: in the first phase those of the same
+    // tile's second half, in the second, behind the barrier that says that the next tile has come and that this one is read, those of the next tile's
+    // first half, while the tile after that is loaded over this one.
+    Frag<E> fa[2][MI], fb[2][NI];
+    auto read = [&](auto half, int buf) __attribute__((always_inline)) {
+        constexpr int kk = decltype(half)::value;
         const char *at = lds[buf], *bt = at + TA::kBytes;
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            Frag<E> fa[MI], fb[NI];
-#pragma unroll
-            for (int j = 0; j < NI; ++j) {
-                if constexpr (P == kForward) fb[j] = TB::read(bt + (j >> 1) * TB::kBytes, wn * 32 + (j & 1) * 16, kk, lane);
-                else fb[j] = TB::read(bt, (wn * NI + j) * 16, kk, lane);
-            }
-#pragma unroll
-            for (int i = 0; i < MI; ++i) fa[i] = TA::read(at, (wm * MI + i) * 16, kk, lane);
-#pragma unroll
-            for (int i = 0; i < MI; ++i)
-#pragma unroll
-                for (int j = 0; j < NI; ++j) acc[i][j] = mma(fb[j], fa[i], acc[i][j]);
+        for (int j = 0; j < NI; ++j) {
+            if constexpr (P == kForward) fb[kk][j] = TB::read(bt + (j >> 1) * TB::kBytes, wn * 32 + (j & 1) * 16, kk, lane);
+            else fb[kk][j] = TB::read(bt, (wn * NI + j) * 16, kk, lane);
         }
+#pragma unroll
+        for (int i = 0; i < MI; ++i) fa[kk][i] = TA::read(at, (wm * MI + i) * 16, kk, lane);
+    };
+    auto multiply = [&](auto half) __attribute__((always_inline)) {
+        constexpr int kk = decltype(half)::value;
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) acc[i][j] = mma(fb[kk][j], fa[kk][i], acc[i][j]);
+        // a read after every few products
+        constexpr int kReads = NI * TB::kReads + MI * TA::kReads, kProducts = MI * NI * (kES == 2 ? 1 : 4), kBetween = kProducts / kReads;
+#pragma unroll
+        for (int n = 0; n < kReads; ++n) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, kBetween, 0);
+        }
+    };
+    constexpr std::integral_constant<int, 0> first{};
+    constexpr std::integral_constant<int, 1> second{};
+    // every wave's loads have arrived in LDS, and its reads in registers (a barrier by itself does not wait for the former)
+    auto meet = [&]() __attribute__((always_inline)) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
+    };
+    if (t0 < t1) load(t0, 0);
+    if (t0 + 1 < t1) load(t0 + 1, 1);
+    meet();
+    read(first, 0);
+    for (int t = t0; t < t1; ++t) {
+        const int buf = (t - t0) & 1;
+        read(second, buf);
+        multiply(first);
+        meet();
+        if (t + 2 < t1) load(t + 2, buf);
+        read(first, buf ^ 1);            // (behind the last tile: of no use)
+        multiply(second);
     }
+    __syncthreads();
     // The tile goes through LDS, some rows of each wave at a time, so that a work-group stores whole rows and each result's code stands here once.
     // A lane has four neighbouring columns of one row of each 16 x 16 piece; pieces of 16 bytes are exchanged by XOR with the row.
     constexpr int kRows = sizeof(lds) / (BN * 4) < BM ? sizeof(lds) / (BN * 4) : BM, kPasses = BM / kRows, kSub = MI / kPasses;
