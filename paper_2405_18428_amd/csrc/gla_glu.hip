@@ -5,8 +5,7 @@
 // contraction (64 bf16 or 32 fp32 numbers), which go from memory to LDS directly, two of them in turn.  Operands are stored either with the
 // contraction along their rows (x and the weights forward, dg and du for dx) or across them (the weights for dx, both for dW): the latter
 // are transposed on their way from LDS to registers, by the 16-bit transposing read, or number by number in fp32, so that nothing is transposed in memory.
-// Forward the tile's columns are 32 of Wg beside the same 32 of Wu by turns, so that a lane ends with g and u of the same element and the
-// product needs no second pass.  Sums are fp32 MFMA accumulators; fp32 operands go through fp32 MFMA.
+// Forward the tile's columns are some of Wg and the same ones of Wu, and a wave has both of its columns, so that the product needs no second pass.  Sums are fp32 MFMA accumulators; fp32 operands go through fp32 MFMA.
 //
 // bf16 calls round dg and du once, to bf16, as operands of the second pair of products: what they lose is as random as the rounding
 // of the results and as large, so that gradients are off by 1.4 times their own rounding.
@@ -82,6 +81,7 @@ __device__ __forceinline__ f32x4 mma(const Frag<float> &n, const Frag<float> &m,
 // A tile of one operand, ROWS of the result's rows or columns, in LDS, and what a lane loads and reads of it.
 // Along (ACROSS = false): ROWS rows of 128 bytes, whose eight 16-byte pieces are exchanged by XOR with (row / 2) % 8, so that the 16 rows of a read meet
 // all banks.  ACROSS: 64 (fp32: 32) rows of ROWS numbers, pieces exchanged by a number of the row's that differs between the rows of a read.
+// PAIRED: the first half of the rows is one operand's, the second another's.
 template <typename E, int ROWS, int WAVES, bool ACROSS, bool PAIRED>
 struct Tile {
     static constexpr int kES = sizeof(E), kDepth = kTileBytes / kES, kBytes = ROWS * kTileBytes, kLoads = kBytes / 1024 / WAVES;
@@ -101,13 +101,17 @@ struct Tile {
             piece = (id % kPieces) ^ turned(row);
         }
     }
+    static_assert(kLoads * WAVES * 1024 == kBytes && (!PAIRED || (!ACROSS && ROWS % 16 == 0)), "");
+    // which of a pair a load is of
+    static __device__ __forceinline__ int which(int i, int wave) { return PAIRED && (wave * kLoads + i) * (1024 / kTileBytes) >= ROWS / 2; }
     // `first`: the tile's first row or column of the result, `limit`: how many there are; `depth`: what is left of the contraction (kDepth and more:
-    // a whole tile); `second`: from the first of a pair of operands to the other, in bytes
+    // a whole tile)
     __device__ __forceinline__ void plan(int wave, int lane, long long ld, int first, int limit, int depth) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             int row, piece;
             place(i, wave, lane, row, piece);
+            row -= which(i, wave) * (ROWS / 2);
             bool in;
             if constexpr (!ACROSS) {
                 const int r = first + row;
@@ -119,11 +123,11 @@ struct Tile {
             }
         }
     }
-    __device__ __forceinline__ void load(const char *base, char *lds, int wave) const {
-        const Rsrc r = view(base, 0x7fffffffu);
+    __device__ __forceinline__ void load(const char *base, const char *other, char *lds, int wave) const {
+        const Rsrc one = view(base, 0x7fffffffu), two = view(PAIRED ? other : base, 0x7fffffffu);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)(lds + (wave * kLoads + i) * 1024), 16, (int)off[i], 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(which(i, wave) ? two : one, (lds_ptr)(lds + (wave * kLoads + i) * 1024), 16, (int)off[i], 0, 0, 0);
     }
     // 16 rows or columns from `at` on (a multiple of 16), numbers kk of two of the contraction's halves
     static __device__ __forceinline__ Frag<E> read(const char *lds, int at, int kk, int lane) {
@@ -230,12 +234,12 @@ __device__ __forceinline__ void tile_of(const ProductArgs &p, int &tm, int &tn) 
 template <typename E, Product P, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs p) {
     constexpr int kWaves = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
-    static_assert(P != kForward || NI == 4, "32 columns of each product a wave");
+    static_assert(P != kForward || NI % 2 == 0, "as many columns of each product a wave");
     constexpr int kES = sizeof(E);
     using TA = Tile<E, BM, kWaves, P == kDw, false>;
-    using TB = Tile<E, P == kForward ? BN / 2 : BN, kWaves, P != kForward, false>;     // (forward: one of each matrix)
-    constexpr int kDepth = TA::kDepth, kPair = P == kForward ? 2 : 1;
-    __shared__ __attribute__((aligned(1024))) char lds[2][TA::kBytes + kPair * TB::kBytes];
+    using TB = Tile<E, BN, kWaves, P != kForward, P == kForward>;
+    constexpr int kDepth = TA::kDepth;
+    __shared__ __attribute__((aligned(1024))) char lds[2][TA::kBytes + TB::kBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int wm = wave / WN, wn = wave - wm * WN;
     int tm, tn;
@@ -255,19 +259,18 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
         const int seg = P == kDx ? t >= tiles : 0, k0 = (P == kDx ? t - seg * tiles : t) * kDepth;
         const char *a = p.a[P == kDw ? which : seg] + (P == kDw ? k0 * p.lda + (long long)m0 * kES : m0 * p.lda + (long long)k0 * kES);
         const char *b = p.b[seg] + (P == kForward ? n0 * p.ldb + (long long)k0 * kES : k0 * p.ldb + (long long)n0 * kES);
+        const char *other = P == kForward ? p.b[1] + n0 * p.ldb + (long long)k0 * kES : nullptr;
         char *at = lds[buf];
         if (k0 + kDepth <= p.K) {
-            ta.load(a, at, wave);
-            tb.load(b, at + TA::kBytes, wave);
-            if constexpr (P == kForward) tb.load(p.b[1] + n0 * p.ldb + (long long)k0 * kES, at + TA::kBytes + TB::kBytes, wave);
+            ta.load(a, nullptr, at, wave);
+            tb.load(b, other, at + TA::kBytes, wave);
         } else {
             TA ea;
             TB eb;
             ea.plan(wave, lane, p.lda, m0, p.M, p.K - k0);
             eb.plan(wave, lane, p.ldb, n0, p.N, p.K - k0);
-            ea.load(a, at, wave);
-            eb.load(b, at + TA::kBytes, wave);
-            if constexpr (P == kForward) eb.load(p.b[1] + n0 * p.ldb + (long long)k0 * kES, at + TA::kBytes + TB::kBytes, wave);
+            ea.load(a, nullptr, at, wave);
+            eb.load(b, other, at + TA::kBytes, wave);
         }
     };
     f32x4 acc[MI][NI];
@@ -284,7 +287,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
         const char *at = lds[buf], *bt = at + TA::kBytes;
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
-            if constexpr (P == kForward) fb[kk][j] = TB::read(bt + (j >> 1) * TB::kBytes, wn * 32 + (j & 1) * 16, kk, lane);
+            if constexpr (P == kForward) fb[kk][j] = TB::read(bt, j / (NI / 2) * (BN / 2) + (wn * (NI / 2) + j % (NI / 2)) * 16, kk, lane);
             else fb[kk][j] = TB::read(bt, (wn * NI + j) * 16, kk, lane);
         }
 #pragma unroll
@@ -327,12 +330,11 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
     __syncthreads();
     // The tile goes through LDS, some rows of each wave at a time, so that a work-group stores whole rows and each result's code stands here once.
     // A lane has four neighbouring columns of one row of each 16 x 16 piece; pieces of 16 bytes are exchanged by XOR with the row.
-    constexpr int kRows = sizeof(lds) / (BN * 4) < BM ? sizeof(lds) / (BN * 4) : BM, kPasses = BM / kRows, kSub = MI / kPasses;
-    constexpr int kOut = P == kForward ? BN / 2 : BN, kThreadsARow = kOut / 8, kAtOnce = 64 * kWaves / kThreadsARow;
-    static_assert(kRows * kPasses == BM && kSub * kPasses == MI && kRows % kAtOnce == 0, "");
+    constexpr int kRows = (int)sizeof(lds) >= BM * BN * 4 ? BM : BM / 2, kPasses = BM / kRows, kSub = MI / kPasses;
+    constexpr int kThreadsARow = (P == kForward ? BN / 2 : BN) / 8;
+    static_assert(kSub * kPasses == MI && kRows * BN * 4 <= (int)sizeof(lds) && BN % 64 == 0, "");
     char *const tile = lds[0];
     const int l = lane & 15, g = lane >> 4;
-    const int col = (threadIdx.x % kThreadsARow) * 8, row0 = threadIdx.x / kThreadsARow, n = n0 + col;
 #pragma unroll
     for (int pass = 0; pass < kPasses; ++pass) {
         if (pass > 0) __syncthreads();
@@ -347,12 +349,13 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
         // four at column c of the tile
         auto at = [&](int r, int c) { return *reinterpret_cast<const f32x4 *>(tile + r * (BN * 4) + (((c >> 2) ^ (r & 15)) << 4)); };
 #pragma unroll 1
-        for (int r = row0; r < kRows; r += kAtOnce) {
+        for (int item = threadIdx.x; item < kRows * kThreadsARow; item += 64 * kWaves) {
+            const int r = item / kThreadsARow, col = item % kThreadsARow * 8, n = n0 + col;
             const int sub = r >> 4, m = m0 + ((sub / kSub) * MI + pass * kSub + sub % kSub) * 16 + (r & 15);
             if (m >= p.M) continue;
             if constexpr (P == kForward) {
-                const int c = (col >> 5) * 64 + (col & 31);
-                const f32x4 gt[2] = {at(r, c), at(r, c + 4)}, up[2] = {at(r, c + 32), at(r, c + 36)};
+                const int c = col / (NI * 8) * NI * 16 + col % (NI * 8);
+                const f32x4 gt[2] = {at(r, c), at(r, c + 4)}, up[2] = {at(r, c + NI * 8), at(r, c + NI * 8 + 4)};
                 if (p.d_out != nullptr) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
@@ -514,14 +517,48 @@ hipError_t product(ProductArgs p, hipStream_t stream) {
                        stream, p);
     return hipGetLastError();
 }
-// whether tiles of 256 x 256 leave few compute units idle
-bool large(long long M, long long N) { return ((M + 255) / 256) * ((N + 255) / 256) >= 192; }
+// How a product is cut: tiles, and for dx the parts of its sum.  The cheapest by a model of rounds of tiles: microseconds a tile and step of the contraction
+// (64 bf16 or 32 fp32 numbers), measured with every compute unit at work on 8192 x 2048 x 16384, and what a tile takes at its ends.  Where tiles
+// of 256 x 256 leave the last round nearly empty others are ahead: 4096 x 1152 x 9216 107 us, in tiles of 256 x 192 95, of 128 x 128 101;
+// 2048 rows 72, 60, 59; 1024 x 2048 x 16384 62, 87, 72.
+enum { kBig, kWide, kSmall };            // 256 x 256, 256 x 192 (forward), 128 x 128 (two on a compute unit)
+struct Plan {
+    int tile, splits;
+};
+Plan plan_of(Product product, long long M, long long N, long long K, int dtype) {
+    constexpr int kHigh[] = {256, 256, 128}, kAcross[] = {256, 192, 128}, kSlots[] = {256, 256, 512};
+    constexpr double kStep[2][3] = {{1.95, 1.48, 1.08}, {7.4, 5.6, 3.9}}, kEnds = 6, kJoin = 5, kBytesAUs = 4e6;
+    const int depth = kTileBytes / (dtype == GLA_DT_BF16 ? 2 : 4);
+    const long long steps = (K + depth - 1) / depth * (product == kDx ? 2 : 1);
+    Plan best = {kSmall, 1};
+    double least = 1e300;
+    for (int tile = kBig; tile <= kSmall; ++tile) {
+        if (tile == kWide && product != kForward) continue;
+        const long long high = (M + kHigh[tile] - 1) / kHigh[tile] * (product == kDw ? 2 : 1), tiles = high * ((N + kAcross[tile] - 1) / kAcross[tile]);
+        for (int s = 1; s <= (product == kDx ? 16 : 1) && (s == 1 || steps / s >= 4); ++s) {
+            const double rounds = (double)((tiles * s + kSlots[tile] - 1) / kSlots[tile]);
+            const double us = rounds * ((double)((steps + s - 1) / s) * kStep[dtype == GLA_DT_BF16 ? 0 : 1][tile] + kEnds) +
+                              (s > 1 ? kJoin + (double)s * M * N * 8 / kBytesAUs : 0.);
+            if (us < least) {
+                least = us;
+                best = {tile, s};
+            }
+        }
+    }
+    return best;
+}
 
 template <Product P>
 hipError_t product_of(const ProductArgs &p, int dtype, hipStream_t stream) {
-    const long long M = (long long)p.M * (P == kDw ? 2 : 1), N = (long long)p.N * (P == kForward ? 2 : 1);
-    if (dtype == GLA_DT_BF16) return large(M, N) ? product<uint16_t, P, 256, 256, 2, 4>(p, stream) : product<uint16_t, P, 128, 128, 2, 2>(p, stream);
-    return large(M, N) ? product<float, P, 256, 256, 2, 4>(p, stream) : product<float, P, 128, 128, 2, 2>(p, stream);
+    const Plan plan = plan_of(P, p.M, P == kForward ? 2LL * p.N : p.N, p.K, dtype);
+    auto run = [&](auto e) {
+        using E = decltype(e);
+        if constexpr (P == kForward) {
+            if (plan.tile == kWide) return product<E, P, 256, 192, 4, 2>(p, stream);
+        }
+        return plan.tile == kBig ? product<E, P, 256, 256, 2, 4>(p, stream) : product<E, P, 128, 128, 2, 2>(p, stream);
+    };
+    return dtype == GLA_DT_BF16 ? run(uint16_t{}) : run(float{});
 }
 int element(int dtype) { return dtype == GLA_DT_BF16 ? 2 : 4; }
 
@@ -593,15 +630,7 @@ hipError_t launch_glu_slopes(const GluCall &c, const float *pre, hipStream_t str
     return hipGetLastError();
 }
 
-int glu_splits(int M, int K, int F, int dtype) {
-    // tiles of 128 x 128 that leave compute units idle: the sum over F in parts of eight tiles and more
-    const long long tiles = (long long)((M + 127) / 128) * ((K + 127) / 128);
-    const int depth = kTileBytes / element(dtype), steps = 2 * ((F + depth - 1) / depth);
-    long long n = tiles >= 256 ? 1 : 512 / tiles;
-    if (n > steps / 8) n = steps / 8;
-    if (n > 32) n = 32;
-    return n < 2 ? 1 : (int)n;
-}
+int glu_splits(int M, int K, int F, int dtype) { return plan_of(kDx, M, K, F, dtype).splits; }
 
 hipError_t launch_glu_dx(const GluCall &c, void *dx, hipStream_t stream) {
     ProductArgs p = {};
@@ -618,9 +647,8 @@ hipError_t launch_glu_dx(const GluCall &c, void *dx, hipStream_t stream) {
     p.out[0] = dx;
     p.out_dtype = c.dtype;
     p.part = c.part;
-    if (c.splits == 1) return product_of<kDx>(p, c.dtype, stream);
-    const hipError_t e = c.dtype == GLA_DT_BF16 ? product<uint16_t, kDx, 128, 128, 2, 2>(p, stream) : product<float, kDx, 128, 128, 2, 2>(p, stream);
-    if (e != hipSuccess) return e;
+    const hipError_t e = product_of<kDx>(p, c.dtype, stream);
+    if (e != hipSuccess || c.splits == 1) return e;
     const long long count = (long long)c.M * c.K;
     hipLaunchKernelGGL(join_kernel, dim3((unsigned)((count + 1023) / 1024)), dim3(256), 0, stream, c.part, dx, c.dtype, count, c.splits);
     return hipGetLastError();
