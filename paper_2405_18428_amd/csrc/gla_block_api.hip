@@ -192,8 +192,7 @@ GluRoom glu_room(void *workspace, int M, int K, int F, int dtype, bool back) {
     if (back) {
         r.dg = take(M, whole_pieces(F, dtype), size_of(dtype));
         r.du = take(M, whole_pieces(F, dtype), size_of(dtype));
-        const int splits = glu_splits(M, K, F, dtype);
-        if (splits > 1) r.part = reinterpret_cast<float *>(take((size_t)splits * M, K, sizeof(float)));
+        r.part = reinterpret_cast<float *>(take(1, glu_part_bytes(M, K, F, dtype), 1));
     }
     return r;
 }
@@ -214,17 +213,11 @@ int glu_operands(GluCall &c, const GluRoom &room, const void *x, const void *w_g
     c.act = act;
     c.ld_x = c.ld_w = whole_pieces(K, dtype);
     c.ld_f = whole_pieces(F, dtype);
-    c.x = x;
-    c.w_gate = w_gate;
-    c.w_up = w_up;
-    if (room.x == nullptr) return GLA_OK;
-    if (launch_glu_pad(x, room.x, M, K, c.ld_x, dtype, stream) != hipSuccess || launch_glu_pad(w_gate, room.w_gate, F, K, c.ld_w, dtype, stream) != hipSuccess ||
-        launch_glu_pad(w_up, room.w_up, F, K, c.ld_w, dtype, stream) != hipSuccess)
-        return GLA_ERR_HIP;
-    c.x = room.x;
-    c.w_gate = room.w_gate;
-    c.w_up = room.w_up;
-    return GLA_OK;
+    const bool copied = room.x != nullptr;
+    c.x = copied ? room.x : x;
+    c.w_gate = copied ? room.w_gate : w_gate;
+    c.w_up = copied ? room.w_up : w_up;
+    return !copied || launch_glu_pad(c, x, w_gate, w_up, stream) == hipSuccess ? GLA_OK : GLA_ERR_HIP;
 }
 
 }  // namespace
@@ -428,7 +421,6 @@ int gla_glu_bwd(const void *x, const void *w_gate, const void *w_up, const void 
     c.dg = room.dg;
     c.du = room.du;
     c.part = room.part;
-    c.splits = glu_splits(M, K, F, dtype);
     if (launch_glu_slopes(c, pre, stream) != hipSuccess) return GLA_ERR_HIP;
     if (dx != nullptr && launch_glu_dx(c, dx, stream) != hipSuccess) return GLA_ERR_HIP;
     if (dw_gate != nullptr && launch_glu_dw(c, dw_gate, dw_up, stream) != hipSuccess) return GLA_ERR_HIP;

@@ -12,8 +12,7 @@ struct GluCall {
     // backward
     void *dg, *du;                      // [M, ld_f]: gradients of the two products, rows beginning at 16 bytes
     int ld_f;
-    float *part;                        // [splits, M, K]
-    int splits;
+    float *part;                        // glu_part_bytes()
 };
 // y = act(x Wg^T) * (x Wu^T) -> out [M, F], and the two products to pre [2, M, F] if that is given
 hipError_t launch_glu_fwd(const GluCall &c, void *out, int out_dtype, float *pre, hipStream_t stream);
@@ -21,9 +20,9 @@ hipError_t launch_glu_fwd(const GluCall &c, void *out, int out_dtype, float *pre
 hipError_t launch_glu_slopes(const GluCall &c, const float *pre, hipStream_t stream);
 hipError_t launch_glu_dx(const GluCall &c, void *dx, hipStream_t stream);
 hipError_t launch_glu_dw(const GluCall &c, void *dw_gate, void *dw_up, hipStream_t stream);
-// parts that dx's sum over 2 F products is taken in
-int glu_splits(int M, int K, int F, int dtype);
-// [rows, cols] -> rows of `ld` elements, zeros behind
-hipError_t launch_glu_pad(const void *from, void *to, int rows, int cols, int ld, int dtype, hipStream_t stream);
+// room for the parts that dx's and dW's sums are taken in, one after the other
+size_t glu_part_bytes(int M, int K, int F, int dtype);
+// x and the weights -> c.x, c.w_gate, c.w_up, whose rows have c.ld_x elements, zeros behind K
+hipError_t launch_glu_pad(const GluCall &c, const void *x, const void *w_gate, const void *w_up, hipStream_t stream);
 
 }  // namespace gla

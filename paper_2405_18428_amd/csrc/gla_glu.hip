@@ -89,7 +89,7 @@ struct Tile {
     static constexpr int kReads = !ACROSS ? 1 : kES == 2 ? 2 : 4;
     uint32_t off[kLoads];               // of the lane's pieces from the operand's first one in the tile, or nowhere
 
-    static __device__ __forceinline__ int turned(int k) { return kES == 2 ? 2 * ((k & 3) | ((k >> 3) & 1) << 2) : 4 * ((k >> 2) & 3); }
+    static __device__ __forceinline__ int turned(int k) { return (kES == 2 ? 2 * ((k & 3) | ((k >> 3) & 1) << 2) : 4 * ((k >> 2) & 3)) & (kPieces - 1); }
     // row of the tile and piece of the row for the i-th load of a lane
     static __device__ __forceinline__ void place(int i, int wave, int lane, int &row, int &piece) {
         const int id = (wave * kLoads + i) * 64 + lane;
@@ -101,6 +101,7 @@ struct Tile {
             piece = (id % kPieces) ^ turned(row);
         }
     }
+    static_assert(!ACROSS || (kPieces & (kPieces - 1)) == 0, "");
     static_assert(kLoads * WAVES * 1024 == kBytes && (!PAIRED || (!ACROSS && ROWS % 16 == 0)), "");
     // which of a pair a load is of
     static __device__ __forceinline__ int which(int i, int wave) { return PAIRED && (wave * kLoads + i) * (1024 / kTileBytes) >= ROWS / 2; }
@@ -377,8 +378,8 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
 #pragma unroll
                     for (int e = 0; e < 4; ++e) y[h][e] = activation<false>(p.act, gt[h][e]).y * up[h][e];
                 store8(p.out[0], p.out_dtype, m, n, p.N, y[0], y[1]);
-            } else if (P == kDx && p.splits > 1) {
-                store8(p.part + (long long)blockIdx.y * p.M * p.N, GLA_DT_F32, m, n, p.N, at(r, col), at(r, col + 4));
+            } else if (p.splits > 1) {
+                store8(p.part + (blockIdx.y * (P == kDw ? 2LL : 1LL) + which) * p.M * p.N, GLA_DT_F32, m, n, p.N, at(r, col), at(r, col + 4));
             } else {
                 store8(p.out[which], p.out_dtype, m, n, p.N, at(r, col), at(r, col + 4));
             }
@@ -449,26 +450,37 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(const ProductArgs 
     }
 }
 
-// dx from the parts of its sum, added in one order; four numbers a thread
-__global__ __launch_bounds__(256) void join_kernel(const float *part, void *out, int dtype, long long count, int splits) {
-    const long long at = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (at >= count) return;
-    if (at + 4 <= count && count % 4 == 0) {
-        f32x4 s = *reinterpret_cast<const f32x4 *>(part + at);
-        for (int i = 1; i < splits; ++i) s += *reinterpret_cast<const f32x4 *>(part + i * count + at);
-        if (dtype == GLA_DT_BF16) {
-            const u32x2 b = {pack_bf16(s[0], s[1]), pack_bf16(s[2], s[3])};
-            *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(out) + at) = b;
-        } else {
-            *reinterpret_cast<f32x4 *>(static_cast<float *>(out) + at) = s;
-        }
+// dx, or both dW, from the parts of their sums, added in one order; four numbers a thread
+struct JoinArgs {
+    const float *part;                  // [splits, tensors, count]
+    void *out[2];
+    long long count;
+    int dtype, splits;
+};
+__global__ __launch_bounds__(256) void join_kernel(const JoinArgs p) {
+    const long long at = ((long long)blockIdx.x * 256 + threadIdx.x) * 4, stride = p.count * gridDim.y;
+    if (at >= p.count) return;
+    const float *part = p.part + p.count * blockIdx.y + at;
+    void *out = p.out[blockIdx.y];
+    if (p.count % 4 == 0) {
+        f32x4 s = *reinterpret_cast<const f32x4 *>(part);
+#pragma unroll 4
+        for (int i = 1; i < p.splits; ++i) s += *reinterpret_cast<const f32x4 *>(part + i * stride);
+        if (p.dtype == GLA_DT_BF16) *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(out) + at) = u32x2{pack_bf16(s[0], s[1]), pack_bf16(s[2], s[3])};
+        else *reinterpret_cast<f32x4 *>(static_cast<float *>(out) + at) = s;
         return;
     }
-    for (long long e = at; e < count && e < at + 4; ++e) {
-        float s = part[e];
-        for (int i = 1; i < splits; ++i) s += part[i * count + e];
-        if (dtype == GLA_DT_BF16) static_cast<uint16_t *>(out)[e] = (uint16_t)pack_bf16(s, 0.f);
-        else static_cast<float *>(out)[e] = s;
+    const int n = (int)min(4LL, p.count - at);
+    float s[4] = {};
+#pragma unroll 4
+    for (int i = 0; i < p.splits; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] += e < n ? part[i * stride + e] : 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (e >= n) continue;
+        if (p.dtype == GLA_DT_BF16) static_cast<uint16_t *>(out)[at + e] = (uint16_t)pack_bf16(s[e], 0.f);
+        else static_cast<float *>(out)[at + e] = s[e];
     }
 }
 
@@ -500,12 +512,25 @@ __global__ __launch_bounds__(256) void slopes_kernel(const GluCall c, const floa
     store4(c.du, c.dtype, m, f, c.ld_f, du);
 }
 
+// Rows of `cols` elements to rows of `ld`, zeros behind: three tensors in one launch, four rows a work-group
+struct PadArgs {
+    const void *from[3];
+    void *to[3];
+    int rows[3], cols, ld;
+};
+constexpr int kPadRows = 4;
 template <typename E>
-__global__ __launch_bounds__(256) void pad_kernel(const E *from, E *to, int rows, int cols, int ld) {
-    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
-    const long long r = id / ld;
-    const int c = (int)(id - r * ld);
-    if (r < rows) to[id] = c < cols ? from[r * cols + c] : (E)0;
+__global__ __launch_bounds__(256) void pad_kernel(const PadArgs p) {
+    const int which = blockIdx.y, rows = p.rows[which];
+    const E *from = static_cast<const E *>(p.from[which]);
+    E *to = static_cast<E *>(p.to[which]);
+    for (int c = threadIdx.x; c < p.ld; c += 256) {
+#pragma unroll
+        for (int i = 0; i < kPadRows; ++i) {
+            const long long r = (long long)blockIdx.x * kPadRows + i;
+            if (r < rows) to[r * p.ld + c] = c < p.cols ? from[r * p.cols + c] : (E)0;
+        }
+    }
 }
 
 template <typename E, Product P, int BM, int BN, int WM, int WN>
@@ -521,24 +546,24 @@ hipError_t product(ProductArgs p, hipStream_t stream) {
 // (64 bf16 or 32 fp32 numbers), measured with every compute unit at work on 8192 x 2048 x 16384, and what a tile takes at its ends.  Where tiles
 // of 256 x 256 leave the last round nearly empty others are ahead: 4096 x 1152 x 9216 107 us, in tiles of 256 x 192 95, of 128 x 128 101;
 // 2048 rows 72, 60, 59; 1024 x 2048 x 16384 62, 87, 72.
-enum { kBig, kWide, kSmall };            // 256 x 256, 256 x 192 (forward), 128 x 128 (two on a compute unit)
+enum { kBig, kWide, kSmall, kTiny };     // 256 x 256, 256 x 192 (forward), 128 x 128 (two on a compute unit), 64 x 64 (four)
 struct Plan {
     int tile, splits;
 };
 Plan plan_of(Product product, long long M, long long N, long long K, int dtype) {
-    constexpr int kHigh[] = {256, 256, 128}, kAcross[] = {256, 192, 128}, kSlots[] = {256, 256, 512};
-    constexpr double kStep[2][3] = {{1.95, 1.48, 1.08}, {7.4, 5.6, 3.9}}, kEnds = 6, kJoin = 5, kBytesAUs = 4e6;
+    constexpr int kHigh[] = {256, 256, 128, 64}, kAcross[] = {256, 192, 128, 64}, kSlots[] = {256, 256, 512, 1024};
+    constexpr double kStep[2][4] = {{1.95, 1.48, 1.08, 0.75}, {7.4, 5.6, 3.9, 2.1}}, kEnds = 6, kJoin = 5, kBytesAUs = 4e6;
     const int depth = kTileBytes / (dtype == GLA_DT_BF16 ? 2 : 4);
     const long long steps = (K + depth - 1) / depth * (product == kDx ? 2 : 1);
-    Plan best = {kSmall, 1};
+    Plan best = {kBig, 1};
     double least = 1e300;
-    for (int tile = kBig; tile <= kSmall; ++tile) {
+    for (int tile = kBig; tile <= kTiny; ++tile) {
         if (tile == kWide && product != kForward) continue;
         const long long high = (M + kHigh[tile] - 1) / kHigh[tile] * (product == kDw ? 2 : 1), tiles = high * ((N + kAcross[tile] - 1) / kAcross[tile]);
-        for (int s = 1; s <= (product == kDx ? 16 : 1) && (s == 1 || steps / s >= 4); ++s) {
+        for (int s = 1; s <= (product == kForward ? 1 : 16) && (s == 1 || steps / s >= 4); ++s) {
             const double rounds = (double)((tiles * s + kSlots[tile] - 1) / kSlots[tile]);
             const double us = rounds * ((double)((steps + s - 1) / s) * kStep[dtype == GLA_DT_BF16 ? 0 : 1][tile] + kEnds) +
-                              (s > 1 ? kJoin + (double)s * M * N * 8 / kBytesAUs : 0.);
+                              (s > 1 ? kJoin + (double)s * M * N * (product == kDw ? 16 : 8) / kBytesAUs : 0.);
             if (us < least) {
                 least = us;
                 best = {tile, s};
@@ -556,7 +581,8 @@ hipError_t product_of(const ProductArgs &p, int dtype, hipStream_t stream) {
         if constexpr (P == kForward) {
             if (plan.tile == kWide) return product<E, P, 256, 192, 4, 2>(p, stream);
         }
-        return plan.tile == kBig ? product<E, P, 256, 256, 2, 4>(p, stream) : product<E, P, 128, 128, 2, 2>(p, stream);
+        if (plan.tile == kBig) return product<E, P, 256, 256, 2, 4>(p, stream);
+        return plan.tile == kSmall ? product<E, P, 128, 128, 2, 2>(p, stream) : product<E, P, 64, 64, 2, 2>(p, stream);
     };
     return dtype == GLA_DT_BF16 ? run(uint16_t{}) : run(float{});
 }
@@ -630,7 +656,21 @@ hipError_t launch_glu_slopes(const GluCall &c, const float *pre, hipStream_t str
     return hipGetLastError();
 }
 
-int glu_splits(int M, int K, int F, int dtype) { return plan_of(kDx, M, K, F, dtype).splits; }
+size_t glu_part_bytes(int M, int K, int F, int dtype) {
+    const int dx = plan_of(kDx, M, K, F, dtype).splits, dw = plan_of(kDw, F, K, M, dtype).splits;
+    const size_t a = dx > 1 ? (size_t)dx * M * K : 0, b = dw > 1 ? (size_t)dw * 2 * F * K : 0;
+    return (a > b ? a : b) * sizeof(float);
+}
+// A product whose sum may be taken in parts
+template <Product P>
+static hipError_t in_parts(ProductArgs p, int dtype, hipStream_t stream) {
+    p.splits = plan_of(P, p.M, p.N, p.K, dtype).splits;
+    const hipError_t e = product_of<P>(p, dtype, stream);
+    if (e != hipSuccess || p.splits == 1) return e;
+    const JoinArgs j = {p.part, {p.out[0], p.out[1]}, (long long)p.M * p.N, dtype, p.splits};
+    hipLaunchKernelGGL(join_kernel, dim3((unsigned)((j.count + 1023) / 1024), P == kDw ? 2 : 1), dim3(256), 0, stream, j);
+    return hipGetLastError();
+}
 
 hipError_t launch_glu_dx(const GluCall &c, void *dx, hipStream_t stream) {
     ProductArgs p = {};
@@ -643,15 +683,10 @@ hipError_t launch_glu_dx(const GluCall &c, void *dx, hipStream_t stream) {
     p.M = c.M;
     p.N = c.K;
     p.K = c.F;
-    p.splits = c.splits;
     p.out[0] = dx;
     p.out_dtype = c.dtype;
     p.part = c.part;
-    const hipError_t e = product_of<kDx>(p, c.dtype, stream);
-    if (e != hipSuccess || c.splits == 1) return e;
-    const long long count = (long long)c.M * c.K;
-    hipLaunchKernelGGL(join_kernel, dim3((unsigned)((count + 1023) / 1024)), dim3(256), 0, stream, c.part, dx, c.dtype, count, c.splits);
-    return hipGetLastError();
+    return in_parts<kDx>(p, c.dtype, stream);
 }
 
 hipError_t launch_glu_dw(const GluCall &c, void *dw_gate, void *dw_up, hipStream_t stream) {
@@ -664,19 +699,19 @@ hipError_t launch_glu_dw(const GluCall &c, void *dw_gate, void *dw_up, hipStream
     p.M = c.F;
     p.N = c.K;
     p.K = c.M;
-    p.splits = 1;
     p.out[0] = dw_gate;
     p.out[1] = dw_up;
     p.out_dtype = c.dtype;
-    return product_of<kDw>(p, c.dtype, stream);
+    p.part = c.part;
+    return in_parts<kDw>(p, c.dtype, stream);
 }
 
-hipError_t launch_glu_pad(const void *from, void *to, int rows, int cols, int ld, int dtype, hipStream_t stream) {
-    const dim3 grid((unsigned)(((long long)rows * ld + 255) / 256));
-    if (dtype == GLA_DT_BF16)
-        hipLaunchKernelGGL(pad_kernel<uint16_t>, grid, dim3(256), 0, stream, static_cast<const uint16_t *>(from), static_cast<uint16_t *>(to), rows, cols, ld);
-    else
-        hipLaunchKernelGGL(pad_kernel<float>, grid, dim3(256), 0, stream, static_cast<const float *>(from), static_cast<float *>(to), rows, cols, ld);
+hipError_t launch_glu_pad(const GluCall &c, const void *x, const void *w_gate, const void *w_up, hipStream_t stream) {
+    const PadArgs p = {{x, w_gate, w_up}, {const_cast<void *>(c.x), const_cast<void *>(c.w_gate), const_cast<void *>(c.w_up)}, {c.M, c.F, c.F}, c.K, c.ld_x};
+    const int most = c.M > c.F ? c.M : c.F;
+    const dim3 grid((unsigned)((most + kPadRows - 1) / kPadRows), 3);
+    if (c.dtype == GLA_DT_BF16) hipLaunchKernelGGL(pad_kernel<uint16_t>, grid, dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL(pad_kernel<float>, grid, dim3(256), 0, stream, p);
     return hipGetLastError();
 }
 
