@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import os
 import re
 from typing import List, Optional
@@ -1037,37 +1038,53 @@ def gla_recur_step(x, gate, state, gate_kind=GATE_PRE, tau=16.0, complement=Fals
     return out, state_out
 
 
+_Strides = ctypes.c_longlong * 3
+
+
+def _want_rows(name, t, dtype, gpu):
+    """Raises unless t is a 4-d tensor of this element type on GPU number `gpu` whose last dimension is dense."""
+    if gpu < 0 or t.get_device() != gpu or t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] > 1):
+        raise ValueError(f"{name} must be a 4-d GPU tensor on the device of the others whose rows' channels lie side by side")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be of element type {dtype}")
+
+
+def _row_strides(t, layout):
+    """Batch, head and token strides of rows; None for dense ones."""
+    if t is None or t.is_contiguous():
+        return None
+    s = t.stride()
+    return _Strides(s[0], s[1], s[2]) if layout == LAYOUT_BHTD else _Strides(s[0], s[2], s[1])
+
+
+@functools.lru_cache(maxsize=64)
+def _section_array(sections):
+    return (ctypes.c_int * max(len(sections), 1))(*[int(w) for w in sections])
+
+
 def _prep_qk(q, k, q_weight, k_weight, positions, sections, layout):
-    """Sizes (B, H, Hk, T, d), both tensors' strides and the sections of a call on rows of queries and keys, after checking the tensors."""
+    """Sizes (B, H, Hk, T, d) and the sections of a call on rows of queries and keys after checking the tensors."""
     torch = _torch()
     if layout not in (LAYOUT_BHTD, LAYOUT_BTHD):
         raise ValueError("unknown layout")
-    dev = q.get_device()
-    strides, sizes = [], []
-    for name, t, w in (("q", q, q_weight), ("k", k, k_weight)):
-        if t is None:
-            if w is not None:
-                raise ValueError("k_weight without k")
-            strides.append(None)
-            sizes.append(0)
-            continue
-        if dev < 0 or t.get_device() != dev or t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] > 1):
-            raise ValueError(f"{name} must be a 4-d GPU tensor on the device of the others whose rows' channels lie side by side")
-        if t.dtype is not q.dtype:
-            raise TypeError(f"{name} must be of element type {q.dtype}")
-        B, H, T, d = t.shape if layout == LAYOUT_BHTD else (t.shape[0], t.shape[2], t.shape[1], t.shape[3])
-        if (B, T, d) != (q.shape[0], q.shape[2 if layout == LAYOUT_BHTD else 1], q.shape[3]):
-            raise ValueError("q and k must agree in batches, tokens and channels")
-        if w is not None:
-            _want(name + "_weight", w, (d,), torch.float32, dev)
-        s = t.stride()
-        strides.append((ctypes.c_longlong * 3)(s[0], *((s[1], s[2]) if layout == LAYOUT_BHTD else (s[2], s[1]))))
-        sizes.append(H)
+    dev, Hk = q.get_device(), 0
     _dt(q)
-    axes = len(sections)
+    _want_rows("q", q, q.dtype, dev)
+    B, H, T, d = q.shape if layout == LAYOUT_BHTD else (q.shape[0], q.shape[2], q.shape[1], q.shape[3])
+    if k is not None:
+        _want_rows("k", k, q.dtype, dev)
+        Hk = k.shape[1 if layout == LAYOUT_BHTD else 2]
+        if k.shape != ((B, Hk, T, d) if layout == LAYOUT_BHTD else (B, T, Hk, d)):
+            raise ValueError("q and k must agree in batches, tokens and channels")
+        if k_weight is not None:
+            _want("k_weight", k_weight, (d,), torch.float32, dev)
+    elif k_weight is not None:
+        raise ValueError("k_weight without k")
+    if q_weight is not None:
+        _want("q_weight", q_weight, (d,), torch.float32, dev)
     if positions is not None:
-        _want("positions", positions, (B, T, axes), torch.int32, dev)
-    return (q.shape[0], sizes[0], sizes[1], T, d), strides, (ctypes.c_int * max(axes, 1))(*[int(w) for w in sections])
+        _want("positions", positions, (B, T, len(sections)), torch.int32, dev)
+    return (B, H, Hk, T, d), _section_array(tuple(sections))
 
 
 def gla_qk_norm_fwd(q, k, q_weight=None, k_weight=None, sections=(), eps=1e-6, grid_h=0, grid_w=0, positions=None, base=10000.0,
@@ -1078,7 +1095,7 @@ def gla_qk_norm_fwd(q, k, q_weight=None, k_weight=None, sections=(), eps=1e-6, g
     if _elsewhere(stream, q):
         return _call_on(stream, gla_qk_norm_fwd, locals())
     lib = load_library()
-    (B, H, Hk, T, d), strides, secs = _prep_qk(q, k, q_weight, k_weight, positions, sections, layout)
+    (B, H, Hk, T, d), secs = _prep_qk(q, k, q_weight, k_weight, positions, sections, layout)
     if k is None and out_k is not None:
         raise ValueError("out_k without k")
     dt = q.dtype if out_dtype is None else out_dtype
@@ -1088,7 +1105,7 @@ def gla_qk_norm_fwd(q, k, q_weight=None, k_weight=None, sections=(), eps=1e-6, g
         if t is not None:
             _want(name, t, like.shape, out_q.dtype, q.get_device())
     with _on_device_of(q):
-        _check(lib.gla_qk_norm_fwd(q.data_ptr(), strides[0], H, _ptr(k), strides[1], Hk, _ptr(q_weight), _ptr(k_weight), float(eps), _ptr(positions), secs,
+        _check(lib.gla_qk_norm_fwd(q.data_ptr(), _row_strides(q, layout), H, _ptr(k), _row_strides(k, layout), Hk, _ptr(q_weight), _ptr(k_weight), float(eps), _ptr(positions), secs,
                                    len(sections), float(base), pairing, B, T, d, grid_h, grid_w, _dt(q), _dt(out_q), layout, out_q.data_ptr(), _ptr(out_k),
                                    _stream_ptr(stream, q)))
     return out_q, out_k
@@ -1106,7 +1123,7 @@ def gla_qk_norm_bwd(q, k, d_out_q, d_out_k, q_weight=None, k_weight=None, sectio
         return _call_on(stream, gla_qk_norm_bwd, locals())
     torch = _torch()
     lib = load_library()
-    (B, H, Hk, T, d), strides, secs = _prep_qk(q, k, q_weight, k_weight, positions, sections, layout)
+    (B, H, Hk, T, d), secs = _prep_qk(q, k, q_weight, k_weight, positions, sections, layout)
     if (k is None) != (d_out_k is None):
         raise ValueError("d_out_k belongs to k")
     _want("d_out_q", d_out_q, q.shape, q.dtype, q.get_device())
@@ -1117,7 +1134,7 @@ def gla_qk_norm_bwd(q, k, d_out_q, d_out_k, q_weight=None, k_weight=None, sectio
     dqw, dkw = (w.new_empty(d) if w is not None and want_d_weight else None for w in (q_weight, k_weight))
     workspace = _room(lambda: gla_qk_norm_bwd_workspace_bytes(B, H, Hk, T, d), workspace, q)
     with _on_device_of(q):
-        _check(lib.gla_qk_norm_bwd(q.data_ptr(), strides[0], H, _ptr(k), strides[1], Hk, d_out_q.data_ptr(), _ptr(d_out_k), _ptr(q_weight), _ptr(k_weight),
+        _check(lib.gla_qk_norm_bwd(q.data_ptr(), _row_strides(q, layout), H, _ptr(k), _row_strides(k, layout), Hk, d_out_q.data_ptr(), _ptr(d_out_k), _ptr(q_weight), _ptr(k_weight),
                                    float(eps), _ptr(positions), secs, len(sections), float(base), pairing, B, T, d, grid_h, grid_w, _dt(q), _dt(dq), layout,
                                    dq.data_ptr(), _ptr(dk), _ptr(dqw), _ptr(dkw), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                    _stream_ptr(stream, q)))
