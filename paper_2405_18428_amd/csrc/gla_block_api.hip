@@ -254,7 +254,7 @@ int gla_recur_fwd(const void *x, const void *gate, int gate_kind, float tau, int
     const Span xs = {x, n * size_of(x_dtype)}, gs = {gate, n * size_of(gate_dtype)}, os = {out, n * size_of(out_dtype)};
     const Span first = {initial_state, state_bytes}, last = {final_state, state_bytes};
     // (in place is each element's own place: a wave has read its rows before it writes them)
-    const bool in_place = touch(os, xs) || touch(os, gs);
+    const bool in_place = touch(os, xs) || touch(os, gs) || touch(first, last);
     if (touch(os, xs) && (out != x || out_dtype != x_dtype)) return GLA_ERR_SHAPE;
     if (touch(os, gs) && (out != gate || out_dtype != gate_dtype)) return GLA_ERR_SHAPE;
     if (touch(os, first) || touch(os, last) || touch(last, xs) || touch(last, gs) || (touch(first, last) && initial_state != final_state)) return GLA_ERR_SHAPE;

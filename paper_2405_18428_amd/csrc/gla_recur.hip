@@ -409,6 +409,7 @@ __global__ __launch_bounds__(64 * kWaves) void walk_kernel(const RecurCall c, co
     if (first != nullptr && p.any) load_state<V>(first, p.cell(c), carry);
     Given<EX, EG, V, kSteps, KIND, false> in;
     in.load(c, p, nullptr, wave * kSteps);
+    asm volatile("" : "+v"(carry[0]), "+v"(carry[V - 1]));      // (read before any wave may write a final state over it)
     int buf = 0;
     for (int s0 = 0; s0 < c.T; s0 += round, buf ^= 1) {
         const int s = s0 + wave * kSteps;
@@ -481,7 +482,7 @@ __global__ __launch_bounds__(64 * kChainWaves, 4) void chain_kernel(const RecurC
     Given<EX, EG, V, kChainSteps, KIND, false> in;
     in.load(c, p, nullptr, s);
     float enter[V] = {};
-    if (unit < kRecurBlock && first != nullptr && p.any) load_state<V>(first, p.cell(c), enter);
+    if (wave == 0 && unit < kRecurBlock && first != nullptr && p.any) load_state<V>(first, p.cell(c), enter);
     const Piece<EX, EG, V, kChainSteps, KIND, REST> q(in, c.inv_tau);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -502,6 +503,8 @@ __global__ __launch_bounds__(64 * kChainWaves, 4) void chain_kernel(const RecurC
     const int block = unit / kRecurBlock, in_block = unit - block * kRecurBlock;
     const bool last = unit == c.nunits - 1;
     if (wave == 0 && !last && in_block < kRecurBlock - 1) {
+        // (what is published also says that this unit has read what enters it, which a final state may be written over)
+        asm volatile("" ::"v"(enter[0]), "v"(enter[V - 1]));
 #pragma unroll
         for (int i = 0; i < V; ++i) publish(local(unit, i), lg[i], z[i]);
     }
