@@ -188,6 +188,9 @@ __device__ __forceinline__ EG open_gate() {
     else return __builtin_inff();
 }
 
+template <typename E>
+__device__ __forceinline__ const char *row_of(const void *base, long long row) { return static_cast<const char *>(base) + row * (long long)sizeof(E); }
+
 // x, gates and (backward) dO of L steps from s on.  Steps behind the sequence's end get zeros, and gates that let everything through
 template <typename EX, typename EG, int V, int L, int KIND, bool BACK>
 struct Given {
@@ -197,7 +200,19 @@ struct Given {
     __device__ __forceinline__ void load(const RecurCall &c, const Place<V> &p, const void *d_out, int s) {
         whole = __all(s + L <= p.loads);
         Cursor k(c, p, s);
-        if (whole) {
+        if (whole && c.scan_dir <= GLA_SCAN_ROW_REV) {   // (a third of the scalar instructions)
+            const char *px = row_of<EX>(c.x, k.at), *pg = row_of<EG>(c.gate, k.at), *po = BACK ? row_of<EX>(d_out, k.at) : nullptr;
+            const long long sx = c.step * (long long)sizeof(EX), sg = c.step * (long long)sizeof(EG);
+#pragma unroll
+            for (int j = 0; j < L; ++j) {
+                x.r[j] = load_raw<EX, V>(px + p.at * (uint32_t)sizeof(EX));
+                g.r[j] = load_raw<EG, V>(pg + p.at * (uint32_t)sizeof(EG));
+                if constexpr (BACK) o.r[j] = load_raw<EX, V>(po + p.at * (uint32_t)sizeof(EX));
+                px += sx;
+                pg += sg;
+                if constexpr (BACK) po += sx;
+            }
+        } else if (whole) {
 #pragma unroll
             for (int j = 0; j < L; ++j) {
                 x.load(j, c.x, k.at, p.at);
@@ -389,6 +404,17 @@ template <typename EX, typename EG, int V, int L, int KIND, bool REST>
 __device__ __forceinline__ void put_outputs(const RecurCall &c, const Place<V> &p, const Piece<EX, EG, V, L, KIND, REST> &q, float (&h)[V], void *out, int dtype, int s,
                                             bool whole) {
     Cursor k(c, p, s);
+    if (whole && c.scan_dir <= GLA_SCAN_ROW_REV && dtype == GLA_DT_BF16) {
+        char *row = static_cast<char *>(out) + k.at * 2;
+#pragma unroll
+        for (int j = 0; j < L; ++j) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) h[i] = __builtin_fmaf(q.a[j][i], h[i], q.u[j][i]);
+            store<V>(row, GLA_DT_BF16, 0, p.at, h);
+            row += c.step * 2;
+        }
+        return;
+    }
 #pragma unroll
     for (int j = 0; j < L; ++j) {
 #pragma unroll
