@@ -34,16 +34,28 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 constexpr int kSteps = kRecurSteps, kWaves = kRecurWaves;
 constexpr float kLog2E = 1.44269504f, kLn2 = 0.693147181f;
 
-template <typename E, int V> struct RawOf { E e[V]; };
+// V neighbouring channels as they lie in memory
+template <typename E, int V>
+struct RawOf {
+    static constexpr int kWords = (sizeof(E) * V + 3) / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ float operator[](int i) const {
+        if constexpr (sizeof(E) == 4) return __builtin_bit_cast(float, w[i]);
+        else return __builtin_bit_cast(float, i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+    }
+    __device__ __forceinline__ void fill(uint32_t bits) {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = sizeof(E) == 2 ? bits | bits << 16 : bits;
+    }
+};
 
 template <typename E, int V>
 __device__ __forceinline__ RawOf<E, V> load_raw(const char *p) {
     RawOf<E, V> r;
-    __builtin_memcpy(&r, __builtin_assume_aligned(p, sizeof(E) * V), sizeof(r));
+    if constexpr (sizeof(E) * V == 2) r.w[0] = *reinterpret_cast<const uint16_t *>(p);
+    else __builtin_memcpy(&r, __builtin_assume_aligned(p, sizeof(E) * V), sizeof(r));
     return r;
 }
-__device__ __forceinline__ float to_float(float e) { return e; }
-__device__ __forceinline__ float to_float(uint16_t e) { return __builtin_bit_cast(float, (uint32_t)e << 16); }
 __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), bf16x2));
 }
@@ -175,18 +187,11 @@ struct Rows {
     __device__ __forceinline__ void load(int j, const void *base, long long row, uint32_t at) {
         r[j] = load_raw<E, V>(static_cast<const char *>(base) + row * (long long)sizeof(E) + at * (uint32_t)sizeof(E));
     }
-    __device__ __forceinline__ void fill(int j, E other) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) r[j].e[i] = other;
-    }
+    __device__ __forceinline__ void fill(int j, uint32_t bits) { r[j].fill(bits); }
 };
-// a gate of one: log 1, or the pre-activation +infinity
+// the bits of a gate of one: log 1, or the pre-activation +infinity
 template <typename EG, int KIND>
-__device__ __forceinline__ EG open_gate() {
-    if constexpr (KIND == GLA_GATE_LOG) return (EG)0;
-    else if constexpr (sizeof(EG) == 2) return (EG)0x7f80;
-    else return __builtin_inff();
-}
+constexpr uint32_t kOpenGate = KIND == GLA_GATE_LOG ? 0u : sizeof(EG) == 2 ? 0x7f80u : 0x7f800000u;
 
 template <typename E>
 __device__ __forceinline__ const char *row_of(const void *base, long long row) { return static_cast<const char *>(base) + row * (long long)sizeof(E); }
@@ -223,9 +228,9 @@ struct Given {
         } else {
 #pragma unroll
             for (int j = 0; j < L; ++j) {
-                x.fill(j, (EX)0);
-                g.fill(j, open_gate<EG, KIND>());
-                if constexpr (BACK) o.fill(j, (EX)0);
+                x.fill(j, 0);
+                g.fill(j, kOpenGate<EG, KIND>);
+                if constexpr (BACK) o.fill(j, 0);
                 if (s + j < p.loads) {
                     x.load(j, c.x, k.at, p.at);
                     g.load(j, c.gate, k.at, p.at);
@@ -250,8 +255,8 @@ struct Piece {
         for (int j = 0; j < L; ++j)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const Gate t = gate_of<KIND, false>(to_float(in.g.r[j].e[i]), inv_tau);
-                const float v = to_float(in.x.r[j].e[i]);
+                const Gate t = gate_of<KIND, false>(in.g.r[j][i], inv_tau);
+                const float v = in.x.r[j][i];
                 a[j][i] = t.a;
                 u[j][i] = REST ? -less_one(t.lg * kLn2, t.a) * v : v;
                 lg[i] += t.lg;
@@ -294,7 +299,7 @@ __global__ __launch_bounds__(256) void units_kernel(const RecurCall c, const voi
 #pragma unroll
         for (int j = 0; j < kSteps; ++j)
 #pragma unroll
-            for (int i = 0; i < V; ++i) dd[j][i] = to_float(in.o.r[j].e[i]);
+            for (int i = 0; i < V; ++i) dd[j][i] = in.o.r[j][i];
         if (s + kSteps < end) in.load(c, p, d_out, s + kSteps);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -327,7 +332,7 @@ __global__ __launch_bounds__(64 * kWaves) void units_apart_kernel(const RecurCal
     for (int i = 0; i < V; ++i) {
         float b = 0.f;
 #pragma unroll
-        for (int j = kSteps - 1; j >= 0; --j) b = q.a[j][i] * (to_float(in.o.r[j].e[i]) + b);
+        for (int j = kSteps - 1; j >= 0; --j) b = q.a[j][i] * (in.o.r[j][i] + b);
         lds_lg[wave][lane][i] = q.lg[i];
         lds_h[wave][lane][i] = q.from_zero(i);
         lds_o[wave][lane][i] = b;
@@ -491,7 +496,9 @@ __global__ __launch_bounds__(256) void clear_kernel(uint32_t *words, long long c
 template <typename EX, typename EG, int V, int KIND, bool REST>
 __global__ __launch_bounds__(64 * kChainWaves, 4) void chain_kernel(const RecurCall c, const RecurChain ch, const float *first, void *out, int out_dtype, float *final_state,
                                                             bool flat, int groups) {
-    __shared__ float lds_lg[kChainWaves][64][V], lds_a[kChainWaves][64][V], lds_h[kChainWaves][64][V], far_lgs[kChainWaves][64][V], far_zs[kChainWaves][64][V], lds_s[64][V];
+    // of a wave's steps, and of the units that it looks back at: log2 of their decay, the state they make of zero
+    __shared__ __attribute__((aligned(16))) float parts[kChainWaves][64][2 * V], fars[kChainWaves][64][2 * V];
+    __shared__ float lds_s[64][V];
     __shared__ bool outs[kChainWaves];
     __shared__ uint32_t lds_ticket;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -512,18 +519,22 @@ __global__ __launch_bounds__(64 * kChainWaves, 4) void chain_kernel(const RecurC
     const Piece<EX, EG, V, kChainSteps, KIND, REST> q(in, c.inv_tau);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        lds_lg[wave][lane][i] = q.lg[i];
-        lds_a[wave][lane][i] = __builtin_amdgcn_exp2f(q.lg[i]);
-        lds_h[wave][lane][i] = q.from_zero(i);
+        parts[wave][lane][i] = q.lg[i];
+        parts[wave][lane][V + i] = q.from_zero(i);
     }
     __syncthreads();
     // of the waves before this one (the first wave: of the whole unit)
     float z[V] = {}, lg[V] = {};
-    for (int w = 0; w < (wave == 0 ? kChainWaves : wave); ++w) {
+    const int before = wave == 0 ? kChainWaves : wave;
+#pragma unroll
+    for (int w = 0; w < kChainWaves; ++w) {
+        if (w >= before) continue;
+        float part[2 * V];
+        __builtin_memcpy(part, &parts[w][lane][0], sizeof(part));
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            z[i] = __builtin_fmaf(lds_a[w][lane][i], z[i], lds_h[w][lane][i]);
-            lg[i] += lds_lg[w][lane][i];
+            z[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(part[i]), z[i], part[V + i]);
+            lg[i] += part[i];
         }
     }
     const int block = unit / kRecurBlock, in_block = unit - block * kRecurBlock;
@@ -580,8 +591,8 @@ __global__ __launch_bounds__(64 * kChainWaves, 4) void chain_kernel(const RecurC
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        far_lgs[wave][lane][i] = far_lg[i];
-        far_zs[wave][lane][i] = far_z[i];
+        fars[wave][lane][i] = far_lg[i];
+        fars[wave][lane][V + i] = far_z[i];
         if (wave == 0) lds_s[lane][i] = enter[i];
     }
     if (lane == 0) outs[wave] = ran_out;
@@ -590,12 +601,15 @@ __global__ __launch_bounds__(64 * kChainWaves, 4) void chain_kernel(const RecurC
 #pragma unroll
     for (int i = 0; i < V; ++i) far_lg[i] = far_z[i] = 0.f;
     ran_out = false;
+#pragma unroll
     for (int w = kChainWaves - 1; w >= 0; --w) {
         ran_out = ran_out || outs[w];
+        float part[2 * V];
+        __builtin_memcpy(part, &fars[w][lane][0], sizeof(part));
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            far_z[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(far_lg[i]), far_zs[w][lane][i], far_z[i]);
-            far_lg[i] += far_lgs[w][lane][i];
+            far_z[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(far_lg[i]), part[V + i], far_z[i]);
+            far_lg[i] += part[i];
         }
     }
 #pragma unroll
@@ -657,8 +671,8 @@ __global__ __launch_bounds__(64 * kWaves, 4) void back_kernel(const RecurCall c,
     for (int j = 0; j < kSteps; ++j) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const Gate gt = gate_of<KIND, true>(to_float(in.g.r[j].e[i]), c.inv_tau);
-            const float x = to_float(in.x.r[j].e[i]);
+            const Gate gt = gate_of<KIND, true>(in.g.r[j][i], c.inv_tau);
+            const float x = in.x.r[j][i];
             a[j][i] = gt.a;
             b[j][i] = KIND == GLA_GATE_PRE ? gt.a * gt.slope : gt.a;
             asm volatile("" : "+v"(b[j][i]));            // (formed here: left for later its parts take twice the registers)
@@ -675,7 +689,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void back_kernel(const RecurCall c,
         lds_h[wave][lane][i] = z[i];
         float r = 0.f;
 #pragma unroll
-        for (int j = kSteps - 1; j >= 0; --j) r = a[j][i] * (to_float(in.o.r[j].e[i]) + r);
+        for (int j = kSteps - 1; j >= 0; --j) r = a[j][i] * (in.o.r[j][i] + r);
         lds_o[wave][lane][i] = r;
         lg[i] = z[i] = 0.f;
     }
@@ -708,7 +722,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void back_kernel(const RecurCall c,
         k.next(c);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float x = to_float(in.x.r[j].e[i]);
+            const float x = in.x.r[j][i];
             b[j][i] *= REST ? h[i] - x : h[i];           // (the state before the step)
             h[i] = REST ? fmaf(a[j][i], h[i], rest[j][i] * x) : fmaf(a[j][i], h[i], x);
         }
@@ -719,7 +733,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void back_kernel(const RecurCall c,
         float gx[V], gg[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float G = to_float(in.o.r[j].e[i]) + adj[i];
+            const float G = in.o.r[j][i] + adj[i];
             gx[i] = REST ? rest[j][i] * G : G;
             gg[i] = b[j][i] * G;
             adj[i] = a[j][i] * G;
@@ -753,8 +767,8 @@ __global__ __launch_bounds__(64) void step_kernel(const RecurCall c, const float
     load_state<V>(state, at, h);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const Gate t = gate_of<KIND, false>(to_float(g.e[i]), c.inv_tau);
-        const float v = to_float(x.e[i]), rest = -less_one(t.lg * kLn2, t.a);
+        const Gate t = gate_of<KIND, false>(g[i], c.inv_tau);
+        const float v = x[i], rest = -less_one(t.lg * kLn2, t.a);
         const float near = t.a > 0.7f ? __builtin_fmaf(-rest, h[i], h[i]) : t.a * h[i];
         h[i] = near + (REST ? rest * v : v);
     }
