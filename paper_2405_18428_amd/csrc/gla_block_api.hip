@@ -109,7 +109,7 @@ bool sized_recur(RecurCall &c, int B, int T, int D) {
 size_t reach(const QkSide &s, int B, int T, int d, int dtype) {
     return (size_t)((B - 1) * s.sb + (s.heads - 1) * s.sh + (T - 1) * s.st + d) * size_of(dtype);
 }
-int side_in(QkSide &s, const void *x, const long long *strides, const float *weight, int heads, int T, int d, int layout) {
+int side_in(QkSide &s, const void *x, const long long *strides, const float *weight, int B, int heads, int T, int d, int layout) {
     s.x = x;
     s.weight = weight;
     s.heads = x != nullptr ? heads : 0;
@@ -117,7 +117,10 @@ int side_in(QkSide &s, const void *x, const long long *strides, const float *wei
         s.sb = strides[0];
         s.sh = strides[1];
         s.st = strides[2];
-        if (s.sb < 0 || s.sh < 0 || s.st < 0 || s.sb > (1LL << 40) || s.sh > (1LL << 40) || s.st > (1LL << 40)) return GLA_ERR_SHAPE;
+        // (elements to the last batch, head and token: what they add up to has to be an address)
+        const long long strides_of[] = {s.sb, s.sh, s.st}, counts[] = {B, heads, T};
+        for (int i = 0; i < 3; ++i)
+            if (strides_of[i] < 0 || strides_of[i] > (1LL << 40) / (counts[i] > 1 ? counts[i] - 1 : 1)) return GLA_ERR_SHAPE;
     } else {
         s.sb = (long long)heads * T * d;
         s.sh = layout == GLA_LAYOUT_BHTD ? (long long)T * d : d;
@@ -141,8 +144,8 @@ int check_qk(QkParams &p, const void *q, const long long *q_strides, int H, cons
     }
     // 32-bit numbers of tokens and heads
     if ((long long)B * T >= (1LL << 31) || H > (1 << 20) || Hk > (1 << 20)) return GLA_ERR_UNSUPPORTED;
-    int st = side_in(p.side[0], q, q_strides, q_weight, H, T, d, layout);
-    if (st == GLA_OK) st = side_in(p.side[1], k, k_strides, k_weight, Hk, T, d, layout);
+    int st = side_in(p.side[0], q, q_strides, q_weight, B, H, T, d, layout);
+    if (st == GLA_OK) st = side_in(p.side[1], k, k_strides, k_weight, B, Hk, T, d, layout);
     if (st != GLA_OK) return st;
     if (off_element(q, dtype) || off_element(k, dtype) || any_misaligned((const void *)q_weight, (const void *)k_weight) ||
         (reinterpret_cast<uintptr_t>(positions) & 3u) != 0)

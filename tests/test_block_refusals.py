@@ -69,7 +69,7 @@ QK_SHARED = [({"q": None}, NULL), ({"sec": None}, NULL), ({"H": 0}, SHAPE), ({"H
              ({"odt": 5}, SHAPE), ({"layout": 2}, SHAPE), ({"pairing": 2}, SHAPE), ({"eps": cf(-1.0)}, SHAPE), ({"eps": cf(float("nan"))}, SHAPE), ({"eps": cf(float("inf"))}, SHAPE),
              ({"base": cf(0.0)}, SHAPE), ({"sec": (16, 18)}, SHAPE), ({"sec": (15, 16)}, SHAPE), ({"gw": 5}, SHAPE), ({"axes": 4, "sec": (4,) * 4}, SHAPE),
              ({"axes": 5, "sec": (2,) * 5, "pos": at(12)}, UNSUPPORTED), ({"d": 257}, UNSUPPORTED), ({"B": 1 << 16, "T": 1 << 15, "axes": 0}, UNSUPPORTED), ({"H": (1 << 20) + 1}, UNSUPPORTED),
-             ({"qs": (-1, 0, 0)}, SHAPE), ({"ks": (0, 0, 1 << 41)}, SHAPE), ({"q": vp(FAR + 1)}, ALIGN), ({"qw": OFF}, ALIGN), ({"pos": vp(4098)}, ALIGN), ({"k": None}, NULL)]
+             ({"qs": (-1, 0, 0)}, SHAPE), ({"ks": (0, 0, 1 << 41)}, SHAPE), ({"B": 1 << 24, "qs": (1 << 40, 0, 32)}, SHAPE), ({"B": 1 << 24, "ks": (1 << 17, 0, 32)}, SHAPE), ({"q": vp(FAR + 1)}, ALIGN), ({"qw": OFF}, ALIGN), ({"pos": vp(4098)}, ALIGN), ({"k": None}, NULL)]
 
 
 def qk_args(d):
