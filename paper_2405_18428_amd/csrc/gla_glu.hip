@@ -38,7 +38,8 @@ __device__ __forceinline__ Activation activation(int act, float g) {
         r.y = g * phi;
         if constexpr (SLOPE) r.slope = fmaf(g * 0.398942280f, __builtin_amdgcn_exp2f(-0.721347520f * g * g), phi);
     } else {                            // g sigmoid(2 k (g + 0.044715 g^3)), k = sqrt(2 / pi)
-        const float q = g * g, s = 1.f / (1.f + __builtin_amdgcn_exp2f(-2.30220819f * g * fmaf(0.044715f, q, 1.f)));
+        // (past |g| = 100, where s is 0 or 1, a larger square would only overflow; a NaN stays one by g)
+        const float q = fminf(g * g, 1e4f), s = 1.f / (1.f + __builtin_amdgcn_exp2f(-2.30220819f * g * fmaf(0.044715f, q, 1.f)));
         r.y = g * s;
         if constexpr (SLOPE) r.slope = s * fmaf(g * (1.f - s), 1.59576912f * fmaf(0.134145f, q, 1.f), 1.f);
     }
@@ -512,25 +513,26 @@ __global__ __launch_bounds__(256) void slopes_kernel(const GluCall c, const floa
     store4(c.du, c.dtype, m, f, c.ld_f, du);
 }
 
-// Rows of `cols` elements to rows of `ld`, zeros behind: three tensors in one launch, four rows a work-group
+// Rows of `cols` elements to rows of `ld`, zeros behind: three tensors in one launch, four rows a work-group at a time
 struct PadArgs {
     const void *from[3];
     void *to[3];
     int rows[3], cols, ld;
 };
-constexpr int kPadRows = 4;
+constexpr int kPadRows = 4, kPadGroups = 1 << 16;
 template <typename E>
 __global__ __launch_bounds__(256) void pad_kernel(const PadArgs p) {
     const int which = blockIdx.y, rows = p.rows[which];
     const E *from = static_cast<const E *>(p.from[which]);
     E *to = static_cast<E *>(p.to[which]);
-    for (int c = threadIdx.x; c < p.ld; c += 256) {
+    for (long long r0 = (long long)blockIdx.x * kPadRows; r0 < rows; r0 += (long long)gridDim.x * kPadRows)
+        for (int c = threadIdx.x; c < p.ld; c += 256) {
 #pragma unroll
-        for (int i = 0; i < kPadRows; ++i) {
-            const long long r = (long long)blockIdx.x * kPadRows + i;
-            if (r < rows) to[r * p.ld + c] = c < p.cols ? from[r * p.cols + c] : (E)0;
+            for (int i = 0; i < kPadRows; ++i) {
+                const long long r = r0 + i;
+                if (r < rows) to[r * p.ld + c] = c < p.cols ? from[r * p.cols + c] : (E)0;
+            }
         }
-    }
 }
 
 template <typename E, Product P, int BM, int BN, int WM, int WN>
@@ -708,8 +710,8 @@ hipError_t launch_glu_dw(const GluCall &c, void *dw_gate, void *dw_up, hipStream
 
 hipError_t launch_glu_pad(const GluCall &c, const void *x, const void *w_gate, const void *w_up, hipStream_t stream) {
     const PadArgs p = {{x, w_gate, w_up}, {const_cast<void *>(c.x), const_cast<void *>(c.w_gate), const_cast<void *>(c.w_up)}, {c.M, c.F, c.F}, c.K, c.ld_x};
-    const int most = c.M > c.F ? c.M : c.F;
-    const dim3 grid((unsigned)((most + kPadRows - 1) / kPadRows), 3);
+    const int most = c.M > c.F ? c.M : c.F, groups = (most + kPadRows - 1) / kPadRows;
+    const dim3 grid((unsigned)(groups < kPadGroups ? groups : kPadGroups), 3);
     if (c.dtype == GLA_DT_BF16) hipLaunchKernelGGL(pad_kernel<uint16_t>, grid, dim3(256), 0, stream, p);
     else hipLaunchKernelGGL(pad_kernel<float>, grid, dim3(256), 0, stream, p);
     return hipGetLastError();

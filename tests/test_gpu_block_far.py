@@ -98,6 +98,21 @@ def test_product():
     assert float((dwg.double() - a.double() - b.double()).norm() / dwg.double().norm()) < 2.0 ** -7
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_product_of_many_odd_rows(dtype):
+    """Rows whose copies, a thread for each of 256 columns of four rows of three tensors, would be more than 2^32 threads."""
+    M, K, F, n = 23_000_000, 9, 8, 200
+    gen = torch.Generator(device=DEV).manual_seed(6)
+    x = torch.randn(M, K, generator=gen, device=DEV, dtype=dtype)
+    wg, wu = (torch.randn(F, K, generator=gen, device=DEV, dtype=dtype) for _ in range(2))
+    y = gla.gla_glu_fwd(x, wg, wu)
+    for s in (slice(0, n), slice(M // 2, M // 2 + n), slice(M - n, M)):
+        assert torch.equal(y[s], gla.gla_glu_fwd(x[s].clone(), wg, wu))
+    dx, _, _ = gla.gla_glu_bwd(x, wg, wu, y, want_dw=False)
+    tail = gla.gla_glu_bwd(x[-n:].clone(), wg, wu, y[-n:].clone(), want_dw=False)[0]
+    assert float((dx[-n:].double() - tail.double()).norm() / tail.double().norm()) < torch.finfo(dtype).eps
+
+
 @pytest.mark.parametrize("T,D,lens", [(5000, 512, None), (3000, 1024, [3000, 1, 1700])])
 def test_waits_that_run_out(T, D, lens):
     """Units whose waits run out at once form the state that enters them from the inputs."""

@@ -95,6 +95,23 @@ def test_activations_far_from_zero(act, dtype):
     check(40, 48, 56, dtype, act, seed=act, scale=12.0)
 
 
+@pytest.mark.parametrize("act", [0, 1, 2])
+def test_activations_without_end(act):
+    """Products up to 1e30: the activation is g or nothing there, and its slope one or nothing."""
+    g = torch.tensor([[1e3, 1e10, 1e20, 1e30, -1e3, -1e10, -1e20, -1e30]], device=DEV)
+    one, eye = torch.ones(8, 1, device=DEV), torch.zeros(8, 4, device=DEV)
+    eye[:, 0] = g[0]
+    x = torch.tensor([[1.0, 0, 0, 0]], device=DEV)
+    up = torch.tensor([[1.0, 0, 0, 0]], device=DEV) * one
+    y = gla.gla_glu_fwd(x, eye, up, act)
+    assert torch.equal(y, g.clamp(min=0))
+    do = torch.zeros(1, 8, device=DEV)
+    for i in range(8):
+        do.zero_()[0, i] = 1.0
+        dx, dwg, dwu = gla.gla_glu_bwd(x, eye, up, do, act)
+        assert float(dwg[i, 0]) == (1.0 if i < 4 else 0.0) and float(dwu[i, 0]) == float(y[0, i]), (i, dwg[i, 0], dwu[i, 0])
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("M,K,F", [(1, 2048, 8192), (7, 1152, 4608), (33, 2048, 1000), (100, 1152, 4608), (1000, 1152, 2000), (3000, 500, 2048), (2100, 2300, 2056), (700, 4100, 1030)])
 def test_large(M, K, F, dtype):
