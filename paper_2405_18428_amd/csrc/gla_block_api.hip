@@ -40,10 +40,12 @@ bool any_touch(const Span (&mine)[N], const Span (&others)[M]) {
 
 // --- gated recurrence of channels ---
 
-// Forward: the sequence in units, unless a work-group may as well walk it
-constexpr int kWalkGroups = 512;
+// Forward: the sequence in units, or walked by one work-group, where there are many of those or few units.  bf16, 2048 channels, walked and in
+// units: 4096 steps of 64 groups of 128 channels 151 us and 49, of 128 groups 154 and 106, of 256 groups 171 and 176 (1024 steps 44 and 46, 512 steps 25 and 29);
+// 512 steps of 128 groups 22.6 and 20.4, 256 steps 12.3 and 12.9, of 64 groups 11.7 and 10.6, 160 steps 9.3 and 10.9.
+constexpr int kWalkGroups = 256, kWalkUnits = 2;
 void plan_forward(RecurCall &c) {
-    const bool units = c.T > kRecurChain && ((long long)c.B * c.D + 127) / 128 < kWalkGroups;
+    const bool units = c.T > kWalkUnits * kRecurChain && ((long long)c.B * c.D + 127) / 128 < kWalkGroups;
     c.unit = units ? kRecurChain : c.T;
     c.nunits = units ? (c.T + kRecurChain - 1) / kRecurChain : 1;
 }

@@ -107,7 +107,7 @@ KINDS = [(gla.GATE_LOG, 1.0), (gla.GATE_PRE, 1.0), (gla.GATE_PRE, 16.0)]
 
 
 @pytest.mark.parametrize("kind,tau", KINDS)
-@pytest.mark.parametrize("T", [1, 2, 7, 8, 9, 63, 64, 65, 127, 128, 129, 200, 513, 1000])
+@pytest.mark.parametrize("T", [1, 2, 7, 8, 9, 63, 64, 65, 127, 128, 129, 200, 256, 257, 513, 1000])
 def test_lengths(T, kind, tau):
     check(make(2, T, 66, BF16, kind, T), 1, T, 0, kind, tau, T % 2 == 0, F32)
     check(make(1, T, 5, F32, kind, T + 1), 1, T, 1, kind, tau, T % 2 == 1, F32)
@@ -119,6 +119,7 @@ def test_channels(B, D, dtype, out_dtype):
     for rest in (False, True):
         check(make(B, 150, D, dtype, gla.GATE_PRE, D), 1, 150, 0, gla.GATE_PRE, 16.0, rest, out_dtype)
     check(make(B, 150, D, dtype, gla.GATE_LOG, D), 10, 15, 2, gla.GATE_LOG, 1.0, True, out_dtype, states=False)
+    check(make(B, 390, D, dtype, gla.GATE_PRE, D), 15, 26, 3, gla.GATE_PRE, 16.0, True, out_dtype)
 
 
 @pytest.mark.parametrize("kind,tau", KINDS)
