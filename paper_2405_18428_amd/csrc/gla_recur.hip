@@ -35,7 +35,7 @@ typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
 constexpr int kSteps = kRecurSteps, kWaves = kRecurWaves;
-constexpr float kLog2E = 1.44269504f, kLn2 = 0.693147181f;
+constexpr float kLog2E = 1.44269504f;
 
 // V neighbouring channels as they lie in memory
 template <typename E, int V>
@@ -81,20 +81,19 @@ __device__ __forceinline__ void store(void *base, int dtype, long long row, uint
     }
 }
 
-// exp(y) - 1, y <= 0 (natural units); a = exp(y)
-__device__ __forceinline__ float less_one(float y, float a) {
-    float p = fmaf(y, 1.f / 5040.f, 1.f / 720.f);
-    p = fmaf(y, p, 1.f / 120.f);
-    p = fmaf(y, p, 1.f / 24.f);
-    p = fmaf(y, p, 1.f / 6.f);
-    p = fmaf(y, p, 0.5f);
-    p = fmaf(y, p, 1.f);
-    return y > -0.35f ? y * p : a - 1.f;     // (the next term of the series is 2e-8 of the result)
+// 2^lg - 1, lg <= 0; a = 2^lg.  Near zero lg times the polynomial that meets (2^t - 1) / t at five Chebyshev points of [-1/2, 0]: off by 1.4e-8 of the
+// result, with its roundings by 2.2 2^-24; below, a - 1 has lost two bits at most.
+__device__ __forceinline__ float less_one(float lg, float a) {
+    float p = fmaf(lg, 1.15543997e-3f, 9.54227503e-3f);
+    p = fmaf(lg, p, 5.54907198e-2f);
+    p = fmaf(lg, p, 0.240225675f);
+    p = fmaf(lg, p, 0.693147172f);
+    return lg > -0.5f ? lg * p : a - 1.f;
 }
 // 2^lg s
 __device__ __forceinline__ float decayed(float lg, float s) {
-    const float a = __builtin_amdgcn_exp2f(lg), y = lg * kLn2;
-    return y > -0.35f ? __builtin_fmaf(less_one(y, a), s, s) : a * s;
+    const float a = __builtin_amdgcn_exp2f(lg);
+    return lg > -0.5f ? __builtin_fmaf(less_one(lg, a), s, s) : a * s;
 }
 struct Gate {
     float lg, a;                         // log2 of the gate, the gate
@@ -261,7 +260,7 @@ struct Piece {
                 const Gate t = gate_of<KIND, false>(in.g.r[j][i], inv_tau);
                 const float v = in.x.r[j][i];
                 a[j][i] = t.a;
-                u[j][i] = REST ? -less_one(t.lg * kLn2, t.a) * v : v;
+                u[j][i] = REST ? -less_one(t.lg, t.a) * v : v;
                 lg[i] += t.lg;
             }
     }
@@ -689,7 +688,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void back_kernel(const RecurCall c,
             a[j][i] = gt.a;
             b[j][i] = KIND == GLA_GATE_PRE ? gt.a * gt.slope : gt.a;
             asm volatile("" : "+v"(b[j][i]));            // (formed here: left for later its parts take twice the registers)
-            if constexpr (REST) rest[j][i] = -less_one(gt.lg * kLn2, gt.a);
+            if constexpr (REST) rest[j][i] = -less_one(gt.lg, gt.a);
             lg[i] += gt.lg;
             z[i] = REST ? fmaf(a[j][i], z[i], rest[j][i] * x) : fmaf(a[j][i], z[i], x);
         }
@@ -781,7 +780,7 @@ __global__ __launch_bounds__(64) void step_kernel(const RecurCall c, const float
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const Gate t = gate_of<KIND, false>(g[i], c.inv_tau);
-        const float v = x[i], rest = -less_one(t.lg * kLn2, t.a);
+        const float v = x[i], rest = -less_one(t.lg, t.a);
         const float near = t.a > 0.7f ? __builtin_fmaf(-rest, h[i], h[i]) : t.a * h[i];
         h[i] = near + (REST ? rest * v : v);
     }
