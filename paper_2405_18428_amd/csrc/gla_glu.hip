@@ -9,11 +9,11 @@
 // fp32 MFMA accumulators; fp32 operands go through fp32 MFMA.
 //
 // What bounds it: the matrix units are busy 45 to 48 % of a large call.  8192 x 2048 x 8192, bf16, tiles of 256 x 256: both products with the activation, and
-// their fp32 copies kept, 553 us (994 TFLOP/s; without the copies 537), dx 532 (1033), both dW 508 (1083); products of these shapes by the vendor's library reach 1203,
-// 1098 and 963.  Left without MFMAs dx takes 438 us, without loads 334, without LDS reads 444: tiles of the contraction come at 17 bytes a clock and compute unit,
+// their fp32 copies kept, 537 us (1024 TFLOP/s; in a row without pauses 501, without the copies 494), dx 532 (1033), both dW 502 (1095); products of these shapes by the
+// vendor's library reach 1203, 1098 and 963.  Left without MFMAs dx takes 438 us, without loads 334, without LDS reads 444: tiles of the contraction come at 17 bytes a clock and compute unit,
 // a fifth of their lines from beyond L2, and a tile is there when its slowest line is.  Tiles of 64 bytes, five of them under way, 650 us (lines
-// are fetched twice); three tiles of A, two of B 533.  fp32, 1021 x 381 x 1531: 34 to 37 us
-// a pair of products (64 to 70 TFLOP/s of the 154 that large ones reach): 768 short tiles of 64 x 64, ragged ones among them.
+// are fetched twice); three tiles of A, two of B 533.  fp32, 1021 x 381 x 1531: 31 to 32 us
+// a pair of products (75 TFLOP/s of the 154 that large ones reach): 768 short tiles of 64 x 64, ragged ones among them.
 //
 // bf16 calls round dg and du once, to bf16, as operands of the second pair of products: what they lose is as random as the rounding
 // of the results and as large, so that gradients are off by 1.4 times their own rounding.  As two numbers each they would double dx and dW.
@@ -186,6 +186,13 @@ __device__ __forceinline__ void store4(void *base, int dtype, long long row, int
     }
 }
 
+// Four fp32 numbers that nothing reads soon, and that are too many for the last-level cache: with it full of them, what comes after waits for their way to memory
+// (8192 x 2048 x 8192: both products kept, 517 us for 585 forward, 163 for 192 where they are read)
+__device__ __forceinline__ void keep4(float *base, long long row, int col, int n, f32x4 v) {
+    if (n % 4 == 0) __builtin_nontemporal_store(v, reinterpret_cast<f32x4 *>(base + row * n + col));
+    else store4(base, GLA_DT_F32, row, col, n, v);
+}
+
 // Eight
 __device__ __forceinline__ void store8(void *base, int dtype, long long row, int col, int n, f32x4 v, f32x4 w) {
     if (dtype == GLA_DT_BF16 && n % 8 == 0) {
@@ -341,7 +348,6 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
     // The tile goes through LDS, some rows of each wave at a time, so that a work-group stores whole rows and each result's code stands here once.
     // A lane has four neighbouring columns of one row of each 16 x 16 piece; pieces of 16 bytes are exchanged by XOR with the row.
     constexpr int kRows = (int)sizeof(lds) >= BM * BN * 4 ? BM : BM / 2, kPasses = BM / kRows, kSub = MI / kPasses;
-    constexpr int kThreadsARow = (P == kForward ? BN / 2 : BN) / 8;
     static_assert(kSub * kPasses == MI && kRows * BN * 4 <= (int)sizeof(lds) && BN % 64 == 0, "");
     char *const tile = lds[0];
     const int l = lane & 15, g = lane >> 4;
@@ -358,41 +364,50 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
         __syncthreads();
         // four at column c of the tile
         auto at = [&](int r, int c) { return *reinterpret_cast<const f32x4 *>(tile + r * (BN * 4) + (((c >> 2) ^ (r & 15)) << 4)); };
+        // columns a thread: 16 bytes of results, or of what is stored in fp32, so that a wave's store leaves no holes in lines
+        auto results = [&](auto columns) __attribute__((always_inline)) {
+            constexpr int kColumns = decltype(columns)::value, kThreadsARow = (P == kForward ? BN / 2 : BN) / kColumns;
 #pragma unroll 1
-        for (int item = threadIdx.x; item < kRows * kThreadsARow; item += 64 * kWaves) {
-            const int r = item / kThreadsARow, col = item % kThreadsARow * 8, n = n0 + col;
-            const int sub = r >> 4, m = m0 + ((sub / kSub) * MI + pass * kSub + sub % kSub) * 16 + (r & 15);
-            if (m >= p.M) continue;
-            if constexpr (P == kForward) {
-                const int c = col / (NI * 8) * NI * 16 + col % (NI * 8);
-                const f32x4 gt[2] = {at(r, c), at(r, c + 4)}, up[2] = {at(r, c + NI * 8), at(r, c + NI * 8 + 4)};
-                if (p.d_out != nullptr) {
+            for (int item = threadIdx.x; item < kRows * kThreadsARow; item += 64 * kWaves) {
+                const int r = item / kThreadsARow, col = item % kThreadsARow * kColumns, n = n0 + col;
+                const int sub = r >> 4, m = m0 + ((sub / kSub) * MI + pass * kSub + sub % kSub) * 16 + (r & 15);
+                if (m >= p.M) continue;
+                if constexpr (P == kForward) {
+                    const int c = col / (NI * 8) * NI * 16 + col % (NI * 8);
+                    f32x4 y[kColumns / 4];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        if (n + 4 * h >= p.ld_f) continue;
-                        f32x4 dg, du;
-                        slopes<E>(p.act, static_cast<const E *>(p.d_out), m, n + 4 * h, p.N, gt[h], up[h], dg, du);
-                        store4(p.slope[0], kES == 2 ? GLA_DT_BF16 : GLA_DT_F32, m, n + 4 * h, p.ld_f, dg);
-                        store4(p.slope[1], kES == 2 ? GLA_DT_BF16 : GLA_DT_F32, m, n + 4 * h, p.ld_f, du);
+                    for (int h = 0; h < kColumns / 4; ++h) {
+                        const f32x4 gt = at(r, c + 4 * h), up = at(r, c + NI * 8 + 4 * h);
+                        if (kColumns == 4 && p.d_out != nullptr) {
+                            if (n >= p.ld_f) continue;
+                            f32x4 dg, du;
+                            slopes<E>(p.act, static_cast<const E *>(p.d_out), m, n, p.N, gt, up, dg, du);
+                            store4(p.slope[0], kES == 2 ? GLA_DT_BF16 : GLA_DT_F32, m, n, p.ld_f, dg);
+                            store4(p.slope[1], kES == 2 ? GLA_DT_BF16 : GLA_DT_F32, m, n, p.ld_f, du);
+                            continue;
+                        }
+                        if (kColumns == 4 && p.pre != nullptr && n < p.N) {
+                            keep4(p.pre, m, n, p.N, gt);
+                            keep4(p.pre + (long long)p.M * p.N, m, n, p.N, up);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[h][e] = activation<false>(p.act, gt[e]).y * up[e];
                     }
-                    continue;
+                    if constexpr (kColumns == 8) {
+                        store8(p.out[0], p.out_dtype, m, n, p.N, y[0], y[1]);
+                    } else {
+                        if (p.d_out == nullptr && n < p.N) store4(p.out[0], p.out_dtype, m, n, p.N, y[0]);
+                    }
+                } else if constexpr (kColumns == 8) {
+                    store8(p.out[which], p.out_dtype, m, n, p.N, at(r, col), at(r, col + 4));
+                } else if (n < p.N) {
+                    if (p.splits > 1) store4(p.part + (blockIdx.y * (P == kDw ? 2LL : 1LL) + which) * p.M * p.N, GLA_DT_F32, m, n, p.N, at(r, col));
+                    else store4(p.out[which], p.out_dtype, m, n, p.N, at(r, col));
                 }
-                if (p.pre != nullptr) {
-                    store8(p.pre, GLA_DT_F32, m, n, p.N, gt[0], gt[1]);
-                    store8(p.pre + (long long)p.M * p.N, GLA_DT_F32, m, n, p.N, up[0], up[1]);
-                }
-                f32x4 y[2];
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) y[h][e] = activation<false>(p.act, gt[h][e]).y * up[h][e];
-                store8(p.out[0], p.out_dtype, m, n, p.N, y[0], y[1]);
-            } else if (p.splits > 1) {
-                store8(p.part + (blockIdx.y * (P == kDw ? 2LL : 1LL) + which) * p.M * p.N, GLA_DT_F32, m, n, p.N, at(r, col), at(r, col + 4));
-            } else {
-                store8(p.out[which], p.out_dtype, m, n, p.N, at(r, col), at(r, col + 4));
             }
-        }
+        };
+        if (p.out_dtype == GLA_DT_BF16 && p.splits == 1 && p.pre == nullptr && p.d_out == nullptr) results(std::integral_constant<int, 8>{});
+        else results(std::integral_constant<int, 4>{});
     }
 }
 
@@ -497,7 +512,7 @@ __global__ __launch_bounds__(256) void join_kernel(const JoinArgs p) {
 }
 
 // dg and du of the two products that a forward call has kept: four columns a thread, those from F to the end of a row as zeros.  Bound by HBM: 8192 x 8192, bf16,
-// 940 MB, 191 us, 4.9 TB/s
+// 940 MB, 152 us, 6.2 TB/s with what is still in the last-level cache
 template <typename E>
 __global__ __launch_bounds__(256) void slopes_kernel(const GluCall c, const float *pre) {
     const int pieces = c.ld_f / 4;
@@ -509,8 +524,8 @@ __global__ __launch_bounds__(256) void slopes_kernel(const GluCall c, const floa
     f32x4 gt = {0, 0, 0, 0}, up = gt, dg, du;
     if (c.F % 4 == 0) {
         if (f < c.F) {
-            gt = *reinterpret_cast<const f32x4 *>(g);
-            up = *reinterpret_cast<const f32x4 *>(u);
+            gt = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(g));     // (the last that reads them: 162 -> 153 us)
+            up = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(u));
         }
     } else {
 #pragma unroll
@@ -526,7 +541,7 @@ __global__ __launch_bounds__(256) void slopes_kernel(const GluCall c, const floa
 }
 
 // Rows of `cols` elements to rows of `ld`, zeros behind: three tensors in one launch, four rows a work-group at a time.  Direct loads to LDS take pieces of 16
-// bytes from addresses of as many; 1021, 1531 and 1531 rows of 381 floats 5.6 us, twice in a training step of 131
+// bytes from addresses of as many; 1021, 1531 and 1531 rows of 381 floats 5.6 us, twice in a training step of 125
 struct PadArgs {
     const void *from[3];
     void *to[3];
