@@ -131,7 +131,8 @@ typedef enum {
     GLA_OPT_CARRY = 2,           /* gla_carry */
     GLA_OPT_BWD_SPLIT = 3,       /* 0 = the backward pass computes dk and dv of a chunk in one kernel (MFMA engine);
                                     1 = in two kernels (the forward output pass for dv, the row read for dk) */
-    GLA_OPT_LOOK_BACK_POLLS = 5, /* how often a wave of the single-launch forward kernels polls for the state of an earlier span
+    GLA_OPT_LOOK_BACK_POLLS = 5, /* how often a wave of the single-launch forward kernels (gla_recur_fwd's too, but for calls in
+                                    place, which have no inputs left to start from) polls for the state of an earlier span
                                     before it forms the state entering its own from the inputs (default 32768: tens of
                                     milliseconds, which only runs out where other work keeps the earlier spans off the
                                     GPU; 0 = never, for tests) */
@@ -658,7 +659,7 @@ int gla_recur_step(const void *x, const void *gate, int gate_kind, float tau, in
  *               they overlap the inputs or each other otherwise                                                 (written)
  *
  * 1 <= d <= 256.  q and k may begin at any element, the other tensors at 16 bytes.  Sums and angles as in gla_norm_fwd and gla_rope; a row's
- * squares have to add up to a finite fp32 number.  Needs no workspace and never allocates.
+ * squares have to add up to a finite fp32 number, and with eps = 0 to one that is not zero.  Needs no workspace and never allocates.
  */
 int gla_qk_norm_fwd(const void *q, const long long *q_strides, int H, const void *k, const long long *k_strides, int Hk, const float *q_weight,
                     const float *k_weight, float eps, const int *positions, const int *sections, int axes, float base, int pairing,
@@ -684,7 +685,7 @@ int gla_qk_norm_bwd(const void *q, const long long *q_strides, int H, const void
 size_t gla_qk_norm_bwd_workspace_bytes(int B, int H, int Hk, int T, int d);
 
 /*
- * gla_glu_fwd - gated feed-forward product: both projections of M tokens, the activation and the product, in one kernel:
+ * gla_glu_fwd - gated feed-forward product: both projections of M tokens, the activation and the product, without the projections' way through memory:
  *   out = act(x w_gate^T) * (x w_up^T).
  *
  *   x              DEVICE, dtype, [M,K]                                                                       (read)

@@ -541,7 +541,7 @@ __global__ __launch_bounds__(256) void slopes_kernel(const GluCall c, const floa
 }
 
 // Rows of `cols` elements to rows of `ld`, zeros behind: three tensors in one launch, four rows a work-group at a time.  Direct loads to LDS take pieces of 16
-// bytes from addresses of as many; 1021, 1531 and 1531 rows of 381 floats 5.6 us, twice in a training step of 125
+// bytes from addresses of as many; 1021, 1531 and 1531 rows of 381 floats 5.6 us, twice in a training step of 119
 struct PadArgs {
     const void *from[3];
     void *to[3];

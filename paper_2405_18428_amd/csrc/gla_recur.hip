@@ -283,7 +283,7 @@ __device__ __forceinline__ void store_state(float *p, long long at, const float 
 }
 
 // Backward, first pass: a wave takes one unit of 64 V channels, 8 steps at a time with the next 8 on their way.  Reads x, gates and dO: 4 x 4096 x 2048,
-// bf16, 45 us, 4.5 TB/s.
+// bf16, 43 us, 4.7 TB/s, the vector units busy for 83 % of it.
 template <typename EX, typename EG, int V, int KIND, bool REST>
 __global__ __launch_bounds__(256) void units_kernel(const RecurCall c, const void *d_out, const RecurUnits u, bool flat, int groups) {
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -360,7 +360,7 @@ __global__ __launch_bounds__(64 * kWaves) void units_apart_kernel(const RecurCal
 }
 
 // Chains the units of 64 channels: 16 waves take as many runs of units, compose each, chain the runs through LDS and walk their runs again, where
-// what enters a unit takes the place of what it makes of zero.  Bound by latency: 64 units of 4 x 2048 channels, in both directions, 6.3 us.
+// what enters a unit takes the place of what it makes of zero.  Bound by latency: 64 units of 4 x 2048 channels, in both directions, 6.0 us.
 constexpr int kCarryWaves = 16;
 __global__ __launch_bounds__(64 * kCarryWaves) void carry_kernel(const RecurCall c, const RecurUnits u, const float *first, const float *last, float *d_first) {
     __shared__ float run_lg[kCarryWaves][64], run_s[kCarryWaves][64];
@@ -500,7 +500,7 @@ __global__ __launch_bounds__(256) void clear_kernel(uint32_t *words, long long c
 
 // Forward pass in units of 128 steps, 16 a wave.  Decays and inputs of the wave's 16 steps stay in registers, 64 with two channels a lane, while the
 // look-back waits, so two work-groups fit a compute unit; their loads, wait and stores overlap each other's.  65536 x 2048, bf16: 182 to 190 us, 4.3 TB/s;
-// 4 x 4096 x 2048 with u = (1 - a) x 61 us; 8 sequences of 1 to 2047 steps, 130 MB moved, 46 us, some 20 of them the first loads and the last stores.  Units
+// 4 x 4096 x 2048 with u = (1 - a) x 59 us; 8 sequences of 1 to 2047 steps, 130 MB moved, 44 us, some 20 of them the first loads and the last stores.  Units
 // of 64 steps (8 a wave) took 393 us, of 256 (16 waves) 396, work-groups of 4 waves 236.  One ticket for all groups is ahead of one for each, 188 us
 // and 215: neighbouring groups' units, whose rows lie beside each other, then run together.
 template <typename EX, typename EG, int V, int KIND, bool REST>
@@ -653,8 +653,8 @@ __global__ __launch_bounds__(64 * kChainWaves, 4) void chain_kernel(const RecurC
     put_outputs(c, p, q, enter, out, out_dtype, s, __all(s + kChainSteps <= p.n));
 }
 
-// Gradients of one round of 64 V channels: states from the front, adjoints from behind, 8 steps a wave.  Bound by HBM and the vector units (two thirds busy):
-// 4 x 4096 x 2048, bf16, 335 MB, 82 us, 4.1 TB/s.  118 registers let two work-groups share a compute unit; the compiler's own order takes 163
+// Gradients of one round of 64 V channels: states from the front, adjoints from behind, 8 steps a wave.  Bound by HBM and the vector units (72 % busy):
+// 4 x 4096 x 2048, bf16, 335 MB, 78 us, 4.3 TB/s.  118 registers let two work-groups share a compute unit; the compiler's own order takes 163
 // (110 us), and held to 128 without the fences below it spills (160 us).
 template <typename EX, typename EG, int V, int KIND, bool REST>
 __global__ __launch_bounds__(64 * kWaves, 4) void back_kernel(const RecurCall c, const void *d_out, const RecurUnits u, const float *first, const float *last,
