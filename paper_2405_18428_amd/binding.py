@@ -1099,11 +1099,14 @@ def gla_qk_norm_fwd(q, k, q_weight=None, k_weight=None, sections=(), eps=1e-6, g
     if k is None and out_k is not None:
         raise ValueError("out_k without k")
     dt = q.dtype if out_dtype is None else out_dtype
-    out_q = _like(q, dt) if out_q is None else out_q
-    out_k = _like(k, out_q.dtype) if out_k is None and k is not None else out_k
-    for name, t, like in (("out_q", out_q, q), ("out_k", out_k, k)):
-        if t is not None:
-            _want(name, t, like.shape, out_q.dtype, q.get_device())
+    if out_q is None:
+        out_q = _like(q, dt)
+    else:
+        _want("out_q", out_q, q.shape, out_q.dtype, q.get_device())
+    if out_k is not None:
+        _want("out_k", out_k, k.shape, out_q.dtype, q.get_device())
+    elif k is not None:
+        out_k = _like(k, out_q.dtype)
     with _on_device_of(q):
         _check(lib.gla_qk_norm_fwd(q.data_ptr(), _row_strides(q, layout), H, _ptr(k), _row_strides(k, layout), Hk, _ptr(q_weight), _ptr(k_weight), float(eps), _ptr(positions), secs,
                                    len(sections), float(base), pairing, B, T, d, grid_h, grid_w, _dt(q), _dt(out_q), layout, out_q.data_ptr(), _ptr(out_k),

@@ -9,9 +9,9 @@
 // one wave's, so there are no barriers.  Forward the norm's factor is applied last, so that the exchange does not wait for the row's sum.  Sums
 // for dw stay in registers, are added over a work-group and go to memory as one partial sum a work-group, which a second kernel adds in one order.
 //
-// Bound by HBM: 4 x 4095 tokens of 16 + 16 heads of 128 channels, bf16, forward 268 MB in 63 us, 4.3 TB/s, backward 403 MB in 82, 4.9 TB/s.  Work-groups of 16
+// Bound by HBM: 4 x 4095 tokens of 16 + 16 heads of 128 channels, bf16, forward 268 MB in 52 us, 5.2 TB/s, backward 403 MB in 82, 4.9 TB/s.  Work-groups of 16
 // tokens, a group of lanes each, which read 256 bytes a token at a time: 110 and 139 us.  Three or four turns of heads on their way instead of two: 65 and
-// 91, 63 and 90.  64 single tokens of 16 + 4 heads 4.8 us, a launch and one row's loads, sum and stores.
+// 91, 63 and 90 (63 and 82 then).  Rows asked for before the angles are formed: 51 and 85.  64 single tokens of 16 + 4 heads 4.8 us, a launch and one row's loads, sum and stores.
 #include "gla_qk.h"
 #include "gla_rope_util.h"
 #include "gla_rows.h"
@@ -269,14 +269,23 @@ hipError_t qk(const QkParams &p, hipStream_t stream) {
     while (each > 1 && tokens * ((turns + each - 1) / each) < 2048) each = (each + 1) / 2;
     const int parts = (turns + each - 1) / each;         // (at most 2048 items where there is more than one)
     const long long groups = (tokens * parts + kWaves - 1) / kWaves;
-    const unsigned grid = BACK ? (unsigned)p.slots : (unsigned)(groups < (1 << 23) ? groups : 1 << 23);
     const RopeParams &r = p.rope;
     bool whole = 2 * r.pairs == LANES * kEach;           // (sections, or their halves, in whole pieces)
     for (int x = 0; x < r.axes; ++x) whole = whole && r.first[x] % kEach == 0 && r.half[x] % (r.adjacent ? 1 : kEach) == 0;
-    if (whole && r.adjacent) hipLaunchKernelGGL((qk_kernel<E, LANES, BACK, kNeighbours>), dim3(grid), dim3(kThreads), 0, stream, p, each, parts);
-    else if (whole) hipLaunchKernelGGL((qk_kernel<E, LANES, BACK, kHalves>), dim3(grid), dim3(kThreads), 0, stream, p, each, parts);
-    else hipLaunchKernelGGL((qk_kernel<E, LANES, BACK, kAny>), dim3(grid), dim3(kThreads), 0, stream, p, each, parts);
-    return hipGetLastError();
+    auto run = [&](auto mode) {
+        constexpr int MODE = decltype(mode)::value;
+        // forward as many work-groups as the GPU holds (4 x 4095 tokens of 16 + 16 heads of 128 channels 54 us, with one for each four tokens 63; 20000 of
+        // 12 + 12 heads of 64 38 and 51)
+        static const int held = [] {
+            int n = 0;
+            return hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, (const void *)qk_kernel<E, LANES, BACK, MODE>, kThreads, 0) == hipSuccess && n > 0 ? 256 * n : 1024;
+        }();
+        const unsigned grid = BACK ? (unsigned)p.slots : (unsigned)(groups < held ? groups : held);
+        hipLaunchKernelGGL((qk_kernel<E, LANES, BACK, MODE>), dim3(grid), dim3(kThreads), 0, stream, p, each, parts);
+        return hipGetLastError();
+    };
+    if (whole) return r.adjacent ? run(std::integral_constant<int, kNeighbours>{}) : run(std::integral_constant<int, kHalves>{});
+    return run(std::integral_constant<int, kAny>{});
 }
 template <bool BACK>
 hipError_t qk_of(const QkParams &p, int dtype, hipStream_t stream) {
