@@ -197,7 +197,8 @@ __global__ __launch_bounds__(kThreads) void qk_kernel(const QkParams p, int each
 #pragma unroll
                             for (int j = 0; j < kEach; ++j) g[j] = fmaf(q[j], -sn[j], g[j] * cs[j]);
                         }
-                        const float rstd = __builtin_amdgcn_rsqf(fmaf(row_sum<LANES>(ss), inv, p.eps));
+                        // (lanes without a row add to the weight's sums too: nothing, also where no eps keeps their root from zero)
+                        const float root = __builtin_amdgcn_rsqf(fmaf(row_sum<LANES>(ss), inv, p.eps)), rstd = h + sub < end ? root : 0.f;
                         float m = 0.f;
 #pragma unroll
                         for (int j = 0; j < kEach; ++j) {
