@@ -49,7 +49,8 @@ __device__ __forceinline__ Activation activation(int act, float g) {
         // (past |g| = 100, where s is 0 or 1, a larger square would only overflow; a NaN stays one by g)
         const float q = fminf(g * g, 1e4f), s = 1.f / (1.f + __builtin_amdgcn_exp2f(-2.30220819f * g * fmaf(0.044715f, q, 1.f)));
         r.y = g * s;
-        if constexpr (SLOPE) r.slope = s * fmaf(g * (1.f - s), 1.59576912f * fmaf(0.134145f, q, 1.f), 1.f);
+        // (and so would a larger g, whose slope's second term is 0 from there on)
+        if constexpr (SLOPE) r.slope = s * fmaf((g < -100.f ? -100.f : g) * (1.f - s), 1.59576912f * fmaf(0.134145f, q, 1.f), 1.f);
     }
     return r;
 }
