@@ -61,7 +61,7 @@ RecurChain chain_in(const RecurCall &c, void *workspace, bool in_place) {
     r.local = reinterpret_cast<unsigned long long *>(p);
     r.after = reinterpret_cast<uint32_t *>(p + (size_t)recur_chain_columns(c) * c.nunits * 8);
     r.ticket = reinterpret_cast<uint32_t *>(p + chain_bytes(c) - 256);
-    r.polls = in_place ? 0x7fffffff : gla_get_option(GLA_OPT_LOOK_BACK_POLLS);
+    r.looks = in_place ? kRecurNoEnd : gla_get_option(GLA_OPT_LOOK_BACK_POLLS);
     return r;
 }
 size_t units_bytes(const RecurCall &c) { return c.nunits > 1 ? 3 * align_up((size_t)c.B * c.nunits * c.D * sizeof(float)) : 0; }

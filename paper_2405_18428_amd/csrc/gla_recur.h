@@ -1,6 +1,7 @@
 // Gated recurrence of channels, h_t = a_t h_{t-1} + u_t (host + gfx950 device code): parameters and launchers.
 #pragma once
 #include "gla_common.h"
+#include "gla_recur_plan.h"
 
 namespace gla {
 
@@ -21,7 +22,7 @@ struct RecurCall {
 struct RecurChain {
     unsigned long long *local;          // [nunits, columns]
     uint32_t *after, *ticket;           // [blocks, columns]
-    int polls;
+    int looks;                          // of a wait, or kRecurNoEnd
 };
 long long recur_chain_columns(const RecurCall &c);
 // of 4 bytes, a column

@@ -13,7 +13,7 @@
 //
 // Looking back: what is published are words that hold their own validity (all ones: not there yet), written and read at device scope, so nothing
 // has to be ordered.  Work-groups take their units in the order in which they start (a ticket), and a unit waits for earlier ones only, which
-// have all started and publish before they wait: the earliest unit that waits can always go on.  A poll that runs out all the same (`polls`) forms the
+// have all started and publish before they wait: the earliest unit that waits can always go on.  A wait that runs out of looks all the same (`looks`) forms the
 // state that enters its unit from the inputs, step by step: every wait ends.  (Calls in place have no inputs left for that: their waits end because earlier
 // units go on.)
 //
@@ -561,9 +561,9 @@ __global__ __launch_bounds__(64 * kChainWaves, 4) void chain_kernel(const RecurC
     float far_lg[V] = {}, far_z[V] = {};
     bool ran_out = false;
     if (count > 0) {
-        word_t part[kEach][V];
+        word_t part[kEach][V] = {};
         bool there = false;
-        for (int polls = 0; !there && !ran_out; ran_out = !there && ++polls > ch.polls) {
+        for (RecurLooks looks = {ch.looks, 0}; !there && looks.another();) {
             there = true;
 #pragma unroll
             for (int k = 0; k < kEach; ++k)
@@ -575,6 +575,7 @@ __global__ __launch_bounds__(64 * kChainWaves, 4) void chain_kernel(const RecurC
                 for (int i = 0; i < V; ++i) there = there && part[k][i] != ~0ull;
             there = __all(there);
         }
+        ran_out = !there;
 #pragma unroll
         for (int k = 0; k < kEach; ++k)
             if (k < count) {
@@ -588,7 +589,7 @@ __global__ __launch_bounds__(64 * kChainWaves, 4) void chain_kernel(const RecurC
     }
     if (wave == 0 && block > 0) {
         bool there = false;
-        for (int polls = 0; !there && !ran_out; ran_out = !there && ++polls > ch.polls) {
+        for (RecurLooks looks = {ch.looks, 0}; !there && !ran_out && looks.another();) {
             there = true;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -598,6 +599,7 @@ __global__ __launch_bounds__(64 * kChainWaves, 4) void chain_kernel(const RecurC
             }
             there = __all(there);
         }
+        ran_out = !there;
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) {

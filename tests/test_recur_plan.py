@@ -1,0 +1,46 @@
+"""What the gated recurrence counts by (gla_recur_plan.h), on the CPU."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2405_18428_amd", "csrc")
+SOURCE = r"""
+#include "gla_recur_plan.h"
+using namespace gla;
+extern "C" {
+// looks that a wait makes of `tries` tries; -1 if what it has counted is out of line
+long long looks(int most, long long tries) {
+    RecurLooks l = {most, 0};
+    long long made = 0;
+    for (long long i = 0; i < tries; ++i) made += l.another();
+    return l.made == (most == kRecurNoEnd ? 0 : made) ? made : -1;
+}
+int no_end() { return kRecurNoEnd; }
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    where = tmp_path_factory.mktemp("plan")
+    (where / "plan.cpp").write_text(SOURCE)
+    # (a count that overflows ends the process)
+    subprocess.run(["g++", "-O2", "-std=c++17", "-Wall", "-fsanitize=signed-integer-overflow", "-fsanitize-undefined-trap-on-error", "-shared", "-fPIC", "-I", CSRC, "-o",
+                    str(where / "plan.so"), str(where / "plan.cpp")], check=True)
+    lib = ctypes.CDLL(str(where / "plan.so"))
+    for f in (lib.looks,):
+        f.restype = ctypes.c_longlong
+    lib.looks.argtypes = [ctypes.c_int, ctypes.c_longlong]
+    return lib
+
+
+@pytest.mark.parametrize("most,tries,made", [(0, 100, 0), (1, 100, 1), (1 << 15, 1 << 20, 1 << 15), (100, 7, 7)])
+def test_a_wait_looks_as_often_as_it_may(plan, most, tries, made):
+    assert plan.looks(most, tries) == made
+
+
+def test_a_wait_without_an_end_counts_nothing(plan):
+    """More looks than an int can count."""
+    assert plan.no_end() < 0 and plan.looks(plan.no_end(), (1 << 31) + 100) == (1 << 31) + 100
