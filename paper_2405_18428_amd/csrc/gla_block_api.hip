@@ -71,38 +71,45 @@ RecurUnits units_in(const RecurCall &c, void *workspace) {
     return {reinterpret_cast<float *>(p), reinterpret_cast<float *>(p + each), reinterpret_cast<float *>(p + 2 * each)};
 }
 
-int check_recur(RecurCall &c, const void *x, const void *gate, int kind, float tau, int complement, const int *seq_lens, int B, int T, int D,
+// Work-groups of 512 threads, and backward the chain's of 1024 for each 64 channels of a sequence: fewer than 2^32 threads in a launch
+bool fits(const RecurCall &c, bool back) {
+    const long long groups = recur_groups(c), most = 1LL << 23;
+    return groups < most && groups * c.nunits < most && (!back || c.nunits == 1 || (long long)c.B * ((c.D + 63) / 64) < (1LL << 22));
+}
+
+int check_recur(RecurCall &c, bool back, const void *x, const void *gate, int kind, float tau, int complement, const int *seq_lens, int B, int T, int D,
                 int grid_h, int grid_w, int scan_dir, int dtype, int other_dtype) {
     if (B <= 0 || T <= 0 || D <= 0 || grid_h <= 0 || grid_w <= 0) return GLA_ERR_SHAPE;
     if ((long long)grid_h * grid_w != T || scan_dir < 0 || scan_dir > 3) return GLA_ERR_SHAPE;
     if (bad_dtype(dtype) || bad_dtype(other_dtype) || (kind != GLA_GATE_LOG && kind != GLA_GATE_PRE)) return GLA_ERR_SHAPE;
     if (kind == GLA_GATE_PRE && (!(tau > 0.f) || isinf(tau))) return GLA_ERR_SHAPE;
     if (seq_lens != nullptr && scan_dir > GLA_SCAN_ROW_REV) return GLA_ERR_UNSUPPORTED;
-    // work-groups of 512 threads for as few as 64 channels and 64 steps, fewer than 2^32 threads in a launch; D as 32-bit byte offsets
+    // (steps and what lies behind the last unit as int; a row's channels as 32-bit byte offsets)
     if (T > (1 << 30) || D > (1 << 26)) return GLA_ERR_UNSUPPORTED;
-    if ((long long)B * ((D + 63) / 64) * ((T + kRecurRound - 1) / kRecurRound) >= (1LL << 22)) return GLA_ERR_UNSUPPORTED;
-    if (any_misaligned(x, gate) || (reinterpret_cast<uintptr_t>(seq_lens) & 3u) != 0) return GLA_ERR_ALIGN;
     c = {};
-    c.x = x;
-    c.gate = gate;
-    c.seq_lens = seq_lens;
     c.B = B;
     c.T = T;
     c.D = D;
+    back ? plan_backward(c) : plan_forward(c);
+    if (!fits(c, back)) return GLA_ERR_UNSUPPORTED;
+    if (any_misaligned(x, gate) || (reinterpret_cast<uintptr_t>(seq_lens) & 3u) != 0) return GLA_ERR_ALIGN;
+    c.x = x;
+    c.gate = gate;
+    c.seq_lens = seq_lens;
     c.grid_h = grid_h;
     c.grid_w = grid_w;
     c.scan_dir = scan_dir;
-    const bool back = scan_dir & 1;
-    c.step = (scan_dir >= GLA_SCAN_COL_FWD ? (long long)grid_w : 1) * (back ? -D : D);
-    c.wrap = (1 - (long long)(grid_h - 1) * grid_w) * (back ? -D : D);
+    const long long onward = scan_dir & 1 ? -D : D;
+    c.step = (scan_dir >= GLA_SCAN_COL_FWD ? (long long)grid_w : 1) * onward;
+    c.wrap = (1 - (long long)(grid_h - 1) * grid_w) * onward;
     c.dtype = dtype;
     c.kind = kind;
     c.rest = complement != 0;
     c.inv_tau = kind == GLA_GATE_PRE ? 1.f / tau : 1.f;
     return GLA_OK;
 }
-bool sized_recur(RecurCall &c, int B, int T, int D) {
-    return check_recur(c, nullptr, nullptr, GLA_GATE_LOG, 1.f, 0, nullptr, B, T, D, 1, T, 0, GLA_DT_F32, GLA_DT_F32) == GLA_OK;
+bool sized_recur(RecurCall &c, bool back, int B, int T, int D) {
+    return check_recur(c, back, nullptr, nullptr, GLA_GATE_LOG, 1.f, 0, nullptr, B, T, D, 1, T, 0, GLA_DT_F32, GLA_DT_F32) == GLA_OK;
 }
 
 // --- norm and rotation of queries and keys ---
@@ -234,14 +241,12 @@ extern "C" {
 
 size_t gla_recur_fwd_workspace_bytes(int B, int T, int D) {
     RecurCall c;
-    if (!sized_recur(c, B, T, D)) return 0;
-    plan_forward(c);
+    if (!sized_recur(c, false, B, T, D)) return 0;
     return chain_bytes(c);
 }
 size_t gla_recur_bwd_workspace_bytes(int B, int T, int D) {
     RecurCall c;
-    if (!sized_recur(c, B, T, D)) return 0;
-    plan_backward(c);
+    if (!sized_recur(c, true, B, T, D)) return 0;
     return units_bytes(c);
 }
 
@@ -250,10 +255,9 @@ int gla_recur_fwd(const void *x, const void *gate, int gate_kind, float tau, int
                   void *workspace, size_t workspace_bytes, gla_stream_t stream_) {
     if (!x || !gate || !out) return GLA_ERR_NULL;
     RecurCall c;
-    const int st = check_recur(c, x, gate, gate_kind, tau, complement, seq_lens, B, T, D, grid_h, grid_w, scan_dir, x_dtype, out_dtype);
+    const int st = check_recur(c, false, x, gate, gate_kind, tau, complement, seq_lens, B, T, D, grid_h, grid_w, scan_dir, x_dtype, out_dtype);
     if (st != GLA_OK) return st;
     if (any_misaligned((const void *)initial_state, (const void *)out, (const void *)final_state)) return GLA_ERR_ALIGN;
-    plan_forward(c);
     const int gate_dtype = gate_kind == GLA_GATE_LOG ? GLA_DT_F32 : x_dtype;
     const size_t n = (size_t)B * T * D, state_bytes = (size_t)B * D * sizeof(float);
     const Span xs = {x, n * size_of(x_dtype)}, gs = {gate, n * size_of(gate_dtype)}, os = {out, n * size_of(out_dtype)};
@@ -275,11 +279,10 @@ int gla_recur_bwd(const void *x, const void *gate, int gate_kind, float tau, int
                   int grad_dtype, void *dx, void *d_gate, float *d_initial_state, void *workspace, size_t workspace_bytes, gla_stream_t stream_) {
     if (!x || !gate || !d_out || !dx || !d_gate) return GLA_ERR_NULL;
     RecurCall c;
-    const int st = check_recur(c, x, gate, gate_kind, tau, complement, seq_lens, B, T, D, grid_h, grid_w, scan_dir, x_dtype, grad_dtype);
+    const int st = check_recur(c, true, x, gate, gate_kind, tau, complement, seq_lens, B, T, D, grid_h, grid_w, scan_dir, x_dtype, grad_dtype);
     if (st != GLA_OK) return st;
     if (any_misaligned(d_out, (const void *)initial_state, (const void *)d_final_state, (const void *)dx, (const void *)d_gate, (const void *)d_initial_state))
         return GLA_ERR_ALIGN;
-    plan_backward(c);
     const size_t n = (size_t)B * T * D, state_bytes = (size_t)B * D * sizeof(float);
     const Span outs[] = {{dx, n * size_of(grad_dtype)}, {d_gate, n * size_of(grad_dtype)}, {d_initial_state, state_bytes}};
     const Span ins[] = {{x, n * size_of(x_dtype)}, {gate, n * size_of(gate_kind == GLA_GATE_LOG ? GLA_DT_F32 : x_dtype)}, {d_out, n * size_of(x_dtype)},

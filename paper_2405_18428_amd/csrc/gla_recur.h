@@ -25,6 +25,8 @@ struct RecurChain {
     int looks;                          // of a wait, or kRecurNoEnd
 };
 long long recur_chain_columns(const RecurCall &c);
+// work-groups that a launch has for each unit of steps
+long long recur_groups(const RecurCall &c);
 // of 4 bytes, a column
 inline long long recur_chain_words(const RecurCall &c) { return 2LL * c.nunits + (c.nunits + kRecurBlock - 1) / kRecurBlock; }
 // Backward, per unit and channel, [B, nunits, D]: log2 of its decay, its state from zero and its adjoint from zero at its first step, the gate

@@ -806,21 +806,26 @@ hipError_t instance(const RecurCall &c, bool two, F &&run) {
 // Whether a wave's columns may be those of several sequences, and the groups of 64 columns
 struct Groups {
     bool flat;
-    int count;
+    int count;                           // (of calls within the limits)
 };
-Groups groups_of(const RecurCall &c, int V) {
+constexpr int width(const RecurCall &c) { return c.D % 2 == 0 ? 2 : 1; }
+bool is_flat(const RecurCall &c, int V) {
     const long long cols = c.D / V, spanned = 64 / cols + 2;                       // sequences that a wave can touch
     // (elements up to the last of them in 32 bits as bytes)
-    const bool flat = cols % 64 != 0 && spanned * c.T < (1LL << 30) / c.D;
-    return {flat, (int)(flat ? (c.B * cols + 63) / 64 : c.B * ((cols + 63) / 64))};
+    return cols % 64 != 0 && spanned * c.T < (1LL << 30) / c.D;
 }
+long long count_of(const RecurCall &c, int V) {
+    const long long cols = c.D / V;
+    return is_flat(c, V) ? (c.B * cols + 63) / 64 : c.B * ((cols + 63) / 64);
+}
+Groups groups_of(const RecurCall &c, int V) { return {is_flat(c, V), (int)count_of(c, V)}; }
 
 }  // namespace
 
 // Below so many units each gets a work-group, not a wave (backward calls: 192 units 18 us instead of 26, 1152 47 instead of 52, 2048 66 instead of 65)
 constexpr long long kFewUnits = 2048;
 hipError_t launch_recur_units(const RecurCall &c, const void *d_out, const RecurUnits &u, hipStream_t stream) {
-    return instance(c, c.D % 2 == 0, [&](auto x, auto g, auto kind, auto rest, auto v) {
+    return instance(c, width(c) == 2, [&](auto x, auto g, auto kind, auto rest, auto v) {
         constexpr int V = decltype(v)::value;
         const Groups n = groups_of(c, V);
         const long long units = (long long)n.count * c.nunits;
@@ -845,7 +850,7 @@ static unsigned waves_for(int steps) {
 }
 
 hipError_t launch_recur_walk(const RecurCall &c, const float *first, void *out, int out_dtype, float *final_state, hipStream_t stream) {
-    return instance(c, c.D % 2 == 0, [&](auto x, auto g, auto kind, auto rest, auto v) {
+    return instance(c, width(c) == 2, [&](auto x, auto g, auto kind, auto rest, auto v) {
         constexpr int V = decltype(v)::value;
         const Groups n = groups_of(c, V);
         hipLaunchKernelGGL((walk_kernel<decltype(x), decltype(g), V, kind.value, rest.value>), dim3((unsigned)n.count), dim3(waves_for(c.T)), 0, stream, c, first, out,
@@ -854,17 +859,15 @@ hipError_t launch_recur_walk(const RecurCall &c, const float *first, void *out, 
     });
 }
 
-long long recur_chain_columns(const RecurCall &c) {
-    const int V = c.D % 2 == 0 ? 2 : 1;
-    return (long long)groups_of(c, V).count * V * 64;
-}
+long long recur_groups(const RecurCall &c) { return count_of(c, width(c)); }
+long long recur_chain_columns(const RecurCall &c) { return recur_groups(c) * width(c) * 64; }
 
 hipError_t launch_recur_chain(const RecurCall &c, const RecurChain &ch, const float *first, void *out, int out_dtype, float *final_state, hipStream_t stream) {
     const long long words = recur_chain_columns(c) * recur_chain_words(c);
     hipLaunchKernelGGL(clear_kernel, dim3((unsigned)((words + 1023) / 1024)), dim3(256), 0, stream, reinterpret_cast<uint32_t *>(ch.local), words, ch.ticket);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    return instance(c, c.D % 2 == 0, [&](auto x, auto g, auto kind, auto rest, auto v) {
+    return instance(c, width(c) == 2, [&](auto x, auto g, auto kind, auto rest, auto v) {
         constexpr int V = decltype(v)::value;
         const Groups n = groups_of(c, V);
         hipLaunchKernelGGL((chain_kernel<decltype(x), decltype(g), V, kind.value, rest.value>), dim3((unsigned)((long long)n.count * c.nunits)), dim3(64 * kChainWaves), 0, stream,
@@ -875,7 +878,7 @@ hipError_t launch_recur_chain(const RecurCall &c, const RecurChain &ch, const fl
 
 hipError_t launch_recur_back(const RecurCall &c, const void *d_out, const RecurUnits &u, const float *first, const float *last, void *dx,
                              void *dgate, int grad_dtype, float *d_first, hipStream_t stream) {
-    return instance(c, c.D % 2 == 0, [&](auto x, auto g, auto kind, auto rest, auto v) {
+    return instance(c, width(c) == 2, [&](auto x, auto g, auto kind, auto rest, auto v) {
         constexpr int V = decltype(v)::value;
         const Groups n = groups_of(c, V);
         hipLaunchKernelGGL((back_kernel<decltype(x), decltype(g), V, kind.value, rest.value>), dim3((unsigned)((long long)n.count * c.nunits)),
@@ -887,7 +890,7 @@ hipError_t launch_recur_back(const RecurCall &c, const void *d_out, const RecurU
 hipError_t launch_recur_step(const RecurCall &c, const float *state, float *state_out, void *out, int out_dtype, hipStream_t stream) {
     // (rows of single tokens are often slices of something larger)
     const uintptr_t all = reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(c.x) | reinterpret_cast<uintptr_t>(c.gate);
-    return instance(c, c.D % 2 == 0 && all % 8 == 0, [&](auto x, auto g, auto kind, auto rest, auto v) {
+    return instance(c, width(c) == 2 && all % 8 == 0, [&](auto x, auto g, auto kind, auto rest, auto v) {
         constexpr int V = decltype(v)::value;
         const long long lanes = (long long)c.B * c.D / V;
         hipLaunchKernelGGL((step_kernel<decltype(x), decltype(g), V, kind.value, rest.value>), dim3((unsigned)((lanes + 63) / 64)), dim3(64), 0, stream, c,

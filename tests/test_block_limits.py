@@ -1,0 +1,62 @@
+"""Sizes up to which the operators around the mixer in a block take calls, as include/gla.h states them, and those behind: on the host, before anything is
+enqueued (no GPU).  A call that the limits let pass is stopped by what is checked behind them: a tensor that is not aligned."""
+import ctypes
+
+import pytest
+
+import paper_2405_18428_amd as gla
+from tests import test_block_refusals as tb
+
+UNSUPPORTED, ALIGN = tb.UNSUPPORTED, tb.ALIGN
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return gla.load_library()
+
+
+def sized(call, B, T, D):
+    return {**call, "B": B, "T": T, "D": D, "gh": 1, "gw": T, "x": tb.OFF}
+
+
+# Work-groups, below 2^23 of them: groups of 64 channels for odd D, of 128 for even D, or the columns (channels, or pairs of them) of all sequences, 64 each,
+# where few channels let sequences share a group; forward a group for each 128 steps, or one for all steps from 256 x 128 channels on
+FORWARD = [
+    # (B, T, D): 2^23 - 1 units; 2^23; 2 (2^22 - 1); 2 2^22; 3 2^22; 8 (2^20 - 1); 8 2^20
+    ((1, (1 << 30) - 128, 64), ALIGN), ((1, 1 << 30, 64), UNSUPPORTED), ((1, (1 << 29) - 128, 130), ALIGN), ((1, 1 << 29, 130), UNSUPPORTED),
+    ((1, (1 << 29) - 128, 129), UNSUPPORTED), ((1, (1 << 27) - 128, 1024), ALIGN), ((1, 1 << 27, 1024), UNSUPPORTED),
+    # walked: 64 x 16; 2^16 (64 sequences a group); 2^22; 2^23 - 1; 2^23; 7 2^20; 8 2^20; 127 2^16; 129 2^16
+    ((64, 131072, 2048), ALIGN), ((1 << 22, 3, 1), ALIGN), ((1 << 22, 3, 128), ALIGN), (((1 << 23) - 1, 3, 128), ALIGN), ((1 << 23, 3, 128), UNSUPPORTED),
+    ((1 << 20, 1 << 20, 896), ALIGN), ((1 << 20, 1 << 20, 1024), UNSUPPORTED), ((1 << 22, 300, 127), ALIGN), ((1 << 22, 300, 129), UNSUPPORTED),
+    ((1 << 30, 1 << 30, 1 << 26), UNSUPPORTED),
+]
+# A group for each 64 steps; where there are several of these, below 2^22 times 64 channels of one sequence as well
+BACKWARD = [
+    # 2^23 - 1; 2^23; 64 x 64 x 2047; 64 x 64 x 2048; 64 x 128 x 2047; 64 x 16 x 2048
+    ((1, (1 << 29) - 64, 64), ALIGN), ((1, 1 << 29, 64), UNSUPPORTED), ((64, (1 << 17) - 64, 8192), ALIGN), ((64, 1 << 17, 8192), UNSUPPORTED),
+    ((64, (1 << 17) - 64, 8191), UNSUPPORTED), ((64, 131072, 2048), ALIGN),
+    # one round: 2^16, 2^22, 2^23; several: 2^17 and 2^22 sequences, 2^22 - 1, 3 2^20 and 3 2^21 times 64 channels
+    ((1 << 22, 64, 1), ALIGN), ((1 << 22, 3, 128), ALIGN), ((1 << 23, 3, 128), UNSUPPORTED), ((1 << 22, 65, 1), UNSUPPORTED), (((1 << 22) - 1, 65, 1), ALIGN),
+    ((1 << 20, 65, 130), ALIGN), ((1 << 21, 65, 130), UNSUPPORTED), ((1 << 30, 1 << 30, 1 << 26), UNSUPPORTED),
+]
+
+
+@pytest.mark.parametrize("sizes,status", FORWARD)
+def test_recurrence_forward(lib, sizes, status):
+    assert lib.gla_recur_fwd(*sized(tb.RECUR, *sizes).values()) == status
+    assert status == ALIGN or gla.gla_recur_fwd_workspace_bytes(*sizes) == 0
+
+
+@pytest.mark.parametrize("sizes,status", BACKWARD)
+def test_recurrence_backward(lib, sizes, status):
+    assert lib.gla_recur_bwd(*sized(tb.RECUR_BWD, *sizes).values()) == status
+    assert status == ALIGN or gla.gla_recur_bwd_workspace_bytes(*sizes) == 0
+
+
+def test_recurrence_workspaces_of_the_largest_calls():
+    """A word of 64 bits a unit and channel, one of 32 a block of 16 units; three numbers a round and channel."""
+    T = (1 << 30) - 128
+    units = T // 128
+    assert gla.gla_recur_fwd_workspace_bytes(1, T, 64) >= 64 * (units * 8 + units // 16 * 4)
+    T = (1 << 29) - 64
+    assert gla.gla_recur_bwd_workspace_bytes(1, T, 64) >= 3 * 4 * 64 * (T // 64)
