@@ -701,8 +701,9 @@ size_t gla_qk_norm_bwd_workspace_bytes(int B, int H, int Hk, int T, int d);
  *   workspace      DEVICE, 16-byte aligned, gla_glu_fwd_workspace_bytes(...) bytes (0 where rows of K are whole pieces of 16 bytes: may be
  *                  NULL; else for copies whose rows are)
  *
- * Sums in fp32 (bf16 or fp32 MFMA).  Tensors 16-byte aligned.  Outputs must not overlap inputs or each other (GLA_ERR_SHAPE).  K, F up to 2^20.
- * Never allocates; nothing is kept between calls.  Calls that may overlap, captured ones among them, need workspaces of their own.
+ * Sums in fp32 (bf16 or fp32 MFMA).  Tensors 16-byte aligned.  Outputs must not overlap inputs or each other (GLA_ERR_SHAPE).  K, F up to 2^20,
+ * M up to 2^28, M (max(K, F) + 8) < 2^34 and F (K + 8) < 2^32: others are refused (GLA_ERR_UNSUPPORTED).  Never allocates;
+ * nothing is kept between calls.  Calls that may overlap, captured ones among them, need workspaces of their own.
  */
 typedef enum { GLA_ACT_SILU = 0, GLA_ACT_GELU = 1, GLA_ACT_GELU_TANH = 2 } gla_activation;
 int gla_glu_fwd(const void *x, const void *w_gate, const void *w_up, int M, int K, int F, int act, int dtype, int out_dtype,

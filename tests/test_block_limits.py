@@ -60,3 +60,15 @@ def test_recurrence_workspaces_of_the_largest_calls():
     assert gla.gla_recur_fwd_workspace_bytes(1, T, 64) >= 64 * (units * 8 + units // 16 * 4)
     T = (1 << 29) - 64
     assert gla.gla_recur_bwd_workspace_bytes(1, T, 64) >= 3 * 4 * 64 * (T // 64)
+
+
+PRODUCT = [((1 << 28, 8, 8), ALIGN), (((1 << 28) + 1, 1, 1), UNSUPPORTED), ((1 << 28, 55, 8), ALIGN), ((1 << 28, 56, 8), UNSUPPORTED), ((1 << 28, 8, 55), ALIGN), ((1 << 28, 8, 56), UNSUPPORTED),
+           ((1, 1 << 20, 4095), ALIGN), ((1, 1 << 20, 4096), UNSUPPORTED), ((1, 4088, (1 << 20) - 1), ALIGN), ((1, 4088, 1 << 20), UNSUPPORTED), ((1, (1 << 20) + 1, 8), UNSUPPORTED),
+           ((1, 8, (1 << 20) + 1), UNSUPPORTED), ((16383, 4, 1 << 20), ALIGN), ((16384, 4, 1 << 20), UNSUPPORTED)]
+
+
+@pytest.mark.parametrize("sizes,status", PRODUCT)
+def test_product(lib, sizes, status):
+    m = dict(zip("MKF", sizes), x=tb.OFF)
+    assert lib.gla_glu_fwd(*{**tb.GLU, **m}.values()) == status and lib.gla_glu_bwd(*{**tb.GLU_BWD, **m}.values()) == status
+    assert (gla.gla_glu_bwd_workspace_bytes(*sizes) > 0) == (status == ALIGN)
