@@ -593,7 +593,7 @@ size_t gla_norm_bwd_workspace_bytes(int B, int H, int T, int D);
  *   gate           DEVICE, [B,T,D] (read): by gate_kind (a gla_gate_kind)
  *                  GLA_GATE_LOG: log a in fp32, <= 0 down to -inf (a gate of zero)
  *                  GLA_GATE_PRE: z in x_dtype, a = sigmoid(z)^(1/tau)   (Eq. (gate_gla))
- *   tau            > 0, finite; ignored for GLA_GATE_LOG
+ *   tau            from 2^-64 on, finite; ignored for GLA_GATE_LOG
  *   complement     not 0: u_t = (1 - a_t) x_t
  *   seq_lens       DEVICE, int32 [B], 0 .. T, or NULL: all T; as in gla_decay_fwd (row scans only): rows behind a sequence's end may hold
  *                  anything and those of `out` are left as they were                                          (read)

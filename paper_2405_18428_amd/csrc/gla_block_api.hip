@@ -40,6 +40,9 @@ bool any_touch(const Span (&mine)[N], const Span (&others)[M]) {
 
 // --- gated recurrence of channels ---
 
+// (e^-z is lost below 2^-126, which is 2^-62 of a gate's logarithm from 1 / tau = 2^64 on; an infinite reciprocal would make NaN of a gate of one)
+bool bad_tau(float tau) { return !(tau >= 0x1p-64f) || isinf(tau); }
+
 // Forward: the sequence in units, or walked by one work-group, where there are many of those or few units.  bf16, 2048 channels, walked and in
 // units: 4096 steps of 64 groups of 128 channels 151 us and 49, of 128 groups 154 and 106, of 256 groups 171 and 176 (1024 steps 44 and 46, 512 steps 25 and 29);
 // 512 steps of 128 groups 22.6 and 20.4, 256 steps 12.3 and 12.9, of 64 groups 11.7 and 10.6, 160 steps 9.3 and 10.9.
@@ -82,7 +85,7 @@ int check_recur(RecurCall &c, bool back, const void *x, const void *gate, int ki
     if (B <= 0 || T <= 0 || D <= 0 || grid_h <= 0 || grid_w <= 0) return GLA_ERR_SHAPE;
     if ((long long)grid_h * grid_w != T || scan_dir < 0 || scan_dir > 3) return GLA_ERR_SHAPE;
     if (bad_dtype(dtype) || bad_dtype(other_dtype) || (kind != GLA_GATE_LOG && kind != GLA_GATE_PRE)) return GLA_ERR_SHAPE;
-    if (kind == GLA_GATE_PRE && (!(tau > 0.f) || isinf(tau))) return GLA_ERR_SHAPE;
+    if (kind == GLA_GATE_PRE && bad_tau(tau)) return GLA_ERR_SHAPE;
     if (seq_lens != nullptr && scan_dir > GLA_SCAN_ROW_REV) return GLA_ERR_UNSUPPORTED;
     // (steps and what lies behind the last unit as int; a row's channels as 32-bit byte offsets)
     if (T > (1 << 30) || D > (1 << 26)) return GLA_ERR_UNSUPPORTED;
@@ -302,7 +305,7 @@ int gla_recur_step(const void *x, const void *gate, int gate_kind, float tau, in
                    const float *state, float *state_out, void *out, gla_stream_t stream) {
     if (!x || !gate || !state || !state_out || !out) return GLA_ERR_NULL;
     if (B <= 0 || D <= 0 || bad_dtype(x_dtype) || bad_dtype(out_dtype) || (gate_kind != GLA_GATE_LOG && gate_kind != GLA_GATE_PRE)) return GLA_ERR_SHAPE;
-    if (gate_kind == GLA_GATE_PRE && (!(tau > 0.f) || isinf(tau))) return GLA_ERR_SHAPE;
+    if (gate_kind == GLA_GATE_PRE && bad_tau(tau)) return GLA_ERR_SHAPE;
     if ((long long)B * D >= (1LL << 31)) return GLA_ERR_UNSUPPORTED;
     const int gate_dtype = gate_kind == GLA_GATE_LOG ? GLA_DT_F32 : x_dtype;
     if (any_misaligned((const void *)state, (const void *)state_out) || off_element(x, x_dtype) || off_element(gate, gate_dtype) || off_element(out, out_dtype))

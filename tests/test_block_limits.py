@@ -72,3 +72,17 @@ def test_product(lib, sizes, status):
     m = dict(zip("MKF", sizes), x=tb.OFF)
     assert lib.gla_glu_fwd(*{**tb.GLU, **m}.values()) == status and lib.gla_glu_bwd(*{**tb.GLU_BWD, **m}.values()) == status
     assert (gla.gla_glu_bwd_workspace_bytes(*sizes) > 0) == (status == ALIGN)
+
+
+# (a subnormal temperature's reciprocal is infinite, and a gate of one NaN; below 2^-64 what fp32 loses of e^-z, 2^-126, begins to show in a gate)
+TAUS = [(2.0 ** -64, ALIGN), (3.0e38, ALIGN), (2.0 ** -65, tb.SHAPE), (2.0 ** -127, tb.SHAPE), (1e-45, tb.SHAPE), (-1.0, tb.SHAPE)]
+
+
+@pytest.mark.parametrize("tau,status", TAUS)
+def test_temperatures(lib, tau, status):
+    tau = ctypes.c_float(tau)
+    for call, args in ((lib.gla_recur_fwd, tb.RECUR), (lib.gla_recur_bwd, tb.RECUR_BWD)):
+        assert call(*{**args, "x": tb.OFF, "tau": tau}.values()) == status
+        assert call(*{**args, "x": tb.OFF, "tau": tau, "kind": 0}.values()) == ALIGN
+    for kind, want in ((1, status), (0, ALIGN)):
+        assert lib.gla_recur_step(*{**tb.STEP, "s": tb.OFF, "tau": tau, "kind": kind}.values()) == want
