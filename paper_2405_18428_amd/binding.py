@@ -941,11 +941,20 @@ def gla_norm_bwd(x, d_out, weight=None, bias=None, eps=1e-5, r_pre=None, layout=
     return dx, dr, dw, db
 
 
+_MOST = (1 << 31) - 1
+
+
+def _no_int():
+    raise ValueError("sizes must be below 2^31")
+
+
 def _prep_recur(x, gate, gate_kind, shape, seq_lens, states):
     """Checks the tensors of a gated recurrence; x has `shape`, states its first and last size."""
     torch = _torch()
     if gate_kind not in (GATE_LOG, GATE_PRE):
         raise ValueError("unknown gate kind")
+    if x.numel() > _MOST and max(shape) > _MOST:
+        _no_int()
     _dt(x)
     dev = x.get_device()
     _want("x", x, shape, x.dtype, dev)
@@ -1071,9 +1080,13 @@ def _prep_qk(q, k, q_weight, k_weight, positions, sections, layout):
     _dt(q)
     _want_rows("q", q, q.dtype, dev)
     B, H, T, d = q.shape if layout == LAYOUT_BHTD else (q.shape[0], q.shape[2], q.shape[1], q.shape[3])
+    if q.numel() > _MOST and max(q.shape) > _MOST:
+        _no_int()
     if k is not None:
         _want_rows("k", k, q.dtype, dev)
         Hk = k.shape[1 if layout == LAYOUT_BHTD else 2]
+        if Hk > _MOST:
+            _no_int()
         if k.shape != ((B, Hk, T, d) if layout == LAYOUT_BHTD else (B, T, Hk, d)):
             raise ValueError("q and k must agree in batches, tokens and channels")
         if k_weight is not None:
@@ -1152,12 +1165,15 @@ def _prep_glu(x, w_gate, w_up, pre):
     if x.dim() < 2 or w_gate.dim() != 2:
         raise ValueError("x must be [..., K], w_gate and w_up [F, K]")
     K, F = x.shape[-1], w_gate.shape[0]
+    M = x.numel() // max(K, 1)
+    if M > _MOST or K > _MOST or F > _MOST:
+        _no_int()
     _want("x", x, x.shape, x.dtype, dev)
     _want("w_gate", w_gate, (F, K), x.dtype, dev)
     _want("w_up", w_up, (F, K), x.dtype, dev)
     if pre is not None:
         _want("pre", pre, (2, *x.shape[:-1], F), torch.float32, dev)
-    return x.numel() // max(K, 1), K, F
+    return M, K, F
 
 
 def gla_glu_fwd_workspace_bytes(M, K, F, dtype=DT_BF16) -> int:

@@ -86,3 +86,29 @@ def test_temperatures(lib, tau, status):
         assert call(*{**args, "x": tb.OFF, "tau": tau, "kind": 0}.values()) == ALIGN
     for kind, want in ((1, status), (0, ALIGN)):
         assert lib.gla_recur_step(*{**tb.STEP, "s": tb.OFF, "tau": tau, "kind": kind}.values()) == want
+
+
+HUGE = (1 << 32) + 5                     # as a C int: 5
+
+
+@pytest.mark.parametrize("call", ["fwd", "bwd", "step", "qk_fwd", "qk_bwd", "qk_keys", "glu_fwd", "glu_bwd", "glu_columns"])
+def test_sizes_that_are_no_c_int_are_refused(call, monkeypatch):
+    """They would be cut off to 32 bits on their way into the library, which would then work on a part of the tensors.  (Tensors without memory.)"""
+    torch = pytest.importorskip("torch")
+    from paper_2405_18428_amd import binding
+
+    class Library:
+        def __getattr__(self, name):
+            raise AssertionError("the library was reached")
+    new = lambda *s, dtype=torch.bfloat16: torch.empty(*s, dtype=dtype, device="meta")  # noqa: E731
+    monkeypatch.setattr(binding, "load_library", Library)
+    monkeypatch.setattr(binding, "_want", lambda *args: None)
+    monkeypatch.setattr(binding, "_want_rows", lambda *args: None)
+    monkeypatch.setattr(binding, "_room", lambda *args: None)
+    rows, q, k = new(1, HUGE, 1), new(1, 1, HUGE, 2), new(1, 1, 5, 2)
+    x, w = new(HUGE, 1), new(1, 1)
+    with pytest.raises(ValueError, match="2\\^31"):
+        {"fwd": lambda: gla.gla_recur_fwd(rows, rows, 1, HUGE), "bwd": lambda: gla.gla_recur_bwd(rows, rows, rows, 1, HUGE),
+         "step": lambda: gla.gla_recur_step(x, x, new(HUGE, 1, dtype=torch.float32)), "qk_fwd": lambda: gla.gla_qk_norm_fwd(q, None),
+         "qk_bwd": lambda: gla.gla_qk_norm_bwd(q, None, q, None), "qk_keys": lambda: gla.gla_qk_norm_fwd(new(1, 1, 5, 2), new(1, HUGE, 5, 2)),
+         "glu_fwd": lambda: gla.gla_glu_fwd(x, w, w), "glu_bwd": lambda: gla.gla_glu_bwd(x, w, w, x), "glu_columns": lambda: gla.gla_glu_fwd(w, x, x)}[call]()
