@@ -663,7 +663,7 @@ int gla_recur_step(const void *x, const void *gate, int gate_kind, float tau, in
  *               they overlap the inputs or each other otherwise                                                 (written)
  *
  * 1 <= d <= 256.  q and k may begin at any element, the other tensors at 16 bytes.  Sums and angles as in gla_norm_fwd and gla_rope; a row's
- * squares have to add up to a finite fp32 number, and with eps = 0 to one that is not zero.  Needs no workspace and never allocates.
+ * squares have to add up to a finite fp32 number, and their mean and eps to no less than 2^-126: a row that is all but zero needs an eps.  Needs no workspace and never allocates.
  */
 int gla_qk_norm_fwd(const void *q, const long long *q_strides, int H, const void *k, const long long *k_strides, int Hk, const float *q_weight,
                     const float *k_weight, float eps, const int *positions, const int *sections, int axes, float base, int pairing,

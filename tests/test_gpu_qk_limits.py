@@ -37,3 +37,18 @@ def test_no_eps_of_queries_alone():
     near, _, dwn, _ = gla.gla_qk_norm_bwd(x, None, dy, None, w, sections=(64,), eps=1e-12)
     assert torch.isfinite(dx).all() and torch.isfinite(dw).all()
     assert float((dx - near).abs().max()) < 1e-5 and float((dw - dwn).abs().max()) < 1e-4 * np.sqrt(2 * 7 * 3)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("scale", [2.0 ** -40, 2.0 ** 40])
+def test_no_eps_of_small_and_large_rows(scale, dtype):
+    """Squares by a power of two smaller or larger, all of them normal numbers: the same bits, and dx by as much larger or smaller."""
+    gen = torch.Generator(device="cuda:0").manual_seed(3)
+    x, k, dy, dk = (torch.randn(2, n, 9, 64, generator=gen, device="cuda:0").to(dtype) for n in (6, 2, 6, 2))
+    x, k = (torch.where(t.abs() < 2.0 ** -16, 1.0, t).to(dtype) for t in (x, k))
+    w, v = 1 + 0.1 * torch.randn(2, 64, generator=gen, device="cuda:0")
+    how = {"sections": (64,), "eps": 0.0}
+    want, got = (gla.gla_qk_norm_fwd(s * x, s * k, w, v, **how) for s in (1.0, scale))
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.isfinite(got[0]).all()
+    want, got = (gla.gla_qk_norm_bwd(s * x, s * k, dy, dk, w, v, **how) for s in (1.0, scale))
+    assert all(torch.equal(a * scale, b) for a, b in zip(got[:2], want[:2])) and all(torch.equal(a, b) for a, b in zip(got[2:], want[2:]))
