@@ -608,9 +608,9 @@ size_t gla_norm_bwd_workspace_bytes(int B, int H, int T, int D);
  * finite, but for gates of zero; a NaN makes NaN of what comes after it in its channel.  Tensors 16-byte aligned.  Never
  * allocates; nothing is kept between calls.  Calls that may overlap, captured ones among them, need workspaces of their own.
  *
- * T up to 2^30, D up to 2^26, and with c = ceil(D / 128) for even D, ceil(D / 64) for odd D, B c ceil(T / 128) < 2^23 (calls of T > 256 with B D / 128
- * < 256) or B c < 2^23 (all others); gla_recur_bwd: B c ceil(T / 64) < 2^23, and for T > 64 B ceil(D / 64) < 2^22.  Others are refused
- * (GLA_ERR_UNSUPPORTED), but for some of few channels, of which several sequences share a work-group.
+ * T up to 2^30, D up to 2^26, and with c = ceil(D / 128) for even D, ceil(D / 64) for odd D: B c < 2^23, where T > 256 and B D < 2^15 (odd D: 2^14) also
+ * B c ceil(T / 128) < 2^23; gla_recur_bwd: B c ceil(T / 64) < 2^23, and for T > 64 B ceil(D / 64) < 2^22.  Others are refused (GLA_ERR_UNSUPPORTED), but
+ * for some of few channels, of which several sequences share a work-group.
  */
 typedef enum { GLA_GATE_LOG = 0, GLA_GATE_PRE = 1 } gla_gate_kind;
 int gla_recur_fwd(const void *x, const void *gate, int gate_kind, float tau, int complement, const int *seq_lens,

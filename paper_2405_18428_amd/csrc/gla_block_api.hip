@@ -44,13 +44,19 @@ bool any_touch(const Span (&mine)[N], const Span (&others)[M]) {
 bool bad_tau(float tau) { return !(tau >= 0x1p-64f) || isinf(tau); }
 
 // Forward: the sequence in units, or walked by one work-group, where there are many of those or few units.  bf16, 2048 channels, walked and in
-// units: 4096 steps of 64 groups of 128 channels 151 us and 49, of 128 groups 154 and 106, of 256 groups 171 and 176 (1024 steps 44 and 46, 512 steps 25 and 29);
-// 512 steps of 128 groups 22.6 and 20.4, 256 steps 12.3 and 12.9, of 64 groups 11.7 and 10.6, 160 steps 9.3 and 10.9.
-constexpr int kWalkGroups = 256, kWalkUnits = 2;
+// units: 4096 steps of 64 groups of 128 channels 151 us and 49, of 128 groups 154 and 106, of 192 groups 154 and 136, of 256 groups 160 and 193 (1024 steps 43 and
+// 46, 512 steps 24 and 29); 512 steps of 128 groups 22.6 and 20.4, 256 steps 12.3 and 12.9, of 64 groups 11.7 and 10.6, 160 steps 9.3 and 10.9.
+// Odd D, whose groups have 64 channels and loads half as wide: 256 groups of 2047 channels, 300 steps 14 us and 23, 768 29 and 38, 1024 38 and 45, 1500 55 and
+// 59, 2048 73 and 73, 4096 146 and 148; 512 groups 21 and 36, 50 and 58, 67 and 72, 95 and 98, 153 and 153, 302 and 271; 320 groups, the least fit for a walk,
+// 20 and 27, 43 and 42, 56 and 52, 83 and 69, 110 and 86, 239 and 167.
+constexpr int kWalkGroups = 256, kWalkUnits = 2, kWalkOddSteps = 1024;
+constexpr long long kMostGroups = 1LL << 23;         // work-groups of 512 threads: fewer than 2^32 threads in a launch
 void plan_forward(RecurCall &c) {
-    const bool units = c.T > kWalkUnits * kRecurChain && ((long long)c.B * c.D + 127) / 128 < kWalkGroups;
-    c.unit = units ? kRecurChain : c.T;
-    c.nunits = units ? (c.T + kRecurChain - 1) / kRecurChain : 1;
+    const bool odd = c.D % 2 != 0;
+    const long long units = (c.T + kRecurChain - 1) / kRecurChain, groups = ((long long)c.B * c.D + (odd ? 63 : 127)) / (odd ? 64 : 128);
+    const bool walks = c.T <= kWalkUnits * kRecurChain || (groups >= kWalkGroups && (!odd || c.T <= kWalkOddSteps || recur_groups(c) >= kMostGroups / units));
+    c.unit = walks ? c.T : kRecurChain;
+    c.nunits = walks ? 1 : (int)units;
 }
 void plan_backward(RecurCall &c) {
     c.unit = kRecurRound;
@@ -74,10 +80,10 @@ RecurUnits units_in(const RecurCall &c, void *workspace) {
     return {reinterpret_cast<float *>(p), reinterpret_cast<float *>(p + each), reinterpret_cast<float *>(p + 2 * each)};
 }
 
-// Work-groups of 512 threads, and backward the chain's of 1024 for each 64 channels of a sequence: fewer than 2^32 threads in a launch
+// (backward also the chain's work-groups, of 1024 threads for each 64 channels of a sequence)
 bool fits(const RecurCall &c, bool back) {
-    const long long groups = recur_groups(c), most = 1LL << 23;
-    return groups < most && groups * c.nunits < most && (!back || c.nunits == 1 || (long long)c.B * ((c.D + 63) / 64) < (1LL << 22));
+    const long long groups = recur_groups(c);
+    return groups < kMostGroups && groups * c.nunits < kMostGroups && (!back || c.nunits == 1 || (long long)c.B * ((c.D + 63) / 64) < (1LL << 22));
 }
 
 int check_recur(RecurCall &c, bool back, const void *x, const void *gate, int kind, float tau, int complement, const int *seq_lens, int B, int T, int D,
