@@ -414,8 +414,9 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
 
 // Forward for few rows, where the weights' reading is all: a work-group has 16 NT columns of both products, its waves a part of K each, whose weights go
 // from memory to the matrix units' registers; rows of x, which all work-groups share, come from L2.  The waves' sums meet in LDS.  MT: tiles of 16 rows.
-// Bound by HBM and by how short it is: one row of 2048 x 8192, bf16, 67 MB, 18.6 us from HBM (13.0 at a copy's rate), 12.1 where part of the weights is in the
-// last-level cache; of 4096 x 16384 64 us for 52.  Eight pieces a wave under way instead of four: 19.0 and 64 us, 16 rows 21.4 for 20.9.
+// Bound by HBM and by how short it is: one row of 2048 x 8192, bf16, 67 MB, 15.2 us from HBM, 64 sets of weights in turn (13.0 at a copy's rate), 12.4 where the
+// weights are in the last-level cache; 33 rows 22.3 and 17.8; of 4096 x 16384 one row 49 us for 52, 33 rows 71.  Comparisons here and below are of short graphs with weights from
+// HBM, whose starts add some 3 us a call: one row 18.6; eight pieces a wave under way instead of four 19.0, 16 rows 21.4 for 20.9.
 template <typename E, int WAVES, int MT, int NT>
 __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(const ProductArgs p) {
     constexpr int kES = sizeof(E), kAhead = MT + 2 * NT <= 8 ? 4 : 2;

@@ -11,7 +11,8 @@
 //
 // Bound by HBM: 4 x 4095 tokens of 16 + 16 heads of 128 channels, bf16, forward 268 MB in 52 us, 5.2 TB/s, backward 403 MB in 82, 4.9 TB/s.  Work-groups of 16
 // tokens, a group of lanes each, which read 256 bytes a token at a time: 110 and 139 us.  Three or four turns of heads on their way instead of two: 65 and
-// 91, 63 and 90 (63 and 82 then).  Rows asked for before the angles are formed: 51 and 85.  64 single tokens of 16 + 4 heads 4.8 us, a launch and one row's loads, sum and stores.
+// 91, 63 and 90 (63 and 82 then).  Rows asked for before the angles are formed: 51 and 85.  64 single tokens of 16 + 4 heads 4.7 us a call in a
+// graph (6.0 in a trace), a launch and one row's loads, sum and stores.
 #include "gla_qk.h"
 #include "gla_rope_util.h"
 #include "gla_rows.h"
@@ -264,7 +265,7 @@ hipError_t qk(const QkParams &p, hipStream_t stream) {
     constexpr int kRows = 64 / LANES, kWaves = kThreads / 64;
     const int turns = (p.side[0].heads + kRows - 1) / kRows + (p.side[1].heads + kRows - 1) / kRows;
     const long long tokens = (long long)p.rope.B * p.rope.T;
-    // turns that share a token's sines and cosines: all, unless that leaves the GPU idle (64 tokens of 16 + 4 heads 4.8 us, with all turns together 6.2; 2048
+    // turns that share a token's sines and cosines: all, unless that leaves the GPU idle (64 tokens of 16 + 4 heads 4.7 us, with all turns together 6.2; 2048
     // tokens 8.0, in parts 13.2)
     int each = turns;
     while (each > 1 && tokens * ((turns + each - 1) / each) < 2048) each = (each + 1) / 2;
@@ -275,7 +276,7 @@ hipError_t qk(const QkParams &p, hipStream_t stream) {
     for (int x = 0; x < r.axes; ++x) whole = whole && r.first[x] % kEach == 0 && r.half[x] % (r.adjacent ? 1 : kEach) == 0;
     auto run = [&](auto mode) {
         constexpr int MODE = decltype(mode)::value;
-        // forward as many work-groups as the GPU holds (4 x 4095 tokens of 16 + 16 heads of 128 channels 54 us, with one for each four tokens 63; 20000 of
+        // forward as many work-groups as the GPU holds (4 x 4095 tokens of 16 + 16 heads of 128 channels 52 us, with one for each four tokens 63; 20000 of
         // 12 + 12 heads of 64 38 and 51)
         static const int held = [] {
             int n = 0;

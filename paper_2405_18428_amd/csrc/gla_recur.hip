@@ -23,7 +23,8 @@
 // pre-activation's gate gets back what 1 + e rounds off.  What a gate lacks of one comes from expm1 too.
 //
 // What bounds it: HBM, and beside it the vector units, which are busy for more than half of a forward call: two exponentials and a logarithm, at a quarter of
-// the rate, are 12 of some 27 issue slots an element.  One MI355X, whose copies reach 5.17 TB/s; times stand at the kernels.
+// the rate, are 12 of some 27 issue slots an element.  One MI355X, whose copies reach 5.17 TB/s; times stand at the kernels, a trace's
+// unless it says call: under a trace kernels are longer (a training step's five add up to 191 us, the step takes 194 traced and 174 by itself).
 #include "gla_recur.h"
 
 namespace gla {
@@ -434,7 +435,7 @@ __device__ __forceinline__ void put_outputs(const RecurCall &c, const Place<V> &
 }
 
 // Forward pass with a sequence to itself: a work-group walks 64 V channels in rounds, 8 steps a wave, with the next round on its way.  Bound by HBM where
-// work-groups fill the GPU (16 x 4096 x 2048, bf16: 171 us, 4.7 TB/s), by a round's loads, exchange and stores one after the other elsewhere (2.4 us for 64
+// work-groups fill the GPU (16 x 4096 x 2048, bf16: a call 160 us, 5.0 TB/s), by a round's loads, exchange and stores one after the other elsewhere (2.4 us for 64
 // steps of 64 groups).
 template <typename EX, typename EG, int V, int KIND, bool REST>
 __global__ __launch_bounds__(64 * kWaves) void walk_kernel(const RecurCall c, const float *first, void *out, int out_dtype, float *final_state, bool flat) {
@@ -499,10 +500,10 @@ __global__ __launch_bounds__(256) void clear_kernel(uint32_t *words, long long c
 }
 
 // Forward pass in units of 128 steps, 16 a wave.  Decays and inputs of the wave's 16 steps stay in registers, 64 with two channels a lane, while the
-// look-back waits, so two work-groups fit a compute unit; their loads, wait and stores overlap each other's.  65536 x 2048, bf16: 182 to 190 us, 4.3 TB/s;
-// 4 x 4096 x 2048 with u = (1 - a) x 59 us; 8 sequences of 1 to 2047 steps, 130 MB moved, 44 us, some 20 of them the first loads and the last stores.  Units
-// of 64 steps (8 a wave) took 393 us, of 256 (16 waves) 396, work-groups of 4 waves 236.  One ticket for all groups is ahead of one for each, 188 us
-// and 215: neighbouring groups' units, whose rows lie beside each other, then run together.
+// look-back waits, so two work-groups fit a compute unit; their loads, wait and stores overlap each other's.  65536 x 2048, bf16: a call 178 us, 4.5 TB/s
+// (the kernel 189 in a trace); 4 x 4096 x 2048 with u = (1 - a) x a call 50 us (the kernel 59); 8 sequences of 1 to 2047 steps,
+// 130 MB moved, a call 45 us, some 20 of them the first loads and the last stores.  In traces of 65536 x 2048 units of 64 steps (8 a wave) took 393 us, of 256 (16
+// waves) 396, work-groups of 4 waves 236.  One ticket for all groups is ahead of one for each, 188 us and 215: neighbouring groups' units, whose rows lie beside each other, then run together.
 template <typename EX, typename EG, int V, int KIND, bool REST>
 __global__ __launch_bounds__(64 * kChainWaves, 4) void chain_kernel(const RecurCall c, const RecurChain ch, const float *first, void *out, int out_dtype, float *final_state,
                                                             bool flat, int groups) {
