@@ -136,6 +136,10 @@ typedef enum {
                                     before it forms the state entering its own from the inputs (default 32768: tens of
                                     milliseconds, which only runs out where other work keeps the earlier spans off the
                                     GPU; 0 = never, for tests) */
+    GLA_OPT_GLU_SPLIT = 6,       /* 1 = gla_glu_bwd takes dg and du of bf16 calls as two bf16 numbers each into the second pair of
+                                    products: gradients are off by their own rounding alone, for twice that pair's operations and
+                                    twice the workspace's two arrays (gla_glu_bwd_workspace_bytes goes by it too); 0 (default) =
+                                    as one */
     GLA_OPT_RANGE_FALLBACK = 4   /* 1 (default) = after the fp16 engine's passes, the (batch, head) sequences that
                                     left its range are recomputed by the bf16 hi/lo kernel (one more launch, whose
                                     work-groups return at once when no flag is raised); 0 = that launch is skipped
@@ -721,7 +725,7 @@ size_t gla_glu_fwd_workspace_bytes(int M, int K, int F, int dtype);
  *   workspace   DEVICE, 16-byte aligned, gla_glu_bwd_workspace_bytes(...) bytes
  *
  * Gradients have the inputs' element type.  From bf16, dg and du are rounded to bf16 once as operands: gradients are off by 1.4 times what
- * their own rounding takes (2.3e-3 in the 2-norm, not 1.7e-3); callers for whom that matters give all tensors in fp32.  Sums are always added in
+ * their own rounding takes (2.3e-3 in the 2-norm, not 1.7e-3); GLA_OPT_GLU_SPLIT takes them as two numbers each.  Sums are always added in
  * one order.  Everything else as gla_glu_fwd.
  */
 int gla_glu_bwd(const void *x, const void *w_gate, const void *w_up, const void *d_out, const float *pre, int M, int K, int F, int act,

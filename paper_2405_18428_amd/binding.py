@@ -15,7 +15,7 @@ from typing import List, Optional
 
 SCAN_ROW_FWD, SCAN_ROW_REV, SCAN_COL_FWD, SCAN_COL_REV = 0, 1, 2, 3
 DT_F32, DT_BF16 = 0, 1
-OPT_CHUNKS_PER_SPAN, OPT_ENGINE, OPT_CARRY, OPT_BWD_SPLIT, OPT_RANGE_FALLBACK, OPT_LOOK_BACK_POLLS = 0, 1, 2, 3, 4, 5
+OPT_CHUNKS_PER_SPAN, OPT_ENGINE, OPT_CARRY, OPT_BWD_SPLIT, OPT_RANGE_FALLBACK, OPT_LOOK_BACK_POLLS, OPT_GLU_SPLIT = 0, 1, 2, 3, 4, 5, 6
 CARRY_AUTO, CARRY_KERNEL, CARRY_IN_OUTPUT_PASS = 0, 1, 2
 LAYOUT_BHTD, LAYOUT_BTHD = 0, 1
 DECAY_HEAD, DECAY_TOKEN = 0, 1
@@ -1204,7 +1204,8 @@ def gla_glu_fwd(x, w_gate, w_up, act=ACT_SILU, out_dtype=None, out=None, pre=Non
 
 def gla_glu_bwd(x, w_gate, w_up, d_out, act=ACT_SILU, pre=None, want_dx=True, want_dw=True, workspace=None, stream=None):
     """Gradients of gla_glu_fwd: (dx or None, dw_gate or None, dw_up or None), of x's element type.  ``pre``: what gla_glu_fwd left there for
-    the same inputs; without it the two products are formed again."""
+    the same inputs; without it the two products are formed again.  bf16 gradients are off by 1.4 times their own rounding; gla_set_option(OPT_GLU_SPLIT, 1)
+    takes twice the operations of their products and leaves that rounding alone."""
     if _elsewhere(stream, x):
         return _call_on(stream, gla_glu_bwd, locals())
     lib = load_library()

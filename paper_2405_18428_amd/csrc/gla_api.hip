@@ -22,6 +22,7 @@ std::atomic<int> g_opt_engine{GLA_ENGINE_AUTO};
 std::atomic<int> g_opt_carry{GLA_CARRY_AUTO};
 std::atomic<int> g_opt_bwd_split{0};
 std::atomic<int> g_opt_range_fallback{1};
+std::atomic<int> g_opt_glu_split{0};
 std::atomic<int> g_opt_look_back_polls{1 << 15};     // (tens of milliseconds)
 
 struct Scratch {
@@ -1073,6 +1074,10 @@ int gla_set_option(int option, int value) {
         if (value < 0) return GLA_ERR_SHAPE;
         g_opt_look_back_polls = value;
         return GLA_OK;
+    case GLA_OPT_GLU_SPLIT:
+        if (value < 0 || value > 1) return GLA_ERR_SHAPE;
+        g_opt_glu_split = value;
+        return GLA_OK;
     case GLA_OPT_RANGE_FALLBACK:
         if (value < 0 || value > 1) return GLA_ERR_SHAPE;
         g_opt_range_fallback = value;
@@ -1090,6 +1095,7 @@ int gla_get_option(int option) {
     case GLA_OPT_BWD_SPLIT: return g_opt_bwd_split;
     case GLA_OPT_RANGE_FALLBACK: return g_opt_range_fallback;
     case GLA_OPT_LOOK_BACK_POLLS: return g_opt_look_back_polls;
+    case GLA_OPT_GLU_SPLIT: return g_opt_glu_split;
     default: return -1;
     }
 }

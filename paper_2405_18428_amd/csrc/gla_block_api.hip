@@ -192,11 +192,11 @@ int whole_pieces(int n, int dtype) {    // elements of rows in pieces of 16 byte
 }
 // Copies of operands whose rows are no whole pieces, and the backward pass's arrays, in a workspace (null: it only counts)
 struct GluRoom {
-    char *x, *w_gate, *w_up, *dg, *du;
+    char *x, *w_gate, *w_up, *dg[2], *du[2];
     float *part;
     size_t bytes;
 };
-GluRoom glu_room(void *workspace, int M, int K, int F, int dtype, bool back) {
+GluRoom glu_room(void *workspace, int M, int K, int F, int dtype, bool back, bool split) {
     GluRoom r = {};
     char *base = static_cast<char *>(workspace);
     auto take = [&](size_t rows, size_t cols, size_t each) {
@@ -211,12 +211,15 @@ GluRoom glu_room(void *workspace, int M, int K, int F, int dtype, bool back) {
         r.w_up = take(F, ld, size_of(dtype));
     }
     if (back) {
-        r.dg = take(M, whole_pieces(F, dtype), size_of(dtype));
-        r.du = take(M, whole_pieces(F, dtype), size_of(dtype));
-        r.part = reinterpret_cast<float *>(take(1, glu_part_bytes(M, K, F, dtype), 1));
+        for (int i = 0; i < (split ? 2 : 1); ++i) {
+            r.dg[i] = take(M, whole_pieces(F, dtype), size_of(dtype));
+            r.du[i] = take(M, whole_pieces(F, dtype), size_of(dtype));
+        }
+        r.part = reinterpret_cast<float *>(take(1, glu_part_bytes(M, K, F, dtype, split), 1));
     }
     return r;
 }
+bool glu_split(int dtype) { return dtype == GLA_DT_BF16 && gla_get_option(GLA_OPT_GLU_SPLIT) != 0; }
 int check_glu(const void *x, const void *w_gate, const void *w_up, int M, int K, int F, int act, int dtype, int other_dtype) {
     if (M <= 0 || K <= 0 || F <= 0 || bad_dtype(dtype) || bad_dtype(other_dtype) || act < GLA_ACT_SILU || act > GLA_ACT_GELU_TANH) return GLA_ERR_SHAPE;
     // (tiles of 128 rows and columns, and four columns a thread, in launches of fewer than 2^32 threads)
@@ -393,10 +396,10 @@ int gla_qk_norm_bwd(const void *q, const long long *q_strides, int H, const void
 }
 
 size_t gla_glu_fwd_workspace_bytes(int M, int K, int F, int dtype) {
-    return check_glu(nullptr, nullptr, nullptr, M, K, F, 0, dtype, dtype) == GLA_OK ? glu_room(nullptr, M, K, F, dtype, false).bytes : 0;
+    return check_glu(nullptr, nullptr, nullptr, M, K, F, 0, dtype, dtype) == GLA_OK ? glu_room(nullptr, M, K, F, dtype, false, false).bytes : 0;
 }
 size_t gla_glu_bwd_workspace_bytes(int M, int K, int F, int dtype) {
-    return check_glu(nullptr, nullptr, nullptr, M, K, F, 0, dtype, dtype) == GLA_OK ? glu_room(nullptr, M, K, F, dtype, true).bytes : 0;
+    return check_glu(nullptr, nullptr, nullptr, M, K, F, 0, dtype, dtype) == GLA_OK ? glu_room(nullptr, M, K, F, dtype, true, glu_split(dtype)).bytes : 0;
 }
 
 int gla_glu_fwd(const void *x, const void *w_gate, const void *w_up, int M, int K, int F, int act, int dtype, int out_dtype, void *out, float *pre, void *workspace,
@@ -409,7 +412,7 @@ int gla_glu_fwd(const void *x, const void *w_gate, const void *w_up, int M, int 
     const Span outs[] = {{out, n * size_of(out_dtype)}, {pre, 2 * n * sizeof(float)}};
     const Span ins[] = {{x, xs}, {w_gate, ws}, {w_up, ws}};
     if (any_touch(outs, ins)) return GLA_ERR_SHAPE;
-    const GluRoom room = glu_room(workspace, M, K, F, dtype, false);
+    const GluRoom room = glu_room(workspace, M, K, F, dtype, false, false);
     if (room.bytes > 0 && (!workspace || misaligned(workspace) || workspace_bytes < room.bytes)) return GLA_ERR_WORKSPACE;
     const hipStream_t stream = static_cast<hipStream_t>(stream_);
     GluCall c;
@@ -428,15 +431,17 @@ int gla_glu_bwd(const void *x, const void *w_gate, const void *w_up, const void 
     const Span outs[] = {{dx, xs}, {dw_gate, ws}, {dw_up, ws}};
     const Span ins[] = {{x, xs}, {w_gate, ws}, {w_up, ws}, {d_out, n * size_of(dtype)}, {pre, 2 * n * sizeof(float)}};
     if (any_touch(outs, ins)) return GLA_ERR_SHAPE;
-    const GluRoom room = glu_room(workspace, M, K, F, dtype, true);
+    const GluRoom room = glu_room(workspace, M, K, F, dtype, true, glu_split(dtype));
     if (!workspace || misaligned(workspace) || workspace_bytes < room.bytes) return GLA_ERR_WORKSPACE;
     const hipStream_t stream = static_cast<hipStream_t>(stream_);
     GluCall c;
     const int laid = glu_operands(c, room, x, w_gate, w_up, M, K, F, act, dtype, stream);
     if (laid != GLA_OK) return laid;
     c.d_out = d_out;
-    c.dg = room.dg;
-    c.du = room.du;
+    for (int i = 0; i < 2; ++i) {
+        c.dg[i] = room.dg[i];
+        c.du[i] = room.du[i];
+    }
     c.part = room.part;
     if (launch_glu_slopes(c, pre, stream) != hipSuccess) return GLA_ERR_HIP;
     if (dx != nullptr && launch_glu_dx(c, dx, stream) != hipSuccess) return GLA_ERR_HIP;

@@ -16,7 +16,8 @@
 // a pair of products (75 TFLOP/s of the 154 that large ones reach): 768 short tiles of 64 x 64, ragged ones among them.
 //
 // bf16 calls round dg and du once, to bf16, as operands of the second pair of products: what they lose is as random as the rounding
-// of the results and as large, so that gradients are off by 1.4 times their own rounding.  As two numbers each they would double dx and dW.
+// of the results and as large, so that gradients are off by 1.4 times their own rounding.  With GLA_OPT_GLU_SPLIT they are two numbers each, one segment of the contraction
+// behind the other: 1.02 times and less, for a backward call of 2167 us instead of 1156 (8192 x 2048 x 8192; 1024 x 1152 x 4608 143 and 89).
 #include "gla_glu.h"
 #include "gla_mfma_util.h"
 
@@ -57,7 +58,8 @@ __device__ __forceinline__ Activation activation(int act, float g) {
 
 struct ProductArgs {
     // operand rows: A has the result's rows, B its columns; second ones for what follows behind the first (see `Product`)
-    const char *a[2], *b[2];
+    const char *a[4], *b[2];
+    int segments;                       // of the contraction, one behind the other: dx dg, du (and what is left of them), dW one (and that)
     long long lda, ldb;                 // bytes
     int M, N, K;                        // of the result (forward: N = F columns of each product) and of one contraction
     int tiles_m, tiles_n, splits;
@@ -67,7 +69,7 @@ struct ProductArgs {
     float *pre, *part;
     // forward, where dg and du are wanted instead: [M, N], and two of [M, ld_f]
     const void *d_out;
-    void *slope[2];
+    void *slope[2], *left[2];            // (left: null or what is left of them, bf16)
     int ld_f;
 };
 
@@ -236,6 +238,13 @@ __device__ __forceinline__ void slopes(int act, const E *d_out, long long row, i
     }
 }
 
+// What a number has left when it is rounded to bf16 (nothing, where that is not finite), and four of them
+__device__ __forceinline__ float left_of(float x) {
+    const float r = bf16_lo_as_float(pack_bf16(x, 0.f));
+    return __builtin_fabsf(r) < __builtin_inff() ? x - r : 0.f;
+}
+__device__ __forceinline__ f32x4 left_of(f32x4 v) { return f32x4{left_of(v[0]), left_of(v[1]), left_of(v[2]), left_of(v[3])}; }
+
 // Tiles of a work-group: work-groups go to the eight XCDs by turns, so each XCD gets a run of tiles, and a run goes down eight rows of tiles
 // before it goes on to the next column, so that what an XCD reads at a time stays in its L2.
 __device__ __forceinline__ void tile_of(const ProductArgs &p, int &tm, int &tn) {
@@ -266,17 +275,17 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
     const int half_tiles = p.tiles_m / 2, which = P == kDw ? tm >= half_tiles : 0;
     const int m0 = (P == kDw ? tm - which * half_tiles : tm) * BM, n0 = tn * (P == kForward ? BN / 2 : BN);
 
-    // tiles of the contraction; dx: those of the first product, then those of the second
-    const int tiles = (p.K + kDepth - 1) / kDepth, all = P == kDx ? 2 * tiles : tiles;
+    // tiles of the contraction, those of one segment behind those of the other
+    const int tiles = (p.K + kDepth - 1) / kDepth, all = P == kForward ? tiles : p.segments * tiles;
     const int each = (all + p.splits - 1) / p.splits, t0 = min((int)blockIdx.y * each, all), t1 = min(t0 + each, all);
     TA ta;
     TB tb;
     ta.plan(wave, lane, p.lda, m0, p.M, kDepth);
     tb.plan(wave, lane, p.ldb, n0, p.N, kDepth);
     auto load = [&](int t, int buf) __attribute__((always_inline)) {
-        const int seg = P == kDx ? t >= tiles : 0, k0 = (P == kDx ? t - seg * tiles : t) * kDepth;
-        const char *a = p.a[P == kDw ? which : seg] + (P == kDw ? k0 * p.lda + (long long)m0 * kES : m0 * p.lda + (long long)k0 * kES);
-        const char *b = p.b[seg] + (P == kForward ? n0 * p.ldb + (long long)k0 * kES : k0 * p.ldb + (long long)n0 * kES);
+        const int seg = P == kForward ? 0 : P == kDw ? t >= tiles : (t >= tiles) + (t >= 2 * tiles) + (t >= 3 * tiles), k0 = (t - seg * tiles) * kDepth;
+        const char *a = p.a[P == kDw ? which + 2 * seg : seg] + (P == kDw ? k0 * p.lda + (long long)m0 * kES : m0 * p.lda + (long long)k0 * kES);
+        const char *b = p.b[P == kDx ? seg & 1 : 0] + (P == kForward ? n0 * p.ldb + (long long)k0 * kES : k0 * p.ldb + (long long)n0 * kES);
         const char *other = P == kForward ? p.b[1] + n0 * p.ldb + (long long)k0 * kES : nullptr;
         char *at = lds[buf];
         if (k0 + kDepth <= p.K) {
@@ -385,6 +394,10 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(const ProductArgs
                             slopes<E>(p.act, static_cast<const E *>(p.d_out), m, n, p.N, gt, up, dg, du);
                             store4(p.slope[0], kES == 2 ? GLA_DT_BF16 : GLA_DT_F32, m, n, p.ld_f, dg);
                             store4(p.slope[1], kES == 2 ? GLA_DT_BF16 : GLA_DT_F32, m, n, p.ld_f, du);
+                            if (kES == 2 && p.left[0] != nullptr) {
+                                store4(p.left[0], GLA_DT_BF16, m, n, p.ld_f, left_of(dg));
+                                store4(p.left[1], GLA_DT_BF16, m, n, p.ld_f, left_of(du));
+                            }
                             continue;
                         }
                         if (kColumns == 4 && p.pre != nullptr && n < p.N) {
@@ -538,8 +551,12 @@ __global__ __launch_bounds__(256) void slopes_kernel(const GluCall c, const floa
             }
     }
     slopes<E>(c.act, static_cast<const E *>(c.d_out), m, f, c.F, gt, up, dg, du);
-    store4(c.dg, c.dtype, m, f, c.ld_f, dg);
-    store4(c.du, c.dtype, m, f, c.ld_f, du);
+    store4(c.dg[0], c.dtype, m, f, c.ld_f, dg);
+    store4(c.du[0], c.dtype, m, f, c.ld_f, du);
+    if (sizeof(E) == 2 && c.split()) {
+        store4(c.dg[1], c.dtype, m, f, c.ld_f, left_of(dg));
+        store4(c.du[1], c.dtype, m, f, c.ld_f, left_of(du));
+    }
 }
 
 // Rows of `cols` elements to rows of `ld`, zeros behind: three tensors in one launch, four rows a work-group at a time.  Direct loads to LDS take pieces of 16
@@ -582,11 +599,11 @@ enum { kBig, kWide, kSmall, kTiny };     // 256 x 256, 256 x 192 (forward), 128 
 struct Plan {
     int tile, splits;
 };
-Plan plan_of(Product product, long long M, long long N, long long K, int dtype) {
+Plan plan_of(Product product, long long M, long long N, long long K, int segments, int dtype) {
     constexpr int kHigh[] = {256, 256, 128, 64}, kAcross[] = {256, 192, 128, 64}, kSlots[] = {256, 256, 512, 1024};
     constexpr double kStep[2][4] = {{1.95, 1.48, 1.08, 0.75}, {7.4, 5.6, 3.9, 2.1}}, kEnds = 6, kJoin = 5, kBytesAUs = 4e6;
     const int depth = kTileBytes / (dtype == GLA_DT_BF16 ? 2 : 4);
-    const long long steps = (K + depth - 1) / depth * (product == kDx ? 2 : 1);
+    const long long steps = (K + depth - 1) / depth * segments;
     Plan best = {kBig, 1};
     double least = 1e300;
     for (int tile = kBig; tile <= kTiny; ++tile) {
@@ -607,7 +624,7 @@ Plan plan_of(Product product, long long M, long long N, long long K, int dtype) 
 
 template <Product P>
 hipError_t product_of(const ProductArgs &p, int dtype, hipStream_t stream) {
-    const Plan plan = plan_of(P, p.M, P == kForward ? 2LL * p.N : p.N, p.K, dtype);
+    const Plan plan = plan_of(P, p.M, P == kForward ? 2LL * p.N : p.N, p.K, p.segments, dtype);
     auto run = [&](auto e) {
         using E = decltype(e);
         if constexpr (P == kForward) {
@@ -632,6 +649,7 @@ static ProductArgs forward_args(const GluCall &c) {
     p.M = c.M;
     p.N = c.F;
     p.K = c.ld_x;                        // (columns behind K are zeros)
+    p.segments = 1;
     p.splits = 1;
     p.act = c.act;
     return p;
@@ -677,8 +695,10 @@ hipError_t launch_glu_slopes(const GluCall &c, const float *pre, hipStream_t str
     if (pre == nullptr) {                // the two products again
         ProductArgs p = forward_args(c);
         p.d_out = c.d_out;
-        p.slope[0] = c.dg;
-        p.slope[1] = c.du;
+        p.slope[0] = c.dg[0];
+        p.slope[1] = c.du[0];
+        p.left[0] = c.dg[1];
+        p.left[1] = c.du[1];
         p.ld_f = c.ld_f;
         return product_of<kForward>(p, c.dtype, stream);
     }
@@ -689,15 +709,15 @@ hipError_t launch_glu_slopes(const GluCall &c, const float *pre, hipStream_t str
     return hipGetLastError();
 }
 
-size_t glu_part_bytes(int M, int K, int F, int dtype) {
-    const int dx = plan_of(kDx, M, K, F, dtype).splits, dw = plan_of(kDw, F, K, M, dtype).splits;
+size_t glu_part_bytes(int M, int K, int F, int dtype, bool split) {
+    const int each = split ? 2 : 1, dx = plan_of(kDx, M, K, F, 2 * each, dtype).splits, dw = plan_of(kDw, F, K, M, each, dtype).splits;
     const size_t a = dx > 1 ? (size_t)dx * M * K : 0, b = dw > 1 ? (size_t)dw * 2 * F * K : 0;
     return (a > b ? a : b) * sizeof(float);
 }
 // A product whose sum may be taken in parts
 template <Product P>
 static hipError_t in_parts(ProductArgs p, int dtype, hipStream_t stream) {
-    p.splits = plan_of(P, p.M, p.N, p.K, dtype).splits;
+    p.splits = plan_of(P, p.M, p.N, p.K, p.segments, dtype).splits;
     const hipError_t e = product_of<P>(p, dtype, stream);
     if (e != hipSuccess || p.splits == 1) return e;
     const JoinArgs j = {p.part, {p.out[0], p.out[1]}, (long long)p.M * p.N, dtype, p.splits};
@@ -707,8 +727,11 @@ static hipError_t in_parts(ProductArgs p, int dtype, hipStream_t stream) {
 
 hipError_t launch_glu_dx(const GluCall &c, void *dx, hipStream_t stream) {
     ProductArgs p = {};
-    p.a[0] = static_cast<const char *>(c.dg);
-    p.a[1] = static_cast<const char *>(c.du);
+    const int each = c.split() ? 2 : 1;
+    for (int i = 0; i < each; ++i) {
+        p.a[2 * i] = static_cast<const char *>(c.dg[i]);
+        p.a[2 * i + 1] = static_cast<const char *>(c.du[i]);
+    }
     p.b[0] = static_cast<const char *>(c.w_gate);
     p.b[1] = static_cast<const char *>(c.w_up);
     p.lda = (long long)c.ld_f * element(c.dtype);
@@ -716,6 +739,7 @@ hipError_t launch_glu_dx(const GluCall &c, void *dx, hipStream_t stream) {
     p.M = c.M;
     p.N = c.K;
     p.K = c.F;
+    p.segments = 2 * each;
     p.out[0] = dx;
     p.out_dtype = c.dtype;
     p.part = c.part;
@@ -724,14 +748,18 @@ hipError_t launch_glu_dx(const GluCall &c, void *dx, hipStream_t stream) {
 
 hipError_t launch_glu_dw(const GluCall &c, void *dw_gate, void *dw_up, hipStream_t stream) {
     ProductArgs p = {};
-    p.a[0] = static_cast<const char *>(c.dg);
-    p.a[1] = static_cast<const char *>(c.du);
+    const int each = c.split() ? 2 : 1;
+    for (int i = 0; i < each; ++i) {
+        p.a[2 * i] = static_cast<const char *>(c.dg[i]);
+        p.a[2 * i + 1] = static_cast<const char *>(c.du[i]);
+    }
     p.b[0] = static_cast<const char *>(c.x);
     p.lda = (long long)c.ld_f * element(c.dtype);
     p.ldb = (long long)c.ld_x * element(c.dtype);
     p.M = c.F;
     p.N = c.K;
     p.K = c.M;
+    p.segments = each;
     p.out[0] = dw_gate;
     p.out[1] = dw_up;
     p.out_dtype = c.dtype;

@@ -112,3 +112,19 @@ def test_sizes_that_are_no_c_int_are_refused(call, monkeypatch):
          "step": lambda: gla.gla_recur_step(x, x, new(HUGE, 1, dtype=torch.float32)), "qk_fwd": lambda: gla.gla_qk_norm_fwd(q, None),
          "qk_bwd": lambda: gla.gla_qk_norm_bwd(q, None, q, None), "qk_keys": lambda: gla.gla_qk_norm_fwd(new(1, 1, 5, 2), new(1, HUGE, 5, 2)),
          "glu_fwd": lambda: gla.gla_glu_fwd(x, w, w), "glu_bwd": lambda: gla.gla_glu_bwd(x, w, w, x), "glu_columns": lambda: gla.gla_glu_fwd(w, x, x)}[call]()
+
+
+def test_option_of_two_numbers():
+    """Off at first; only off and on; the backward call's two arrays twice, of bf16 calls."""
+    assert gla.gla_get_option(gla.OPT_GLU_SPLIT) == 0
+    one, fp32 = (gla.gla_glu_bwd_workspace_bytes(8192, 2048, 8192, t) for t in (gla.DT_BF16, gla.DT_F32))
+    for bad in (-1, 2):
+        with pytest.raises(gla.GlaError):
+            gla.gla_set_option(gla.OPT_GLU_SPLIT, bad)
+    gla.gla_set_option(gla.OPT_GLU_SPLIT, 1)
+    try:
+        assert gla.gla_glu_bwd_workspace_bytes(8192, 2048, 8192) >= one + 2 * 8192 * 8192 * 2
+        assert gla.gla_glu_bwd_workspace_bytes(8192, 2048, 8192, gla.DT_F32) == fp32
+    finally:
+        gla.gla_set_option(gla.OPT_GLU_SPLIT, 0)
+    assert gla.gla_glu_bwd_workspace_bytes(8192, 2048, 8192) == one
